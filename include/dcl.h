@@ -94,7 +94,7 @@ typedef struct {
   int32_t capacity;
 } dcl_kv;
 
-enum { DCL_DTYPE_F32 = 0, DCL_DTYPE_BF16 = 1 };
+enum { DCL_DTYPE_F32 = 0, DCL_DTYPE_BF16 = 1, DCL_DTYPE_E4M3 = 2 };
 
 /* dcl_denoise_step flags */
 #define DCL_SCORE_ALL_UNCOMMITTED 0x1u  /* score every position p <= i < gen_end, not only masks */
@@ -255,6 +255,65 @@ size_t dcl_score_workspace_bytes(dcl_model_t model, int32_t n);
  * and n*d_model < 2^31 (DCL_E_UNSUPPORTED otherwise). */
 dcl_status dcl_score_hidden(dcl_model_t model, const void* hidden, int32_t n, dcl_row_stats out,
                             void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---- Serving operators: sequences of different lengths in one pool of pages ----------------------------------
+ * A batch of B sequences is packed: rows of T tokens one behind the other, sequence b owning rows [cu[b], cu[b + 1])
+ * (cu: device int32 [B + 1], not decreasing; rows outside every sequence are neither read nor written). A row is
+ * [heads, head_dim] of bf16, 16-byte aligned, rows `stride` elements apart (a multiple of 8, at least heads *
+ * head_dim: q, k and v may be parts of one fused projection). head_dim is 64 or 128. `max_new` / `max_len` (host) is
+ * at least the longest sequence's number of rows: rows past it are left as they are. 1 <= B <= 2^16, 0 <= T <= 2^22;
+ * T = 0 does nothing. Device data is never trusted for an address: borders, lengths and page numbers outside their
+ * ranges give fewer rows or keys, not a fault. */
+
+/* A pool of pages for keys (after RoPE) and values of many sequences: page_len (a power of two, 16 to 1024) positions
+ * each. dtype DCL_DTYPE_BF16: bf16 elements, scales NULL. DCL_DTYPE_E4M3: elements are 8-bit floats (sign, 4 exponent
+ * bits, 3 fraction bits, no infinity) times one power-of-two scale 2^(byte - 127) per (position, KV head), the byte
+ * in [1, 254]. All arrays 16-byte aligned, device memory, the caller's. */
+typedef struct {
+  void* k;          /* [n_pages, n_kv_heads, page_len, head_dim] */
+  void* v;          /* [n_pages, n_kv_heads, head_dim, page_len] (position contiguous) */
+  uint8_t* k_scale; /* [n_pages, n_kv_heads, page_len], E4M3 only */
+  uint8_t* v_scale;
+  int32_t n_pages, page_len, n_kv_heads, head_dim, dtype;
+} dcl_pages;
+
+/* In the three calls below position x of sequence b lies in page table[b][x / page_len] (device int32 [B, max_pages],
+ * max_pages * page_len <= 2^28); entries outside [0, n_pages) name no page. len[b] (device int32 [B]) counts the
+ * sequence's positions with the call's tokens, which are its last: with n = cu[b + 1] - cu[b], row cu[b] + i is
+ * position len[b] - n + i. */
+
+/* Keys and values of the tokens into their pages. Tokens whose position no page holds are skipped. E4M3: with amax
+ * the largest finite magnitude of the (token, head)'s row, the scale is the least power of two with amax <= 448 *
+ * scale (2^-126 for a row of zeros) and elements are x / scale rounded to nearest even; infinities and NaN become
+ * NaN. No two positions of one call may share a place (a page listed twice): which one stays there is not defined.
+ * Pages that several sequences share are fine as long as no token is written to them. */
+dcl_status dcl_pages_write(const dcl_pages* pages, const int32_t* table, int32_t max_pages, const int32_t* len,
+                           const int32_t* cu, int32_t B, int32_t T, int32_t max_new, const void* k, int64_t k_stride,
+                           const void* v, int64_t v_stride, hipStream_t stream);
+
+/* The reverse: keys and values of those positions into rows of bf16 (E4M3: the values they stand for, which are bf16
+ * numbers but for subnormals below 2^-133 and a value rounded up to 2^128, read as infinity).
+ * A row whose position no page holds becomes zeros. */
+dcl_status dcl_pages_read(const dcl_pages* pages, const int32_t* table, int32_t max_pages, const int32_t* len,
+                          const int32_t* cu, int32_t B, int32_t T, int32_t max_new, void* k, int64_t k_stride, void* v,
+                          int64_t v_stride, hipStream_t stream);
+
+/* Workspace bytes of dcl_pages_attention for these sizes; 0 if they are invalid. */
+size_t dcl_pages_attention_workspace_bytes(const dcl_pages* pages, int32_t n_heads, int32_t B, int32_t T,
+                                           int32_t max_new, int32_t max_pages);
+
+/* Attention of each sequence's new tokens (one, or a block) over its pages: out[t, h] = sum_j softmax_j(scale q[t, h]
+ * . k_j) v_j over the sequence's len[b] positions, or with causal = 1 over those up to the token's own (the tokens'
+ * keys are already in the pages). Head h reads KV head h / (n_heads / n_kv_heads). Positions that no page holds take
+ * no part. out: bf16 [T, n_heads, head_dim]; lse (NULL: not written): float32 [T, n_heads], the natural logarithm of
+ * the sum of exponentials. A token that sees no position gets zeros and -inf. Work is split over the length where few
+ * rows would leave CUs idle; the parts go through ws (device, 256-byte aligned, ws_bytes >=
+ * dcl_pages_attention_workspace_bytes) and are joined in order: results are bitwise reproducible. Calls that overlap
+ * in time need their own workspaces. */
+dcl_status dcl_pages_attention(const dcl_pages* pages, const int32_t* table, int32_t max_pages, const int32_t* len,
+                               const int32_t* cu, int32_t B, int32_t T, int32_t max_new, const void* q,
+                               int64_t q_stride, int32_t n_heads, float scale, int32_t causal, void* out, float* lse,
+                               void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Test support: the same forward as dcl_denoise_step, then float32 logits of the rows listed in
  * `rows` (device [n_rows], flat indices b*S + i; an index outside [0, B*S) gives a zero hidden

@@ -15,7 +15,7 @@ import os
 from typing import Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-DCL_DTYPE_F32, DCL_DTYPE_BF16 = 0, 1
+DCL_DTYPE_F32, DCL_DTYPE_BF16, DCL_DTYPE_E4M3 = 0, 1, 2
 DCL_SCORE_ALL_UNCOMMITTED = 0x1
 DCL_SCORE_SUPPRESS_MASK = 0x2
 DCL_SEL_NO_PROGRESS_GUARD = 0x1
@@ -43,6 +43,11 @@ class DclConfig(ctypes.Structure):
 class DclRowStats(ctypes.Structure):
     _fields_ = [("top1", ctypes.c_void_p), ("top2", ctypes.c_void_p), ("conf", ctypes.c_void_p),
                 ("p2", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("entropy", ctypes.c_void_p)]
+
+
+class DclPages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "page_len", "n_kv_heads", "head_dim", "dtype")]
 
 
 PROF_CLASSES = ("embed", "rmsnorm", "gemm_qkv_rope", "attention", "gemm_o_residual", "gemm_gate_up_swiglu",
@@ -79,6 +84,8 @@ def load_library():
         raise RuntimeError(f"{path} is missing: build it with `python -c 'import __graft_entry__ as g; g.build()'`")
     lib = ctypes.CDLL(path)
     vp, i32, u32, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_float, ctypes.c_size_t
+    i64, pages = ctypes.c_int64, ctypes.POINTER(DclPages)
+    batch = [pages, vp, i32, vp, vp, i32, i32, i32]     # pool, table, max_pages, len, cu, B, T, max_new
     sig = {
         "dcl_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "dcl_last_error": (ctypes.c_char_p, []),
@@ -102,6 +109,10 @@ def load_library():
         "dcl_score_hidden": (ctypes.c_int, [vp, vp, i32, DclRowStats, vp, sz, vp]),
         "dcl_debug_logits": (ctypes.c_int, [vp, vp, i32, i32, ctypes.POINTER(DclKV), vp, i32, vp, vp, vp, sz, vp]),
         "dcl_debug_layer": (ctypes.c_int, [vp, i32, i32, ctypes.POINTER(DclKV), i32, vp, DclLayerTaps, vp, sz, vp]),
+        "dcl_pages_write": (ctypes.c_int, batch + [vp, i64, vp, i64, vp]),
+        "dcl_pages_read": (ctypes.c_int, batch + [vp, i64, vp, i64, vp]),
+        "dcl_pages_attention_workspace_bytes": (sz, [pages, i32, i32, i32, i32, i32]),
+        "dcl_pages_attention": (ctypes.c_int, batch + [vp, i64, i32, f32, i32, vp, vp, vp, sz, vp]),
         "dcl_debug_gemm_plan": (ctypes.c_int, [i32, i32, i32, i32, i32, ctypes.POINTER(i32)]),
     }
     for name, (res, args) in sig.items():
@@ -369,6 +380,137 @@ def dcl_debug_gemm_plan(Nw: int, T: int, K: int, lm_head: int = False, max_split
     _check(load_library().dcl_debug_gemm_plan(Nw, T, K, lm, max_split, info), "dcl_debug_gemm_plan")
     keys = ("cfg", "nsplit", "bw", "bt", "kd", "stages", "ww", "wt")
     return dict(zip(keys, list(info)))
+
+
+# ---------------------------------------------------------------- serving operators: packed batches, pages
+
+def _here(x, name, where, kinds, numel):
+    """``_arg`` for the serving operators, which also refuse a tensor of another device than the current one (the
+    call's stream belongs to that)."""
+    if x is None or isinstance(x, int):
+        return x
+    p = _arg(x, name, where, kinds, numel)
+    _on_current(x, name, where)
+    return p
+
+
+def _on_current(x, name, where):
+    import torch
+    if x.get_device() != torch.cuda.current_device():
+        raise DclError(1, where, f"{name} is on device {x.get_device()}, the current one is {torch.cuda.current_device()}")
+
+
+def _packed(x, name, where, T, heads, dim):
+    """Address and row stride of a packed operand [>= T, heads, dim] of bfloat16, whose rows may be apart."""
+    if isinstance(x, int):
+        return x, heads * dim
+    bad = None
+    if not getattr(x, "is_cuda", False):
+        bad = "must be a device (cuda) tensor"
+    elif str(x.dtype).replace("torch.", "") not in _B16:
+        bad = f"has dtype {x.dtype}, expected {' or '.join(_B16)}"
+    elif x.dim() != 3 or x.shape[1] != heads or x.shape[2] != dim or x.shape[0] < T:
+        bad = f"has shape {tuple(x.shape)}, expected ({T}, {heads}, {dim})"
+    elif T > 0 and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != dim)):
+        bad = f"has strides {x.stride()}, a row must be contiguous"
+    if bad:
+        raise DclError(1, where, f"{name} {bad}")
+    _on_current(x, name, where)
+    return x.data_ptr(), x.stride(0) if T > 1 else heads * dim
+
+
+def _batch(pages, table, length, cu, B, T, max_new, where):
+    """The leading arguments of the calls over pages."""
+    if not isinstance(pages, KVPages):
+        raise DclError(1, where, "pages must be a KVPages")
+    if getattr(table, "dim", lambda: 0)() != 2:
+        raise DclError(1, where, "table must be a [B, max_pages] tensor")
+    pages.check(where)
+    width = table.shape[1]
+    n = max(B, 0)
+    return (ctypes.byref(pages.struct), _here(table, "table", where, _I32, n * width), width,
+            _here(length, "len", where, _I32, n), _here(cu, "cu", where, _I32, n + 1), B, T, max_new)
+
+
+class KVPages:
+    """A pool of cache pages (``dcl_pages``): owns the tensors, or takes the caller's. dtype: DCL_DTYPE_BF16 or
+    DCL_DTYPE_E4M3 (8-bit values, one power-of-two scale per position and KV head)."""
+
+    def __init__(self, n_pages: int, page_len: int, n_kv_heads: int, head_dim: int, dtype: int = DCL_DTYPE_BF16,
+                 k=None, v=None, k_scale=None, v_scale=None, device=None):
+        import torch
+        w = "KVPages"
+        if min(n_pages, page_len, n_kv_heads, head_dim) < 1:
+            raise DclError(1, w, "sizes must be positive")
+        if dtype not in (DCL_DTYPE_BF16, DCL_DTYPE_E4M3):
+            raise DclError(2, w, f"dtype {dtype}: DCL_DTYPE_BF16 or DCL_DTYPE_E4M3")
+        e4m3 = dtype == DCL_DTYPE_E4M3
+        shape_k, shape_v = (n_pages, n_kv_heads, page_len, head_dim), (n_pages, n_kv_heads, head_dim, page_len)
+        if device is None:
+            device = next((t.device for t in (k, v, k_scale, v_scale) if t is not None), "cuda")
+
+        def take(t, name, shape, kinds, new):
+            if t is None:
+                return torch.zeros(shape, dtype=new, device=device)
+            if tuple(t.shape) != shape:
+                raise DclError(1, w, f"{name} has shape {tuple(t.shape)}, expected {shape}")
+            _arg(t, name, w, kinds)
+            return t
+        b8 = ("uint8", "int8", "float8_e4m3fn")
+        kinds, new = (b8, torch.uint8) if e4m3 else (_B16, torch.bfloat16)
+        self.k = take(k, "k", shape_k, kinds, new)
+        self.v = take(v, "v", shape_v, kinds, new)
+        if not e4m3 and (k_scale is not None or v_scale is not None):
+            raise DclError(1, w, "bfloat16 pages have no scales")
+        self.k_scale = take(k_scale, "k_scale", shape_k[:3], ("uint8",), torch.uint8) if e4m3 else None
+        self.v_scale = take(v_scale, "v_scale", shape_k[:3], ("uint8",), torch.uint8) if e4m3 else None
+        self.device = self.k.get_device()
+        if any(t is not None and t.get_device() != self.device for t in (self.v, self.k_scale, self.v_scale)):
+            raise DclError(1, w, "the pool's tensors are on different devices")
+        self.n_pages, self.page_len, self.n_kv_heads, self.head_dim, self.dtype = n_pages, page_len, n_kv_heads, \
+            head_dim, dtype
+        self.struct = DclPages(self.k.data_ptr(), self.v.data_ptr(), _ptr(self.k_scale), _ptr(self.v_scale), n_pages,
+                               page_len, n_kv_heads, head_dim, dtype)
+
+    def check(self, where):
+        _on_current(self.k, "pages", where)
+
+
+def dcl_pages_write(pages: KVPages, table, length, cu, B: int, T: int, max_new: int, k, v, stream=None) -> None:
+    """Rows k, v [T, n_kv_heads, head_dim] into the pages (``table`` [B, max_pages], ``length`` [B], ``cu`` [B + 1])."""
+    w = "dcl_pages_write"
+    a = _batch(pages, table, length, cu, B, T, max_new, w)
+    kp, ks = _packed(k, "k", w, T, pages.n_kv_heads, pages.head_dim)
+    vp, vs = _packed(v, "v", w, T, pages.n_kv_heads, pages.head_dim)
+    _check(load_library().dcl_pages_write(*a, kp, ks, vp, vs, _stream(stream)), w)
+
+
+def dcl_pages_read(pages: KVPages, table, length, cu, B: int, T: int, max_new: int, k, v, stream=None) -> None:
+    """The last rows of each sequence out of the pages into k, v [T, n_kv_heads, head_dim]."""
+    w = "dcl_pages_read"
+    a = _batch(pages, table, length, cu, B, T, max_new, w)
+    kp, ks = _packed(k, "k", w, T, pages.n_kv_heads, pages.head_dim)
+    vp, vs = _packed(v, "v", w, T, pages.n_kv_heads, pages.head_dim)
+    _check(load_library().dcl_pages_read(*a, kp, ks, vp, vs, _stream(stream)), w)
+
+
+def dcl_pages_attention_workspace_bytes(pages: KVPages, n_heads: int, B: int, T: int, max_new: int,
+                                        max_pages: int) -> int:
+    return load_library().dcl_pages_attention_workspace_bytes(ctypes.byref(pages.struct), n_heads, B, T, max_new,
+                                                              max_pages)
+
+
+def dcl_pages_attention(pages: KVPages, table, length, cu, B: int, T: int, max_new: int, q, n_heads: int, scale: float,
+                        causal: bool, out, lse, ws, ws_bytes: int, stream=None) -> None:
+    """q [T, n_heads, head_dim] over the pages; out like q (contiguous), lse [T, n_heads] float32 or None."""
+    w = "dcl_pages_attention"
+    a = _batch(pages, table, length, cu, B, T, max_new, w)
+    qp, qs = _packed(q, "q", w, T, n_heads, pages.head_dim)
+    n = max(T, 0) * n_heads
+    _check(load_library().dcl_pages_attention(*a, qp, qs, n_heads, scale, int(causal),
+                                              _here(out, "out", w, _B16, n * pages.head_dim),
+                                              _here(lse, "lse", w, _F32, n),
+                                              _arg(ws, "ws", w, _ANY, nbytes=ws_bytes), ws_bytes, _stream(stream)), w)
 
 
 # ---------------------------------------------------------------- convenience owner of device buffers

@@ -14,9 +14,9 @@
 
 using namespace dcl;
 
-namespace {
+static thread_local char g_err[512] = "";
 
-thread_local char g_err[512] = "";
+namespace dcl {
 
 dcl_status fail(dcl_status s, const char* fmt, ...) {
   va_list ap;
@@ -30,6 +30,10 @@ dcl_status hip_check(hipError_t e, const char* what) {
   if (e != hipSuccess) return fail(DCL_E_HIP, "%s: %s", what, hipGetErrorString(e));
   return DCL_OK;
 }
+
+}  // namespace dcl
+
+namespace {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 

@@ -178,4 +178,38 @@ void launch_attention(const AttnArgs& a, hipStream_t s);
 void launch_kv_writeback(const bf16_t* k, const bf16_t* vt, bf16_t* kc, bf16_t* vc, int B, int Hkv, int S, int Sk,
                          int Sp, int koff, int dh, int P, int Pc, hipStream_t s);
 
+
+// ---------------------------------------------------------------- paged cache, packed prompts, sampling
+// Records a message for dcl_last_error() and returns `s`.
+dcl_status fail(dcl_status s, const char* fmt, ...);
+dcl_status hip_check(hipError_t e, const char* what);
+
+// A pool of pages with the batch's table and lengths, as the kernels take them.
+struct Pages {
+  uint8_t *k, *v;                // [n_pages, Hkv, page, dh], [n_pages, Hkv, dh, page]
+  uint8_t *ks, *vs;              // [n_pages, Hkv, page] exponents of the scales (E4M3)
+  const int32_t *table, *len;    // [B, max_pages], [B]
+  const int32_t* cu;             // [B + 1]
+  int n_pages, shift, max_pages, Hkv, dh, e4m3;  // pages of 2^shift positions
+  int B, T, max_new;
+};
+// Rows k, v [T, Hkv, dh] (row strides in elements) into the pages, or out of them.
+void launch_pages_write(const Pages& p, const bf16_t* k, long ks, const bf16_t* v, long vs, hipStream_t s);
+void launch_pages_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, hipStream_t s);
+
+struct PagesAttn {
+  Pages p;
+  const bf16_t* q;               // [T, H, dh], row stride q_stride
+  long q_stride;
+  bf16_t* out;                   // [T, H, dh]
+  float* lse;                    // [T, H] or null
+  float* po;                     // partial outputs [nsplit, T, H, dh] (nsplit > 1)
+  float2* pml;                   // their (reference, sum) [nsplit, T, H]
+  int H, g, causal, nsplit, row_tiles;
+  float scale_log2;
+};
+// Parts that a call's key lengths are split into: from sizes that the host knows.
+int pages_attention_splits(int Hkv, int g, int B, int max_new, int capacity);
+void launch_pages_attention(PagesAttn a, hipStream_t s);
+
 }  // namespace dcl

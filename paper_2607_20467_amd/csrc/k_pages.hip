@@ -1,0 +1,706 @@
+// The paged cache: keys and values of packed tokens into pages and back (bfloat16, or 8 bits with a scale), and
+// attention from a sequence's newest tokens to its pages, split over the cache's length and joined.
+#include <type_traits>
+
+#include "dcl_internal.h"
+#include "pages_index.h"
+
+namespace dcl {
+
+// ---------------------------------------------------------------- 8-bit rows
+// A row of head_dim elements is stored as e4m3 values (4 significant bits, 2^-6 to 448, subnormals down to 2^-9) times
+// one scale 2^(e - 127), e a byte in [1, 254]: the least power of two with amax <= 448 * scale. A power of two costs a
+// floating-point format no precision (only the subnormal end moves), makes x / scale exact, so that e4m3's rounding to
+// nearest even is the only one, and keeps every stored value a bfloat16 number, so that the products of attention see
+// exactly what is stored. amax is the largest finite magnitude; infinities and NaN are stored as e4m3 NaN (the format
+// has no infinity), with their sign.
+__device__ __forceinline__ int e4m3_exponent(uint32_t amax_bits) {  // bfloat16 bits of amax, sign cleared
+  // amax = 1.f * 2^(E - 127), 448 = 1.75 * 2^8
+  const int e = (int)(amax_bits >> 7) - 8 + ((amax_bits & 127) > 96 ? 1 : 0);
+  return e < 1 ? 1 : e;  // at most 247
+}
+__device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(e << 23); }
+
+// Eight bfloat16 (as loaded) to eight e4m3 bytes, times `inv` (a power of two).
+__device__ __forceinline__ uint2 quantise8(const uint4& x, float inv) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t o[2];
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int p = 0;
+    p = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(w[2 * i] << 16) * inv,
+                                        __uint_as_float(w[2 * i] & 0xFFFF0000u) * inv, p, false);
+    p = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(w[2 * i + 1] << 16) * inv,
+                                        __uint_as_float(w[2 * i + 1] & 0xFFFF0000u) * inv, p, true);
+    o[i] = (uint32_t)p;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) odd |= (w[i] & 0x7F80u) == 0x7F80u || (w[i] & 0x7F800000u) == 0x7F800000u;
+  if (odd) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t h = (w[i >> 1] >> (16 * (i & 1))) & 0xFFFFu;
+      if ((h & 0x7F80u) == 0x7F80u) {
+        const uint32_t b = 0x7Fu | ((h >> 8) & 0x80u);
+        o[i >> 2] = (o[i >> 2] & ~(0xFFu << (8 * (i & 3)))) | (b << (8 * (i & 3)));
+      }
+    }
+  }
+  return make_uint2(o[0], o[1]);
+}
+// Largest finite magnitude of eight bfloat16, as bits.
+__device__ __forceinline__ uint32_t amax8(const uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t a = w[i] & 0x7FFFu, b = (w[i] >> 16) & 0x7FFFu;
+    m = max(m, a < 0x7F80u ? a : 0u);
+    m = max(m, b < 0x7F80u ? b : 0u);
+  }
+  return m;
+}
+
+// ---------------------------------------------------------------- write
+// One workgroup takes 64 positions (aligned to 64 in the sequence) of one KV head. Rows arrive with the dimension
+// innermost; keys go out the same way, values through LDS with the position innermost, in chunks of 16 positions that
+// never straddle a page. Memory-bound: each row is read once and each byte of the pages written once.
+constexpr int kGroup = 64;
+
+template <int DH, bool E4>
+__global__ void __launch_bounds__(256) pages_write_kernel(Pages p, const bf16_t* __restrict__ k, long kst,
+                                                         const bf16_t* __restrict__ v, long vst, int groups) {
+  constexpr int ES = E4 ? 1 : 2, L = DH / 8, TPR = 256 / L, R = kGroup / TPR;
+  constexpr int PITCH = DH * ES + 4;  // four chunks of 16 rows apart: other banks
+  __shared__ __attribute__((aligned(16))) uint8_t sv[kGroup * PITCH];
+  const int grp = blockIdx.x % groups, bh = blockIdx.x / groups, h = bh % p.Hkv, b = bh / p.Hkv;
+  const SeqRows r = seq_rows(p.cu, b, p.T);
+  const int n = min(r.n, p.max_new), start = seq_len(p.len, b) - r.n;  // position of the first row
+  const int g0 = (start & ~(kGroup - 1)) + grp * kGroup;
+  if (g0 >= start + n) return;
+  const int32_t* row = p.table + (size_t)b * p.max_pages;
+  const int plen = 1 << p.shift, tid = threadIdx.x, c = tid % L;
+  uint4 xk[R], xv[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int t = g0 + i * TPR + tid / L - start;
+    xk[i] = xv[i] = make_uint4(0, 0, 0, 0);
+    if (t >= 0 && t < n) {
+      const size_t at = (size_t)(r.first + t);
+      xk[i] = *reinterpret_cast<const uint4*>(k + at * kst + (size_t)h * DH + 8 * c);
+      xv[i] = *reinterpret_cast<const uint4*>(v + at * vst + (size_t)h * DH + 8 * c);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int local = i * TPR + tid / L, t = g0 + local - start;
+    const int page = t >= 0 && t < n ? page_of(row, p.max_pages, p.n_pages, p.shift, (g0 + local) >> 4) : -1;
+    const int off = (g0 + local) & (plen - 1);
+    const size_t slot = ((size_t)max(page, 0) * p.Hkv + h) * plen + off;
+    if constexpr (E4) {
+      uint32_t ak = amax8(xk[i]), av = amax8(xv[i]);
+#pragma unroll
+      for (int o = L / 2; o >= 1; o >>= 1) {
+        ak = max(ak, (uint32_t)__shfl_xor((int)ak, o, 64));
+        av = max(av, (uint32_t)__shfl_xor((int)av, o, 64));
+      }
+      const int ek = e4m3_exponent(ak), ev = e4m3_exponent(av);
+      const uint2 qk = quantise8(xk[i], scale_of(254 - ek)), qv = quantise8(xv[i], scale_of(254 - ev));
+      uint32_t* d = reinterpret_cast<uint32_t*>(sv + local * PITCH + 8 * c);
+      d[0] = qv.x;
+      d[1] = qv.y;
+      if (page >= 0) {
+        *reinterpret_cast<uint2*>(p.k + slot * DH + 8 * c) = qk;
+        if (c == 0) {
+          p.ks[slot] = (uint8_t)ek;
+          p.vs[slot] = (uint8_t)ev;
+        }
+      }
+    } else {
+      uint32_t* d = reinterpret_cast<uint32_t*>(sv + local * PITCH + 16 * c);
+      d[0] = xv[i].x;
+      d[1] = xv[i].y;
+      d[2] = xv[i].z;
+      d[3] = xv[i].w;
+      if (page >= 0) *reinterpret_cast<uint4*>(p.k + (slot * DH + 8 * c) * 2) = xk[i];
+    }
+  }
+  __syncthreads();
+  for (int u = tid; u < DH * 4; u += 256) {
+    const int ch = u & 3, d = u >> 2, p0 = g0 + 16 * ch;
+    const int lo = max(0, start - p0), hi = min(16, start + n - p0);
+    if (lo >= hi) continue;
+    const int page = page_of(row, p.max_pages, p.n_pages, p.shift, p0 >> 4);
+    if (page < 0) continue;
+    uint8_t* dst = p.v + ((((size_t)page * p.Hkv + h) * DH + d) * plen + (p0 & (plen - 1))) * ES;
+    const uint8_t* src = sv + 16 * ch * PITCH + d * ES;
+    if (hi - lo == 16) {
+      uint32_t w[4 * ES];
+#pragma unroll
+      for (int j = 0; j < 4 * ES; ++j) {
+        if constexpr (E4) {
+          w[j] = src[4 * j * PITCH] | src[(4 * j + 1) * PITCH] << 8 | src[(4 * j + 2) * PITCH] << 16 |
+                 (uint32_t)src[(4 * j + 3) * PITCH] << 24;
+        } else {
+          w[j] = *reinterpret_cast<const uint16_t*>(src + 2 * j * PITCH) |
+                 (uint32_t)*reinterpret_cast<const uint16_t*>(src + (2 * j + 1) * PITCH) << 16;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < ES; ++j)
+        reinterpret_cast<uint4*>(dst)[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+    } else {
+      for (int j = lo; j < hi; ++j) {
+        if constexpr (E4) dst[j] = src[j * PITCH];
+        else reinterpret_cast<uint16_t*>(dst)[j] = *reinterpret_cast<const uint16_t*>(src + j * PITCH);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- read
+// The reverse, in the same groups: values come in by rows of positions and leave by rows of dimensions. A row whose
+// position no page holds is zeros.
+template <int DH, bool E4>
+__global__ void __launch_bounds__(256) pages_read_kernel(Pages p, bf16_t* __restrict__ k, long kst,
+                                                        bf16_t* __restrict__ v, long vst, int groups) {
+  constexpr int ES = E4 ? 1 : 2, L = DH / 8, TPR = 256 / L, R = kGroup / TPR;
+  constexpr int PITCH = kGroup * ES + 4;
+  __shared__ __attribute__((aligned(16))) uint8_t sv[DH * PITCH];
+  const int grp = blockIdx.x % groups, bh = blockIdx.x / groups, h = bh % p.Hkv, b = bh / p.Hkv;
+  const SeqRows r = seq_rows(p.cu, b, p.T);
+  const int n = min(r.n, p.max_new), start = seq_len(p.len, b) - r.n;
+  const int g0 = (start & ~(kGroup - 1)) + grp * kGroup;
+  if (g0 >= start + n) return;
+  const int32_t* row = p.table + (size_t)b * p.max_pages;
+  const int plen = 1 << p.shift, tid = threadIdx.x, c = tid % L;
+#pragma unroll
+  for (int i = 0; i < DH * 4 / 256; ++i) {
+    const int u = tid + 256 * i, ch = u & 3, d = u >> 2, p0 = g0 + 16 * ch;
+    const int page = p0 < start + n && p0 + 16 > start ? page_of(row, p.max_pages, p.n_pages, p.shift, p0 >> 4) : -1;
+    if (page < 0) continue;
+    const uint4* src = reinterpret_cast<const uint4*>(
+        p.v + ((((size_t)page * p.Hkv + h) * DH + d) * plen + (p0 & (plen - 1))) * ES);
+    uint32_t* dst = reinterpret_cast<uint32_t*>(sv + d * PITCH + 16 * ch * ES);
+#pragma unroll
+    for (int j = 0; j < ES; ++j) {
+      const uint4 x = src[j];
+      dst[4 * j] = x.x;
+      dst[4 * j + 1] = x.y;
+      dst[4 * j + 2] = x.z;
+      dst[4 * j + 3] = x.w;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int local = i * TPR + tid / L, t = g0 + local - start;
+    if (t < 0 || t >= n) continue;
+    const int page = page_of(row, p.max_pages, p.n_pages, p.shift, (g0 + local) >> 4);
+    const int off = (g0 + local) & (plen - 1);
+    const size_t slot = ((size_t)max(page, 0) * p.Hkv + h) * plen + off, at = (size_t)(r.first + t);
+    uint4 ok = make_uint4(0, 0, 0, 0), ov = ok;
+    if (page >= 0) {
+      if constexpr (E4) {
+        const uint2 x = *reinterpret_cast<const uint2*>(p.k + slot * DH + 8 * c);
+        const float fk = scale_of(p.ks[slot]), fv = scale_of(p.vs[slot]);
+        uint32_t y[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint8_t* s = sv + (8 * c + 4 * j) * PITCH + local;
+          y[j] = s[0] | s[PITCH] << 8 | s[2 * PITCH] << 16 | (uint32_t)s[3 * PITCH] << 24;
+        }
+        auto pair = [](uint32_t w, bool hi, float f) -> uint32_t {
+          const auto q = hi ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+          return f2bf2(q[0] * f, q[1] * f);
+        };
+        ok = make_uint4(pair(x.x, false, fk), pair(x.x, true, fk), pair(x.y, false, fk), pair(x.y, true, fk));
+        ov = make_uint4(pair(y[0], false, fv), pair(y[0], true, fv), pair(y[1], false, fv), pair(y[1], true, fv));
+      } else {
+        ok = *reinterpret_cast<const uint4*>(p.k + (slot * DH + 8 * c) * 2);
+        uint32_t y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint8_t* s = sv + (8 * c + 2 * j) * PITCH + 2 * local;
+          y[j] = *reinterpret_cast<const uint16_t*>(s) | (uint32_t)*reinterpret_cast<const uint16_t*>(s + PITCH) << 16;
+        }
+        ov = make_uint4(y[0], y[1], y[2], y[3]);
+      }
+    }
+    *reinterpret_cast<uint4*>(k + at * kst + (size_t)h * DH + 8 * c) = ok;
+    *reinterpret_cast<uint4*>(v + at * vst + (size_t)h * DH + 8 * c) = ov;
+  }
+}
+
+// Groups of kGroup positions that `n` consecutive positions can touch.
+static int groups_of(int n) { return (n + kGroup - 2) / kGroup + 1; }
+
+void launch_pages_write(const Pages& p, const bf16_t* k, long ks, const bf16_t* v, long vs, hipStream_t s) {
+  if (p.T == 0 || p.max_new == 0) return;
+  const int groups = groups_of(p.max_new);
+  const dim3 grid((unsigned)groups * p.Hkv * p.B);
+  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, p, k, ks, v, vs, groups); };
+  if (p.dh == 128) p.e4m3 ? go(pages_write_kernel<128, true>) : go(pages_write_kernel<128, false>);
+  else p.e4m3 ? go(pages_write_kernel<64, true>) : go(pages_write_kernel<64, false>);
+}
+
+void launch_pages_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, hipStream_t s) {
+  if (p.T == 0 || p.max_new == 0) return;
+  const int groups = groups_of(p.max_new);
+  const dim3 grid((unsigned)groups * p.Hkv * p.B);
+  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, p, k, ks, v, vs, groups); };
+  if (p.dh == 128) p.e4m3 ? go(pages_read_kernel<128, true>) : go(pages_read_kernel<128, false>);
+  else p.e4m3 ? go(pages_read_kernel<64, true>) : go(pages_read_kernel<64, false>);
+}
+
+// ---------------------------------------------------------------- attention over pages
+// o = sum_j softmax_j(scale q.k_j) v_j over the keys j of the sequence, per query row one running maximum and sum.
+// The rows of one KV head (its g = H / Hkv query heads times the sequence's new tokens) are tiles of 16 QF; a workgroup
+// takes one tile and one of `nsplit` equal parts of the keys, its four waves every fourth tile of KT keys. The cache is
+// read once from HBM straight into the registers of the matrix instructions (no LDS: with one new token nothing is
+// shared between waves), the scores are S^T = K Q^T and the probabilities feed O^T = V^T P^T from the same lanes.
+//
+// Which key sits in which row of a matrix instruction is free as long as scores and values agree: with PK = KT / 4, row
+// 4 a + r of score step kt is key PK a + 4 kt + r, so that lane group a (= lane / 16) ends up with the probabilities of PK
+// adjacent keys, which lie in one page, and reads its values as whole pieces of the position-innermost rows. In the same
+// way a lane holds 16 adjacent dimensions of a key, two steps of 32. KT is 64 for 8-bit pages (16-byte pieces of values)
+// and 32 for bfloat16 ones, and for 8-bit ones under four query fragments, whose registers a larger tile would spill.
+//
+// 8-bit rows become bfloat16 without their scales (exact). A key's scale multiplies its score, a value's its
+// probability, in float32; the probability is then rounded to bfloat16 once, 2^-9 of itself, while the sum that divides
+// takes it unrounded: over many keys these roundings average out, far below the rounding of the output.
+__device__ __forceinline__ f32x4_t mfma16p(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float max_groups(float v) {  // over the lanes l, l ^ 16, l ^ 32, l ^ 48
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float sum_groups(float v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+__device__ __forceinline__ bf16x8_t widen8(uint32_t lo, uint32_t hi) {  // eight e4m3 bytes, exactly
+  uint4 o;
+  o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
+  o.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
+  o.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
+  o.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
+  return __builtin_bit_cast(bf16x8_t, o);
+}
+
+// Keys that each part of a sequence with `keys` keys takes, in tiles of 64: part i has [i, i + 1) * the result.
+__device__ __forceinline__ int tiles_per_part(int keys, int nsplit) {
+  const int tiles = (keys + 63) >> 6;
+  return (tiles + nsplit - 1) / nsplit;
+}
+
+// A reference point, and what a row without keys (reference -inf) is taken relative to.
+__device__ __forceinline__ float finite_ref(float m) { return m == -INFINITY ? 0.f : m; }
+
+template <int DH, bool E4, int QF>
+__global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesAttn a) {
+  constexpr int ES = E4 ? 1 : 2, KT = E4 && QF < 4 ? 64 : 32, PK = KT / 4, NKT = KT / 16, S2 = KT / 32;
+  constexpr int KS = DH / 32, DT = DH / 16;
+  constexpr int NK = DH * ES / 64;  // 16-byte pieces of a lane's dimensions of one key
+  constexpr int VW = PK * ES / 4;   // words of a lane's keys of one dimension
+  constexpr int SW = PK / 4;        // words of their scales
+  __shared__ f32x4_t xo[3][DT][64];
+  __shared__ float2 xml[3][64];
+  const Pages& p = a.p;
+  // units: row tiles of one (part, sequence, KV head) follow each other on one XCD and share its L2
+  const int u = blockIdx.x, item = (u / (8 * a.row_tiles)) * 8 + (u & 7), tile = (u >> 3) % a.row_tiles;
+  if (item >= a.nsplit * p.B * p.Hkv) return;
+  const int h = item % p.Hkv, b = (item / p.Hkv) % p.B, part = item / (p.Hkv * p.B);
+  const SeqRows r = seq_rows(p.cu, b, p.T);
+  const int n = min(r.n, p.max_new), rows = n * a.g, row0 = tile * 16 * QF;
+  if (row0 >= rows) return;
+  const int len = seq_len(p.len, b), plen = 1 << p.shift;
+  const int kend = min(len, p.max_pages << p.shift);  // keys that the table can name
+  const int per = tiles_per_part(kend, a.nsplit) * (64 / KT), t0 = part * per, t1 = min(t0 + per, (kend + KT - 1) / KT);
+  if (part > 0 && t0 >= t1) return;  // part 0 always answers
+  const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 15, lg = lane >> 4, la = lq >> 2, lr = lq & 3;
+  const int32_t* row = p.table + (size_t)b * p.max_pages;
+
+  // the wave's queries, and how many keys each may see (rows past the last one: like any other, never written)
+  bf16x8_t qf[QF][KS];
+  int lim[QF], lim_min = kend;
+#pragma unroll
+  for (int f = 0; f < QF; ++f) {
+    const int rr = min(row0 + 16 * f + lq, rows - 1), i = rr / a.g, head = h * a.g + rr % a.g;
+    const bf16_t* qp = a.q + (size_t)(r.first + i) * a.q_stride + (size_t)head * DH + 16 * lg;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      qf[f][ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(qp + 64 * (ks >> 1) + 8 * (ks & 1)));
+    lim[f] = a.causal ? min(kend, max(0, len - r.n + i + 1)) : kend;
+  }
+  if (a.causal) lim_min = min(kend, max(0, len - r.n + row0 / a.g + 1));
+
+  f32x4_t o[QF][DT];
+  float m[QF], l[QF];
+#pragma unroll
+  for (int f = 0; f < QF; ++f) {
+    m[f] = -INFINITY;
+    l[f] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[f][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  uint4 kr[NKT][NK];                 // the tile's keys, values and scales, as loaded
+  uint32_t vr[DT][VW], ksr[SW], vsr[SW];
+  int pid_v = -1;                    // page of the lane group's PK keys of the tile whose values are in vr
+  const size_t page_bytes = (size_t)p.Hkv * plen * DH * ES, head_bytes = (size_t)h * plen * DH * ES;
+  auto load_words = [](uint32_t* w, const uint8_t* src, auto words) {
+    if constexpr (decltype(words)::value == 4) {
+      const uint4 x = *reinterpret_cast<const uint4*>(src);
+      w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+    } else {
+      const uint2 x = *reinterpret_cast<const uint2*>(src);
+      w[0] = x.x, w[1] = x.y;
+    }
+  };
+  auto load_keys = [&](int t, int pid) {  // pid: page of keys KT t + PK la ..
+    const int off = ((KT * t + PK * la) & (plen - 1)) + lr;
+    const uint8_t* base = p.k + (size_t)max(pid, 0) * page_bytes + head_bytes + (size_t)off * (DH * ES) + lg * 16 * ES;
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+      for (int x = 0; x < NK; ++x)
+        kr[kt][x] = *reinterpret_cast<const uint4*>(base + kt * 4 * DH * ES + (E4 ? 64 * x : 128 * (x >> 1) + 16 * (x & 1)));
+  };
+  auto load_values = [&](int t, int pid) {  // pid: page of keys KT t + PK lg ..
+    const int off = (KT * t + PK * lg) & (plen - 1);
+    const uint8_t* base = p.v + (size_t)max(pid, 0) * page_bytes + head_bytes + ((size_t)lq * plen + off) * ES;
+    const size_t step = (size_t)16 * plen * ES;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) load_words(vr[dt], base + dt * step, std::integral_constant<int, VW>());
+    if constexpr (E4) {
+      const size_t at = ((size_t)max(pid, 0) * p.Hkv + h) * plen + off;
+      load_words(ksr, p.ks + at, std::integral_constant<int, SW>());
+      load_words(vsr, p.vs + at, std::integral_constant<int, SW>());
+    }
+    pid_v = pid;
+  };
+  // eight values of one dimension, of score steps 2 s2 and 2 s2 + 1
+  auto value_fragment = [&](int dt, int s2) -> bf16x8_t {
+    if constexpr (E4) return widen8(vr[dt][2 * s2], vr[dt][2 * s2 + 1]);
+    else return __builtin_bit_cast(bf16x8_t, make_uint4(vr[dt][0], vr[dt][1], vr[dt][2], vr[dt][3]));
+  };
+  auto page_at = [&](int t, int grp) { return page_of(row, p.max_pages, p.n_pages, p.shift, (KT * t + PK * grp) >> 4); };
+
+  int t = t0 + wid;
+  int pk = -1, pv = -1;  // pages of tile t, then of the next one
+  if (t < t1) {
+    pk = page_at(t, la);
+    pv = page_at(t, lg);
+    load_keys(t, pk);
+    load_values(t, pv);
+    pk = t + 4 < t1 ? page_at(t + 4, la) : -1;
+    pv = t + 4 < t1 ? page_at(t + 4, lg) : -1;
+  }
+  for (; t < t1; t += 4) {
+    const int k0 = KT * t + PK * lg;  // the lane group's first key
+    f32x4_t sc[QF][NKT];
+#pragma unroll
+    for (int f = 0; f < QF; ++f)
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) sc[f][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt) {
+      bf16x8_t kf[KS];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if constexpr (E4) {
+          const uint4 x = kr[kt][ks >> 1];
+          kf[ks] = ks & 1 ? widen8(x.z, x.w) : widen8(x.x, x.y);
+        } else {
+          kf[ks] = __builtin_bit_cast(bf16x8_t, kr[kt][ks]);
+        }
+      }
+#pragma unroll
+      for (int f = 0; f < QF; ++f)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sc[f][kt] = mfma16p(kf[ks], qf[f][ks], sc[f][kt]);
+    }
+    if (t + 4 < t1) load_keys(t + 4, pk);
+
+    // log2 units; then the keys that a row does not see: past its limit, past the last key, in no page
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr) {
+        const float f1 = E4 ? scale_of((ksr[kt] >> (8 * rr)) & 255u) * a.scale_log2 : a.scale_log2;
+#pragma unroll
+        for (int f = 0; f < QF; ++f) sc[f][kt][rr] *= f1;
+      }
+    const bool whole = KT * t + KT <= lim_min && __builtin_amdgcn_ballot_w64(pid_v < 0) == 0;
+    auto dead = [&](int f, int kt, int rr) { return pid_v < 0 || k0 + 4 * kt + rr >= lim[f]; };
+    if (!whole) {
+#pragma unroll
+      for (int f = 0; f < QF; ++f)
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+          for (int rr = 0; rr < 4; ++rr)
+            if (dead(f, kt, rr)) sc[f][kt][rr] = -INFINITY;
+    }
+    // The reference point m moves only when a score passes it by more than 2^8 (any reference gives the same
+    // quotient), so that most tiles need no maximum across the lanes and no rescaling.
+    float tmax[QF];
+    bool move = false;
+#pragma unroll
+    for (int f = 0; f < QF; ++f) {
+      tmax[f] = -INFINITY;
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) tmax[f] = fmaxf(tmax[f], sc[f][kt][rr]);
+      move |= tmax[f] > m[f] + 8.f;
+    }
+    if (__builtin_amdgcn_ballot_w64(move)) {
+#pragma unroll
+      for (int f = 0; f < QF; ++f) {
+        const float ts = max_groups(tmax[f]);
+        const float mn = ts > m[f] + 8.f ? ts : m[f];
+        const float alpha = mn == m[f] ? 1.f : __builtin_amdgcn_exp2f(m[f] - mn);
+        l[f] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[f][dt] *= alpha;
+        m[f] = mn;
+      }
+    }
+    bf16x8_t pf[QF][S2];
+#pragma unroll
+    for (int f = 0; f < QF; ++f) {
+      const float mr = finite_ref(m[f]);
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) {
+          const float pv1 = __builtin_amdgcn_exp2f(sc[f][kt][rr] - mr);
+          l[f] += pv1;
+          sc[f][kt][rr] = pv1;
+          if constexpr (E4) {
+            const float w = pv1 * scale_of((vsr[kt] >> (8 * rr)) & 255u);
+            sc[f][kt][rr] = whole || !dead(f, kt, rr) ? w : 0.f;  // the scale of an unused slot may be infinite
+          }
+        }
+#pragma unroll
+      for (int s2 = 0; s2 < S2; ++s2) {
+        const f32x4_t &x = sc[f][2 * s2], &y = sc[f][2 * s2 + 1];
+        pf[f][s2] = __builtin_bit_cast(bf16x8_t, make_uint4(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(y[0], y[1]),
+                                                            f2bf2(y[2], y[3])));
+      }
+    }
+    // Values. In a tile that some row does not see whole, a probability of 0 must meet no infinity or NaN: what lies in
+    // a slot past the last key becomes 0, and a key that only some rows see gives infinities and NaN to just those.
+    if (!whole) {
+      const int nv = pid_v < 0 ? 0 : kend - k0;  // the lane group's keys that are there
+      uint32_t odd = 0;
+#pragma unroll
+      for (int j = 0; j < VW; ++j) {
+        const int bits = E4 ? 8 * (nv - 4 * j) : 16 * (nv - 2 * j);
+        const uint32_t keep = bits >= 32 ? ~0u : bits <= 0 ? 0u : (1u << bits) - 1u;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const uint32_t w = vr[dt][j] &= keep;
+          odd |= E4 ? ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u : ((w & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u;
+        }
+      }
+      if (__builtin_amdgcn_ballot_w64(odd != 0)) {
+        uint4 sees[QF][S2];  // 1 where the row sees the key
+#pragma unroll
+        for (int f = 0; f < QF; ++f)
+#pragma unroll
+          for (int s2 = 0; s2 < S2; ++s2) {
+            uint32_t* sp = &sees[f][s2].x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              sp[j] = (dead(f, 2 * s2 + (j >> 1), 2 * (j & 1)) ? 0u : 0x3F80u) |
+                      (dead(f, 2 * s2 + (j >> 1), 2 * (j & 1) + 1) ? 0u : 0x3F800000u);
+          }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int s2 = 0; s2 < S2; ++s2) {
+            __builtin_amdgcn_sched_barrier(0);
+            // 1 where the value is +inf or NaN, 1 where it is -inf or NaN; those values become 0
+            uint4 up, dn;
+            uint32_t *upp = &up.x, *dnp = &dn.x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              upp[j] = dnp[j] = 0;
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                if constexpr (E4) {
+                  uint32_t* w = &vr[dt][2 * s2 + (j >> 1)];
+                  const int sh = 16 * (j & 1) + 8 * e;
+                  if (((*w >> sh) & 0x7Fu) == 0x7Fu) {
+                    upp[j] |= 0x3F80u << (16 * e);
+                    dnp[j] |= 0x3F80u << (16 * e);
+                    *w &= ~(0xFFu << sh);
+                  }
+                } else {
+                  uint32_t* w = &vr[dt][j];
+                  const uint32_t x = (*w >> (16 * e)) & 0xFFFFu;
+                  if ((x & 0x7F80u) == 0x7F80u) {
+                    if (x != 0xFF80u) upp[j] |= 0x3F80u << (16 * e);
+                    if (x != 0x7F80u) dnp[j] |= 0x3F80u << (16 * e);
+                    *w &= ~(0xFFFFu << (16 * e));
+                  }
+                }
+              }
+            }
+            const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int f = 0; f < QF; ++f) {
+              const bf16x8_t sv = __builtin_bit_cast(bf16x8_t, sees[f][s2]);
+              const f32x4_t cu = mfma16p(__builtin_bit_cast(bf16x8_t, up), sv, zero);
+              const f32x4_t cd = mfma16p(__builtin_bit_cast(bf16x8_t, dn), sv, zero);
+#pragma unroll
+              for (int rr = 0; rr < 4; ++rr) {
+                if (cu[rr] > 0.f) o[f][dt][rr] += INFINITY;
+                if (cd[rr] > 0.f) o[f][dt][rr] -= INFINITY;
+              }
+            }
+          }
+      }
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int s2 = 0; s2 < S2; ++s2) {
+        const bf16x8_t vf = value_fragment(dt, s2);
+#pragma unroll
+        for (int f = 0; f < QF; ++f) o[f][dt] = mfma16p(vf, pf[f][s2], o[f][dt]);
+      }
+    if (t + 4 < t1) {
+      load_values(t + 4, pv);
+      if (t + 8 < t1) {
+        pk = page_at(t + 8, la);
+        pv = page_at(t + 8, lg);
+      }
+    }
+  }
+
+  // the waves' (m, l, o) joined in wave order, query fragment by query fragment
+#pragma unroll
+  for (int f = 0; f < QF; ++f) {
+    if (f) __syncthreads();
+    l[f] = sum_groups(l[f]);
+    if (wid > 0) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) xo[wid - 1][dt][lane] = o[f][dt];
+      xml[wid - 1][lane] = make_float2(m[f], l[f]);
+    }
+    __syncthreads();
+    if (wid > 0) continue;
+    float mm = m[f];
+#pragma unroll
+    for (int w = 0; w < 3; ++w) mm = fmaxf(mm, xml[w][lane].x);
+    const float ref = finite_ref(mm), e0 = __builtin_amdgcn_exp2f(m[f] - ref);
+    float lt = l[f] * e0;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[f][dt] *= e0;
+#pragma unroll
+    for (int w = 0; w < 3; ++w) {
+      const float2 ml = xml[w][lane];
+      if (ml.x == -INFINITY && ml.y == 0.f) continue;  // a wave without keys
+      const float e = __builtin_amdgcn_exp2f(ml.x - ref);
+      lt += ml.y * e;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[f][dt] += xo[w][dt][lane] * e;
+    }
+    const int rr = row0 + 16 * f + lq;
+    if (rr >= rows) continue;
+    const size_t at = (size_t)(r.first + rr / a.g) * a.H + h * a.g + rr % a.g;
+    if (a.nsplit > 1) {
+      float* dst = a.po + ((size_t)part * p.T * a.H + at) * DH + 4 * lg;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = o[f][dt];
+      if (lg == 0) a.pml[(size_t)part * p.T * a.H + at] = make_float2(mm, lt);
+    } else {
+      const float inv = lt == 0.f ? 0.f : 1.0f / lt;  // a row without keys is zeros
+      bf16_t* dst = a.out + at * DH + 4 * lg;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        *reinterpret_cast<uint2*>(dst + 16 * dt) =
+            make_uint2(f2bf2(o[f][dt][0] * inv, o[f][dt][1] * inv), f2bf2(o[f][dt][2] * inv, o[f][dt][3] * inv));
+      if (a.lse && lg == 0) a.lse[at] = lt == 0.f ? -INFINITY : mm * 0.6931471805599453f + logf(lt);
+    }
+  }
+}
+
+// The parts of a sequence's rows joined, in order: DH / 4 lanes per (row, head).
+template <int DH>
+__global__ void __launch_bounds__(256) pages_join_kernel(PagesAttn a, int head_blocks) {
+  constexpr int L = DH / 4, PER = 256 / L;
+  const Pages& p = a.p;
+  const int hb = blockIdx.x % head_blocks, bi = blockIdx.x / head_blocks, i = bi % p.max_new, b = bi / p.max_new;
+  const SeqRows r = seq_rows(p.cu, b, p.T);
+  const int head = hb * PER + threadIdx.x / L, c = threadIdx.x % L;
+  if (i >= r.n || head >= a.H) return;
+  const int kend = min(seq_len(p.len, b), p.max_pages << p.shift), per = tiles_per_part(kend, a.nsplit);
+  const int parts = per == 0 ? 1 : ((kend + 63) / 64 + per - 1) / per;
+  const size_t at = (size_t)(r.first + i) * a.H + head, step = (size_t)p.T * a.H;
+  float mm = -INFINITY;
+  for (int s = 0; s < parts; ++s) mm = fmaxf(mm, a.pml[s * step + at].x);
+  const float ref = finite_ref(mm);
+  float lt = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = 0; s < parts; ++s) {
+    const float2 ml = a.pml[s * step + at];
+    if (ml.x == -INFINITY && ml.y == 0.f) continue;  // a part without keys that the row sees
+    const float e = __builtin_amdgcn_exp2f(ml.x - ref);
+    const float4 x = *reinterpret_cast<const float4*>(a.po + (s * step + at) * DH + 4 * c);
+    lt += ml.y * e;
+    o.x += x.x * e;
+    o.y += x.y * e;
+    o.z += x.z * e;
+    o.w += x.w * e;
+  }
+  const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+  *reinterpret_cast<uint2*>(a.out + at * DH + 4 * c) = make_uint2(f2bf2(o.x * inv, o.y * inv), f2bf2(o.z * inv, o.w * inv));
+  if (a.lse && c == 0) a.lse[at] = lt == 0.f ? -INFINITY : mm * 0.6931471805599453f + logf(lt);
+}
+
+// Query fragments per wave: as many as the rows of a KV head fill, up to four.
+static int query_fragments(int g, int max_new) {
+  const long rows = (long)g * max_new;
+  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+}
+
+int pages_attention_splits(int Hkv, int g, int B, int max_new, int capacity) {
+  const int qf = query_fragments(g, max_new);
+  const long units = (((long)g * max_new + 16 * qf - 1) / (16 * qf)) * Hkv * B;
+  if (units < 1) return 1;
+  const long most = (capacity + 255) / 256;  // at least 64 keys per wave
+  long n = (1024 + units - 1) / units;
+  n = n < 1 ? 1 : n > most ? most : n;
+  return n < 1 ? 1 : n > 64 ? 64 : (int)n;
+}
+
+template <int DH, bool E4>
+static void run_pages_attention(PagesAttn& a, hipStream_t s) {
+  const int qf = query_fragments(a.g, a.p.max_new);
+  a.row_tiles = (int)(((long)a.g * a.p.max_new + 16 * qf - 1) / (16 * qf));
+  const long items = (long)a.nsplit * a.p.B * a.p.Hkv;
+  const dim3 grid((unsigned)((items + 7) / 8 * 8 * a.row_tiles));
+  if (qf == 1) hipLaunchKernelGGL((pages_attn_kernel<DH, E4, 1>), grid, dim3(256), 0, s, a);
+  else if (qf == 2) hipLaunchKernelGGL((pages_attn_kernel<DH, E4, 2>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((pages_attn_kernel<DH, E4, 4>), grid, dim3(256), 0, s, a);
+  if (a.nsplit > 1) {
+    const int blocks = (a.H + 1024 / DH - 1) / (1024 / DH);
+    hipLaunchKernelGGL(pages_join_kernel<DH>, dim3((unsigned)blocks * a.p.max_new * a.p.B), dim3(256), 0, s, a, blocks);
+  }
+}
+
+void launch_pages_attention(PagesAttn a, hipStream_t s) {
+  if (a.p.T == 0 || a.p.max_new == 0) return;
+  if (a.p.dh == 128) a.p.e4m3 ? run_pages_attention<128, true>(a, s) : run_pages_attention<128, false>(a, s);
+  else a.p.e4m3 ? run_pages_attention<64, true>(a, s) : run_pages_attention<64, false>(a, s);
+}
+
+}  // namespace dcl

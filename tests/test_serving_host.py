@@ -1,0 +1,167 @@
+"""The serving operators' refusals (host only: nothing is launched), and their index functions on hostile data."""
+import ctypes
+import os
+import shutil
+import subprocess
+
+import pytest
+import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def dcl():
+    from paper_2607_20467_amd import build
+    if build.is_stale():
+        build.build()
+    import paper_2607_20467_amd as m
+    m.load_library()
+    return m
+
+
+def pool(dcl, **kw):
+    f = dict(k=256, v=256, k_scale=0, v_scale=0, n_pages=4, page_len=16, n_kv_heads=2, head_dim=64, dtype=1)
+    f.update(kw)
+    return dcl.DclPages(*(f[n] for n, _ in dcl.DclPages._fields_))
+
+
+BATCH = dict(table=256, max_pages=2, len=256, cu=256, B=1, T=4, max_new=4)
+
+
+def call(dcl, name, pages, tail, **kw):
+    b = dict(BATCH)
+    b.update(kw)
+    r = getattr(dcl.load_library(), name)(ctypes.byref(pages) if pages is not None else None,
+                                          *(b[n] for n in BATCH), *tail)
+    return r, dcl.dcl_last_error()
+
+
+COPY = (256, 128, 256, 128, None)
+ATTN = (256, 256, 4, 0.125, 1, 256, 256, 256, 1 << 40, None)
+
+
+@pytest.mark.parametrize("name,tail", [("dcl_pages_write", COPY), ("dcl_pages_read", COPY), ("dcl_pages_attention", ATTN)])
+@pytest.mark.parametrize("pages,batch,status,word", [
+    (None, {}, 1, "pages"),
+    (dict(dtype=0), {}, 2, "dtype"),
+    (dict(head_dim=96), {}, 2, "head_dim"),
+    (dict(n_kv_heads=0), {}, 1, "n_kv_heads"),
+    (dict(page_len=24), {}, 1, "page_len"),
+    (dict(page_len=8), {}, 1, "page_len"),
+    (dict(page_len=2048), {}, 1, "page_len"),
+    (dict(n_pages=0), {}, 1, "n_pages"),
+    (dict(k=0), {}, 1, "k / v"),
+    (dict(v=264), {}, 1, "aligned"),
+    (dict(dtype=2), {}, 1, "k_scale"),
+    (dict(dtype=2, k_scale=256, v_scale=257), {}, 1, "aligned"),
+    ({}, dict(table=0), 1, "table"),
+    ({}, dict(len=0), 1, "len"),
+    ({}, dict(cu=0), 1, "cu"),
+    ({}, dict(B=0), 1, "B=0"),
+    ({}, dict(B=70000), 1, "B="),
+    ({}, dict(T=-1), 1, "T="),
+    ({}, dict(T=1 << 23), 1, "T="),
+    ({}, dict(max_new=-1), 1, "max_new"),
+    ({}, dict(max_pages=0), 1, "max_pages"),
+    ({}, dict(max_pages=1 << 25), 1, "max_pages"),
+])
+def test_pages_refusals(dcl, name, tail, pages, batch, status, word):
+    r, msg = call(dcl, name, None if pages is None else pool(dcl, **pages), tail, **batch)
+    assert r == status and word in msg, (r, msg)
+
+
+@pytest.mark.parametrize("tail,status,word", [
+    ((0, 128, 256, 128, None), 1, "k is NULL"),
+    ((256, 120, 256, 128, None), 1, "stride"),
+    ((256, 132, 256, 128, None), 1, "stride"),
+    ((256, 128, 264, 128, None), 1, "aligned"),
+])
+def test_pages_copy_refusals(dcl, tail, status, word):
+    for name in ("dcl_pages_write", "dcl_pages_read"):
+        r, msg = call(dcl, name, pool(dcl), tail)
+        assert r == status and word in msg, (r, msg)
+
+
+@pytest.mark.parametrize("change,status,word", [
+    ({0: 0}, 1, "q is NULL"), ({1: 128}, 1, "stride"), ({2: 3}, 2, "n_heads"), ({2: 0}, 2, "n_heads"),
+    ({3: float("nan")}, 1, "scale"), ({3: float("inf")}, 1, "scale"), ({4: 2}, 1, "causal"), ({5: 0}, 1, "out"),
+    ({5: 8}, 1, "aligned"), ({7: 0}, 1, "workspace"), ({7: 64}, 1, "aligned"), ({8: 16}, 3, "workspace"),
+])
+def test_pages_attention_refusals(dcl, change, status, word):
+    tail = [change.get(i, x) for i, x in enumerate(ATTN)]
+    r, msg = call(dcl, "dcl_pages_attention", pool(dcl), tail)
+    assert r == status and word in msg, (r, msg)
+
+
+def test_pages_workspace_sizes(dcl):
+    f = dcl.load_library().dcl_pages_attention_workspace_bytes
+    g = pool(dcl)
+    assert f(ctypes.byref(g), 4, 1, 4, 4, 2) >= 256
+    assert f(ctypes.byref(g), 4, 1, 0, 0, 2) >= 256               # nothing to do is no error
+    for bad in ((3, 1, 4, 4, 2), (4, 0, 4, 4, 2), (4, 1, -1, 4, 2), (4, 1, 4, -1, 2), (4, 1, 4, 4, 0)):
+        assert f(ctypes.byref(g), *bad) == 0
+    assert f(None, 4, 1, 4, 4, 2) == 0
+    # one token of a long sequence is split; the parts of many tokens need more
+    one, many = f(ctypes.byref(g), 4, 1, 1, 1, 1 << 14), f(ctypes.byref(g), 4, 1, 2, 2, 1 << 14)
+    assert 256 < one < many
+
+
+def test_pools_and_operands_are_checked_by_the_binding(dcl):
+    cpu = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    with pytest.raises(dcl.DclError, match="device"):
+        dcl.KVPages(4, 16, 2, 64, k=cpu)
+    with pytest.raises(dcl.DclError, match="shape"):
+        dcl.KVPages(5, 16, 2, 64, k=cpu)
+    with pytest.raises(dcl.DclError, match="positive"):
+        dcl.KVPages(0, 16, 2, 64)
+    with pytest.raises(dcl.DclError, match="dtype"):
+        dcl.KVPages(4, 16, 2, 64, dtype=0)
+    with pytest.raises(dcl.DclError, match="KVPages"):
+        dcl.dcl_pages_write(None, cpu, cpu, cpu, 1, 4, 4, cpu, cpu)
+
+
+PROBE = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "pages_index.h"
+using namespace dcl;
+int main() {
+  unsigned s = 1;
+  auto rnd = [&]() { s = s * 1664525u + 1013904223u; return (int)s; };
+  const int odd[] = {0, 1, -1, 2147483647, -2147483647 - 1, 64, 63, 1 << 30, -(1 << 30)};
+  auto any = [&]() { int r = rnd(); return (r & 3) ? odd[(unsigned)r % 9] : r >> ((unsigned)r % 31); };
+  for (long i = 0; i < 2000000; ++i) {
+    int cu[3] = {any(), any(), any()}, len[1] = {any()};
+    const int T = (unsigned)any() % 4194305u;
+    for (int b = 0; b < 2; ++b) {
+      const SeqRows r = seq_rows(cu, b, T);
+      if (r.first < 0 || r.n < 0 || r.first > T || r.n > T - r.first) return std::printf("rows %d %d of %d\n", r.first, r.n, T), 1;
+      if (cu[b] >= 0 && cu[b] <= cu[b + 1] && cu[b + 1] <= T && (r.first != cu[b] || r.n != cu[b + 1] - cu[b])) return 2;
+    }
+    const int L = seq_len(len, 0);
+    if (L < 0 || L > 1 << 30) return 3;
+    int table[4] = {any(), any(), any(), any()};
+    const int n_pages = 1 + (unsigned)any() % 1000, shift = 4 + (unsigned)rnd() % 7, width = 1 + (unsigned)rnd() % 4, c = any();
+    const int p = page_of(table, width, n_pages, shift, c);
+    if (p < -1 || p >= n_pages) return 4;
+    if (p >= 0 && (c < 0 || (c >> (shift - 4)) >= width || table[c >> (shift - 4)] != p)) return 5;
+  }
+  std::puts("ok");
+  return 0;
+}
+"""
+
+
+def test_index_functions_stay_inside_for_any_device_data(tmp_path):
+    """What the kernels make of borders, lengths and page numbers, compiled for the host with bounds checking."""
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("g++ is not installed")
+    src = tmp_path / "probe.cpp"
+    src.write_text(PROBE)
+    exe = tmp_path / "probe"
+    subprocess.run([cxx, "-O1", "-g", "-std=c++17", "-fsanitize=undefined,bounds", "-fno-sanitize-recover=all", "-I",
+                    os.path.join(ROOT, "paper_2607_20467_amd", "csrc"), str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "ok" in r.stdout, (r.returncode, r.stdout, r.stderr)
