@@ -265,6 +265,16 @@ dcl_status dcl_score_hidden(dcl_model_t model, const void* hidden, int32_t n, dc
  * T = 0 does nothing. Device data is never trusted for an address: borders, lengths and page numbers outside their
  * ranges give fewer rows or keys, not a fault. */
 
+/* Attention over whole prompts: out[t, h] = sum_j softmax_j(scale q[t, h] . k_j) v_j over the rows j of t's own
+ * sequence, with causal = 1 those up to t. q: [T, n_heads, head_dim], k and v: [T, n_kv_heads, head_dim], head h reads
+ * KV head h / (n_heads / n_kv_heads). out: bf16 [T, n_heads, head_dim]; lse (NULL: not written): float32 [T, n_heads],
+ * the natural logarithm of the sum of exponentials. A key that a row does not see has no effect on it, whatever it
+ * holds. Needs no workspace; results are bitwise reproducible. */
+dcl_status dcl_prompt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                int64_t v_stride, const int32_t* cu, int32_t B, int32_t T, int32_t max_len,
+                                int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float scale, int32_t causal,
+                                void* out, float* lse, hipStream_t stream);
+
 /* A pool of pages for keys (after RoPE) and values of many sequences: page_len (a power of two, 16 to 1024) positions
  * each. dtype DCL_DTYPE_BF16: bf16 elements, scales NULL. DCL_DTYPE_E4M3: elements are 8-bit floats (sign, 4 exponent
  * bits, 3 fraction bits, no infinity) times one power-of-two scale 2^(byte - 127) per (position, KV head), the byte

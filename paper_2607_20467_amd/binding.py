@@ -109,6 +109,8 @@ def load_library():
         "dcl_score_hidden": (ctypes.c_int, [vp, vp, i32, DclRowStats, vp, sz, vp]),
         "dcl_debug_logits": (ctypes.c_int, [vp, vp, i32, i32, ctypes.POINTER(DclKV), vp, i32, vp, vp, vp, sz, vp]),
         "dcl_debug_layer": (ctypes.c_int, [vp, i32, i32, ctypes.POINTER(DclKV), i32, vp, DclLayerTaps, vp, sz, vp]),
+        "dcl_prompt_attention": (ctypes.c_int, [vp, i64, vp, i64, vp, i64, vp, i32, i32, i32, i32, i32, i32, f32, i32,
+                                                vp, vp, vp]),
         "dcl_pages_write": (ctypes.c_int, batch + [vp, i64, vp, i64, vp]),
         "dcl_pages_read": (ctypes.c_int, batch + [vp, i64, vp, i64, vp]),
         "dcl_pages_attention_workspace_bytes": (sz, [pages, i32, i32, i32, i32, i32]),
@@ -417,6 +419,21 @@ def _packed(x, name, where, T, heads, dim):
         raise DclError(1, where, f"{name} {bad}")
     _on_current(x, name, where)
     return x.data_ptr(), x.stride(0) if T > 1 else heads * dim
+
+
+def dcl_prompt_attention(q, k, v, cu, B: int, T: int, max_len: int, n_heads: int, n_kv_heads: int, head_dim: int,
+                         scale: float, causal: bool, out, lse=None, stream=None) -> None:
+    """q [T, n_heads, head_dim], k and v [T, n_kv_heads, head_dim] (rows may be apart), sequences by ``cu`` [B + 1];
+    out like q (contiguous), lse [T, n_heads] float32 or None."""
+    w = "dcl_prompt_attention"
+    qp, qs = _packed(q, "q", w, T, n_heads, head_dim)
+    kp, ks = _packed(k, "k", w, T, n_kv_heads, head_dim)
+    vp, vs = _packed(v, "v", w, T, n_kv_heads, head_dim)
+    n = max(T, 0) * n_heads
+    _check(load_library().dcl_prompt_attention(qp, qs, kp, ks, vp, vs, _here(cu, "cu", w, _I32, max(B, 0) + 1), B, T,
+                                               max_len, n_heads, n_kv_heads, head_dim, scale, int(causal),
+                                               _here(out, "out", w, _B16, n * head_dim),
+                                               _here(lse, "lse", w, _F32, n), _stream(stream)), w)
 
 
 def _batch(pages, table, length, cu, B, T, max_new, where):

@@ -197,4 +197,44 @@ dcl_status dcl_pages_attention(const dcl_pages* pages, const int32_t* table, int
   return hip_check(hipGetLastError(), "pages_attention launch");
 }
 
+dcl_status dcl_prompt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                int64_t v_stride, const int32_t* cu, int32_t B, int32_t T, int32_t max_len,
+                                int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float scale, int32_t causal,
+                                void* out, float* lse, hipStream_t stream) {
+  dcl_status st = check_batch(cu, B, T, max_len, "max_len");
+  if (st == DCL_OK) st = check_head_dim(head_dim);
+  if (st == DCL_OK) st = check_heads(n_heads, n_kv_heads);
+  if (st == DCL_OK) st = check_rows("q", q, q_stride, T, n_heads, head_dim);
+  if (st == DCL_OK) st = check_rows("k", k, k_stride, T, n_kv_heads, head_dim);
+  if (st == DCL_OK) st = check_rows("v", v, v_stride, T, n_kv_heads, head_dim);
+  if (st == DCL_OK) st = check_rows("out", out, (int64_t)n_heads * head_dim, T, n_heads, head_dim);
+  if (st != DCL_OK) return st;
+  if (!isfinite(scale)) return fail(DCL_E_ARG, "scale must be finite");
+  if (causal != 0 && causal != 1) return fail(DCL_E_ARG, "causal must be 0 or 1");
+  if (((int64_t)B * n_heads + 8) * (max_len / 64 + 1) >= (1LL << 31))
+    return fail(DCL_E_UNSUPPORTED, "B=%d sequences of %d rows x %d heads: too many for one call", B, max_len, n_heads);
+  PromptAttn a;
+  a.q = static_cast<const bf16_t*>(q);
+  a.k = static_cast<const bf16_t*>(k);
+  a.v = static_cast<const bf16_t*>(v);
+  a.q_stride = (long)q_stride;
+  a.k_stride = (long)k_stride;
+  a.v_stride = (long)v_stride;
+  a.out = static_cast<bf16_t*>(out);
+  a.lse = lse;
+  a.cu = cu;
+  a.B = B;
+  a.T = T;
+  a.max_len = max_len;
+  a.H = n_heads;
+  a.Hkv = n_kv_heads;
+  a.dh = head_dim;
+  a.causal = causal;
+  a.q_tiles = 0;
+  a.scale_log2 = (float)(1.4426950408889634 * (double)scale);
+  (void)hipGetLastError();
+  launch_prompt_attention(a, stream);
+  return hip_check(hipGetLastError(), "prompt_attention launch");
+}
+
 }  // extern "C"

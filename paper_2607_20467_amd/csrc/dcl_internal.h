@@ -212,4 +212,15 @@ struct PagesAttn {
 int pages_attention_splits(int Hkv, int g, int B, int max_new, int capacity);
 void launch_pages_attention(PagesAttn a, hipStream_t s);
 
+struct PromptAttn {
+  const bf16_t *q, *k, *v;       // [T, H, dh], [T, Hkv, dh] with row strides
+  long q_stride, k_stride, v_stride;
+  bf16_t* out;                   // [T, H, dh]
+  float* lse;                    // [T, H] or null
+  const int32_t* cu;             // [B + 1]
+  int B, T, max_len, H, Hkv, dh, causal, q_tiles;
+  float scale_log2;
+};
+void launch_prompt_attention(PromptAttn a, hipStream_t s);
+
 }  // namespace dcl

@@ -165,3 +165,18 @@ def test_index_functions_stay_inside_for_any_device_data(tmp_path):
                     os.path.join(ROOT, "paper_2607_20467_amd", "csrc"), str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and "ok" in r.stdout, (r.returncode, r.stdout, r.stderr)
+
+
+PROMPT = (256, 256, 256, 128, 256, 128, 256, 1, 4, 4, 4, 2, 64, 0.125, 1, 256, 0, None)
+
+
+@pytest.mark.parametrize("change,status,word", [
+    ({0: 0}, 1, "q is NULL"), ({1: 255}, 1, "stride"), ({1: 248}, 1, "stride"), ({2: 0}, 1, "k is NULL"), ({3: 64}, 1, "stride"),
+    ({4: 8}, 1, "aligned"), ({5: 120}, 1, "stride"), ({6: 0}, 1, "cu"), ({7: 0}, 1, "B=0"), ({8: -1}, 1, "T="),
+    ({9: -1}, 1, "max_len"), ({10: 3}, 2, "n_heads"), ({11: 0}, 2, "n_heads"), ({12: 80}, 2, "head_dim"),
+    ({13: float("inf")}, 1, "scale"), ({14: 5}, 1, "causal"), ({15: 0}, 1, "out"),
+    ({7: 60000, 9: 1 << 22, 8: 1 << 22}, 2, "too many"),
+])
+def test_prompt_refusals(dcl, change, status, word):
+    r = dcl.load_library().dcl_prompt_attention(*[change.get(i, x) for i, x in enumerate(PROMPT)])
+    assert r == status and word in dcl.dcl_last_error(), (r, dcl.dcl_last_error())
