@@ -325,6 +325,42 @@ dcl_status dcl_pages_attention(const dcl_pages* pages, const int32_t* table, int
                                int64_t q_stride, int32_t n_heads, float scale, int32_t causal, void* out, float* lse,
                                void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* How tokens are drawn, one value per row (device arrays of n; NULL: the filter is off, temperature 1). */
+typedef struct {
+  const float* temperature; /* > 0; anything else draws the top-1 */
+  const int32_t* top_k;     /* keep the k likeliest ids; <= 0: all */
+  const float* top_p;       /* of those, the shortest prefix whose probability reaches top_p; >= 1: all */
+  const float* min_p;       /* and of the ids those with at least min_p of the likeliest one's probability; <= 0: all */
+  const float* uniform;     /* the random number of the row, in [0, 1); required */
+} dcl_sampling;
+
+/* Workspace bytes of dcl_sample_tokens; 0 if the sizes are invalid. */
+size_t dcl_sample_workspace_bytes(int32_t n, int32_t vocab);
+
+/* Draws a token per row of logits [n, vocab] (dtype DCL_DTYPE_F32 or DCL_DTYPE_BF16, rows row_stride elements apart,
+ * aligned to its elements). The row's ids in order (logit descending, ids ascending among equals) have weights w = exp((x -
+ * max x) / temperature); -inf and NaN take no part. top_k keeps the first k; top_p, of the sum of those weights, every
+ * id before which less than top_p of it lies; min_p the ids with w >= min_p; each keeps at least the first id, and an id
+ * is kept if all keep it. The token is the first kept id at which the running sum of kept weights passes uniform * their
+ * sum. Writes token[n] (-1 for a row without a logit above -inf), conf[n] (may be NULL: the token's share of the kept
+ * sum, 0 without a token) and kept[n] (may be NULL: ids kept; those whose weight is 0 count). The top-1 alone (temperature
+ * not > 0, or top_k 1): token the lowest best id, conf 1, kept 1. Sums are exact in fixed point (42 bits and more below
+ * the row's largest weight), so a border falls as exact arithmetic has it and results are bitwise reproducible.
+ * token and conf can stand for dcl_row_stats' top1 and conf in dcl_select_contiguous. 0 <= n <= 2^22, 1 <= vocab <=
+ * 2^20; ws: device, 256-byte aligned, ws_bytes >= dcl_sample_workspace_bytes. */
+dcl_status dcl_sample_tokens(const void* logits, int32_t dtype, int64_t row_stride, int32_t n, int32_t vocab,
+                             const dcl_sampling* how, int32_t* token, float* conf, int32_t* kept, void* ws,
+                             size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of dcl_sample_hidden over n rows; 0 if the arguments are invalid. */
+size_t dcl_sample_hidden_workspace_bytes(dcl_model_t model, int32_t n);
+
+/* The same on given final hidden states (bf16 [n, d_model], device, 16-byte aligned, already final-normalised, as for
+ * dcl_score_hidden): the model's LM head into float32 logits in ws, then dcl_sample_tokens. n * vocab < 2^31 and
+ * n * d_model < 2^31. */
+dcl_status dcl_sample_hidden(dcl_model_t model, const void* hidden, int32_t n, const dcl_sampling* how, int32_t* token,
+                             float* conf, int32_t* kept, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* Test support: the same forward as dcl_denoise_step, then float32 logits of the rows listed in
  * `rows` (device [n_rows], flat indices b*S + i; an index outside [0, B*S) gives a zero hidden
  * row) into out (device [n_rows, vocab]); if hidden_out is not NULL it also receives those rows'

@@ -16,6 +16,7 @@ from .binding import (  # noqa: F401
 from . import binding  # noqa: F401,E402
 from .binding import DCL_NOALLOC_SCRATCH_BYTES, dcl_denoise_step_noalloc  # noqa: F401,E402
 from .binding import (  # noqa: F401,E402
-    DCL_DTYPE_E4M3, DclPages, KVPages, dcl_pages_attention, dcl_pages_attention_workspace_bytes, dcl_pages_read,
-    dcl_pages_write, dcl_prompt_attention,
+    DCL_DTYPE_E4M3, DclPages, DclSampling, KVPages, dcl_pages_attention, dcl_pages_attention_workspace_bytes, dcl_pages_read,
+    dcl_pages_write, dcl_prompt_attention, dcl_sample_hidden, dcl_sample_hidden_workspace_bytes, dcl_sample_tokens,
+    dcl_sample_workspace_bytes,
 )

@@ -50,6 +50,10 @@ class DclPages(ctypes.Structure):
                [(n, ctypes.c_int32) for n in ("n_pages", "page_len", "n_kv_heads", "head_dim", "dtype")]
 
 
+class DclSampling(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p", "uniform")]
+
+
 PROF_CLASSES = ("embed", "rmsnorm", "gemm_qkv_rope", "attention", "gemm_o_residual", "gemm_gate_up_swiglu",
                 "gemm_down_residual", "compact_rows", "gemm_lm_head_top2", "merge_partials", "select")
 
@@ -85,6 +89,7 @@ def load_library():
     lib = ctypes.CDLL(path)
     vp, i32, u32, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_float, ctypes.c_size_t
     i64, pages = ctypes.c_int64, ctypes.POINTER(DclPages)
+    how = ctypes.POINTER(DclSampling)
     batch = [pages, vp, i32, vp, vp, i32, i32, i32]     # pool, table, max_pages, len, cu, B, T, max_new
     sig = {
         "dcl_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -115,6 +120,10 @@ def load_library():
         "dcl_pages_read": (ctypes.c_int, batch + [vp, i64, vp, i64, vp]),
         "dcl_pages_attention_workspace_bytes": (sz, [pages, i32, i32, i32, i32, i32]),
         "dcl_pages_attention": (ctypes.c_int, batch + [vp, i64, i32, f32, i32, vp, vp, vp, sz, vp]),
+        "dcl_sample_workspace_bytes": (sz, [i32, i32]),
+        "dcl_sample_tokens": (ctypes.c_int, [vp, i32, i64, i32, i32, how, vp, vp, vp, vp, sz, vp]),
+        "dcl_sample_hidden_workspace_bytes": (sz, [vp, i32]),
+        "dcl_sample_hidden": (ctypes.c_int, [vp, vp, i32, how, vp, vp, vp, vp, sz, vp]),
         "dcl_debug_gemm_plan": (ctypes.c_int, [i32, i32, i32, i32, i32, ctypes.POINTER(i32)]),
     }
     for name, (res, args) in sig.items():
@@ -530,6 +539,58 @@ def dcl_pages_attention(pages: KVPages, table, length, cu, B: int, T: int, max_n
                                               _arg(ws, "ws", w, _ANY, nbytes=ws_bytes), ws_bytes, _stream(stream)), w)
 
 
+def dcl_sample_workspace_bytes(n: int, vocab: int) -> int:
+    return load_library().dcl_sample_workspace_bytes(n, vocab)
+
+
+def _sampling(n, temperature, top_k, top_p, min_p, uniform, where):
+    return DclSampling(_here(temperature, "temperature", where, _F32, n), _here(top_k, "top_k", where, _I32, n),
+                       _here(top_p, "top_p", where, _F32, n), _here(min_p, "min_p", where, _F32, n),
+                       _here(uniform, "uniform", where, _F32, n))
+
+
+def dcl_sample_tokens(logits, n: int, vocab: int, temperature, top_k, top_p, min_p, uniform, token, conf, kept, ws,
+                      ws_bytes: int, stream=None) -> None:
+    """logits [n, vocab] float32 or bfloat16 (rows may be apart); temperature, top_p, min_p, uniform float32 [n], top_k
+    int32 [n] (all but uniform may be None); token, kept int32 [n], conf float32 [n] (conf and kept may be None)."""
+    w = "dcl_sample_tokens"
+    kind = str(getattr(logits, "dtype", "")).replace("torch.", "")
+    bad = None
+    if not getattr(logits, "is_cuda", False):
+        bad = "must be a device (cuda) tensor"
+    elif kind not in _F32 + _B16:
+        bad = f"has dtype {logits.dtype}, expected float32 or bfloat16"
+    elif logits.dim() != 2 or logits.shape[0] < n or logits.shape[1] < vocab:
+        bad = f"has shape {tuple(logits.shape)}, the call needs ({n}, {vocab})"
+    elif vocab > 1 and logits.stride(1) != 1:
+        bad = f"has strides {logits.stride()}, a row must be contiguous"
+    if bad:
+        raise DclError(1, w, f"logits {bad}")
+    _on_current(logits, "logits", w)
+    how = _sampling(max(n, 0), temperature, top_k, top_p, min_p, uniform, w)
+    _check(load_library().dcl_sample_tokens(logits.data_ptr(), DCL_DTYPE_F32 if kind == "float32" else DCL_DTYPE_BF16,
+                                            logits.stride(0) if n > 1 else vocab, n, vocab, ctypes.byref(how),
+                                            _here(token, "token", w, _I32, n), _here(conf, "conf", w, _F32, n),
+                                            _here(kept, "kept", w, _I32, n),
+                                            _arg(ws, "ws", w, _ANY, nbytes=ws_bytes), ws_bytes, _stream(stream)), w)
+
+
+def dcl_sample_hidden_workspace_bytes(model: int, n: int) -> int:
+    return load_library().dcl_sample_hidden_workspace_bytes(model, n)
+
+
+def dcl_sample_hidden(model: int, hidden, n: int, temperature, top_k, top_p, min_p, uniform, token, conf, kept, ws,
+                      ws_bytes: int, stream=None) -> None:
+    """The model's LM head on hidden [n, d_model] (bfloat16), then ``dcl_sample_tokens``."""
+    w = "dcl_sample_hidden"
+    g = _cfg_of(model)
+    how = _sampling(max(n, 0), temperature, top_k, top_p, min_p, uniform, w)
+    _check(load_library().dcl_sample_hidden(model, _here(hidden, "hidden", w, _B16, n * g.d_model if g else None), n,
+                                            ctypes.byref(how), _here(token, "token", w, _I32, n),
+                                            _here(conf, "conf", w, _F32, n), _here(kept, "kept", w, _I32, n),
+                                            _arg(ws, "ws", w, _ANY, nbytes=ws_bytes), ws_bytes, _stream(stream)), w)
+
+
 # ---------------------------------------------------------------- convenience owner of device buffers
 
 def config_from_geometry(g, max_positions: int = 4096, rope_enabled: bool = True) -> DclConfig:
@@ -622,6 +683,17 @@ class Runner:
         st = self.new_stats(1, n)
         dcl_score_hidden(self.model, hidden, n, st, ws, need, stream)
         return {k: v.view(n) for k, v in st.items()}
+
+    def sample_hidden(self, hidden, uniform, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+        """Tokens drawn from the head's distribution at given hidden rows: {"token", "conf", "kept"} (each [n])."""
+        n, t = hidden.shape[0], self.torch
+        need = dcl_sample_hidden_workspace_bytes(self.model, n)
+        ws = t.empty(need, dtype=t.uint8, device="cuda")
+        out = {"token": t.empty(n, dtype=t.int32, device="cuda"), "conf": t.empty(n, device="cuda"),
+               "kept": t.empty(n, dtype=t.int32, device="cuda")}
+        dcl_sample_hidden(self.model, hidden, n, temperature, top_k, top_p, min_p, uniform, out["token"], out["conf"],
+                          out["kept"], ws, need, stream)
+        return out
 
     def close(self):
         if self.model:

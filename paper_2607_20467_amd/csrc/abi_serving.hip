@@ -127,6 +127,51 @@ dcl_status check_attention_size(const dcl_pages* g, int32_t n_heads, int32_t B, 
   return DCL_OK;
 }
 
+// Most vocabulary ids of a sampled row: with 2^20 of them weights still have 42 bits.
+constexpr int kSampleVocab = 1 << 20;
+
+size_t sample_workspace(int32_t n, int32_t V) { return 256; }
+
+dcl_status check_sample(int32_t n, int32_t V, const dcl_sampling* how, const int32_t* token) {
+  if (n < 0 || n > (1 << 22)) return fail(DCL_E_ARG, "n=%d outside [0, 2^22]", n);
+  if (V < 1 || V > kSampleVocab) return fail(DCL_E_ARG, "vocab=%d outside [1, 2^20]", V);
+  if (!how) return fail(DCL_E_ARG, "how is NULL");
+  if (n > 0 && !how->uniform) return fail(DCL_E_ARG, "how.uniform is NULL");
+  if (n > 0 && !token) return fail(DCL_E_ARG, "token is NULL");
+  return DCL_OK;
+}
+
+dcl_status check_sample_workspace(const void* ws, size_t ws_bytes, size_t need) {
+  if (!ws) return fail(DCL_E_ARG, "workspace is NULL");
+  if (misaligned(ws, 256)) return fail(DCL_E_ARG, "workspace must be 256-byte aligned");
+  if (ws_bytes < need) return fail(DCL_E_WORKSPACE, "workspace %zu bytes < required %zu", ws_bytes, need);
+  return DCL_OK;
+}
+
+SampleArgs sample_args(const void* logits, int64_t stride, int bf16, int32_t n, int32_t V, const dcl_sampling& how,
+                       int32_t* token, float* conf, int32_t* kept, void* ws) {
+  SampleArgs a;
+  a.logits = logits;
+  a.stride = (long)stride;
+  a.n = n;
+  a.V = V;
+  a.bf16 = bf16;
+  int bits = 0;  // V <= 2^bits: the weights' sum stays below 2^62
+  while ((1 << bits) < V) ++bits;
+  a.shift = 62 - bits;
+  a.temperature = how.temperature;
+  a.top_k = how.top_k;
+  a.top_p = how.top_p;
+  a.min_p = how.min_p;
+  a.uniform = how.uniform;
+  a.token = token;
+  a.conf = conf;
+  a.kept = kept;
+  return a;
+}
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
 }  // namespace
 
 extern "C" {
@@ -235,6 +280,57 @@ dcl_status dcl_prompt_attention(const void* q, int64_t q_stride, const void* k, 
   (void)hipGetLastError();
   launch_prompt_attention(a, stream);
   return hip_check(hipGetLastError(), "prompt_attention launch");
+}
+
+size_t dcl_sample_workspace_bytes(int32_t n, int32_t vocab) {
+  if (n < 0 || n > (1 << 22) || vocab < 1 || vocab > kSampleVocab) return 0;
+  return sample_workspace(n, vocab);
+}
+
+dcl_status dcl_sample_tokens(const void* logits, int32_t dtype, int64_t row_stride, int32_t n, int32_t vocab,
+                             const dcl_sampling* how, int32_t* token, float* conf, int32_t* kept, void* ws,
+                             size_t ws_bytes, hipStream_t stream) {
+  dcl_status st = check_sample(n, vocab, how, token);
+  if (st != DCL_OK) return st;
+  if (dtype != DCL_DTYPE_F32 && dtype != DCL_DTYPE_BF16) return fail(DCL_E_UNSUPPORTED, "logits dtype %d: float32 or bfloat16", dtype);
+  if (n > 0 && !logits) return fail(DCL_E_ARG, "logits is NULL");
+  if (misaligned(logits, dtype == DCL_DTYPE_F32 ? 4 : 2)) return fail(DCL_E_ARG, "logits must be aligned to its elements");
+  if (row_stride < vocab || row_stride > ((int64_t)1 << 40)) return fail(DCL_E_ARG, "row stride %lld < vocab %d", (long long)row_stride, vocab);
+  st = check_sample_workspace(ws, ws_bytes, sample_workspace(n, vocab));
+  if (st != DCL_OK) return st;
+  (void)hipGetLastError();
+  launch_sample(sample_args(logits, row_stride, dtype == DCL_DTYPE_BF16, n, vocab, *how, token, conf, kept, ws), stream);
+  return hip_check(hipGetLastError(), "sample_tokens launch");
+}
+
+size_t dcl_sample_hidden_workspace_bytes(dcl_model_t model, int32_t n) {
+  const Model* m = reinterpret_cast<const Model*>(model);
+  if (!m || n < 0 || n > (1 << 22) || m->cfg.vocab > kSampleVocab || (int64_t)n * m->cfg.vocab >= (1LL << 31)) return 0;
+  return align256((size_t)n * m->cfg.vocab * 4) + sample_workspace(n, m->cfg.vocab);
+}
+
+dcl_status dcl_sample_hidden(dcl_model_t model, const void* hidden, int32_t n, const dcl_sampling* how, int32_t* token,
+                             float* conf, int32_t* kept, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const Model* m = reinterpret_cast<const Model*>(model);
+  if (!m) return fail(DCL_E_ARG, "model is NULL");
+  const int32_t V = m->cfg.vocab;
+  dcl_status st = check_sample(n, V, how, token);
+  if (st != DCL_OK) return st;
+  if ((int64_t)n * V >= (1LL << 31) || (int64_t)n * m->cfg.d_model >= (1LL << 31))
+    return fail(DCL_E_UNSUPPORTED, "n=%d rows: the head addresses fewer than 2^31 elements", n);
+  if (!m->loaded) return fail(DCL_E_STATE, "weights not loaded");
+  if (n > 0 && !hidden) return fail(DCL_E_ARG, "hidden is NULL");
+  if (misaligned(hidden, 16)) return fail(DCL_E_ARG, "hidden must be 16-byte aligned");
+  st = check_sample_workspace(ws, ws_bytes, dcl_sample_hidden_workspace_bytes(model, n));
+  if (st != DCL_OK) return st;
+  if (n == 0) return DCL_OK;
+  (void)hipGetLastError();
+  float* logits = static_cast<float*>(ws);
+  void* rest = static_cast<char*>(ws) + align256((size_t)n * V * 4);
+  gemm_store_f32(reinterpret_cast<const bf16_t*>(static_cast<const char*>(m->wbuf) + m->lay.lm),
+                 static_cast<const bf16_t*>(hidden), V, n, m->cfg.d_model, logits, stream);
+  launch_sample(sample_args(logits, V, 0, n, V, *how, token, conf, kept, rest), stream);
+  return hip_check(hipGetLastError(), "sample_hidden launch");
 }
 
 }  // extern "C"

@@ -223,4 +223,17 @@ struct PromptAttn {
 };
 void launch_prompt_attention(PromptAttn a, hipStream_t s);
 
+struct SampleArgs {
+  const void* logits;            // [n, V], rows `stride` elements apart
+  long stride;
+  int n, V, bf16, shift;         // weights are whole numbers of 2^-shift
+  const float* temperature;      // [n] each, or null
+  const int32_t* top_k;
+  const float *top_p, *min_p, *uniform;
+  int32_t* token;
+  float* conf;                   // or null
+  int32_t* kept;                 // or null
+};
+void launch_sample(const SampleArgs& a, hipStream_t s);
+
 }  // namespace dcl

@@ -136,3 +136,37 @@ class Pool:
 
 def starts(counts):
     return torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32)
+
+
+def sample_row(x, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, u=0.0):
+    """Token, its share of the kept weight and the ids kept, in float64 from a sorted row. x: float64 numpy logits; the
+    settings are the float32 values that the call takes."""
+    x = np.where(np.isnan(x), -np.inf, x) + 0.0
+    if x.max() == -np.inf:
+        return -1, 0.0, 0
+    greedy = not temperature > 0
+    order = np.lexsort((np.arange(len(x)), -x))
+    order = order[x[order] > -np.inf]
+    if greedy:
+        return int(order[0]), 1.0, 1
+    v = x[order]
+    with np.errstate(all="ignore"):
+        w = np.where(v == v[0], 1.0, np.nan_to_num(np.exp((v - v[0]) / temperature), nan=0.0))
+    if top_k > 0:
+        w = w[:top_k]
+    keep = np.ones(len(w), bool)
+    before = np.concatenate([[0.0], np.cumsum(w)[:-1]])
+    if top_p < 1:
+        keep &= before < top_p * w.sum()
+        keep[0] = True
+    if min_p > 0:
+        keep &= w >= min(min_p, 1.0)
+    n = int(keep.sum())
+    assert keep[:n].all()
+    w = w[:n]
+    upto = np.cumsum(w)
+    u = 0.0 if not u > 0 else u
+    at = min(int((upto <= u * upto[-1]).sum()), n - 1)
+    if u >= 1:                                            # past the end: the last id with any weight
+        at = int(np.nonzero(w > 2.0 ** -45)[0][-1])
+    return int(order[at]), float(w[at] / upto[-1]), n

@@ -180,3 +180,48 @@ PROMPT = (256, 256, 256, 128, 256, 128, 256, 1, 4, 4, 4, 2, 64, 0.125, 1, 256, 0
 def test_prompt_refusals(dcl, change, status, word):
     r = dcl.load_library().dcl_prompt_attention(*[change.get(i, x) for i, x in enumerate(PROMPT)])
     assert r == status and word in dcl.dcl_last_error(), (r, dcl.dcl_last_error())
+
+
+def sample_call(dcl, how=None, **kw):
+    f = dict(logits=256, dtype=0, stride=1000, n=2, vocab=1000, token=256, conf=0, kept=0, ws=256, ws_bytes=1 << 40, stream=None)
+    f.update(kw)
+    s = dcl.DclSampling(0, 0, 0, 0, 256) if how is None else how
+    r = dcl.load_library().dcl_sample_tokens(f["logits"], f["dtype"], f["stride"], f["n"], f["vocab"],
+                                             ctypes.byref(s) if how != 0 else None, f["token"], f["conf"], f["kept"], f["ws"],
+                                             f["ws_bytes"], f["stream"])
+    return r, dcl.dcl_last_error()
+
+
+@pytest.mark.parametrize("kw,status,word", [
+    (dict(logits=0), 1, "logits is NULL"), (dict(dtype=2), 2, "dtype"), (dict(stride=999), 1, "stride"), (dict(n=-1), 1, "n=-1"),
+    (dict(n=1 << 23), 1, "n="), (dict(vocab=0), 1, "vocab"), (dict(vocab=(1 << 20) + 1, stride=1 << 21), 1, "vocab"),
+    (dict(token=0), 1, "token"), (dict(ws=0), 1, "workspace"), (dict(ws=128), 1, "aligned"), (dict(ws_bytes=0), 3, "workspace"),
+    (dict(how=0), 1, "how"), (dict(logits=258), 1, "aligned"), (dict(logits=257, dtype=1), 1, "aligned"),
+])
+def test_sample_refusals(dcl, kw, status, word):
+    r, msg = sample_call(dcl, **kw)
+    assert r == status and word in msg, (r, msg)
+
+
+def test_sample_needs_random_numbers_and_sizes(dcl):
+    r, msg = sample_call(dcl, how=dcl.DclSampling(256, 256, 256, 256, 0))
+    assert r == 1 and "uniform" in msg
+    f = dcl.load_library().dcl_sample_workspace_bytes
+    assert f(1, 1) > 0 and f(0, 10) > 0 and f(-1, 10) == 0 and f(1, 0) == 0 and f(1, (1 << 20) + 1) == 0
+
+
+def test_sample_hidden_refusals(dcl):
+    import synth
+    lib = dcl.load_library()
+    m = dcl.dcl_model_create(dcl.config_from_geometry(synth.TINY, max_positions=64))
+    s = dcl.DclSampling(0, 0, 0, 0, 256)
+    try:
+        assert lib.dcl_sample_hidden(None, 256, 1, ctypes.byref(s), 256, 0, 0, 256, 1 << 40, None) == 1
+        assert lib.dcl_sample_hidden(m, 256, 1, ctypes.byref(s), 256, 0, 0, 256, 1 << 40, None) == 5
+        assert lib.dcl_sample_hidden(m, 256, -1, ctypes.byref(s), 256, 0, 0, 256, 1 << 40, None) == 1
+        assert lib.dcl_sample_hidden(m, 256, 1 << 20, ctypes.byref(s), 256, 0, 0, 256, 1 << 40, None) == 2
+        assert lib.dcl_sample_hidden(m, 256, 1, None, 256, 0, 0, 256, 1 << 40, None) == 1
+        assert dcl.dcl_sample_hidden_workspace_bytes(m, 3) >= 3 * synth.TINY.vocab * 4
+        assert dcl.dcl_sample_hidden_workspace_bytes(m, 1 << 20) == 0 and dcl.dcl_sample_hidden_workspace_bytes(m, -1) == 0
+    finally:
+        dcl.dcl_model_destroy(m)
