@@ -395,67 +395,108 @@ def dcl_debug_gemm_plan(Nw: int, T: int, K: int, lm_head: int = False, max_split
 
 # ---------------------------------------------------------------- serving operators: packed batches, pages
 
-def _here(x, name, where, kinds, numel):
-    """``_arg`` for the serving operators, which also refuse a tensor of another device than the current one (the
-    call's stream belongs to that)."""
+# Latency counts in these calls, so that a sound argument passes in a few attribute reads; what is wrong with an
+# unsound one is worked out only then.
+_torch = None
+_dtypes = {}
+
+
+def _device():
+    """The current device's index (the call's stream belongs to it); -2, which no tensor is on, before
+    torch uses any."""
+    global _torch
+    if _torch is None:
+        import torch
+        _dtypes.update({kinds: frozenset(getattr(torch, k) for k in kinds if hasattr(torch, k))
+                        for kinds in (_I32, _F32, _B16)})
+        _torch = torch
+    return _torch.cuda.current_device() if _torch.cuda.is_initialized() else -2
+
+
+def _here(x, name, where, kinds, numel, dev):
+    """``_arg`` for the serving operators, which also refuse a tensor of another device than the current one ``dev``."""
     if x is None or isinstance(x, int):
         return x
+    if x.get_device() == dev and x.dtype in _dtypes[kinds] and x.is_contiguous() and x.numel() >= numel:
+        return x.data_ptr()
     p = _arg(x, name, where, kinds, numel)
-    _on_current(x, name, where)
+    _on_current(x, name, where, dev)
     return p
 
 
-def _on_current(x, name, where):
-    import torch
-    if x.get_device() != torch.cuda.current_device():
-        raise DclError(1, where, f"{name} is on device {x.get_device()}, the current one is {torch.cuda.current_device()}")
+def _on_current(x, name, where, dev):
+    if x.get_device() != dev:
+        raise DclError(1, where, f"{name} is on device {x.get_device()}, the current one is {dev}")
 
 
-def _packed(x, name, where, T, heads, dim):
+def _queue(stream, dev):
+    """``_stream``, with torch's direct look-up of the current stream's handle where it has one (2 us less)."""
+    if stream is None and dev >= 0:
+        raw = getattr(_torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return raw(dev)
+    return _stream(stream)
+
+
+def _space(ws, where, nbytes, dev):
+    p = _arg(ws, "ws", where, _ANY, nbytes=nbytes)
+    if ws is not None and not isinstance(ws, int):
+        _on_current(ws, "ws", where, dev)
+    return p
+
+
+def _packed(x, name, where, T, heads, dim, dev):
     """Address and row stride of a packed operand [>= T, heads, dim] of bfloat16, whose rows may be apart."""
     if isinstance(x, int):
         return x, heads * dim
+    if x.dim() == 3:
+        n, h, d = x.shape
+        step, inner, one = x.stride()
+        if (h == heads and d == dim and n >= T and one == 1 and (inner == dim or heads == 1) and x.get_device() == dev
+                and x.dtype in _dtypes[_B16]):
+            return x.data_ptr(), step if T > 1 else heads * dim
     bad = None
-    if not getattr(x, "is_cuda", False):
+    if not x.is_cuda:
         bad = "must be a device (cuda) tensor"
-    elif str(x.dtype).replace("torch.", "") not in _B16:
+    elif x.dtype not in _dtypes[_B16]:
         bad = f"has dtype {x.dtype}, expected {' or '.join(_B16)}"
     elif x.dim() != 3 or x.shape[1] != heads or x.shape[2] != dim or x.shape[0] < T:
         bad = f"has shape {tuple(x.shape)}, expected ({T}, {heads}, {dim})"
-    elif T > 0 and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != dim)):
+    elif x.get_device() == dev and x.numel() > 0:
         bad = f"has strides {x.stride()}, a row must be contiguous"
     if bad:
         raise DclError(1, where, f"{name} {bad}")
-    _on_current(x, name, where)
-    return x.data_ptr(), x.stride(0) if T > 1 else heads * dim
+    _on_current(x, name, where, dev)
+    return x.data_ptr(), heads * dim                    # no elements: T is 0
+
+
+def _batch(pages, table, length, cu, B, T, max_new, where, dev):
+    """The leading arguments of the calls over pages."""
+    if not isinstance(pages, KVPages):
+        raise DclError(1, where, "pages must be a KVPages")
+    if getattr(table, "dim", int)() != 2:
+        raise DclError(1, where, "table must be a [B, max_pages] tensor")
+    if pages.device != dev:
+        _on_current(pages.k, "pages", where, dev)
+    width = table.shape[1]
+    n = max(B, 0)
+    return (pages.ref, _here(table, "table", where, _I32, n * width, dev), width,
+            _here(length, "len", where, _I32, n, dev), _here(cu, "cu", where, _I32, n + 1, dev), B, T, max_new)
 
 
 def dcl_prompt_attention(q, k, v, cu, B: int, T: int, max_len: int, n_heads: int, n_kv_heads: int, head_dim: int,
                          scale: float, causal: bool, out, lse=None, stream=None) -> None:
     """q [T, n_heads, head_dim], k and v [T, n_kv_heads, head_dim] (rows may be apart), sequences by ``cu`` [B + 1];
     out like q (contiguous), lse [T, n_heads] float32 or None."""
-    w = "dcl_prompt_attention"
-    qp, qs = _packed(q, "q", w, T, n_heads, head_dim)
-    kp, ks = _packed(k, "k", w, T, n_kv_heads, head_dim)
-    vp, vs = _packed(v, "v", w, T, n_kv_heads, head_dim)
+    w, dev = "dcl_prompt_attention", _device()
+    qp, qs = _packed(q, "q", w, T, n_heads, head_dim, dev)
+    kp, ks = _packed(k, "k", w, T, n_kv_heads, head_dim, dev)
+    vp, vs = _packed(v, "v", w, T, n_kv_heads, head_dim, dev)
     n = max(T, 0) * n_heads
-    _check(load_library().dcl_prompt_attention(qp, qs, kp, ks, vp, vs, _here(cu, "cu", w, _I32, max(B, 0) + 1), B, T,
+    _check(load_library().dcl_prompt_attention(qp, qs, kp, ks, vp, vs, _here(cu, "cu", w, _I32, max(B, 0) + 1, dev), B, T,
                                                max_len, n_heads, n_kv_heads, head_dim, scale, int(causal),
-                                               _here(out, "out", w, _B16, n * head_dim),
-                                               _here(lse, "lse", w, _F32, n), _stream(stream)), w)
-
-
-def _batch(pages, table, length, cu, B, T, max_new, where):
-    """The leading arguments of the calls over pages."""
-    if not isinstance(pages, KVPages):
-        raise DclError(1, where, "pages must be a KVPages")
-    if getattr(table, "dim", lambda: 0)() != 2:
-        raise DclError(1, where, "table must be a [B, max_pages] tensor")
-    pages.check(where)
-    width = table.shape[1]
-    n = max(B, 0)
-    return (ctypes.byref(pages.struct), _here(table, "table", where, _I32, n * width), width,
-            _here(length, "len", where, _I32, n), _here(cu, "cu", where, _I32, n + 1), B, T, max_new)
+                                               _here(out, "out", w, _B16, n * head_dim, dev),
+                                               _here(lse, "lse", w, _F32, n, dev), _queue(stream, dev)), w)
 
 
 class KVPages:
@@ -497,27 +538,25 @@ class KVPages:
             head_dim, dtype
         self.struct = DclPages(self.k.data_ptr(), self.v.data_ptr(), _ptr(self.k_scale), _ptr(self.v_scale), n_pages,
                                page_len, n_kv_heads, head_dim, dtype)
-
-    def check(self, where):
-        _on_current(self.k, "pages", where)
+        self.ref = ctypes.byref(self.struct)
 
 
 def dcl_pages_write(pages: KVPages, table, length, cu, B: int, T: int, max_new: int, k, v, stream=None) -> None:
     """Rows k, v [T, n_kv_heads, head_dim] into the pages (``table`` [B, max_pages], ``length`` [B], ``cu`` [B + 1])."""
-    w = "dcl_pages_write"
-    a = _batch(pages, table, length, cu, B, T, max_new, w)
-    kp, ks = _packed(k, "k", w, T, pages.n_kv_heads, pages.head_dim)
-    vp, vs = _packed(v, "v", w, T, pages.n_kv_heads, pages.head_dim)
-    _check(load_library().dcl_pages_write(*a, kp, ks, vp, vs, _stream(stream)), w)
+    w, dev = "dcl_pages_write", _device()
+    a = _batch(pages, table, length, cu, B, T, max_new, w, dev)
+    kp, ks = _packed(k, "k", w, T, pages.n_kv_heads, pages.head_dim, dev)
+    vp, vs = _packed(v, "v", w, T, pages.n_kv_heads, pages.head_dim, dev)
+    _check(load_library().dcl_pages_write(*a, kp, ks, vp, vs, _queue(stream, dev)), w)
 
 
 def dcl_pages_read(pages: KVPages, table, length, cu, B: int, T: int, max_new: int, k, v, stream=None) -> None:
     """The last rows of each sequence out of the pages into k, v [T, n_kv_heads, head_dim]."""
-    w = "dcl_pages_read"
-    a = _batch(pages, table, length, cu, B, T, max_new, w)
-    kp, ks = _packed(k, "k", w, T, pages.n_kv_heads, pages.head_dim)
-    vp, vs = _packed(v, "v", w, T, pages.n_kv_heads, pages.head_dim)
-    _check(load_library().dcl_pages_read(*a, kp, ks, vp, vs, _stream(stream)), w)
+    w, dev = "dcl_pages_read", _device()
+    a = _batch(pages, table, length, cu, B, T, max_new, w, dev)
+    kp, ks = _packed(k, "k", w, T, pages.n_kv_heads, pages.head_dim, dev)
+    vp, vs = _packed(v, "v", w, T, pages.n_kv_heads, pages.head_dim, dev)
+    _check(load_library().dcl_pages_read(*a, kp, ks, vp, vs, _queue(stream, dev)), w)
 
 
 def dcl_pages_attention_workspace_bytes(pages: KVPages, n_heads: int, B: int, T: int, max_new: int,
@@ -529,36 +568,36 @@ def dcl_pages_attention_workspace_bytes(pages: KVPages, n_heads: int, B: int, T:
 def dcl_pages_attention(pages: KVPages, table, length, cu, B: int, T: int, max_new: int, q, n_heads: int, scale: float,
                         causal: bool, out, lse, ws, ws_bytes: int, stream=None) -> None:
     """q [T, n_heads, head_dim] over the pages; out like q (contiguous), lse [T, n_heads] float32 or None."""
-    w = "dcl_pages_attention"
-    a = _batch(pages, table, length, cu, B, T, max_new, w)
-    qp, qs = _packed(q, "q", w, T, n_heads, pages.head_dim)
+    w, dev = "dcl_pages_attention", _device()
+    a = _batch(pages, table, length, cu, B, T, max_new, w, dev)
+    qp, qs = _packed(q, "q", w, T, n_heads, pages.head_dim, dev)
     n = max(T, 0) * n_heads
     _check(load_library().dcl_pages_attention(*a, qp, qs, n_heads, scale, int(causal),
-                                              _here(out, "out", w, _B16, n * pages.head_dim),
-                                              _here(lse, "lse", w, _F32, n),
-                                              _arg(ws, "ws", w, _ANY, nbytes=ws_bytes), ws_bytes, _stream(stream)), w)
+                                              _here(out, "out", w, _B16, n * pages.head_dim, dev),
+                                              _here(lse, "lse", w, _F32, n, dev),
+                                              _space(ws, w, ws_bytes, dev), ws_bytes, _queue(stream, dev)), w)
 
 
 def dcl_sample_workspace_bytes(n: int, vocab: int) -> int:
     return load_library().dcl_sample_workspace_bytes(n, vocab)
 
 
-def _sampling(n, temperature, top_k, top_p, min_p, uniform, where):
-    return DclSampling(_here(temperature, "temperature", where, _F32, n), _here(top_k, "top_k", where, _I32, n),
-                       _here(top_p, "top_p", where, _F32, n), _here(min_p, "min_p", where, _F32, n),
-                       _here(uniform, "uniform", where, _F32, n))
+def _sampling(n, temperature, top_k, top_p, min_p, uniform, where, dev):
+    return DclSampling(_here(temperature, "temperature", where, _F32, n, dev), _here(top_k, "top_k", where, _I32, n, dev),
+                       _here(top_p, "top_p", where, _F32, n, dev), _here(min_p, "min_p", where, _F32, n, dev),
+                       _here(uniform, "uniform", where, _F32, n, dev))
 
 
 def dcl_sample_tokens(logits, n: int, vocab: int, temperature, top_k, top_p, min_p, uniform, token, conf, kept, ws,
                       ws_bytes: int, stream=None) -> None:
     """logits [n, vocab] float32 or bfloat16 (rows may be apart); temperature, top_p, min_p, uniform float32 [n], top_k
     int32 [n] (all but uniform may be None); token, kept int32 [n], conf float32 [n] (conf and kept may be None)."""
-    w = "dcl_sample_tokens"
-    kind = str(getattr(logits, "dtype", "")).replace("torch.", "")
+    w, dev = "dcl_sample_tokens", _device()
+    f32 = logits.dtype is _torch.float32
     bad = None
-    if not getattr(logits, "is_cuda", False):
+    if not logits.is_cuda:
         bad = "must be a device (cuda) tensor"
-    elif kind not in _F32 + _B16:
+    elif not f32 and logits.dtype not in _dtypes[_B16]:
         bad = f"has dtype {logits.dtype}, expected float32 or bfloat16"
     elif logits.dim() != 2 or logits.shape[0] < n or logits.shape[1] < vocab:
         bad = f"has shape {tuple(logits.shape)}, the call needs ({n}, {vocab})"
@@ -566,13 +605,13 @@ def dcl_sample_tokens(logits, n: int, vocab: int, temperature, top_k, top_p, min
         bad = f"has strides {logits.stride()}, a row must be contiguous"
     if bad:
         raise DclError(1, w, f"logits {bad}")
-    _on_current(logits, "logits", w)
-    how = _sampling(max(n, 0), temperature, top_k, top_p, min_p, uniform, w)
-    _check(load_library().dcl_sample_tokens(logits.data_ptr(), DCL_DTYPE_F32 if kind == "float32" else DCL_DTYPE_BF16,
+    _on_current(logits, "logits", w, dev)
+    how = _sampling(max(n, 0), temperature, top_k, top_p, min_p, uniform, w, dev)
+    _check(load_library().dcl_sample_tokens(logits.data_ptr(), DCL_DTYPE_F32 if f32 else DCL_DTYPE_BF16,
                                             logits.stride(0) if n > 1 else vocab, n, vocab, ctypes.byref(how),
-                                            _here(token, "token", w, _I32, n), _here(conf, "conf", w, _F32, n),
-                                            _here(kept, "kept", w, _I32, n),
-                                            _arg(ws, "ws", w, _ANY, nbytes=ws_bytes), ws_bytes, _stream(stream)), w)
+                                            _here(token, "token", w, _I32, n, dev), _here(conf, "conf", w, _F32, n, dev),
+                                            _here(kept, "kept", w, _I32, n, dev),
+                                            _space(ws, w, ws_bytes, dev), ws_bytes, _queue(stream, dev)), w)
 
 
 def dcl_sample_hidden_workspace_bytes(model: int, n: int) -> int:
@@ -582,13 +621,13 @@ def dcl_sample_hidden_workspace_bytes(model: int, n: int) -> int:
 def dcl_sample_hidden(model: int, hidden, n: int, temperature, top_k, top_p, min_p, uniform, token, conf, kept, ws,
                       ws_bytes: int, stream=None) -> None:
     """The model's LM head on hidden [n, d_model] (bfloat16), then ``dcl_sample_tokens``."""
-    w = "dcl_sample_hidden"
+    w, dev = "dcl_sample_hidden", _device()
     g = _cfg_of(model)
-    how = _sampling(max(n, 0), temperature, top_k, top_p, min_p, uniform, w)
-    _check(load_library().dcl_sample_hidden(model, _here(hidden, "hidden", w, _B16, n * g.d_model if g else None), n,
-                                            ctypes.byref(how), _here(token, "token", w, _I32, n),
-                                            _here(conf, "conf", w, _F32, n), _here(kept, "kept", w, _I32, n),
-                                            _arg(ws, "ws", w, _ANY, nbytes=ws_bytes), ws_bytes, _stream(stream)), w)
+    how = _sampling(max(n, 0), temperature, top_k, top_p, min_p, uniform, w, dev)
+    _check(load_library().dcl_sample_hidden(model, _here(hidden, "hidden", w, _B16, n * g.d_model if g else 0, dev), n,
+                                            ctypes.byref(how), _here(token, "token", w, _I32, n, dev),
+                                            _here(conf, "conf", w, _F32, n, dev), _here(kept, "kept", w, _I32, n, dev),
+                                            _space(ws, w, ws_bytes, dev), ws_bytes, _queue(stream, dev)), w)
 
 
 # ---------------------------------------------------------------- convenience owner of device buffers

@@ -8,6 +8,13 @@ using namespace dcl;
 
 namespace {
 
+// |scale| log2(e), at least the least normal number: a masked score -inf times it stays -inf, and a scale of 0 gives
+// every finite score (below 2^100) the exponent 0 to within 2^-26.
+float scale_log2(float scale) {
+  const double s = 1.4426950408889634 * fabs((double)scale);
+  return s < 1.1754943508222875e-38 ? 1.1754943508222875e-38f : (float)s;
+}
+
 bool misaligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
 // Rows [T, heads, dh] of bfloat16 with a row stride.
@@ -276,7 +283,8 @@ dcl_status dcl_prompt_attention(const void* q, int64_t q_stride, const void* k, 
   a.dh = head_dim;
   a.causal = causal;
   a.q_tiles = 0;
-  a.scale_log2 = (float)(1.4426950408889634 * (double)scale);
+  a.q_sign = scale < 0.f ? 0x80008000u : 0u;
+  a.scale_log2 = scale_log2(scale);
   (void)hipGetLastError();
   launch_prompt_attention(a, stream);
   return hip_check(hipGetLastError(), "prompt_attention launch");

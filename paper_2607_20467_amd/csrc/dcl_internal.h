@@ -219,7 +219,8 @@ struct PromptAttn {
   float* lse;                    // [T, H] or null
   const int32_t* cu;             // [B + 1]
   int B, T, max_len, H, Hkv, dh, causal, q_tiles;
-  float scale_log2;
+  uint32_t q_sign;               // the scale's sign, for both halves of a word of queries
+  float scale_log2;              // its magnitude times log2(e), a normal number
 };
 void launch_prompt_attention(PromptAttn a, hipStream_t s);
 

@@ -9,6 +9,8 @@
 // rows that one read touches lie in different banks.
 //
 // The probabilities are rounded to bfloat16 once, 2^-9 of each, the sum that divides takes them unrounded.
+#include <type_traits>
+
 #include "dcl_internal.h"
 #include "pages_index.h"
 
@@ -63,42 +65,57 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
   {
     const bf16_t* qp = a.q + (size_t)(r.first + min(query, n - 1)) * a.q_stride + (size_t)h * DH + 8 * hi;
 #pragma unroll
-    for (int ks = 0; ks < DH / 16; ++ks) qf[ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(qp + 16 * ks));
+    for (int ks = 0; ks < DH / 16; ++ks) {
+      uint4 x = *reinterpret_cast<const uint4*>(qp + 16 * ks);
+      x.x ^= a.q_sign, x.y ^= a.q_sign, x.z ^= a.q_sign, x.w ^= a.q_sign;  // a negative scale is a sign of the query
+      qf[ks] = __builtin_bit_cast(bf16x8_t, x);
+    }
   }
   const bf16_t* kbase = a.k + (size_t)r.first * a.k_stride + (size_t)g * DH;
   const bf16_t* vbase = a.v + (size_t)r.first * a.v_stride + (size_t)g * DH;
 
-  // copy i of wave w fills the 64 chunks from (i * 4 + w) * 64: slot s of row y holds chunk s ^ f(y)
+  // copy i of wave w fills the 64 chunks from (i * 4 + w) * 64: slot c of row y holds chunk c ^ f(y). A tile that lies
+  // whole in the sequence is a scalar base plus a per-lane offset that never changes.
   auto key_swizzle = [](int y) { return DH == 128 ? y & 15 : (y >> 1) & 7; };
   auto value_swizzle = [](int y) { return DH == 128 ? (y & 3) << 2 : ((y >> 1) & 1) << 2; };
-  int row[NL], ck[NL], cv[NL];
+  auto slot_row = [&](int i) { return ((i * 4 + wid) * 64 + lane) / KC; };
+  auto key_chunk = [&](int i) { return 8 * ((lane % KC) ^ key_swizzle(slot_row(i))); };
+  auto value_chunk = [&](int i) { return 8 * ((lane % KC) ^ value_swizzle(slot_row(i))); };
+  uint32_t koff[NL], voff[NL];
 #pragma unroll
   for (int i = 0; i < NL; ++i) {
-    const int pos = (i * 4 + wid) * 64 + lane;
-    row[i] = pos / KC;
-    ck[i] = 8 * ((pos % KC) ^ key_swizzle(row[i]));
-    cv[i] = 8 * ((pos % KC) ^ value_swizzle(row[i]));
+    koff[i] = (uint32_t)(slot_row(i) * (int)a.k_stride + key_chunk(i)) * 2u;
+    voff[i] = (uint32_t)(slot_row(i) * (int)a.v_stride + value_chunk(i)) * 2u;
   }
   const bool near = a.k_stride <= (1 << 24) && a.v_stride <= (1 << 24);  // a tile's offsets stay in 32 bits
   const uint32_t lds = lds_addr_of(sm) + (uint32_t)wid * 1024u;
-  auto issue = [&](int t) {
-    const uint32_t dst = lds + (uint32_t)((t & 1) * STAGE);
+  auto issue = [&](int t, uint32_t stage) {
+    const uint32_t dst = lds + stage;
     const int k0 = t * KT;
     if (near && k0 + KT <= n) {
       const bf16_t* kb = prompt_uniform(kbase + (size_t)k0 * a.k_stride);
       const bf16_t* vb = prompt_uniform(vbase + (size_t)k0 * a.v_stride);
 #pragma unroll
-      for (int i = 0; i < NL; ++i) dma16_sv(kb, (uint32_t)(row[i] * (int)a.k_stride + ck[i]) * 2u, dst + i * 4096u);
+      for (int i = 0; i < NL; ++i) dma16_sv(kb, koff[i], dst + i * 4096u);
 #pragma unroll
-      for (int i = 0; i < NL; ++i) dma16_sv(vb, (uint32_t)(row[i] * (int)a.v_stride + cv[i]) * 2u, dst + CH * 16u + i * 4096u);
+      for (int i = 0; i < NL; ++i) dma16_sv(vb, voff[i], dst + CH * 16u + i * 4096u);
     } else {  // a row past the last key repeats that key: no query sees it there
-#pragma unroll
-      for (int i = 0; i < NL; ++i) dma16_at(kbase + (size_t)min(k0 + row[i], n - 1) * a.k_stride + ck[i], dst + i * 4096u);
-#pragma unroll
-      for (int i = 0; i < NL; ++i)
-        dma16_at(vbase + (size_t)min(k0 + row[i], n - 1) * a.v_stride + cv[i], dst + CH * 16u + i * 4096u);
+#pragma unroll 1
+      for (int i = 0; i < NL; ++i) {
+        const int y = min(k0 + slot_row(i), n - 1);
+        dma16_at(kbase + (size_t)y * a.k_stride + key_chunk(i), dst + i * 4096u);
+        dma16_at(vbase + (size_t)y * a.v_stride + value_chunk(i), dst + CH * 16u + i * 4096u);
+      }
     }
   };
+  // where the lane's fragments lie in a stage (see the reads below)
+  const int key_at = lq * KC * 16 + ((hi ^ key_swizzle(lq)) * 16);
+  int value_at[DH / 32];
+  {
+    const int lr = (lane & 15) >> 2, piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), y = 4 * hi + lr;
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d) value_at[d] = CH * 16 + (y * KC + ((4 * d + piece) ^ value_swizzle(y))) * 16 + 8 * (lane & 1);
+  }
 
   f32x16_t o[DH / 32];
 #pragma unroll
@@ -108,50 +125,45 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
   float m = -INFINITY, l = 0.f;
   const float scale = a.scale_log2;
 
-  issue(0);
-  for (int t = 0; t < tiles; ++t) {
+  auto step = [&](int t, auto which) {
+    constexpr int STG = decltype(which)::value * STAGE;
     prompt_wait_vmcnt<0>();
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (t + 1 < tiles) issue(t + 1);
+    if (t + 1 < tiles) issue(t + 1, STAGE - STG);
     const int k0 = t * KT;
-    if (k0 >= wkeys) continue;  // none of the wave's queries sees this tile
-    const uint8_t* sk = sm + (t & 1) * STAGE;
-    const uint8_t* sv = sk + CH * 16;
+    if (k0 >= wkeys) return;  // none of the wave's queries sees this tile
+    const uint8_t* sv = sm + STG + CH * 16;
 
+    // Keys: step ks takes chunk 2 ks + hi of row y at slot (2 ks + hi) ^ f(y), that is (hi ^ f(y)) ^ 2 ks.
     f32x16_t sc[2];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
-      const int y = 32 * kb + lq;
-#pragma unroll
-      for (int ks = 0; ks < DH / 16; ++ks) {
-        const uint4 x = *reinterpret_cast<const uint4*>(sk + (y * KC + ((2 * ks + hi) ^ key_swizzle(y))) * 16);
-        sc[kb] = mfma32(__builtin_bit_cast(bf16x8_t, x), qf[ks], sc[kb]);
-      }
-    }
-    // register i of step kb is key k0 + 32 kb + 8 (i / 4) + 4 hi + i % 4
-    const bool whole = k0 + KT <= (a.causal ? qw + 1 : n);
-    auto dead = [&](int kb, int i) { return k0 + 32 * kb + 8 * (i >> 2) + 4 * hi + (i & 3) >= lim; };
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[kb][i] *= scale;
+      for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < DH / 16; ++ks)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const uint4 x = *reinterpret_cast<const uint4*>(sm + (key_at ^ (32 * ks)) + STG + kb * 32 * KC * 16);
+        sc[kb] = mfma32(__builtin_bit_cast(bf16x8_t, x), qf[ks], sc[kb]);
+      }
+    // register i of step kb is key k0 + 32 kb + 8 (i / 4) + 4 hi + i % 4
+    const bool whole = k0 + KT <= (a.causal ? qw + 1 : n);
     if (!whole) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (dead(kb, i)) sc[kb][i] = -INFINITY;
+          if (k0 + 32 * kb + 8 * (i >> 2) + 4 * hi + (i & 3) >= lim) sc[kb][i] = -INFINITY;
     }
-    // the reference point moves only when a score passes it by more than 2^8
+    // the reference point (log2 units) moves only when a score passes it by more than 2^8
     float tmax = -INFINITY;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, sc[kb][i]);
-    if (__builtin_amdgcn_ballot_w64(tmax > m + 8.f)) {
-      const float ts = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
+    if (__builtin_amdgcn_ballot_w64(tmax * scale > m + 8.f)) {
+      const float ts = fmaxf(tmax, __shfl_xor(tmax, 32, 64)) * scale;
       const float mn = ts > m + 8.f ? ts : m;
       const float alpha = mn == m ? 1.f : __builtin_amdgcn_exp2f(m - mn);
       l *= alpha;
@@ -159,15 +171,15 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
       for (int d = 0; d < DH / 32; ++d) o[d] *= alpha;
       m = mn;
     }
-    const float mr = m == -INFINITY ? 0.f : m;
+    const float mr = m == -INFINITY ? 0.f : -m;
     bf16x8_t pf[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       uint32_t w[4];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        const float p0 = __builtin_amdgcn_exp2f(sc[s >> 1][8 * (s & 1) + 2 * x] - mr);
-        const float p1 = __builtin_amdgcn_exp2f(sc[s >> 1][8 * (s & 1) + 2 * x + 1] - mr);
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[s >> 1][8 * (s & 1) + 2 * x], scale, mr));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[s >> 1][8 * (s & 1) + 2 * x + 1], scale, mr));
         l += p0;
         l += p1;
         w[x] = f2bf2(p0, p1);
@@ -176,25 +188,20 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
     }
     // Values of 16 keys (step s) and 32 dimensions: lanes 0-15 / 16-31 take 16 dimensions each of keys 16 s + 0..3 and
     // + 8..11, lanes 32-63 the four keys after those, as the probabilities lie.
-    const int lr = (lane & 15) >> 2;
     auto value_fragment = [&](int s, int d) -> uint4 {
-      const int chunk = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-      const int y = 16 * s + 4 * hi + lr;
-      const uint2 x = read_transposed(sv + (y * KC + (chunk ^ value_swizzle(y))) * 16 + 8 * (lane & 1));
-      const uint2 z = read_transposed(sv + ((y + 8) * KC + (chunk ^ value_swizzle(y + 8))) * 16 + 8 * (lane & 1));
+      const uint2 x = read_transposed(sm + value_at[d] + STG + s * 16 * KC * 16);
+      const uint2 z = read_transposed(sm + value_at[d] + STG + (s * 16 + 8) * KC * 16);
       return make_uint4(x.x, x.y, z.x, z.y);
     };
     bool odd_tile = false;
     if (!whole) {  // an infinity or NaN in a value that only some of the queries see must meet no probability of 0
       uint32_t odd = 0;
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-#pragma unroll
-        for (int d = 0; d < DH / 32; ++d) {
-          const uint4 x = value_fragment(s, d);
-          odd |= (((x.x & 0x7FFF7FFFu) + 0x00800080u) | ((x.y & 0x7FFF7FFFu) + 0x00800080u) |
-                  ((x.z & 0x7FFF7FFFu) + 0x00800080u) | ((x.w & 0x7FFF7FFFu) + 0x00800080u)) & 0x80008000u;
-        }
+#pragma unroll 4
+      for (int c = lane; c < CH; c += 64) {
+        const uint4 x = *reinterpret_cast<const uint4*>(sv + c * 16);
+        odd |= (((x.x & 0x7FFF7FFFu) + 0x00800080u) | ((x.y & 0x7FFF7FFFu) + 0x00800080u) |
+                ((x.z & 0x7FFF7FFFu) + 0x00800080u) | ((x.w & 0x7FFF7FFFu) + 0x00800080u)) & 0x80008000u;
+      }
       odd_tile = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
     }
     if (!odd_tile) {
@@ -203,45 +210,39 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
 #pragma unroll
         for (int d = 0; d < DH / 32; ++d) o[d] = mfma32(__builtin_bit_cast(bf16x8_t, value_fragment(s, d)), pf[s], o[d]);
     } else {
+      // rare, and written for few registers: the product without such values, then they alone, key by key
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        uint32_t sees[4];  // 1 where the query sees the key
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-          sees[x] = (dead(s >> 1, 8 * (s & 1) + 2 * x) ? 0u : 0x3F80u) | (dead(s >> 1, 8 * (s & 1) + 2 * x + 1) ? 0u : 0x3F800000u);
-        const bf16x8_t sf = __builtin_bit_cast(bf16x8_t, make_uint4(sees[0], sees[1], sees[2], sees[3]));
+      for (int s = 0; s < 4; ++s)
 #pragma unroll
         for (int d = 0; d < DH / 32; ++d) {
           __builtin_amdgcn_sched_barrier(0);
-          uint4 x = value_fragment(s, d), up, dn;  // 1 where +inf or NaN, 1 where -inf or NaN; those values become 0
-          uint32_t *xp = &x.x, *upp = &up.x, *dnp = &dn.x;
+          uint4 x = value_fragment(s, d);
+          uint32_t* w = &x.x;
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            upp[w] = dnp[w] = 0;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint32_t v = (xp[w] >> (16 * e)) & 0xFFFFu;
-              if ((v & 0x7F80u) == 0x7F80u) {
-                if (v != 0xFF80u) upp[w] |= 0x3F80u << (16 * e);
-                if (v != 0x7F80u) dnp[w] |= 0x3F80u << (16 * e);
-                xp[w] &= ~(0xFFFFu << (16 * e));
-              }
-            }
-          }
-          f32x16_t zero;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+          for (int e = 0; e < 4; ++e)
+            w[e] &= ((w[e] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((w[e] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
           o[d] = mfma32(__builtin_bit_cast(bf16x8_t, x), pf[s], o[d]);
-          const f32x16_t cu = mfma32(__builtin_bit_cast(bf16x8_t, up), sf, zero);
-          const f32x16_t cd = mfma32(__builtin_bit_cast(bf16x8_t, dn), sf, zero);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            if (cu[i] > 0.f) o[d][i] += INFINITY;
-            if (cd[i] > 0.f) o[d][i] -= INFINITY;
-          }
         }
+#pragma unroll 1
+      for (int y = 0; y < KT; ++y) {
+        if (k0 + y >= lim) break;
+#pragma unroll
+        for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const uint2 x = *reinterpret_cast<const uint2*>(sv + (y * KC + ((4 * d + c) ^ value_swizzle(y))) * 16 + 8 * hi);
+            const uint32_t w[4] = {x.x << 16, x.x & 0xFFFF0000u, x.y << 16, x.y & 0xFFFF0000u};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if ((w[e] & 0x7F800000u) == 0x7F800000u) o[d][4 * c + e] += __uint_as_float(w[e]);
+          }
       }
     }
+  };
+  issue(0, 0);
+  for (int t = 0; t < tiles; t += 2) {
+    step(t, std::integral_constant<int, 0>());
+    if (t + 1 < tiles) step(t + 1, std::integral_constant<int, 1>());
   }
 
   const float lt = l + __shfl_xor(l, 32, 64);
