@@ -125,13 +125,15 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
   float m = -INFINITY, l = 0.f;
   const float scale = a.scale_log2;
 
-  auto step = [&](int t, auto which) {
-    constexpr int STG = decltype(which)::value * STAGE;
+  // Tile t in the stage at byte STG. `masked`: some query of the workgroup does not see all of it.
+  auto step = [&](int t, auto stage_of, auto masked_of) {
+    const int STG = stage_of;  // a constant where the tile is whole
+    constexpr bool masked = decltype(masked_of)::value;
     prompt_wait_vmcnt<0>();
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (t + 1 < tiles) issue(t + 1, STAGE - STG);
     const int k0 = t * KT;
-    if (k0 >= wkeys) return;  // none of the wave's queries sees this tile
+    if (masked && k0 >= wkeys) return;  // none of the wave's queries sees this tile
     const uint8_t* sv = sm + STG + CH * 16;
 
     // Keys: step ks takes chunk 2 ks + hi of row y at slot (2 ks + hi) ^ f(y), that is (hi ^ f(y)) ^ 2 ks.
@@ -148,14 +150,20 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
         sc[kb] = mfma32(__builtin_bit_cast(bf16x8_t, x), qf[ks], sc[kb]);
       }
     // register i of step kb is key k0 + 32 kb + 8 (i / 4) + 4 hi + i % 4
-    const bool whole = k0 + KT <= (a.causal ? qw + 1 : n);
-    if (!whole) {
+    if (masked) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (k0 + 32 * kb + 8 * (i >> 2) + 4 * hi + (i & 3) >= lim) sc[kb][i] = -INFINITY;
     }
+    // Values of 16 keys (step s) and 32 dimensions: lanes 0-15 / 16-31 take 16 dimensions each of keys 16 s + 0..3 and
+    // + 8..11, lanes 32-63 the four keys after those, as the probabilities lie.
+    auto value_fragment = [&](int s, int d) -> uint4 {
+      const uint2 x = read_transposed(sm + value_at[d] + STG + s * 16 * KC * 16);
+      const uint2 z = read_transposed(sm + value_at[d] + STG + (s * 16 + 8) * KC * 16);
+      return make_uint4(x.x, x.y, z.x, z.y);
+    };
     // the reference point (log2 units) moves only when a score passes it by more than 2^8
     float tmax = -INFINITY;
 #pragma unroll
@@ -186,15 +194,8 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
       }
       pf[s] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
     }
-    // Values of 16 keys (step s) and 32 dimensions: lanes 0-15 / 16-31 take 16 dimensions each of keys 16 s + 0..3 and
-    // + 8..11, lanes 32-63 the four keys after those, as the probabilities lie.
-    auto value_fragment = [&](int s, int d) -> uint4 {
-      const uint2 x = read_transposed(sm + value_at[d] + STG + s * 16 * KC * 16);
-      const uint2 z = read_transposed(sm + value_at[d] + STG + (s * 16 + 8) * KC * 16);
-      return make_uint4(x.x, x.y, z.x, z.y);
-    };
     bool odd_tile = false;
-    if (!whole) {  // an infinity or NaN in a value that only some of the queries see must meet no probability of 0
+    if (masked) {  // an infinity or NaN in a value that only some of the queries see must meet no probability of 0
       uint32_t odd = 0;
 #pragma unroll 4
       for (int c = lane; c < CH; c += 64) {
@@ -204,7 +205,7 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
       }
       odd_tile = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
     }
-    if (!odd_tile) {
+    if (!masked || !odd_tile) {
 #pragma unroll
       for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -240,10 +241,13 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
     }
   };
   issue(0, 0);
-  for (int t = 0; t < tiles; t += 2) {
-    step(t, std::integral_constant<int, 0>());
-    if (t + 1 < tiles) step(t + 1, std::integral_constant<int, 1>());
+  const int open = (a.causal ? min(n, q0 + 1) : n) / KT;  // tiles that every query of the workgroup sees whole
+  int t = 0;
+  for (; t + 1 < open; t += 2) {
+    step(t, std::integral_constant<int, 0>(), std::false_type());
+    step(t + 1, std::integral_constant<int, STAGE>(), std::false_type());
   }
+  for (; t < tiles; ++t) step(t, (t & 1) * STAGE, std::true_type());
 
   const float lt = l + __shfl_xor(l, 32, 64);
   if (query >= min(n, a.max_len)) return;
