@@ -347,7 +347,7 @@ size_t dcl_sample_workspace_bytes(int32_t n, int32_t vocab);
  * not > 0, or top_k 1): token the lowest best id, conf 1, kept 1. Sums are exact in fixed point (42 bits and more below
  * the row's largest weight), so a border falls as exact arithmetic has it and results are bitwise reproducible.
  * token and conf can stand for dcl_row_stats' top1 and conf in dcl_select_contiguous. 0 <= n <= 2^22, 1 <= vocab <=
- * 2^20; ws: device, 256-byte aligned, ws_bytes >= dcl_sample_workspace_bytes. */
+ * 2^20; ws: device, 256-byte aligned, ws_bytes >= dcl_sample_workspace_bytes; calls that overlap in time need their own. */
 dcl_status dcl_sample_tokens(const void* logits, int32_t dtype, int64_t row_stride, int32_t n, int32_t vocab,
                              const dcl_sampling* how, int32_t* token, float* conf, int32_t* kept, void* ws,
                              size_t ws_bytes, hipStream_t stream);

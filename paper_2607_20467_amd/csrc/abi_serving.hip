@@ -137,7 +137,9 @@ dcl_status check_attention_size(const dcl_pages* g, int32_t n_heads, int32_t B, 
 // Most vocabulary ids of a sampled row: with 2^20 of them weights still have 42 bits.
 constexpr int kSampleVocab = 1 << 20;
 
-size_t sample_workspace(int32_t n, int32_t V) { return 256; }
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+size_t sample_workspace(int32_t n, int32_t V) { return align256(n > 0 ? sample_ws_bytes(n, V) : 1); }
 
 dcl_status check_sample(int32_t n, int32_t V, const dcl_sampling* how, const int32_t* token) {
   if (n < 0 || n > (1 << 22)) return fail(DCL_E_ARG, "n=%d outside [0, 2^22]", n);
@@ -163,9 +165,9 @@ SampleArgs sample_args(const void* logits, int64_t stride, int bf16, int32_t n, 
   a.n = n;
   a.V = V;
   a.bf16 = bf16;
-  int bits = 0;  // V <= 2^bits: the weights' sum stays below 2^62
+  int bits = 0;  // V <= 2^bits: the weights' sum stays below 2^62, a weight below 2^46
   while ((1 << bits) < V) ++bits;
-  a.shift = 62 - bits;
+  a.shift = bits < 17 ? 45 : 62 - bits;
   a.temperature = how.temperature;
   a.top_k = how.top_k;
   a.top_p = how.top_p;
@@ -174,10 +176,9 @@ SampleArgs sample_args(const void* logits, int64_t stride, int bf16, int32_t n, 
   a.token = token;
   a.conf = conf;
   a.kept = kept;
+  a.ws = ws;
   return a;
 }
-
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace
 

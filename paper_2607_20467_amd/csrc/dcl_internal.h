@@ -234,7 +234,9 @@ struct SampleArgs {
   int32_t* token;
   float* conf;                   // or null
   int32_t* kept;                 // or null
+  void* ws;                      // sample_ws_bytes
 };
+size_t sample_ws_bytes(int n, int V);
 void launch_sample(const SampleArgs& a, hipStream_t s);
 
 }  // namespace dcl

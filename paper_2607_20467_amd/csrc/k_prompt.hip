@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
   // (sequence, head) pairs go round the XCDs: a head's query tiles share one L2, every sequence spreads over all of
   // them; the tiles with the most keys come first
   const int heads = a.B * a.H, j = blockIdx.x >> 3;
-  const int bh = (blockIdx.x & 7) + 8 * (j / a.q_tiles), qt = a.q_tiles - 1 - j % a.q_tiles;
+  const int hx = (heads + 7) / 8, bh = (blockIdx.x & 7) + 8 * (j % hx), qt = a.q_tiles - 1 - j / hx;
   if (bh >= heads) return;
   const int b = __builtin_amdgcn_readfirstlane(bh / a.H), h = __builtin_amdgcn_readfirstlane(bh % a.H), g = h / (a.H / a.Hkv);
   const SeqRows r = seq_rows(a.cu, b, a.T);

@@ -37,8 +37,9 @@ def draw(dcl, x, u, temperature=None, top_k=None, top_p=None, min_p=None, n=None
 
 
 def check(x, got, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
-    """The settings as the call took them (float32). Weights are whole numbers of 2^-(62 - bits): each is off by half a
-    unit, their sum by V halves, and conf is rounded to float32."""
+    """The settings as the call took them (float32). Weights are whole numbers of one unit, 2^-45 of the largest or, so that
+    V of them stay below 2^62, 2^-(62 - bits): each is off by half a unit (and 2^-42 of itself: the series and its
+    table), a sum of V of them by V halves, the sum is at least 1, and conf is rounded to float32 (2^-24 of itself)."""
     x = x.double().cpu().numpy()
     n, V = x.shape
     bits = math.ceil(math.log2(V)) if V > 1 else 0
@@ -49,7 +50,8 @@ def check(x, got, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
         k = int(np.broadcast_to(np.asarray(top_k), (n,))[r])
         t, c, kept = sample_row(x[r], at(temperature, r), k, at(top_p, r), at(min_p, r), at(u, r))
         assert (got[0][r], got[2][r]) == (t, kept), (r, got[0][r], t, got[2][r], kept)
-        assert abs(float(got[1][r]) - c) <= c * (2.0 ** -24 + 2.0 ** (2 * bits - 63)) + 2.0 ** (bits - 62), (r, got[1][r], c)
+        half = 2.0 ** -(min(45, 62 - bits) + 1)
+        assert abs(float(got[1][r]) - c) <= c * (2.0 ** -24 + 2.0 ** -41 + V * half) + half, (r, got[1][r], c)
 
 
 def logits(n, V, seed, std=2.0, peaks=True):
