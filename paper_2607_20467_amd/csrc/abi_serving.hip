@@ -115,12 +115,14 @@ dcl_status check_heads(int32_t n_heads, int32_t n_kv_heads) {
 
 // Workspace of an attention call over pages: the parts' outputs and their (reference, sum).
 struct PartLayout {
-  int nsplit;
+  int nsplit, span;
   size_t ml, total;
 };
 PartLayout part_layout(const dcl_pages* g, int32_t n_heads, int32_t B, int32_t T, int32_t max_new, int32_t max_pages) {
   PartLayout L;
-  L.nsplit = pages_attention_splits(g->n_kv_heads, n_heads / g->n_kv_heads, B, max_new, max_pages * g->page_len);
+  const int capacity = max_pages * g->page_len;
+  L.span = pages_attention_span(g->n_kv_heads, n_heads / g->n_kv_heads, B, max_new, capacity, g->dtype == DCL_DTYPE_E4M3);
+  L.nsplit = (capacity + L.span - 1) / L.span;
   const size_t rows = (size_t)L.nsplit * T * n_heads;
   L.ml = L.nsplit > 1 ? rows * g->head_dim * 4 : 0;
   L.total = L.nsplit > 1 ? L.ml + rows * 8 : 256;
@@ -129,7 +131,7 @@ PartLayout part_layout(const dcl_pages* g, int32_t n_heads, int32_t B, int32_t T
 
 dcl_status check_attention_size(const dcl_pages* g, int32_t n_heads, int32_t B, int32_t max_new) {
   const int64_t tiles = ((int64_t)(n_heads / g->n_kv_heads) * max_new + 15) / 16;
-  if (tiles * g->n_kv_heads * B * 64 >= (1LL << 31) || (int64_t)max_new * B * (n_heads + 8) >= (1LL << 31))
+  if (tiles * g->n_kv_heads * B * 128 >= (1LL << 31) || (int64_t)max_new * B * (n_heads + 8) >= (1LL << 31))
     return fail(DCL_E_UNSUPPORTED, "B=%d sequences of %d new tokens x %d heads: too many for one call", B, max_new, n_heads);
   return DCL_OK;
 }
@@ -243,8 +245,10 @@ dcl_status dcl_pages_attention(const dcl_pages* pages, const int32_t* table, int
   a.g = n_heads / pages->n_kv_heads;
   a.causal = causal;
   a.nsplit = L.nsplit;
+  a.span = L.span;
   a.row_tiles = 0;
-  a.scale_log2 = (float)(1.4426950408889634 * (double)scale);
+  a.q_sign = scale < 0.f ? 0x80008000u : 0u;
+  a.scale_log2 = scale_log2(scale);
   (void)hipGetLastError();
   launch_pages_attention(a, stream);
   return hip_check(hipGetLastError(), "pages_attention launch");

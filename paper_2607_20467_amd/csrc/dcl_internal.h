@@ -205,11 +205,12 @@ struct PagesAttn {
   float* lse;                    // [T, H] or null
   float* po;                     // partial outputs [nsplit, T, H, dh] (nsplit > 1)
   float2* pml;                   // their (reference, sum) [nsplit, T, H]
-  int H, g, causal, nsplit, row_tiles;
-  float scale_log2;
+  int H, g, causal, nsplit, span, row_tiles;  // parts of `span` keys (a multiple of 64)
+  uint32_t q_sign;               // the scale's sign, for both halves of a word of queries
+  float scale_log2;              // its magnitude times log2(e), a normal number
 };
-// Parts that a call's key lengths are split into: from sizes that the host knows.
-int pages_attention_splits(int Hkv, int g, int B, int max_new, int capacity);
+// Keys of one part: from sizes that the host knows (capacity: positions that a row of the table can name).
+int pages_attention_span(int Hkv, int g, int B, int max_new, int capacity, int e4m3);
 void launch_pages_attention(PagesAttn a, hipStream_t s);
 
 struct PromptAttn {

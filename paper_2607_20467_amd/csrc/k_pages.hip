@@ -257,19 +257,22 @@ void launch_pages_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, h
 // ---------------------------------------------------------------- attention over pages
 // o = sum_j softmax_j(scale q.k_j) v_j over the keys j of the sequence, per query row one running maximum and sum.
 // The rows of one KV head (its g = H / Hkv query heads times the sequence's new tokens) are tiles of 16 QF; a workgroup
-// takes one tile and one of `nsplit` equal parts of the keys, its four waves every fourth tile of KT keys. The cache is
+// takes one tile and `span` keys of the sequence, its four waves every fourth tile of KT of them. The cache is
 // read once from HBM straight into the registers of the matrix instructions (no LDS: with one new token nothing is
 // shared between waves), the scores are S^T = K Q^T and the probabilities feed O^T = V^T P^T from the same lanes.
 //
 // Which key sits in which row of a matrix instruction is free as long as scores and values agree: with PK = KT / 4, row
 // 4 a + r of score step kt is key PK a + 4 kt + r, so that lane group a (= lane / 16) ends up with the probabilities of PK
 // adjacent keys, which lie in one page, and reads its values as whole pieces of the position-innermost rows. In the same
-// way a lane holds 16 adjacent dimensions of a key, two steps of 32. KT is 64 for 8-bit pages (16-byte pieces of values)
-// and 32 for bfloat16 ones, and for 8-bit ones under four query fragments, whose registers a larger tile would spill.
+// way the dimensions of a step are those of one 16-byte piece of a key per lane, so that a load covers 64 adjacent bytes of
+// each of 16 keys: 8 dimensions of bfloat16, or 16 of 8 bits, which are two steps. KT is 64 for 8-bit pages (16-byte pieces
+// of values) and 32 for bfloat16 ones, and for 8-bit ones under several query fragments, whose registers a larger tile
+// would spill.
 //
-// 8-bit rows become bfloat16 without their scales (exact). A key's scale multiplies its score, a value's its
-// probability, in float32; the probability is then rounded to bfloat16 once, 2^-9 of itself, while the sum that divides
-// takes it unrounded: over many keys these roundings average out, far below the rounding of the output.
+// 8-bit rows become bfloat16, exactly: a key with its scale (the conversion takes one; all of a lane's piece is one key),
+// a value without, since its piece is many keys; that scale multiplies the key's probability in float32. The probability
+// is then rounded to bfloat16 once, 2^-9 of itself, while the sum that divides takes it unrounded: over many keys these
+// roundings average out, far below the rounding of the output.
 __device__ __forceinline__ f32x4_t mfma16p(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -281,27 +284,22 @@ __device__ __forceinline__ float sum_groups(float v) {
   v += __shfl_xor(v, 16, 64);
   return v + __shfl_xor(v, 32, 64);
 }
-__device__ __forceinline__ bf16x8_t widen8(uint32_t lo, uint32_t hi) {  // eight e4m3 bytes, exactly
+// eight e4m3 bytes times a power of two
+__device__ __forceinline__ bf16x8_t widen8(uint32_t lo, uint32_t hi, float scale = 1.0f) {
   uint4 o;
-  o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
-  o.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
-  o.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
-  o.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
+  o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false));
+  o.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true));
+  o.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false));
+  o.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true));
   return __builtin_bit_cast(bf16x8_t, o);
-}
-
-// Keys that each part of a sequence with `keys` keys takes, in tiles of 64: part i has [i, i + 1) * the result.
-__device__ __forceinline__ int tiles_per_part(int keys, int nsplit) {
-  const int tiles = (keys + 63) >> 6;
-  return (tiles + nsplit - 1) / nsplit;
 }
 
 // A reference point, and what a row without keys (reference -inf) is taken relative to.
 __device__ __forceinline__ float finite_ref(float m) { return m == -INFINITY ? 0.f : m; }
 
 template <int DH, bool E4, int QF>
-__global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesAttn a) {
-  constexpr int ES = E4 ? 1 : 2, KT = E4 && QF < 4 ? 64 : 32, PK = KT / 4, NKT = KT / 16, S2 = KT / 32;
+__global__ void __launch_bounds__(256, QF <= 2 ? 2 : 1) pages_attn_kernel(PagesAttn a) {
+  constexpr int ES = E4 ? 1 : 2, KT = E4 && QF == 1 ? 64 : 32, PK = KT / 4, NKT = KT / 16, S2 = KT / 32;
   constexpr int KS = DH / 32, DT = DH / 16;
   constexpr int NK = DH * ES / 64;  // 16-byte pieces of a lane's dimensions of one key
   constexpr int VW = PK * ES / 4;   // words of a lane's keys of one dimension
@@ -318,7 +316,7 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesA
   if (row0 >= rows) return;
   const int len = seq_len(p.len, b), plen = 1 << p.shift;
   const int kend = min(len, p.max_pages << p.shift);  // keys that the table can name
-  const int per = tiles_per_part(kend, a.nsplit) * (64 / KT), t0 = part * per, t1 = min(t0 + per, (kend + KT - 1) / KT);
+  const int t0 = part * (a.span / KT), t1 = min(t0 + a.span / KT, (kend + KT - 1) / KT);
   if (part > 0 && t0 >= t1) return;  // part 0 always answers
   const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 15, lg = lane >> 4, la = lq >> 2, lr = lq & 3;
@@ -330,14 +328,18 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesA
 #pragma unroll
   for (int f = 0; f < QF; ++f) {
     const int rr = min(row0 + 16 * f + lq, rows - 1), i = rr / a.g, head = h * a.g + rr % a.g;
-    const bf16_t* qp = a.q + (size_t)(r.first + i) * a.q_stride + (size_t)head * DH + 16 * lg;
+    const bf16_t* qp = a.q + (size_t)(r.first + i) * a.q_stride + (size_t)head * DH + (E4 ? 16 : 8) * lg;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      qf[f][ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(qp + 64 * (ks >> 1) + 8 * (ks & 1)));
+    for (int ks = 0; ks < KS; ++ks) {
+      uint4 x = *reinterpret_cast<const uint4*>(qp + (E4 ? 64 * (ks >> 1) + 8 * (ks & 1) : 32 * ks));
+      x.x ^= a.q_sign, x.y ^= a.q_sign, x.z ^= a.q_sign, x.w ^= a.q_sign;  // a negative scale is a sign of the query
+      qf[f][ks] = __builtin_bit_cast(bf16x8_t, x);
+    }
     lim[f] = a.causal ? min(kend, max(0, len - r.n + i + 1)) : kend;
   }
   if (a.causal) lim_min = min(kend, max(0, len - r.n + row0 / a.g + 1));
 
+  const float scale = a.scale_log2;
   f32x4_t o[QF][DT];
   float m[QF], l[QF];
 #pragma unroll
@@ -363,12 +365,16 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesA
   };
   auto load_keys = [&](int t, int pid) {  // pid: page of keys KT t + PK la ..
     const int off = ((KT * t + PK * la) & (plen - 1)) + lr;
-    const uint8_t* base = p.k + (size_t)max(pid, 0) * page_bytes + head_bytes + (size_t)off * (DH * ES) + lg * 16 * ES;
+    const uint8_t* base = p.k + (size_t)max(pid, 0) * page_bytes + head_bytes + (size_t)off * (DH * ES) + lg * 16;
 #pragma unroll
     for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
       for (int x = 0; x < NK; ++x)
-        kr[kt][x] = *reinterpret_cast<const uint4*>(base + kt * 4 * DH * ES + (E4 ? 64 * x : 128 * (x >> 1) + 16 * (x & 1)));
+        kr[kt][x] = *reinterpret_cast<const uint4*>(base + kt * 4 * DH * ES + 64 * x);
+    if constexpr (E4) {  // byte lr of word kt
+      const size_t at = ((size_t)max(pid, 0) * p.Hkv + h) * plen + ((KT * t + PK * la) & (plen - 1));
+      load_words(ksr, p.ks + at, std::integral_constant<int, SW>());
+    }
   };
   auto load_values = [&](int t, int pid) {  // pid: page of keys KT t + PK lg ..
     const int off = (KT * t + PK * lg) & (plen - 1);
@@ -378,7 +384,6 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesA
     for (int dt = 0; dt < DT; ++dt) load_words(vr[dt], base + dt * step, std::integral_constant<int, VW>());
     if constexpr (E4) {
       const size_t at = ((size_t)max(pid, 0) * p.Hkv + h) * plen + off;
-      load_words(ksr, p.ks + at, std::integral_constant<int, SW>());
       load_words(vsr, p.vs + at, std::integral_constant<int, SW>());
     }
     pid_v = pid;
@@ -410,11 +415,12 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesA
 #pragma unroll
     for (int kt = 0; kt < NKT; ++kt) {
       bf16x8_t kf[KS];
+      const float key_scale = E4 ? scale_of((ksr[E4 ? kt : 0] >> (8 * lr)) & 255u) : 1.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         if constexpr (E4) {
           const uint4 x = kr[kt][ks >> 1];
-          kf[ks] = ks & 1 ? widen8(x.z, x.w) : widen8(x.x, x.y);
+          kf[ks] = ks & 1 ? widen8(x.z, x.w, key_scale) : widen8(x.x, x.y, key_scale);
         } else {
           kf[ks] = __builtin_bit_cast(bf16x8_t, kr[kt][ks]);
         }
@@ -426,15 +432,7 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesA
     }
     if (t + 4 < t1) load_keys(t + 4, pk);
 
-    // log2 units; then the keys that a row does not see: past its limit, past the last key, in no page
-#pragma unroll
-    for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-      for (int rr = 0; rr < 4; ++rr) {
-        const float f1 = E4 ? scale_of((ksr[kt] >> (8 * rr)) & 255u) * a.scale_log2 : a.scale_log2;
-#pragma unroll
-        for (int f = 0; f < QF; ++f) sc[f][kt][rr] *= f1;
-      }
+    // the keys that a row does not see: past its limit, past the last key, in no page
     const bool whole = KT * t + KT <= lim_min && __builtin_amdgcn_ballot_w64(pid_v < 0) == 0;
     auto dead = [&](int f, int kt, int rr) { return pid_v < 0 || k0 + 4 * kt + rr >= lim[f]; };
     if (!whole) {
@@ -446,7 +444,7 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesA
           for (int rr = 0; rr < 4; ++rr)
             if (dead(f, kt, rr)) sc[f][kt][rr] = -INFINITY;
     }
-    // The reference point m moves only when a score passes it by more than 2^8 (any reference gives the same
+    // The reference point m (log2 units) moves only when a score passes it by more than 2^8 (any reference gives the same
     // quotient), so that most tiles need no maximum across the lanes and no rescaling.
     float tmax[QF];
     bool move = false;
@@ -457,12 +455,12 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesA
       for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
         for (int rr = 0; rr < 4; ++rr) tmax[f] = fmaxf(tmax[f], sc[f][kt][rr]);
-      move |= tmax[f] > m[f] + 8.f;
+      move |= tmax[f] * scale > m[f] + 8.f;
     }
     if (__builtin_amdgcn_ballot_w64(move)) {
 #pragma unroll
       for (int f = 0; f < QF; ++f) {
-        const float ts = max_groups(tmax[f]);
+        const float ts = max_groups(tmax[f]) * scale;
         const float mn = ts > m[f] + 8.f ? ts : m[f];
         const float alpha = mn == m[f] ? 1.f : __builtin_amdgcn_exp2f(m[f] - mn);
         l[f] *= alpha;
@@ -474,12 +472,12 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesA
     bf16x8_t pf[QF][S2];
 #pragma unroll
     for (int f = 0; f < QF; ++f) {
-      const float mr = finite_ref(m[f]);
+      const float mr = -finite_ref(m[f]);
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
         for (int rr = 0; rr < 4; ++rr) {
-          const float pv1 = __builtin_amdgcn_exp2f(sc[f][kt][rr] - mr);
+          const float pv1 = __builtin_amdgcn_exp2f(fmaf(sc[f][kt][rr], scale, mr));
           l[f] += pv1;
           sc[f][kt][rr] = pv1;
           if constexpr (E4) {
@@ -510,62 +508,33 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesA
         }
       }
       if (__builtin_amdgcn_ballot_w64(odd != 0)) {
-        uint4 sees[QF][S2];  // 1 where the row sees the key
-#pragma unroll
-        for (int f = 0; f < QF; ++f)
-#pragma unroll
-          for (int s2 = 0; s2 < S2; ++s2) {
-            uint32_t* sp = &sees[f][s2].x;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              sp[j] = (dead(f, 2 * s2 + (j >> 1), 2 * (j & 1)) ? 0u : 0x3F80u) |
-                      (dead(f, 2 * s2 + (j >> 1), 2 * (j & 1) + 1) ? 0u : 0x3F800000u);
-          }
+        // rare, and written for few registers: such values leave the product and are added key by key, from the page
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-          for (int s2 = 0; s2 < S2; ++s2) {
-            __builtin_amdgcn_sched_barrier(0);
-            // 1 where the value is +inf or NaN, 1 where it is -inf or NaN; those values become 0
-            uint4 up, dn;
-            uint32_t *upp = &up.x, *dnp = &dn.x;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              upp[j] = dnp[j] = 0;
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                if constexpr (E4) {
-                  uint32_t* w = &vr[dt][2 * s2 + (j >> 1)];
-                  const int sh = 16 * (j & 1) + 8 * e;
-                  if (((*w >> sh) & 0x7Fu) == 0x7Fu) {
-                    upp[j] |= 0x3F80u << (16 * e);
-                    dnp[j] |= 0x3F80u << (16 * e);
-                    *w &= ~(0xFFu << sh);
-                  }
-                } else {
-                  uint32_t* w = &vr[dt][j];
-                  const uint32_t x = (*w >> (16 * e)) & 0xFFFFu;
-                  if ((x & 0x7F80u) == 0x7F80u) {
-                    if (x != 0xFF80u) upp[j] |= 0x3F80u << (16 * e);
-                    if (x != 0x7F80u) dnp[j] |= 0x3F80u << (16 * e);
-                    *w &= ~(0xFFFFu << (16 * e));
-                  }
-                }
-              }
-            }
-            const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int f = 0; f < QF; ++f) {
-              const bf16x8_t sv = __builtin_bit_cast(bf16x8_t, sees[f][s2]);
-              const f32x4_t cu = mfma16p(__builtin_bit_cast(bf16x8_t, up), sv, zero);
-              const f32x4_t cd = mfma16p(__builtin_bit_cast(bf16x8_t, dn), sv, zero);
-#pragma unroll
-              for (int rr = 0; rr < 4; ++rr) {
-                if (cu[rr] > 0.f) o[f][dt][rr] += INFINITY;
-                if (cd[rr] > 0.f) o[f][dt][rr] -= INFINITY;
-              }
-            }
+          for (int j = 0; j < VW; ++j) {
+            const uint32_t w = vr[dt][j];
+            const uint32_t m = E4 ? ((((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xFFu
+                                  : ((((w & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u) >> 15) * 0xFFFFu;
+            vr[dt][j] = w & ~m;
           }
+#pragma unroll 1
+        for (int y = 0; y < KT; ++y) {
+          const int key = KT * t + y, pid = page_at(t, y / PK);
+          if (pid < 0 || key >= kend) continue;
+          const uint8_t* at = p.v + (size_t)pid * page_bytes + head_bytes + ((size_t)4 * lg * plen + (key & (plen - 1))) * ES;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int rr = 0; rr < 4; ++rr) {
+              const uint8_t* e = at + (size_t)(16 * dt + rr) * plen * ES;
+              const uint32_t v = E4 ? ((*e & 0x7Fu) == 0x7Fu ? 0x7FC00000u : 0u) : (uint32_t)*reinterpret_cast<const uint16_t*>(e) << 16;
+              if ((v & 0x7F800000u) != 0x7F800000u) continue;
+#pragma unroll
+              for (int f = 0; f < QF; ++f)
+                if (key < lim[f]) o[f][dt][rr] += __uint_as_float(v);
+            }
+        }
       }
     }
 #pragma unroll
@@ -616,7 +585,7 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesA
     const int rr = row0 + 16 * f + lq;
     if (rr >= rows) continue;
     const size_t at = (size_t)(r.first + rr / a.g) * a.H + h * a.g + rr % a.g;
-    if (a.nsplit > 1) {
+    if (a.nsplit > 1) {  // uniform: the join reads all of them
       float* dst = a.po + ((size_t)part * p.T * a.H + at) * DH + 4 * lg;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = o[f][dt];
@@ -633,58 +602,90 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages_attn_kernel(PagesA
   }
 }
 
-// The parts of a sequence's rows joined, in order: DH / 4 lanes per (row, head).
-template <int DH>
+// The parts of a (row, head) joined: DH / 4 lanes take its dimensions, G such groups every G-th part, then the groups' sums
+// in order. One group (and 8 or 16 (row, head)s a workgroup) is enough for up to 16 parts; 128 parts of 131072 keys took
+// 100 us so, a load after the other, and take 5 us with all of a workgroup's groups on one row.
+template <int DH, bool WIDE>
 __global__ void __launch_bounds__(256) pages_join_kernel(PagesAttn a, int head_blocks) {
-  constexpr int L = DH / 4, PER = 256 / L;
+  constexpr int L = DH / 4, PER = 256 / L, G = WIDE ? PER : 1;
+  __shared__ float4 xo[PER][L];
+  __shared__ float xl[PER];
   const Pages& p = a.p;
   const int hb = blockIdx.x % head_blocks, bi = blockIdx.x / head_blocks, i = bi % p.max_new, b = bi / p.max_new;
   const SeqRows r = seq_rows(p.cu, b, p.T);
-  const int head = hb * PER + threadIdx.x / L, c = threadIdx.x % L;
-  if (i >= r.n || head >= a.H) return;
-  const int kend = min(seq_len(p.len, b), p.max_pages << p.shift), per = tiles_per_part(kend, a.nsplit);
-  const int parts = per == 0 ? 1 : ((kend + 63) / 64 + per - 1) / per;
+  const int grp = threadIdx.x / L, c = threadIdx.x % L, head = WIDE ? hb : hb * PER + grp;
+  if (i >= r.n) return;
+  const bool mine = head < a.H;  // uniform over the workgroup where groups meet
+  const int kend = min(seq_len(p.len, b), p.max_pages << p.shift);
+  const int parts = !mine ? 0 : kend == 0 ? 1 : (kend + a.span - 1) / a.span;
   const size_t at = (size_t)(r.first + i) * a.H + head, step = (size_t)p.T * a.H;
   float mm = -INFINITY;
-  for (int s = 0; s < parts; ++s) mm = fmaxf(mm, a.pml[s * step + at].x);
+  for (int s = c; s < parts; s += L) mm = fmaxf(mm, a.pml[s * step + at].x);
+#pragma unroll
+  for (int x = L / 2; x >= 1; x >>= 1) mm = fmaxf(mm, __shfl_xor(mm, x, 64));
   const float ref = finite_ref(mm);
   float lt = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s = 0; s < parts; ++s) {
+  auto add = [](float4& s, const float4& x, float e) {
+    s.x += x.x * e;
+    s.y += x.y * e;
+    s.z += x.z * e;
+    s.w += x.w * e;
+  };
+#pragma unroll 4
+  for (int s = WIDE ? grp : 0; s < parts; s += G) {
     const float2 ml = a.pml[s * step + at];
-    if (ml.x == -INFINITY && ml.y == 0.f) continue;  // a part without keys that the row sees
-    const float e = __builtin_amdgcn_exp2f(ml.x - ref);
     const float4 x = *reinterpret_cast<const float4*>(a.po + (s * step + at) * DH + 4 * c);
+    // a part without keys that the row sees: (-inf, 0), and zeros for an output
+    const float e = __builtin_amdgcn_exp2f(ml.x - ref);
     lt += ml.y * e;
-    o.x += x.x * e;
-    o.y += x.y * e;
-    o.z += x.z * e;
-    o.w += x.w * e;
+    add(o, x, e);
   }
+  if constexpr (WIDE) {
+    xo[grp][c] = o;
+    if (c == 0) xl[grp] = lt;
+    __syncthreads();
+    if (grp > 0) return;
+#pragma unroll
+    for (int s = 1; s < PER; ++s) {
+      lt += xl[s];
+      add(o, xo[s][c], 1.f);
+    }
+  }
+  if (!mine) return;
   const float inv = lt == 0.f ? 0.f : 1.0f / lt;
   *reinterpret_cast<uint2*>(a.out + at * DH + 4 * c) = make_uint2(f2bf2(o.x * inv, o.y * inv), f2bf2(o.z * inv, o.w * inv));
   if (a.lse && c == 0) a.lse[at] = lt == 0.f ? -INFINITY : mm * 0.6931471805599453f + logf(lt);
 }
 
-// Query fragments per wave: as many as the rows of a KV head fill, up to four.
-static int query_fragments(int g, int max_new) {
+// Query fragments (16 rows each) per wave. Four read a KV head's cache once for 64 rows, two let two workgroups share a
+// CU: 8 x 64 queries x 32 / 32 heads over 1280 8-bit keys, 256 or 512 workgroups, 45.9 against 46.5 us (one: 56.5); 8 x 64
+// x 28 / 4 heads, 224, bfloat16 54 against 60 (88); but 8 x 16 x 28 / 4, 64 workgroups, 35.8 against 24.3 (33.1), so four
+// only from 128 workgroups on.
+static int query_fragments(int Hkv, int g, int B, int max_new) {
   const long rows = (long)g * max_new;
-  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  return rows <= 16 ? 1 : rows <= 32 || (rows + 63) / 64 * Hkv * B < 128 ? 2 : 4;
 }
 
-int pages_attention_splits(int Hkv, int g, int B, int max_new, int capacity) {
-  const int qf = query_fragments(g, max_new);
-  const long units = (((long)g * max_new + 16 * qf - 1) / (16 * qf)) * Hkv * B;
-  if (units < 1) return 1;
-  const long most = (capacity + 255) / 256;  // at least 64 keys per wave
-  long n = (1024 + units - 1) / units;
-  n = n < 1 ? 1 : n > most ? most : n;
-  return n < 1 ? 1 : n > 64 ? 64 : (int)n;
+// Keys of a part: about 2048 workgroups if every sequence filled its row of the table (fewer leave CUs idle and the longest
+// sequence's parts last; more spend their time on their first loads: one token of 64 sequences of 200 to 8000, 2048 / 4096 /
+// 8192 workgroups 81 / 85 / 90 us), at most 128 parts. A part's output costs 8 bytes an element of memory traffic: at most
+// an eighth of the part's keys and values, unless there are too few workgroups for that to matter.
+int pages_attention_span(int Hkv, int g, int B, int max_new, int capacity, int e4m3) {
+  const int qf = query_fragments(Hkv, g, B, max_new);
+  const long rows = (long)g * max_new, units = ((rows + 16 * qf - 1) / (16 * qf)) * Hkv * B;
+  if (units < 1) return 64;
+  const long tile = rows < 16 * qf ? rows : 16 * qf, cheap = 32 * tile / (e4m3 ? 1 : 2);
+  long span = ((long)capacity * units + 2047) / 2048;
+  if (span < cheap && units * ((capacity + span - 1) / span) > 256) span = cheap;
+  if (span < 256) span = 256;
+  if (span < (capacity + 127) / 128) span = (capacity + 127) / 128;
+  return (int)((span + 63) / 64 * 64);
 }
 
 template <int DH, bool E4>
 static void run_pages_attention(PagesAttn& a, hipStream_t s) {
-  const int qf = query_fragments(a.g, a.p.max_new);
+  const int qf = query_fragments(a.p.Hkv, a.g, a.p.B, a.p.max_new);
   a.row_tiles = (int)(((long)a.g * a.p.max_new + 16 * qf - 1) / (16 * qf));
   const long items = (long)a.nsplit * a.p.B * a.p.Hkv;
   const dim3 grid((unsigned)((items + 7) / 8 * 8 * a.row_tiles));
@@ -692,8 +693,11 @@ static void run_pages_attention(PagesAttn& a, hipStream_t s) {
   else if (qf == 2) hipLaunchKernelGGL((pages_attn_kernel<DH, E4, 2>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((pages_attn_kernel<DH, E4, 4>), grid, dim3(256), 0, s, a);
   if (a.nsplit > 1) {
-    const int blocks = (a.H + 1024 / DH - 1) / (1024 / DH);
-    hipLaunchKernelGGL(pages_join_kernel<DH>, dim3((unsigned)blocks * a.p.max_new * a.p.B), dim3(256), 0, s, a, blocks);
+    const bool wide = a.nsplit > 16;
+    const int blocks = wide ? a.H : (a.H + 1024 / DH - 1) / (1024 / DH);
+    const dim3 all((unsigned)blocks * a.p.max_new * a.p.B);
+    if (wide) hipLaunchKernelGGL((pages_join_kernel<DH, true>), all, dim3(256), 0, s, a, blocks);
+    else hipLaunchKernelGGL((pages_join_kernel<DH, false>), all, dim3(256), 0, s, a, blocks);
   }
 }
 
