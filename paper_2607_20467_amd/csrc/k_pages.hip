@@ -351,7 +351,9 @@ __global__ void __launch_bounds__(256, QF <= 2 ? 2 : 1) pages_attn_kernel(PagesA
   }
 
   uint4 kr[NKT][NK];                 // the tile's keys, values and scales, as loaded
-  uint32_t vr[DT][VW], ksr[SW], vsr[SW];
+  typedef uint32_t words_t __attribute__((ext_vector_type(VW)));
+  words_t vr[DT];
+  uint32_t ksr[SW], vsr[SW];
   int pid_v = -1;                    // page of the lane group's PK keys of the tile whose values are in vr
   const size_t page_bytes = (size_t)p.Hkv * plen * DH * ES, head_bytes = (size_t)h * plen * DH * ES;
   auto load_words = [](uint32_t* w, const uint8_t* src, auto words) {
@@ -381,7 +383,7 @@ __global__ void __launch_bounds__(256, QF <= 2 ? 2 : 1) pages_attn_kernel(PagesA
     const uint8_t* base = p.v + (size_t)max(pid, 0) * page_bytes + head_bytes + ((size_t)lq * plen + off) * ES;
     const size_t step = (size_t)16 * plen * ES;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) load_words(vr[dt], base + dt * step, std::integral_constant<int, VW>());
+    for (int dt = 0; dt < DT; ++dt) vr[dt] = *reinterpret_cast<const words_t*>(base + dt * step);
     if constexpr (E4) {
       const size_t at = ((size_t)max(pid, 0) * p.Hkv + h) * plen + off;
       load_words(vsr, p.vs + at, std::integral_constant<int, SW>());
@@ -391,19 +393,32 @@ __global__ void __launch_bounds__(256, QF <= 2 ? 2 : 1) pages_attn_kernel(PagesA
   // eight values of one dimension, of score steps 2 s2 and 2 s2 + 1
   auto value_fragment = [&](int dt, int s2) -> bf16x8_t {
     if constexpr (E4) return widen8(vr[dt][2 * s2], vr[dt][2 * s2 + 1]);
-    else return __builtin_bit_cast(bf16x8_t, make_uint4(vr[dt][0], vr[dt][1], vr[dt][2], vr[dt][3]));
+    else return __builtin_bit_cast(bf16x8_t, vr[dt]);
   };
   auto page_at = [&](int t, int grp) { return page_of(row, p.max_pages, p.n_pages, p.shift, (KT * t + PK * grp) >> 4); };
 
+  // Pages of the 64 chunks of 16 keys from `base` on, one a lane, and of the 64 after those: a look-up is then an exchange
+  // between lanes. Loaded tile by tile they came back in order with the values before them, so that the next keys were
+  // asked for only when this tile's values had arrived (8 x 64 tokens x 28 / 4 heads over 1280 keys 53.6 us, so 48.8).
+  int base = t0 * (KT / 16);
+  int ids = page_of(row, p.max_pages, p.n_pages, p.shift, base + lane);
+  int ids_next = page_of(row, p.max_pages, p.n_pages, p.shift, base + 64 + lane);
+  int pk = -1, pv = -1;
+  auto find_pages = [&](int t) {  // of tile t, at most four further than the last one asked for
+    if (t * (KT / 16) - base >= 64) {
+      base += 64;
+      ids = ids_next;
+      ids_next = page_of(row, p.max_pages, p.n_pages, p.shift, base + 64 + lane);
+    }
+    pk = __shfl(ids, (KT * t + PK * la) / 16 - base, 64);
+    pv = __shfl(ids, (KT * t + PK * lg) / 16 - base, 64);
+  };
+
   int t = t0 + wid;
-  int pk = -1, pv = -1;  // pages of tile t, then of the next one
   if (t < t1) {
-    pk = page_at(t, la);
-    pv = page_at(t, lg);
+    find_pages(t);
     load_keys(t, pk);
     load_values(t, pv);
-    pk = t + 4 < t1 ? page_at(t + 4, la) : -1;
-    pv = t + 4 < t1 ? page_at(t + 4, lg) : -1;
   }
   for (; t < t1; t += 4) {
     const int k0 = KT * t + PK * lg;  // the lane group's first key
@@ -430,7 +445,10 @@ __global__ void __launch_bounds__(256, QF <= 2 ? 2 : 1) pages_attn_kernel(PagesA
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) sc[f][kt] = mfma16p(kf[ks], qf[f][ks], sc[f][kt]);
     }
-    if (t + 4 < t1) load_keys(t + 4, pk);
+    if (t + 4 < t1) {
+      find_pages(t + 4);
+      load_keys(t + 4, pk);
+    }
 
     // the keys that a row does not see: past its limit, past the last key, in no page
     const bool whole = KT * t + KT <= lim_min && __builtin_amdgcn_ballot_w64(pid_v < 0) == 0;
@@ -497,27 +515,35 @@ __global__ void __launch_bounds__(256, QF <= 2 ? 2 : 1) pages_attn_kernel(PagesA
     if (!whole) {
       const int nv = pid_v < 0 ? 0 : kend - k0;  // the lane group's keys that are there
       uint32_t odd = 0;
+      words_t keep;
 #pragma unroll
       for (int j = 0; j < VW; ++j) {
         const int bits = E4 ? 8 * (nv - 4 * j) : 16 * (nv - 2 * j);
-        const uint32_t keep = bits >= 32 ? ~0u : bits <= 0 ? 0u : (1u << bits) - 1u;
+        keep[j] = bits >= 32 ? ~0u : bits <= 0 ? 0u : (1u << bits) - 1u;
+      }
+      // Each group of registers is changed as one and pinned as one (the empty assembly): changed word by word, this
+      // compiler gave the product registers of other words (ROCm 7.2, two fragments, bfloat16).
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const uint32_t w = vr[dt][j] &= keep;
-          odd |= E4 ? ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u : ((w & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u;
-        }
+      for (int dt = 0; dt < DT; ++dt) {
+        vr[dt] &= keep;
+        asm volatile("" : "+v"(vr[dt]));
+#pragma unroll
+        for (int j = 0; j < VW; ++j)
+          odd |= E4 ? ((vr[dt][j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u
+                    : ((vr[dt][j] & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u;
       }
       if (__builtin_amdgcn_ballot_w64(odd != 0)) {
         // rare, and written for few registers: such values leave the product and are added key by key, from the page
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+        for (int dt = 0; dt < DT; ++dt) {
+          words_t m;
 #pragma unroll
-          for (int j = 0; j < VW; ++j) {
-            const uint32_t w = vr[dt][j];
-            const uint32_t m = E4 ? ((((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xFFu
-                                  : ((((w & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u) >> 15) * 0xFFFFu;
-            vr[dt][j] = w & ~m;
-          }
+          for (int j = 0; j < VW; ++j)
+            m[j] = E4 ? ((((vr[dt][j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xFFu
+                      : ((((vr[dt][j] & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u) >> 15) * 0xFFFFu;
+          vr[dt] &= ~m;
+          asm volatile("" : "+v"(vr[dt]));
+        }
 #pragma unroll 1
         for (int y = 0; y < KT; ++y) {
           const int key = KT * t + y, pid = page_at(t, y / PK);
@@ -545,13 +571,7 @@ __global__ void __launch_bounds__(256, QF <= 2 ? 2 : 1) pages_attn_kernel(PagesA
 #pragma unroll
         for (int f = 0; f < QF; ++f) o[f][dt] = mfma16p(vf, pf[f][s2], o[f][dt]);
       }
-    if (t + 4 < t1) {
-      load_values(t + 4, pv);
-      if (t + 8 < t1) {
-        pk = page_at(t + 8, la);
-        pv = page_at(t + 8, lg);
-      }
-    }
+    if (t + 4 < t1) load_values(t + 4, pv);
   }
 
   // the waves' (m, l, o) joined in wave order, query fragment by query fragment
@@ -658,29 +678,30 @@ __global__ void __launch_bounds__(256) pages_join_kernel(PagesAttn a, int head_b
   if (a.lse && c == 0) a.lse[at] = lt == 0.f ? -INFINITY : mm * 0.6931471805599453f + logf(lt);
 }
 
-// Query fragments (16 rows each) per wave. Four read a KV head's cache once for 64 rows, two let two workgroups share a
-// CU: 8 x 64 queries x 32 / 32 heads over 1280 8-bit keys, 256 or 512 workgroups, 45.9 against 46.5 us (one: 56.5); 8 x 64
-// x 28 / 4 heads, 224, bfloat16 54 against 60 (88); but 8 x 16 x 28 / 4, 64 workgroups, 35.8 against 24.3 (33.1), so four
-// only from 128 workgroups on.
+// Query fragments (16 rows each) per wave. Two let two workgroups share a CU, four read a KV head's cache once for 64 rows
+// and pay for it where the rows are more and the workgroups enough: us with 1 / 2 / 4, over 1280 keys, 8 x 64 tokens x
+// 32 / 32 heads (64 rows, 8 bits) 56 / 31 / 44; 28 / 4 heads, bfloat16: 8 x 64 (448 rows, 224 workgroups of 64) 88 / 57 / 49,
+// 8 x 32 (112) 51 / 37 / 33, 8 x 16 (64) 33 / 24 / 35.
 static int query_fragments(int Hkv, int g, int B, int max_new) {
   const long rows = (long)g * max_new;
-  return rows <= 16 ? 1 : rows <= 32 || (rows + 63) / 64 * Hkv * B < 128 ? 2 : 4;
+  return rows <= 16 ? 1 : rows <= 64 || (rows + 63) / 64 * Hkv * B < 96 ? 2 : 4;
 }
 
 // Keys of a part: about 2048 workgroups if every sequence filled its row of the table (fewer leave CUs idle and the longest
 // sequence's parts last; more spend their time on their first loads: one token of 64 sequences of 200 to 8000, 2048 / 4096 /
 // 8192 workgroups 81 / 85 / 90 us), at most 128 parts. A part's output costs 8 bytes an element of memory traffic: at most
-// an eighth of the part's keys and values, unless there are too few workgroups for that to matter.
+// a sixteenth of the part's keys and values, unless there are too few workgroups for that to matter.
 int pages_attention_span(int Hkv, int g, int B, int max_new, int capacity, int e4m3) {
   const int qf = query_fragments(Hkv, g, B, max_new);
   const long rows = (long)g * max_new, units = ((rows + 16 * qf - 1) / (16 * qf)) * Hkv * B;
   if (units < 1) return 64;
-  const long tile = rows < 16 * qf ? rows : 16 * qf, cheap = 32 * tile / (e4m3 ? 1 : 2);
+  const long tile = rows < 16 * qf ? rows : 16 * qf, cheap = 64 * tile / (e4m3 ? 1 : 2);
   long span = ((long)capacity * units + 2047) / 2048;
   if (span < cheap && units * ((capacity + span - 1) / span) > 256) span = cheap;
   if (span < 256) span = 256;
-  if (span < (capacity + 127) / 128) span = (capacity + 127) / 128;
-  return (int)((span + 63) / 64 * 64);
+  long parts = (capacity + span / 2) / span;
+  parts = parts < 1 ? 1 : parts > 128 ? 128 : parts;
+  return (int)(((capacity + parts - 1) / parts + 63) / 64 * 64);
 }
 
 template <int DH, bool E4>

@@ -88,6 +88,42 @@ def test_attention_matches_float64(dcl, e4m3, dh, heads, hkv, page, lens, counts
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_many_rows_take_four_fragments(dcl, dh, e4m3):
+    """Enough rows and workgroups for the layout of 64 rows: partial last tiles of rows and keys, NaN behind every end, an
+    infinity (NaN in 8 bits) that only the last token sees, a missing page."""
+    lens, counts = [70, 33, 20, 64, 65, 21, 40, 100], [20, 20, 20, 7, 20, 20, 3, 20]
+    pool = Pool(dcl, lens, 16, 4, dh, e4m3, seed=12, fill=0x7F)
+    pg, off = pool.places(0)
+    pool.v[pg[69], 1, 5, off[69]] = 0x7F if e4m3 else math.inf
+    pool.v[pg[69], 1, dh - 1, off[69]] = 0xFF if e4m3 else -math.inf
+    gone = pool.table[7, 2].clone()
+    pool.table[7, 2] = -1
+    heads = 28
+    assert (heads // 4 * 20 + 63) // 64 * 4 * 8 >= 96
+    out, lse, q, cu, _ = attend(dcl, pool, counts, heads, True, 0.11)
+    pool.table[7, 2] = gone
+
+    def seen(b, n):
+        return torch.arange(n) // 16 != 2 if b == 7 else torch.ones(n, dtype=torch.bool)
+    check(pool, out, lse, q, cu, counts, heads, True, 0.11, seen=seen)
+    assert not torch.isfinite(out[19, 7:14, 5]).any() and torch.isfinite(out[:19]).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_many_parts(dcl, e4m3):
+    """More parts than one group of lanes joins, most of them empty for the short sequence, and a page missing from each."""
+    pool = Pool(dcl, [6000, 300, 0], 32, 1, 128, e4m3, seed=13)
+    missing = pool.table[:2, 3].clone()
+    pool.table[:2, 3] = -1
+    out, lse, q, cu, _ = attend(dcl, pool, [2, 1, 1], 3, True, 0.09)
+    pool.table[:2, 3] = missing
+    check(pool, out, lse, q, cu, [2, 1, 1], 3, True, 0.09, seen=lambda b, n: torch.arange(n) // 32 != 3)
+    again = attend(dcl, pool, [2, 1, 1], 3, True, 0.09)[0]
+    assert torch.equal(attend(dcl, pool, [2, 1, 1], 3, True, 0.09)[0], again)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
 def test_tokens_that_see_nothing(dcl, e4m3):
     """No key at all; fewer keys than new tokens (the first ones precede the sequence's start)."""
     pool = Pool(dcl, [0, 3, 20], 16, 2, 64, e4m3, fill=0xFF)
