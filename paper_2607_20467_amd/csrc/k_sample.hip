@@ -11,9 +11,10 @@
 // depend on timing, and a border falls as exact arithmetic on the weights has it (a float32 sum's error of 1e-7 would move
 // one border in a hundred rows of a flat distribution over 10^5 ids).
 //
-// Two kernels. The first finds the maximum of every row and answers those that need no more (the top-1 alone) or little
-// more (top-k with the ids down to its border in LDS: nothing else of the row needs a weight). The second answers the
-// others from the histogram; it is another kernel because its arithmetic takes twice the registers.
+// Two kernels, a workgroup per row. The first finds the row's maximum and answers rows that need no more (the top-1 alone)
+// or little more (top-k with the ids down to its border in LDS: nothing else of the row needs a weight), the second answers
+// the others from the histogram. Few rows are shared by several workgroups, in three kernels: maxima, then the parts'
+// elements or histograms, then one workgroup a row for the answer.
 #include <limits.h>
 
 #include "dcl_internal.h"
@@ -21,9 +22,11 @@
 namespace dcl {
 
 constexpr int kBins = 2048, kList = 2048, kSampleThreads = 1024, kWaves = kSampleThreads / 64;
-// The last bin starts 31.98 nats below the maximum: weights there are below 2^-46, which rounds to 0 of 2^-45 and more.
-constexpr float kBinsPerNat = 64.f;
-constexpr int kTable = 256;  // 2^(i / 256)
+constexpr int kTable = 256;              // steps of a factor of 2: weights come from a table of 2^(i / 256)
+constexpr int kTop = 64 * kTable;        // the maximum's step, which leaves those that count above 0
+constexpr int kFar = 47 * 32;            // 32 bins per factor of 2; 2^-47 rounds to 0 of 2^-45 and more, so this bin is the last
+constexpr double kMagic = 6755399441055744.0 + kTop;  // 1.5 * 2^52: the sum's last bit is 1, its low word the step
+constexpr int kMaxParts = 16;
 
 typedef unsigned long long u64;
 
@@ -38,55 +41,71 @@ struct Row {
   const char* base;
   const double* table;
   int V, head;       // vocabulary; elements before the row's first 16-byte line
-  int shift;
-  float M, bin_scale;
-  double rate;       // log2(e) / T
+  int p0, p1;        // the 16-byte pieces that this workgroup looks at
+  bool edges;        // and whether the elements before and behind them all
+  int drop;          // low bits that all order_keys have alike, or their complements
+  float M;
+  double rate;       // steps per unit of logit: 256 log2(e) / T
 
   // M finite
   __device__ __forceinline__ void set(float top, float T) {
     M = top;
-    rate = 1.4426950408889634 / (double)T;
-    bin_scale = fminf(fmaxf(kBinsPerNat / T, 1e-36f), 1e38f);
+    rate = kTable * 1.4426950408889634 / (double)T;
   }
-  // 2^shift times the weight of a logit x <= M: 2^(shift + y), y = (x - M) / T log2(e), with y rounded to a multiple of
-  // 1 / 256 from the table and 2^r of the rest, |r| <= 2^-9, by its series to the third power (the next term is 1.4e-13).
-  // Of no use past the histogram's range (where the weight rounds to 0).
-  __device__ __forceinline__ double weight_near(float x) const {
-    const double y = ((double)x - (double)M) * rate;
-    const double magic = 26388279066624.0;  // 1.5 * 2^44: the sum's last bit is 2^-8
-    const double t = y + magic;
-    const int k = (int)(uint32_t)__double_as_longlong(t);
-    const double z = (y - (t - magic)) * 0.6931471805599453;
-    double p = fma(z, 1.0 / 6.0, 0.5);
+  // A logit's step, added to kMagic - kTop: rises with x (as every operation in it does), kMagic for x = M.
+  __device__ __forceinline__ double step(float x) const { return fma((double)x - (double)M, rate, kMagic); }
+  __device__ __forceinline__ static uint32_t low_word(double t) { return (uint32_t)__double_as_longlong(t); }
+  __device__ __forceinline__ static bool near(double t) { return t > kMagic - 8 * kFar; }
+  // place in the histogram of a near one: 0 for x = M
+  __device__ __forceinline__ static int place(double t) { return (int)((kTop - low_word(t)) >> 3); }
+  __device__ __forceinline__ int bin(float x) const {
+    const double t = step(x);
+    return near(t) ? place(t) : kFar;
+  }
+  // 2^shift times the weight of a logit x <= M is 2^(shift - 64) 2^(step / 256) 2^(z / 256), z the rest that `step` rounds
+  // off, |z| <= 1/2: the first two are table[step % 256] with step * 2^12 added to its high word (the entry has its index
+  // taken off there, so that this leaves step / 256 in the exponent), the third is its series to the third power (the next
+  // term is 1.4e-13). For steps above -200 * 256.
+  struct Factors {
+    double scale, rest;
+  };
+  __device__ __forceinline__ Factors factors(float x, double t) const {
+    const double z = fma((double)x - (double)M, rate, kMagic - t);
+    constexpr double c = 0.6931471805599453 / kTable;
+    double p = fma(z, c * c * c / 6.0, c * c / 2.0);
+    p = fma(z, p, c);
     p = fma(z, p, 1.0);
-    p = fma(z, p, 1.0);
-    return __builtin_amdgcn_ldexp(table[k & (kTable - 1)] * p, (k >> 8) + shift);
+    const uint32_t k = low_word(t);
+    const u64 bits = (u64)__double_as_longlong(table[k & (kTable - 1)]) + ((u64)(k << 12) << 32);
+    return {__longlong_as_double((long long)bits), p};
   }
-  __device__ __forceinline__ double weight(float x) const {  // any x <= M
-    return ((double)x - (double)M) * rate > -200.0 ? weight_near(x) : 0.0;
+  __device__ __forceinline__ double weight(float x) const {
+    const double t = step(x);
+    if (!(t > kMagic - 200.0 * kTable)) return 0.0;
+    const Factors f = factors(x, t);
+    return f.scale * f.rest;
   }
-  __device__ __forceinline__ static u64 fixed(double w) {  // 0 <= w < 2^52, to the nearest whole number
-    return (u64)__double_as_longlong(w + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+  // the weight as a whole number (below 2^52), of a near logit and of any
+  __device__ __forceinline__ u64 near_mass(float x, double t) const {
+    const Factors f = factors(x, t);
+    return (u64)__double_as_longlong(fma(f.scale, f.rest, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
   }
-  // place in the histogram: does not decrease while x falls; 0 for x = M
-  __device__ __forceinline__ float place(float x) const { return (M - x) * bin_scale; }
-  __device__ __forceinline__ int bin(float x) const { return (int)fminf(place(x), (float)(kBins - 1)); }
-  // the least logit above -inf for which `keep` holds; keep(M) does, and for whatever lies above one for which it does
-  template <class P>
-  __device__ __forceinline__ float least(P keep) const {
-    uint32_t lo = order_key(-3.4028234663852886e38f), hi = order_key(M);
-#pragma unroll 1
-    while (lo < hi) {
-      const uint32_t mid = lo + (hi - lo) / 2;
-      if (keep(key_value(mid))) hi = mid;
-      else lo = mid + 1;
-    }
-    return key_value(hi);
+  __device__ __forceinline__ u64 mass(float x) const {
+    const double t = step(x);
+    return near(t) ? near_mass(x, t) : 0;
+  }
+  // Every logit of bin b or above it is at least the first, every one of at least the second lies above bin b: a first look
+  // in float, with a step's margin for what `step` rounds.
+  __device__ __forceinline__ float floor_of(int b) const {
+    return nextafterf((float)((double)M - (8.0 * (b + 1) + 1.0) / rate), -INFINITY);
+  }
+  __device__ __forceinline__ float ceiling_of(int b) const {
+    return nextafterf((float)((double)M - (8.0 * b - 1.0) / rate), INFINITY);
   }
 };
 
 template <bool BF>
-__device__ __forceinline__ Row row_of(const SampleArgs& a, int row, const double* table) {
+__device__ __forceinline__ Row row_of(const SampleArgs& a, int row, const double* table, int part = 0, int parts = 1) {
   constexpr int ES = BF ? 2 : 4, VEC = 16 / ES;
   Row r;
   r.base = static_cast<const char*>(a.logits) + (size_t)row * a.stride * ES;
@@ -94,7 +113,11 @@ __device__ __forceinline__ Row row_of(const SampleArgs& a, int row, const double
   r.V = a.V;
   const int at = (int)((reinterpret_cast<uintptr_t>(r.base) & 15) / ES);
   r.head = at ? min(VEC - at, a.V) : 0;
-  r.shift = a.shift;
+  const int pieces = (a.V - r.head) / VEC, each = (pieces + parts - 1) / parts;
+  r.p0 = min(part * each, pieces);
+  r.p1 = min(r.p0 + each, pieces);
+  r.edges = part == 0;
+  r.drop = BF ? 16 : 0;
   return r;
 }
 template <bool BF>
@@ -102,30 +125,35 @@ __device__ __forceinline__ float logit(const Row& r, int id) {
   return BF ? bf2f(reinterpret_cast<const bf16_t*>(r.base)[id]) : reinterpret_cast<const float*>(r.base)[id];
 }
 
+template <bool BF>
+__device__ __forceinline__ void unpack(const uint4& w, float (&x)[BF ? 8 : 4]) {
+  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int e = 0; e < (BF ? 8 : 4); ++e)
+    x[e] = BF ? __uint_as_float(e & 1 ? v[e / 2] & 0xFFFF0000u : v[e / 2] << 16) : __uint_as_float(v[e & 3]);
+}
+
 // piece(x, id0) for the aligned 16 bytes of logits x[0 .. VEC) of ids id0 .., U loads of a thread in flight (past the last
 // one: NaN, which every caller passes over), and one(x, id) for the row's few elements before and behind them.
 template <bool BF, int U, class P, class O>
 __device__ __forceinline__ void each_piece(const Row& r, P piece, O one) {
   constexpr int ES = BF ? 2 : 4, VEC = 16 / ES;
-  const int pieces = (r.V - r.head) / VEC, tail = r.head + pieces * VEC;
+  const int tail = r.head + (r.V - r.head) / VEC * VEC;
   const int edge = (int)threadIdx.x < r.head ? (int)threadIdx.x : tail + (int)threadIdx.x - r.head;
-  if (edge < r.V && (int)threadIdx.x < 2 * VEC) one(logit<BF>(r, edge), edge);
+  if (r.edges && edge < r.V && (int)threadIdx.x < 2 * VEC) one(logit<BF>(r, edge), edge);
   const uint4* src = reinterpret_cast<const uint4*>(r.base + (size_t)r.head * ES);
   auto take = [&](const uint4& w, int p) {
-    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
     float x[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e)
-      x[e] = BF ? __uint_as_float(e & 1 ? v[e / 2] & 0xFFFF0000u : v[e / 2] << 16) : __uint_as_float(v[e & 3]);
+    unpack<BF>(w, x);
     piece(x, r.head + p * VEC);
   };
 #pragma unroll 1
-  for (int p = threadIdx.x; p < pieces; p += kSampleThreads * U) {
+  for (int p = r.p0 + (int)threadIdx.x; p < r.p1; p += kSampleThreads * U) {
     uint4 w[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       w[u] = make_uint4(~0u, ~0u, ~0u, ~0u);
-      if (p + u * kSampleThreads < pieces) w[u] = src[p + u * kSampleThreads];
+      if (p + u * kSampleThreads < r.p1) w[u] = src[p + u * kSampleThreads];
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) take(w[u], p + u * kSampleThreads);
@@ -148,20 +176,56 @@ __device__ __forceinline__ void each_logit(const Row& r, F f) {
       },
       f);
 }
-// f(x, id) for the logits of at least lo, which are taken to be few
+// f(id) for the elements of [lo, hi), taken to be few: what stands in the loop over the row is short, f outside of it and
+// once (a kernel's instructions come from memory every time it starts, some 64 bytes in 0.1 us). `above` counts those from hi
+// on, each wave's in its lane 0.
+template <bool BF, class F>
+__device__ __forceinline__ void each_between(const Row& r, float lo, float hi, uint32_t& above, F f) {
+  constexpr int ES = BF ? 2 : 4, VEC = 16 / ES, U = 4;
+  const int tid = threadIdx.x, tail = r.head + (r.V - r.head) / VEC * VEC;
+  const uint4* src = reinterpret_cast<const uint4*>(r.base + (size_t)r.head * ES);
+  uint32_t from_hi = 0;
+#pragma unroll 1
+  for (int p = r.edges ? r.p0 - kSampleThreads * U : r.p0; p < r.p0 || p < r.p1; p += kSampleThreads * U) {
+    uint32_t hits = 0;  // bit u * VEC + e: element e of the thread's piece u
+    int id0;
+    auto look = [&](float x, int bit) {
+      from_hi += __builtin_popcountll(__builtin_amdgcn_ballot_w64(x >= hi));
+      hits |= x >= lo && x < hi ? 1u << bit : 0u;
+    };
+    if (p < r.p0) {  // the elements before and behind the pieces
+      id0 = tid < r.head ? tid : tail + tid - r.head;
+      look(id0 < r.V && tid < 2 * VEC ? logit<BF>(r, id0) : __uint_as_float(~0u), 0);
+    } else {
+      id0 = r.head + (p + tid) * VEC;
+      uint4 w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        w[u] = make_uint4(~0u, ~0u, ~0u, ~0u);  // NaN
+        if (p + tid + u * kSampleThreads < r.p1) w[u] = src[p + tid + u * kSampleThreads];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float x[VEC];
+        unpack<BF>(w[u], x);
+        if (!__any(largest(x) >= lo)) continue;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) look(x[e], u * VEC + e);
+      }
+    }
+#pragma unroll 1
+    for (; hits; hits &= hits - 1) {
+      const int bit = __builtin_ctz(hits);
+      f(id0 + bit / VEC * (kSampleThreads * VEC) + bit % VEC);
+    }
+  }
+  if ((tid & 63) == 0) above += from_hi;
+}
+// f(x, id) for the logits of at least lo, below +inf
 template <bool BF, class F>
 __device__ __forceinline__ void each_from(const Row& r, float lo, F f) {
-  each_piece<BF, 4>(
-      r,
-      [&](const auto& x, int id0) {
-        if (!(largest(x) >= lo)) return;
-#pragma unroll
-        for (int e = 0; e < (BF ? 8 : 4); ++e)
-          if (x[e] >= lo) f(x[e], id0 + e);
-      },
-      [&](float x, int id) {
-        if (x >= lo) f(x, id);
-      });
+  uint32_t above = 0;
+  each_between<BF>(r, lo, INFINITY, above, [&](int id) { f(logit<BF>(r, id), id); });
 }
 
 // Element at which a running value passes a target.
@@ -175,21 +239,23 @@ struct ListShared {
   double table[kTable];
   u64 list[kList];
   u64 sum[kList];
+  uint32_t start[kList + 1];
   u64 red64[kWaves];
   uint32_t red32[kWaves];
   float red_x[kWaves];
-  int n;
+  uint32_t above;
+  int n, n_ids, found;
 };
 struct FullShared : ListShared {
   u64 mass[kBins + 1];
   uint32_t cnt[kBins + 1];
-  uint32_t lo, hi, m_cnt;
+  uint32_t lo, hi, m_cnt, dead;
   u64 m_mass;
 };
 
 // The row's settings and what follows from them.
 struct How {
-  float T, pf, uf;
+  float T, pf, uf, m_log;
   int k;
   bool by_p, by_m;
   double m_least;
@@ -202,6 +268,11 @@ struct How {
     by_p = pf < 1.f;
     by_m = mf > 0.f;
     m_least = ldexp(mf < 1.f ? (double)mf : 1.0, a.shift);
+    m_log = log2f(fminf(mf, 1.f));
+  }
+  // every logit that min-p keeps is at least this: two steps' margin
+  __device__ __forceinline__ float m_floor(const Row& r) const {
+    return nextafterf((float)((double)r.M + ((double)m_log * kTable - 2.0) / r.rate), -INFINITY);
   }
   // targets for the running sum: the prefix ends, the draw lies at the first element whose sum is above them
   __device__ __forceinline__ u64 p_target(u64 total) const {  // elements whose sum before them is below p * total
@@ -221,120 +292,140 @@ __device__ __forceinline__ void answer(const SampleArgs& a, int row, int token, 
   if (a.conf) a.conf[row] = (float)conf;
   if (a.kept) a.kept[row] = kept;
 }
-__device__ __forceinline__ void fill_table(double* table) {
-  if (threadIdx.x < kTable) table[threadIdx.x] = exp2((int)threadIdx.x * (1.0 / kTable));
+__device__ __forceinline__ void fill_table(double* table, int shift) {
+  const int i = threadIdx.x;
+  if (i >= kTable) return;
+  const u64 bits = (u64)__double_as_longlong(ldexp(exp2(i * (1.0 / kTable)), shift - kTop / kTable));
+  table[i] = __longlong_as_double((long long)(bits - ((u64)i << 44)));
 }
 
-// Exclusive prefix sums of 2048 counts (and sums) in place, totals behind the last. All threads; ends with a barrier.
-template <bool MASS>
-__device__ __forceinline__ void scan_bins(uint32_t* cnt, u64* mass, ListShared& sh) {
+// Exclusive prefix sums of 2048 counts or sums in place, the total behind the last; `red`: a word a wave. All threads; ends
+// with a barrier.
+template <class T>
+__device__ __forceinline__ void scan_bins(T* v, T* red) {
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   static_assert(kBins == 2 * kSampleThreads, "two bins a thread");
-  const uint32_t c0 = cnt[2 * tid], c1 = cnt[2 * tid + 1];
-  const u64 m0 = MASS ? mass[2 * tid] : 0, m1 = MASS ? mass[2 * tid + 1] : 0;
-  uint32_t c = c0 + c1;
-  u64 m = m0 + m1;
+  const T v0 = v[2 * tid], v1 = v[2 * tid + 1];
+  T s = v0 + v1;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t cu = __shfl_up(c, o, 64);
-    if (lane >= o) c += cu;
-    if constexpr (MASS) {
-      const u64 mu = __shfl_up(m, o, 64);
-      if (lane >= o) m += mu;
+    const T u = __shfl_up(s, o, 64);
+    if (lane >= o) s += u;
+  }
+  if (lane == 63) red[wid] = s;
+  __syncthreads();
+  for (int w = 0; w < wid; ++w) s += red[w];
+  v[2 * tid] = s - v0 - v1;
+  v[2 * tid + 1] = s - v1;
+  if (tid == kSampleThreads - 1) v[kBins] = s;
+  __syncthreads();
+}
+
+// The bin in which the running value passes t, below the total of the scanned ones: every thread looks at its two. All
+// threads; ends with a barrier.
+template <class T>
+__device__ __forceinline__ int bin_of(const T* excl, T t, ListShared& sh) {
+  const int i = 2 * threadIdx.x;
+  if (excl[i] <= t && t < excl[i + 1]) sh.found = i;
+  if (excl[i + 1] <= t && t < excl[i + 2]) sh.found = i + 1;
+  __syncthreads();
+  const int b = sh.found;
+  __syncthreads();
+  return b;
+}
+
+// The elements x of [lo, hi) for which side(x) is 0 into the list as (~key, id), if those of [lo, hi) fit it; sh.n counts
+// them, sh.above those for which side is negative and those from hi on. All threads.
+template <bool BF, class P>
+__device__ __forceinline__ bool collect(const Row& r, float lo, float hi, ListShared& sh, P side) {
+  const int tid = threadIdx.x;
+  uint32_t* ids = sh.start;
+  __syncthreads();
+  if (tid == 0) sh.n = sh.n_ids = 0, sh.above = 0;
+  __syncthreads();
+  uint32_t above = 0;
+  each_between<BF>(r, lo, hi, above, [&](int id) {
+    const int at = atomicAdd(&sh.n_ids, 1);
+    if (at < kList) ids[at] = (uint32_t)id;
+  });
+  if (above) atomicAdd(&sh.above, above);
+  __syncthreads();
+  const int n = sh.n_ids;
+  if (n <= kList) {
+#pragma unroll 1
+    for (int i = tid; i < n; i += kSampleThreads) {
+      const float x = logit<BF>(r, (int)ids[i]);
+      const int at = side(x);
+      if (at < 0) atomicAdd(&sh.above, 1u);
+      if (at == 0) sh.list[atomicAdd(&sh.n, 1)] = ((u64)~order_key(x) << 32) | ids[i];
     }
   }
-  if (lane == 63) sh.red32[wid] = c, sh.red64[wid] = m;
   __syncthreads();
-  for (int w = 0; w < wid; ++w) {
-    c += sh.red32[w];
-    if constexpr (MASS) m += sh.red64[w];
-  }
-  cnt[2 * tid] = c - c0 - c1;
-  cnt[2 * tid + 1] = c - c1;
-  if (tid == kSampleThreads - 1) cnt[kBins] = c;
-  if constexpr (MASS) {
-    mass[2 * tid] = m - m0 - m1;
-    mass[2 * tid + 1] = m - m1;
-    if (tid == kSampleThreads - 1) mass[kBins] = m;
-  }
-  __syncthreads();
+  return n <= kList;
 }
-
-// Last bin whose exclusive prefix is at most t.
-template <class T>
-__device__ __forceinline__ int bin_of(const T* excl, T t) {
-  int lo = 0, hi = kBins - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (excl[mid] <= t) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
-}
-
-// The elements with lo <= x < hi into the list as (~key, id), if they fit it; sh.n counts them. All threads.
+// those of bins from .. b
 template <bool BF>
-__device__ __forceinline__ bool collect_between(const Row& r, float lo, float hi, ListShared& sh) {
-  __syncthreads();
-  if (threadIdx.x == 0) sh.n = 0;
-  __syncthreads();
-  each_from<BF>(r, lo, [&](float x, int id) {
-    if (!(x < hi)) return;
-    const int i = atomicAdd(&sh.n, 1);
-    if (i < kList) sh.list[i] = ((u64)~order_key(x) << 32) | (uint32_t)id;
+__device__ __forceinline__ bool collect_bins(const Row& r, int from, int b, ListShared& sh) {
+  return collect<BF>(r, r.floor_of(b), from > 0 ? r.ceiling_of(from) : INFINITY, sh, [&](float x) {
+    const int at = r.bin(x);
+    return at < from ? -1 : at > b;
   });
-  __syncthreads();
-  return sh.n <= kList;
 }
 
 // The sh.n collected pairs in order, and the running sums of their weights from `above`. All threads.
+// More than 128 are first put into up to 2048 groups by value and id, as if those lay evenly between the extremes (as they
+// do in one bin, or among equal values); the elements of a group are then ranked one against the other. (Sorted by a network,
+// 1000 took 20 us and more: 55 steps that wait.)
 __device__ __forceinline__ void order_list(const Row& r, u64 above, ListShared& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, n = sh.n;
-  // A bitonic network, element e * 1024 + thread in register e: partners 1024 apart meet in a thread, those less than 64
-  // apart in a wave, and only the rest through LDS, two buffers in turn and so one barrier each.
-  int m = 64;
-  while (m < n) m <<= 1;
-  u64 v[2] = {tid < n ? sh.list[tid] : ~0ull, tid + kSampleThreads < n ? sh.list[tid + kSampleThreads] : ~0ull};
-  auto order = [&](int e, u64 other, int size, int step) {
-    const int i = e * kSampleThreads + tid;
-    const bool low = ((i & step) == 0) == ((i & size) == 0);  // this place takes the smaller one
-    v[e] = low ? (v[e] < other ? v[e] : other) : (v[e] < other ? other : v[e]);
-  };
-  int turn = 0;
-  __syncthreads();
-#pragma unroll 1
-  for (int size = 2; size <= m; size <<= 1)
-#pragma unroll 1
-    for (int step = size >> 1; step > 0; step >>= 1) {
-      if (step == kSampleThreads) {
-        const u64 x = v[0], y = v[1];
-        order(0, y, size, step);
-        order(1, x, size, step);
-      } else if (step < 64) {
-        const u64 x = __shfl_xor(v[0], step, 64);
-        order(0, x, size, step);
-        if (m > kSampleThreads) {
-          const u64 y = __shfl_xor(v[1], step, 64);
-          order(1, y, size, step);
-        }
-      } else {
-        u64* buf = turn ? sh.list : sh.sum;
-        turn ^= 1;
-        buf[tid] = v[0];
-        buf[tid + kSampleThreads] = v[1];
-        __syncthreads();
-        order(0, buf[tid ^ step], size, step);
-        order(1, buf[kSampleThreads + (tid ^ step)], size, step);
+  u64 v[2];
+  int at[2] = {0, 0};
+#pragma unroll
+  for (int e = 0; e < 2; ++e) v[e] = e * kSampleThreads + tid < n ? sh.list[e * kSampleThreads + tid] : ~0ull;
+  const bool grouped = n > 128;
+  if (grouped) {
+    uint32_t lo = min((uint32_t)(v[0] >> 32), (uint32_t)(v[1] >> 32));
+    uint32_t hi = max(tid < n ? (uint32_t)(v[0] >> 32) : 0u, kSampleThreads + tid < n ? (uint32_t)(v[1] >> 32) : 0u);
+    for (int o = 32; o >= 1; o >>= 1) lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64)), hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
+    if (lane == 0) sh.red32[wid] = lo, sh.red64[wid] = hi;
+    for (int i = tid; i <= kList; i += kSampleThreads) sh.start[i] = 0;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) lo = min(lo, sh.red32[w]), hi = max(hi, (uint32_t)sh.red64[w]);
+    const int drop = r.drop;  // bits that all keys have alike
+    const double ids = (double)r.V, scale = (kList - 0.5) / ((double)((hi - lo) >> drop) * ids + ids);
+    int slot[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (e * kSampleThreads + tid < n) {
+        at[e] = (int)(fma((double)(((uint32_t)(v[e] >> 32) - lo) >> drop), ids, (double)(uint32_t)v[e]) * scale);
+        slot[e] = (int)atomicAdd(&sh.start[at[e]], 1u);
       }
-    }
+    __syncthreads();
+    scan_bins(sh.start, sh.red32);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (e * kSampleThreads + tid < n) sh.sum[sh.start[at[e]] + slot[e]] = v[e];
+  }
   __syncthreads();
-  sh.list[tid] = v[0];
-  sh.list[tid + kSampleThreads] = v[1];
+  const u64* from = grouped ? sh.sum : sh.list;
+  int rank[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    if (e * kSampleThreads + tid >= n) continue;
+    int i = grouped ? (int)sh.start[at[e]] : 0;
+    const int end = grouped ? (int)sh.start[at[e] + 1] : n;
+    rank[e] = i;
+    for (; i < end; ++i) rank[e] += from[i] < v[e];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    if (e * kSampleThreads + tid < n) sh.list[rank[e]] = v[e];
   __syncthreads();
   static_assert(kList == 2 * kSampleThreads, "two elements a thread");
   u64 w0 = 0, w1 = 0;
-  if (2 * tid < n) w0 = Row::fixed(r.weight(key_value(~(uint32_t)(sh.list[2 * tid] >> 32))));
-  if (2 * tid + 1 < n) w1 = Row::fixed(r.weight(key_value(~(uint32_t)(sh.list[2 * tid + 1] >> 32))));
+  if (2 * tid < n) w0 = r.mass(key_value(~(uint32_t)(sh.list[2 * tid] >> 32)));
+  if (2 * tid + 1 < n) w1 = r.mass(key_value(~(uint32_t)(sh.list[2 * tid + 1] >> 32)));
   u64 s = w0 + w1;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -350,20 +441,19 @@ __device__ __forceinline__ void order_list(const Row& r, u64 above, ListShared& 
   __syncthreads();
 }
 
-// In the ordered list, whose elements follow `above` (sum) and `before` (count): by count (0-based index) or sum.
-__device__ __forceinline__ Found in_list(bool by_count, u64 t, u64 above, uint32_t before, const ListShared& sh) {
-  int i;
+// In the ordered list, whose elements follow `above` (sum) and `before` (count): by count (0-based index) or by a sum below
+// the list's last. All threads.
+__device__ __forceinline__ Found in_list(bool by_count, u64 t, u64 above, uint32_t before, ListShared& sh) {
   if (by_count) {
-    i = (int)((uint32_t)t - before);
+    if (threadIdx.x == 0) sh.found = (int)((uint32_t)t - before);
   } else {
-    int lo = 0, hi = sh.n - 1;  // first running sum above t
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (sh.sum[mid] > t) hi = mid;
-      else lo = mid + 1;
-    }
-    i = lo;
+#pragma unroll
+    for (int i = threadIdx.x; i < kList; i += kSampleThreads)
+      if (i < sh.n && sh.sum[i] > t && (i == 0 || sh.sum[i - 1] <= t)) sh.found = i;
   }
+  __syncthreads();
+  const int i = sh.found;
+  __syncthreads();
   const u64 prev = i > 0 ? sh.sum[i - 1] : above;
   return {sh.sum[i], sh.sum[i] - prev, (int)before + i + 1, (int)(uint32_t)sh.list[i]};
 }
@@ -407,9 +497,23 @@ __device__ __forceinline__ int equal_id(const Row& r, uint32_t k, u64 j, ListSha
   return m ? lo + (int)__builtin_ctzll(m) : -1;
 }
 
-// What the first kernel leaves for the second: the row's maximum, NaN where the row is answered.
-struct RowTop {
-  float M;
+// What a row's kernels leave for the next ones (in the workspace).
+struct RowState {
+  float M;             // the row's maximum, NaN where the row is answered
+  uint32_t n_list;     // split rows: elements that reach top-k's bound, collected if they fit; ~0: no bound was set
+  uint32_t m_cnt;      // elements that min-p keeps
+  uint32_t dead;       // elements that are -inf or NaN
+  u64 m_mass;          // the sum of those that min-p keeps
+};
+// A row that several workgroups share: its parts' maxima, 1024 maxima of groups that cover it, the collected elements, the
+// histogram.
+struct SplitRow {
+  float part_max[kMaxParts];
+  int part_id[kMaxParts];
+  float group_max[kSampleThreads];
+  u64 list[kList];
+  u64 mass[kBins];
+  uint32_t cnt[kBins];
 };
 
 // Rows whose logits are +inf somewhere: those ids share the weight alike, all others have none.
@@ -436,6 +540,64 @@ __device__ __forceinline__ void infinite_row(const SampleArgs& a, int row, const
   answer(a, row, id, 1.0 / (double)total, (int)count);
 }
 
+// How many of the ordered list's first `count` elements min-p keeps: weights fall along it. All threads.
+__device__ __forceinline__ int in_list_by_weight(const Row& r, const How& how, int count, const ListShared& sh) {
+  int kept = 0;
+#pragma unroll 1
+  for (int i0 = 0; i0 < count; i0 += kSampleThreads) {
+    const int i = i0 + (int)threadIdx.x;
+    kept += __syncthreads_count(i < count && r.weight(key_value(~(uint32_t)(sh.list[i] >> 32))) >= how.m_least);
+  }
+  return kept;
+}
+
+// The answer from the list of all elements that reach some bound, at least k of them. All threads.
+__device__ __forceinline__ void answer_from_list(const SampleArgs& a, int row, const Row& r, const How& how, ListShared& sh) {
+  order_list(r, 0, sh);
+  int count = how.k;
+  if (how.by_p) count = min(count, in_list(false, how.p_target(sh.sum[count - 1]), 0, 0, sh).count);
+  if (how.by_m) count = in_list_by_weight(r, how, count, sh);
+  const u64 total = sh.sum[count - 1];
+  const Found f = in_list(false, how.u_target(total), 0, 0, sh);
+  answer(a, row, f.id, (double)f.weight / (double)total, count);
+}
+
+// A lower bound for the k-th largest element, k up to 512: with 1024 groups that cover the row, the k-th largest of their
+// maxima is one, and not many more elements reach it (about 710 for 512 of 152064 in no order). To within 1 / 1000 of the
+// maxima's range, from a histogram of them. `own`: the thread's group's maximum, `least`: the smallest above -inf. False
+// where fewer than k groups have any element. All threads; cnt is all zeros.
+__device__ __forceinline__ bool bound_of(const Row& r, int k, float own, float least, uint32_t* cnt, ListShared& sh, float& lo) {
+  const float step = fminf(2047.f / (r.M - least), 1e30f);
+  auto bin = [&](float x) { return (int)fminf((r.M - x) * step, 2047.f); };  // does not decrease while x falls
+  if (own > -INFINITY) atomicAdd(&cnt[bin(own)], 1u);
+  __syncthreads();
+  scan_bins(cnt, sh.red32);
+  if (cnt[kBins] < (uint32_t)k) return false;
+  // the k-th lies in this bin, within (b + 1) / step of M but for the rounding of `bin`; none lies below the least
+  lo = fmaxf(least, r.M - (float)(bin_of(cnt, (uint32_t)(k - 1), sh) + 2) / step);
+  return true;
+}
+__device__ __forceinline__ bool takes_bound(const How& how) { return how.k > 0 && how.k <= kSampleThreads / 2; }
+
+__device__ __forceinline__ void lower_id(float x, int id, float& best, int& best_id) {  // the larger, then the lower id
+  if (x > best || (x == best && id < best_id)) best = x, best_id = id;
+}
+// The largest logit of the workgroup's pieces and its lowest id: the thread's own.
+template <bool BF>
+__device__ __forceinline__ void thread_max(const Row& r, float& best, int& best_id) {
+  best = -INFINITY;
+  best_id = INT_MAX;
+  each_piece<BF, 4>(
+      r,
+      [&](const auto& x, int id0) {
+        if (!(largest(x) >= best)) return;  // an equal one may have a lower id than an edge element's
+#pragma unroll
+        for (int e = 0; e < (BF ? 8 : 4); ++e) lower_id(x[e], id0 + e, best, best_id);
+      },
+      [&](float x, int id) { lower_id(x, id, best, best_id); });
+  if (best == -INFINITY) best_id = INT_MAX;
+}
+
 template <bool BF>
 __global__ void __launch_bounds__(kSampleThreads, 8) sample_top_kernel(SampleArgs a) {
   __shared__ ListShared sh;
@@ -444,88 +606,78 @@ __global__ void __launch_bounds__(kSampleThreads, 8) sample_top_kernel(SampleArg
   __shared__ float red_least[kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, row = blockIdx.x;
   Row r = row_of<BF>(a, row, sh.table);
-  RowTop* left = static_cast<RowTop*>(a.ws) + row;
-  // the maximum and its lowest id; the threads' own maxima
-  float best = -INFINITY;
-  int best_id = INT_MAX;
-  auto lower = [](float x, int id, float& bx, int& bid) {
-    if (x > bx || (x == bx && id < bid)) bx = x, bid = id;
-  };
-  each_piece<BF, 4>(
-      r,
-      [&](const auto& x, int id0) {
-        if (!(largest(x) >= best)) return;  // an equal one may have a lower id than an edge element's
-#pragma unroll
-        for (int e = 0; e < (BF ? 8 : 4); ++e) lower(x[e], id0 + e, best, best_id);
-      },
-      [&](float x, int id) { lower(x, id, best, best_id); });
-  if (best == -INFINITY) best_id = INT_MAX;
+  RowState* left = static_cast<RowState*>(a.ws) + row;
+  float best;
+  int best_id;
+  thread_max<BF>(r, best, best_id);
   const float own = best;
+  float least = own > -INFINITY ? own : INFINITY;
   for (int o = 32; o >= 1; o >>= 1) {
     const float x = __shfl_xor(best, o, 64);
     const int id = __shfl_xor(best_id, o, 64);
-    lower(x, id, best, best_id);
+    lower_id(x, id, best, best_id);
+    least = fminf(least, __shfl_xor(least, o, 64));
   }
-  float least = own > -INFINITY ? own : INFINITY;  // of the threads' maxima
-  for (int o = 32; o >= 1; o >>= 1) least = fminf(least, __shfl_xor(least, o, 64));
   if (lane == 0) sh.red_x[wid] = best, red_id[wid] = best_id, red_least[wid] = least;
-  fill_table(sh.table);
+  fill_table(sh.table, a.shift);
   for (int i = tid; i <= kBins; i += kSampleThreads) cnt[i] = 0;
   __syncthreads();
-  for (int w = 0; w < kWaves; ++w) lower(sh.red_x[w], red_id[w], best, best_id);
+  for (int w = 0; w < kWaves; ++w) lower_id(sh.red_x[w], red_id[w], best, best_id), least = fminf(least, red_least[w]);
   const How how(a, row);
   if (tid == 0) left->M = __uint_as_float(0x7FC00000u);
   if (best == -INFINITY) return answer(a, row, -1, 0.0, 0);  // nothing but -inf and NaN
   if (!(how.T > 0.f) || how.k == 1) return answer(a, row, best_id, 1.0, 1);
   if (best == INFINITY) return infinite_row<BF>(a, row, r, how, sh);
   r.set(best, how.T);
-  // Top-k: the k-th largest of the threads' maxima is a lower bound for the k-th largest element, and for k up to half the
-  // threads not many more elements reach it (about 710 for 512 of 152064 in no order). The bound to within 1 / 2047 of the
-  // maxima's range, from a histogram of them.
-  if (how.k > 0 && how.k <= kSampleThreads / 2) {
-    for (int w = 0; w < kWaves; ++w) least = fminf(least, red_least[w]);
-    const float step = fminf(2047.f / (best - least), 1e30f);
-    auto bin = [&](float x) { return (int)fminf((best - x) * step, 2047.f); };  // does not decrease while x falls
-    if (own > -INFINITY) atomicAdd(&cnt[bin(own)], 1u);
-    __syncthreads();
-    scan_bins<false>(cnt, nullptr, sh);
-    if (cnt[kBins] >= (uint32_t)how.k) {
-      const int b = bin_of<uint32_t>(cnt, (uint32_t)(how.k - 1));
-      if (collect_between<BF>(r, r.least([&](float x) { return bin(x) <= b; }), INFINITY, sh)) {
-        order_list(r, 0, sh);
-        int count = how.k;
-        if (how.by_p) count = min(count, in_list(false, how.p_target(sh.sum[count - 1]), 0, 0, sh).count);
-        if (how.by_m) {  // weights fall along the list: the first one below min-p
-          int lo = 1, hi = count;
-          while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (r.weight(key_value(~(uint32_t)(sh.list[mid] >> 32))) >= how.m_least) lo = mid + 1;
-            else hi = mid;
-          }
-          count = lo;
-        }
-        const u64 total = sh.sum[count - 1];
-        const Found f = in_list(false, how.u_target(total), 0, 0, sh);
-        return answer(a, row, f.id, (double)f.weight / (double)total, count);
-      }
-    }
-  }
+  float lo;
+  if (takes_bound(how) && bound_of(r, how.k, own, least, cnt, sh, lo) && collect<BF>(r, lo, INFINITY, sh, [](float) { return 0; }))
+    return answer_from_list(a, row, r, how, sh);
   if (tid == 0) left->M = best;
+}
+
+// Rows that `parts` workgroups share (few rows: one CU reads 30 GB/s, a row of 126464 float32 16 us). First the parts'
+// maxima and those of 1024 groups of threads, and zeros where the next kernel counts.
+template <bool BF>
+__global__ void __launch_bounds__(kSampleThreads, 8) sample_part_kernel(SampleArgs a, int parts) {
+  __shared__ float red_x[kWaves];
+  __shared__ int red_id[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, row = blockIdx.x / parts, part = blockIdx.x % parts;
+  RowState* state = static_cast<RowState*>(a.ws) + row;
+  SplitRow* split = reinterpret_cast<SplitRow*>(static_cast<RowState*>(a.ws) + a.n) + row;
+  for (int i = part * kSampleThreads + tid; i < kBins; i += parts * kSampleThreads) split->cnt[i] = 0, split->mass[i] = 0;
+  if (part == 0 && tid == 0) *state = RowState{};
+  const Row r = row_of<BF>(a, row, nullptr, part, parts);
+  float best;
+  int best_id;
+  thread_max<BF>(r, best, best_id);
+  float group = best;  // of `parts` neighbouring threads (a power of two)
+  for (int o = 1; o < parts; o <<= 1) group = fmaxf(group, __shfl_xor(group, o, 64));
+  if (tid % parts == 0) split->group_max[(part * kSampleThreads + tid) / parts] = group;
+  for (int o = 32; o >= 1; o >>= 1) {
+    const float x = __shfl_xor(best, o, 64);
+    const int id = __shfl_xor(best_id, o, 64);
+    lower_id(x, id, best, best_id);
+  }
+  if (lane == 0) red_x[wid] = best, red_id[wid] = best_id;
+  __syncthreads();
+  if (tid != 0) return;
+  for (int w = 1; w < kWaves; ++w) lower_id(red_x[w], red_id[w], best, best_id);
+  split->part_max[part] = best;
+  split->part_id[part] = best_id;
 }
 
 // The question inside one bin with more elements than the list holds. All threads; the list is overwritten.
 template <bool BF>
-__device__ Found in_large_bin(const Row& r, int b, bool by_count, u64 t, u64 above, uint32_t before, FullShared& sh) {
+__device__ __forceinline__ Found in_large_bin(const Row& r, int b, bool by_count, u64 t, u64 above, uint32_t before, FullShared& sh) {
   const int tid = threadIdx.x;
   constexpr int PARTS = 1024;
   uint32_t* cnt = reinterpret_cast<uint32_t*>(sh.sum);
   u64* mass = sh.list;
   static_assert(PARTS <= kList, "counts and sums of the parts lie in the list's memory");
   // the values that are left, in order_key's terms
-  uint32_t klo = order_key(r.least([&](float x) { return r.bin(x) <= b; }));
-  uint32_t khi = b == 0 ? order_key(r.M) : order_key(r.least([&](float x) { return r.bin(x) < b; })) - 1;
+  uint32_t klo = order_key(fmaxf(r.floor_of(b), -3.4028234663852886e38f)), khi = order_key(r.M);
 #pragma unroll 1
-  for (;;) {
+  for (bool whole = true;; whole = false) {  // the whole bin at first
     // the range that they really take
     __syncthreads();
     if (tid == 0) sh.lo = 0xFFFFFFFFu, sh.hi = 0, sh.n = 0;
@@ -533,7 +685,7 @@ __device__ Found in_large_bin(const Row& r, int b, bool by_count, u64 t, u64 abo
     uint32_t lo = 0xFFFFFFFFu, hi = 0, n = 0;
     each_from<BF>(r, key_value(klo), [&](float x, int) {
       const uint32_t k = order_key(x);
-      if (k <= khi) lo = min(lo, k), hi = max(hi, k), ++n;
+      if (whole ? r.bin(x) == b : k <= khi) lo = min(lo, k), hi = max(hi, k), ++n;
     });
     if (n) {
       atomicMin(&sh.lo, lo);
@@ -546,13 +698,13 @@ __device__ Found in_large_bin(const Row& r, int b, bool by_count, u64 t, u64 abo
     const int left = sh.n;
     __syncthreads();
     if (klo == khi) {  // equal values: element j of them, by arithmetic; its id by counting in order
-      const u64 w = Row::fixed(r.weight(key_value(klo)));
+      const u64 w = r.mass(key_value(klo));
       const u64 j = by_count ? (uint32_t)t - before : w ? (t - above) / w : 0;
       const int id = equal_id<BF>(r, klo, j, sh);
       return {above + (j + 1) * w, w, (int)(before + (uint32_t)j + 1), id};
     }
     if (left <= kList) {
-      collect_between<BF>(r, key_value(klo), key_value(khi + 1), sh);
+      collect<BF>(r, key_value(klo), key_value(khi + 1), sh, [](float) { return 0; });
       order_list(r, above, sh);
       return in_list(by_count, t, above, before, sh);
     }
@@ -565,7 +717,7 @@ __device__ Found in_large_bin(const Row& r, int b, bool by_count, u64 t, u64 abo
       const uint32_t k = order_key(x);
       if (k > khi) return;
       atomicAdd(&cnt[part(k)], 1u);
-      atomicAdd(&mass[part(k)], Row::fixed(r.weight(x)));
+      atomicAdd(&mass[part(k)], r.mass(x));
     });
     __syncthreads();
     // running sums by one thread: this path is for rows of many nearly equal values
@@ -595,97 +747,223 @@ __device__ Found in_large_bin(const Row& r, int b, bool by_count, u64 t, u64 abo
   }
 }
 
+// The histogram over the workgroup's pieces, all zeros before: the bins' counts into sh.cnt where top-k asks by count, their
+// sums into sh.mass. An atomic addition in LDS costs about as much as the arithmetic of an element, so the passes do not
+// take both at once, and the far elements (most of a row at a low temperature) take none. All threads; ends with a barrier.
 template <bool BF>
-__global__ void __launch_bounds__(kSampleThreads, 8) sample_full_kernel(SampleArgs a) {
+__device__ __forceinline__ void count_bins(const Row& r, FullShared& sh) {
+  uint32_t far = 0;
+  each_logit<BF>(r, [&](float x, int) {
+    const double t = r.step(x);
+    if (Row::near(t)) atomicAdd(&sh.cnt[Row::place(t)], 1u);
+    else far += x > -INFINITY;
+  });
+  if (far) atomicAdd(&sh.cnt[kFar], far);
+  __syncthreads();
+}
+// Also counts the dead elements, and count and sum of those that min-p keeps (by a pass of their own: they are few).
+template <bool BF>
+__device__ __forceinline__ void sum_bins(const Row& r, const How& how, FullShared& sh) {
+  uint32_t dead = 0;
+  each_logit<BF>(r, [&](float x, int) {
+    const double t = r.step(x);
+    if (Row::near(t)) atomicAdd(&sh.mass[Row::place(t)], r.near_mass(x, t));
+    else dead += !(x > -INFINITY);
+  });
+  if (dead) atomicAdd(&sh.dead, dead);
+  if (how.by_m) {
+    u64 m_mass = 0;
+    uint32_t m_cnt = 0;
+    each_from<BF>(r, how.m_floor(r), [&](float x, int) {
+      if (r.weight(x) >= how.m_least) ++m_cnt, m_mass += r.mass(x);
+    });
+    if (m_cnt) atomicAdd(&sh.m_cnt, m_cnt), atomicAdd(&sh.m_mass, m_mass);
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ void clear_histogram(FullShared& sh) {
+  for (int i = threadIdx.x; i <= kBins; i += kSampleThreads) sh.cnt[i] = 0, sh.mass[i] = 0;
+  if (threadIdx.x == 0) sh.m_mass = 0, sh.m_cnt = 0, sh.dead = 0;
+}
+
+// Second kernel of shared rows: the parts' elements that reach top-k's bound go to the row's list, or the parts' histograms
+// to the row's.
+template <bool BF>
+__global__ void __launch_bounds__(kSampleThreads, 8) sample_gather_kernel(SampleArgs a, int parts) {
+  __shared__ FullShared sh;
+  __shared__ int base;
+  const int tid = threadIdx.x, lane = tid & 63, row = blockIdx.x / parts, part = blockIdx.x % parts;
+  RowState* state = static_cast<RowState*>(a.ws) + row;
+  SplitRow* split = reinterpret_cast<SplitRow*>(static_cast<RowState*>(a.ws) + a.n) + row;
+  Row r = row_of<BF>(a, row, sh.table, part, parts);
+  const How how(a, row);
+  float best = split->part_max[0];
+  int best_id = split->part_id[0];
+  for (int p = 1; p < parts; ++p) lower_id(split->part_max[p], split->part_id[p], best, best_id);
+  const bool answered = best == -INFINITY || !(how.T > 0.f) || how.k == 1;
+  if (answered || best == INFINITY) {
+    if (part == 0) {
+      if (tid == 0) state->M = answered ? __uint_as_float(0x7FC00000u) : best;
+      if (best == -INFINITY) answer(a, row, -1, 0.0, 0);
+      else if (answered) answer(a, row, best_id, 1.0, 1);
+    }
+    return;
+  }
+  if (part == 0 && tid == 0) state->M = best;
+  r.set(best, how.T);
+  fill_table(sh.table, a.shift);
+  clear_histogram(sh);
+  const float own = split->group_max[tid];
+  float least = own > -INFINITY ? own : INFINITY;
+  for (int o = 32; o >= 1; o >>= 1) least = fminf(least, __shfl_xor(least, o, 64));
+  if (lane == 0) sh.red_x[tid >> 6] = least;
+  __syncthreads();
+  if (takes_bound(how)) {
+    for (int w = 0; w < kWaves; ++w) least = fminf(least, sh.red_x[w]);
+    float lo;
+    if (bound_of(r, how.k, own, least, sh.cnt, sh, lo)) {
+      const bool fits = collect<BF>(r, lo, INFINITY, sh, [](float) { return 0; });
+      if (tid == 0) base = (int)atomicAdd(&state->n_list, (uint32_t)(fits ? sh.n : kList + 1));
+      __syncthreads();
+      if (fits && base + sh.n <= kList)
+        for (int i = tid; i < sh.n; i += kSampleThreads) split->list[base + i] = sh.list[i];
+      return;
+    }
+    if (part == 0 && tid == 0) state->n_list = ~0u;  // the same in every part: none of them adds to it
+    return;
+  }
+  if (how.k > 0) count_bins<BF>(r, sh);
+  sum_bins<BF>(r, how, sh);
+  for (int i = tid; i <= kFar; i += kSampleThreads) {
+    if (sh.cnt[i]) atomicAdd(&split->cnt[i], sh.cnt[i]);
+    if (sh.mass[i]) atomicAdd(&split->mass[i], sh.mass[i]);
+  }
+  if (tid != 0) return;
+  if (sh.m_cnt) atomicAdd(&state->m_cnt, sh.m_cnt), atomicAdd(&state->m_mass, sh.m_mass);
+  if (sh.dead) atomicAdd(&state->dead, sh.dead);
+}
+
+// The rows that are not answered yet, one workgroup each; of shared rows the list or the histogram is there.
+template <bool BF, bool SHARED>
+__global__ void __launch_bounds__(kSampleThreads, 4) sample_full_kernel(SampleArgs a) {
   __shared__ FullShared sh;
   const int tid = threadIdx.x, row = blockIdx.x;
-  const float top = static_cast<const RowTop*>(a.ws)[row].M;
-  if (!(top > -INFINITY)) return;  // answered
+  const RowState state = static_cast<const RowState*>(a.ws)[row];
+  if (!(state.M > -INFINITY)) return;  // answered
   Row r = row_of<BF>(a, row, sh.table);
   const How how(a, row);
-  r.set(top, how.T);
-  fill_table(sh.table);
-  for (int i = tid; i <= kBins; i += kSampleThreads) sh.cnt[i] = 0, sh.mass[i] = 0;
-  if (tid == 0) sh.m_mass = 0, sh.m_cnt = 0;
+  fill_table(sh.table, a.shift);
+  clear_histogram(sh);
   __syncthreads();
+  if (SHARED && state.M == INFINITY) return infinite_row<BF>(a, row, r, how, sh);
+  r.set(state.M, how.T);
+  const SplitRow* split = reinterpret_cast<const SplitRow*>(static_cast<const RowState*>(a.ws) + a.n) + row;
+  const bool gathered = SHARED && takes_bound(how) && state.n_list <= kList;  // the list is in the workspace
+  const bool summed = SHARED && !takes_bound(how);                            // the histogram is
+  if (summed) {
+    for (int i = tid; i <= kFar; i += kSampleThreads) sh.cnt[i] = split->cnt[i], sh.mass[i] = split->mass[i];
+    if (tid == 0) sh.m_cnt = state.m_cnt, sh.m_mass = state.m_mass, sh.dead = state.dead;
+    __syncthreads();
+  }
+  if (how.k > 0 && !gathered) {
+    if (!summed) count_bins<BF>(r, sh);
+    scan_bins(sh.cnt, sh.red32);
+  }
 
-  // counts and sums of the bins, and of the elements that min-p keeps (few, as a rule)
-  const float m_lo = how.by_m ? r.least([&](float x) { return r.weight(x) >= how.m_least; }) : INFINITY;
-  u64 m_mass = 0;
-  uint32_t far = 0, m_cnt = 0;
-  auto count_in = [&](float x, float at, u64 f) {
-    if (x >= m_lo) ++m_cnt, m_mass += at < (float)(kBins - 1) ? f : 0;
-    if (at < (float)(kBins - 1)) {
-      atomicAdd(&sh.cnt[(int)at], 1u);
-      atomicAdd(&sh.mass[(int)at], f);
-    }
-    far += x > -INFINITY && !(at < (float)(kBins - 1));  // most of a row at a low temperature: no atomics on one word
-  };
-  each_piece<BF, 1>(
-      r,
-      [&](const auto& x, int) {
-        constexpr int N = BF ? 8 : 4, H = 2;  // elements whose arithmetic overlaps
-#pragma unroll
-        for (int e0 = 0; e0 < N; e0 += H) {
-          float at[H];
-          u64 f[H];
-#pragma unroll
-          for (int e = 0; e < H; ++e) at[e] = r.place(x[e0 + e]), f[e] = Row::fixed(r.weight_near(x[e0 + e]));
-#pragma unroll
-          for (int e = 0; e < H; ++e) count_in(x[e0 + e], at[e], f[e]);
-        }
-      },
-      [&](float x, int) { count_in(x, r.place(x), Row::fixed(r.weight_near(x))); });
-  if (far) atomicAdd(&sh.cnt[kBins - 1], far);
-  if (m_cnt) atomicAdd(&sh.m_cnt, m_cnt), atomicAdd(&sh.m_mass, m_mass);
-  __syncthreads();
-  scan_bins<true>(sh.cnt, sh.mass, sh);
-
-  int list_lo = 1, list_hi = 0;  // bins that the list holds
-  uint32_t count = sh.cnt[kBins];
-  u64 total = sh.mass[kBins], k_total = total;
+  bool sums = false, whole = false;  // the bins' sums are there; the list holds all that top-k keeps
+  int list_lo = 1, list_hi = 0;      // bins that the list holds
+  uint32_t list_before = 0;          // elements above them
+  uint32_t count = 0;
+  u64 total = 0, k_total = 0;
   Found f;
 #pragma unroll 1
   for (int q = 0; q < 3; ++q) {  // the border of top-k, that of top-p, the draw: one copy of the search
-    if (q == 0 ? how.k <= 0 || (uint32_t)how.k >= count : q == 1 && !how.by_p) continue;
-    if (q == 2 && how.by_m && sh.m_cnt < count) count = sh.m_cnt, total = sh.m_mass;
-    const bool by_count = q == 0;
-    const u64 t = q == 0 ? (u64)(how.k - 1) : q == 1 ? how.p_target(k_total) : how.u_target(total);
-    const int b = by_count ? bin_of<uint32_t>(sh.cnt, (uint32_t)t) : bin_of<u64>(sh.mass, t);
-    if (by_count && b == kBins - 1) {  // past every id with a weight: the sum is all there is
+    int b = kFar;
+    bool fresh = false;  // the list was collected just now
+    if (q == 0) {
+      if (how.k <= 0 || (!gathered && (uint32_t)how.k >= sh.cnt[kBins])) continue;
+      if (gathered) {
+        for (int i = tid; i < (int)state.n_list; i += kSampleThreads) sh.list[i] = split->list[i];
+        if (tid == 0) sh.n = (int)state.n_list;
+        __syncthreads();
+        whole = fresh = true;
+      } else {
+        b = bin_of(sh.cnt, (uint32_t)(how.k - 1), sh);
+        whole = b < kFar && sh.cnt[b + 2] <= kList;  // fits with all that `collect` looks at
+      }
+    }
+    if (!whole && !sums) {
+      if (!summed) sum_bins<BF>(r, how, sh);
+      if (how.k <= 0) {
+        // not counted: from the sums, whose weights all but agree in a bin. Only says what is collected.
+        for (int i = tid; i < kFar; i += kSampleThreads)
+          sh.cnt[i] = (uint32_t)((float)sh.mass[i] * exp2f((float)(i + 1) * (1 / 32.f) - (float)a.shift)) + (sh.mass[i] > 0);
+        __syncthreads();
+        scan_bins(sh.cnt, sh.red32);
+      }
+      scan_bins(sh.mass, sh.red64);
+      sums = true;
+      count = (uint32_t)r.V - sh.dead;
+      total = k_total = sh.mass[kBins];
+    }
+    if (q == 0 && !whole && b == kFar) {  // past every id with a weight: the sum is all there is
       count = (uint32_t)how.k;
       continue;
     }
-    const int from = sh.cnt[b + 1] <= kList ? 0 : b;
-    if (b >= list_lo && b <= list_hi) {
-      f = in_list(by_count, t, sh.mass[list_lo], sh.cnt[list_lo], sh);
-    } else if (sh.cnt[b + 1] - sh.cnt[from] > kList) {
-      list_lo = 1, list_hi = 0;
-      f = in_large_bin<BF>(r, b, by_count, t, sh.mass[b], sh.cnt[b], sh);
-    } else {
-      collect_between<BF>(r, r.least([&](float x) { return r.bin(x) <= b; }),
-                          from > 0 ? r.least([&](float x) { return r.bin(x) < from; }) : INFINITY, sh);
-      order_list(r, sh.mass[from], sh);
-      list_lo = from;
-      list_hi = b;
-      f = in_list(by_count, t, sh.mass[from], sh.cnt[from], sh);
+    if (q == 1 && !how.by_p) continue;
+    if (q == 2 && how.by_m) {
+      if (whole) count = (uint32_t)in_list_by_weight(r, how, (int)count, sh), total = sh.sum[count - 1];
+      else if (sh.m_cnt < count) count = sh.m_cnt, total = sh.m_mass;
     }
+    const u64 t = q == 0 ? (u64)(how.k - 1) : q == 1 ? how.p_target(k_total) : how.u_target(total);
+    if (q > 0 && !whole) b = bin_of(sh.mass, t, sh);
+    if (!fresh && (q == 0 || (!whole && (b < list_lo || b > list_hi)))) {
+      list_hi = b;
+      for (list_lo = sh.cnt[b + 2] <= kList ? 0 : b;; list_lo = b) {
+        fresh = collect_bins<BF>(r, list_lo, b, sh);
+        if (fresh || list_lo == b) break;
+      }
+      list_before = sh.above;
+      if (!fresh) list_lo = 1, list_hi = 0;
+    }
+    const u64 above = sums && list_lo <= list_hi ? sh.mass[list_lo] : 0;
+    if (fresh) order_list(r, above, sh);
+    if (whole || list_lo <= list_hi) f = in_list(q == 0, t, above, list_before, sh);
+    else f = in_large_bin<BF>(r, b, q == 0, t, sh.mass[b], list_before, sh);
     if (q == 0) count = (uint32_t)how.k, total = k_total = f.incl;
     if (q == 1 && (uint32_t)f.count < count) count = (uint32_t)f.count, total = f.incl;
   }
   answer(a, row, f.id, (double)f.weight / (double)total, (int)count);
 }
 
-size_t sample_ws_bytes(int n, int V) { return (size_t)n * sizeof(RowTop); }
+// Workgroups that share a row: a power of two, up to about two a CU and at least 4096 ids each.
+static int sample_parts(int n, int V) {
+  int parts = 1;
+  while (parts < kMaxParts && (long)n * parts * 2 <= 256 && V / (parts * 2) >= 4096) parts *= 2;
+  return parts;
+}
+
+size_t sample_ws_bytes(int n, int V) {
+  return (size_t)n * (sizeof(RowState) + (sample_parts(n, V) > 1 ? sizeof(SplitRow) : 0));
+}
+
+template <bool BF>
+static void run_sample(const SampleArgs& a, hipStream_t s) {
+  const int parts = sample_parts(a.n, a.V);
+  const dim3 rows(a.n), shares((unsigned)a.n * parts), threads(kSampleThreads);
+  if (parts > 1) {
+    hipLaunchKernelGGL(sample_part_kernel<BF>, shares, threads, 0, s, a, parts);
+    hipLaunchKernelGGL(sample_gather_kernel<BF>, shares, threads, 0, s, a, parts);
+    hipLaunchKernelGGL((sample_full_kernel<BF, true>), rows, threads, 0, s, a);
+  } else {
+    hipLaunchKernelGGL(sample_top_kernel<BF>, rows, threads, 0, s, a);
+    hipLaunchKernelGGL((sample_full_kernel<BF, false>), rows, threads, 0, s, a);
+  }
+}
 
 void launch_sample(const SampleArgs& a, hipStream_t s) {
   if (a.n == 0) return;
-  auto go = [&](auto top, auto full) {
-    hipLaunchKernelGGL(top, dim3(a.n), dim3(kSampleThreads), 0, s, a);
-    hipLaunchKernelGGL(full, dim3(a.n), dim3(kSampleThreads), 0, s, a);
-  };
-  if (a.bf16) go(sample_top_kernel<true>, sample_full_kernel<true>);
-  else go(sample_top_kernel<false>, sample_full_kernel<false>);
+  a.bf16 ? run_sample<true>(a, s) : run_sample<false>(a, s);
 }
 
 }  // namespace dcl
