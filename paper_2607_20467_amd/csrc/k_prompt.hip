@@ -58,6 +58,7 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
   const int qw = q0 + 32 * wid, query = qw + lq;
   const int lim = a.causal ? min(n, query + 1) : n;       // keys that the lane's query sees
   const int nkeys = a.causal ? min(n, q0 + kPromptQ) : n;  // that the workgroup's queries see
+  const int wopen = a.causal ? min(n, qw + 1) : n;        // that all of the wave's queries see
   const int wkeys = qw >= n ? 0 : a.causal ? min(n, qw + 32) : n;
   const int tiles = (nkeys + KT - 1) / KT;
 
@@ -150,7 +151,8 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
         sc[kb] = mfma32(__builtin_bit_cast(bf16x8_t, x), qf[ks], sc[kb]);
       }
     // register i of step kb is key k0 + 32 kb + 8 (i / 4) + 4 hi + i % 4
-    if (masked) {
+    const bool cut = masked && k0 + KT > wopen;  // some query of the wave does not see all of the tile
+    if (cut) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -195,7 +197,7 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
       pf[s] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
     }
     bool odd_tile = false;
-    if (masked) {  // an infinity or NaN in a value that only some of the queries see must meet no probability of 0
+    if (cut) {  // an infinity or NaN in a value that only some of the queries see must meet no probability of 0
       uint32_t odd = 0;
 #pragma unroll 4
       for (int c = lane; c < CH; c += 64) {
