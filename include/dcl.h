@@ -334,7 +334,7 @@ typedef struct {
   const float* uniform;     /* the random number of the row, in [0, 1); required */
 } dcl_sampling;
 
-/* Workspace bytes of dcl_sample_tokens; 0 if the sizes are invalid. */
+/* Workspace bytes of dcl_sample_tokens; 0 if the sizes are invalid. Enough for smaller sizes too. */
 size_t dcl_sample_workspace_bytes(int32_t n, int32_t vocab);
 
 /* Draws a token per row of logits [n, vocab] (dtype DCL_DTYPE_F32 or DCL_DTYPE_BF16, rows row_stride elements apart,

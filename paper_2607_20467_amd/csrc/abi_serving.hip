@@ -17,6 +17,9 @@ float scale_log2(float scale) {
 
 bool misaligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
+// A launch has fewer than 2^32 threads, and these kernels' workgroups have 256.
+bool too_many(int64_t workgroups) { return workgroups >= (1 << 24); }
+
 // Rows [T, heads, dh] of bfloat16 with a row stride.
 dcl_status check_rows(const char* name, const void* p, int64_t stride, int32_t T, int32_t heads, int32_t dh) {
   if (T == 0) return DCL_OK;
@@ -102,7 +105,7 @@ dcl_status check_pages_copy(const dcl_pages* g, const int32_t* table, int32_t ma
   if (st == DCL_OK) st = check_rows("k", k, k_stride, T, g->n_kv_heads, g->head_dim);
   if (st == DCL_OK) st = check_rows("v", v, v_stride, T, g->n_kv_heads, g->head_dim);
   if (st != DCL_OK) return st;
-  if (((int64_t)max_new / 64 + 2) * g->n_kv_heads * B >= (1LL << 31))
+  if (too_many(((int64_t)max_new / 64 + 2) * g->n_kv_heads * B))
     return fail(DCL_E_UNSUPPORTED, "B=%d sequences of %d new tokens: too many for one call", B, max_new);
   return DCL_OK;
 }
@@ -129,9 +132,10 @@ PartLayout part_layout(const dcl_pages* g, int32_t n_heads, int32_t B, int32_t T
   return L;
 }
 
-dcl_status check_attention_size(const dcl_pages* g, int32_t n_heads, int32_t B, int32_t max_new) {
-  const int64_t tiles = ((int64_t)(n_heads / g->n_kv_heads) * max_new + 15) / 16;
-  if (tiles * g->n_kv_heads * B * 128 >= (1LL << 31) || (int64_t)max_new * B * (n_heads + 8) >= (1LL << 31))
+dcl_status check_attention_size(const dcl_pages* g, int32_t n_heads, int32_t B, int32_t max_new, int nsplit) {
+  const int64_t rows = (int64_t)(n_heads / g->n_kv_heads) * max_new, tiles = rows <= 16 ? 1 : (rows + 31) / 32;
+  const int64_t joined = nsplit > 16 ? n_heads : n_heads / 8 + 1;
+  if (too_many(((int64_t)nsplit * B * g->n_kv_heads + 8) * tiles) || (nsplit > 1 && too_many(joined * max_new * B)))
     return fail(DCL_E_UNSUPPORTED, "B=%d sequences of %d new tokens x %d heads: too many for one call", B, max_new, n_heads);
   return DCL_OK;
 }
@@ -211,10 +215,10 @@ dcl_status dcl_pages_read(const dcl_pages* pages, const int32_t* table, int32_t 
 size_t dcl_pages_attention_workspace_bytes(const dcl_pages* pages, int32_t n_heads, int32_t B, int32_t T,
                                            int32_t max_new, int32_t max_pages) {
   if (check_pool(pages, max_pages) != DCL_OK || check_heads(n_heads, pages->n_kv_heads) != DCL_OK || B < 1 ||
-      B > (1 << 16) || T < 0 || T > (1 << 22) || max_new < 0 || max_new > (1 << 22) ||
-      check_attention_size(pages, n_heads, B, max_new) != DCL_OK)
+      B > (1 << 16) || T < 0 || T > (1 << 22) || max_new < 0 || max_new > (1 << 22))
     return 0;
-  return part_layout(pages, n_heads, B, T, max_new, max_pages).total;
+  const PartLayout L = part_layout(pages, n_heads, B, T, max_new, max_pages);
+  return check_attention_size(pages, n_heads, B, max_new, L.nsplit) == DCL_OK ? L.total : 0;
 }
 
 dcl_status dcl_pages_attention(const dcl_pages* pages, const int32_t* table, int32_t max_pages, const int32_t* len,
@@ -225,11 +229,12 @@ dcl_status dcl_pages_attention(const dcl_pages* pages, const int32_t* table, int
   if (st == DCL_OK) st = check_heads(n_heads, pages->n_kv_heads);
   if (st == DCL_OK) st = check_rows("q", q, q_stride, T, n_heads, pages->head_dim);
   if (st == DCL_OK) st = check_rows("out", out, (int64_t)n_heads * pages->head_dim, T, n_heads, pages->head_dim);
-  if (st == DCL_OK) st = check_attention_size(pages, n_heads, B, max_new);
   if (st != DCL_OK) return st;
   if (!isfinite(scale)) return fail(DCL_E_ARG, "scale must be finite");
   if (causal != 0 && causal != 1) return fail(DCL_E_ARG, "causal must be 0 or 1");
   const PartLayout L = part_layout(pages, n_heads, B, T, max_new, max_pages);
+  st = check_attention_size(pages, n_heads, B, max_new, L.nsplit);
+  if (st != DCL_OK) return st;
   if (!ws) return fail(DCL_E_ARG, "workspace is NULL");
   if (misaligned(ws, 256)) return fail(DCL_E_ARG, "workspace must be 256-byte aligned");
   if (ws_bytes < L.total) return fail(DCL_E_WORKSPACE, "workspace %zu bytes < required %zu", ws_bytes, L.total);
@@ -268,7 +273,7 @@ dcl_status dcl_prompt_attention(const void* q, int64_t q_stride, const void* k, 
   if (st != DCL_OK) return st;
   if (!isfinite(scale)) return fail(DCL_E_ARG, "scale must be finite");
   if (causal != 0 && causal != 1) return fail(DCL_E_ARG, "causal must be 0 or 1");
-  if (((int64_t)B * n_heads + 8) * (max_len / 64 + 1) >= (1LL << 31))
+  if (too_many(((int64_t)B * n_heads + 8) * ((max_len < T ? max_len : T) / 128 + 1)))
     return fail(DCL_E_UNSUPPORTED, "B=%d sequences of %d rows x %d heads: too many for one call", B, max_len, n_heads);
   PromptAttn a;
   a.q = static_cast<const bf16_t*>(q);

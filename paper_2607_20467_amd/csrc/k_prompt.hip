@@ -85,8 +85,8 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
   uint32_t koff[NL], voff[NL];
 #pragma unroll
   for (int i = 0; i < NL; ++i) {
-    koff[i] = (uint32_t)(slot_row(i) * (int)a.k_stride + key_chunk(i)) * 2u;
-    voff[i] = (uint32_t)(slot_row(i) * (int)a.v_stride + value_chunk(i)) * 2u;
+    koff[i] = ((uint32_t)slot_row(i) * (uint32_t)a.k_stride + (uint32_t)key_chunk(i)) * 2u;
+    voff[i] = ((uint32_t)slot_row(i) * (uint32_t)a.v_stride + (uint32_t)value_chunk(i)) * 2u;
   }
   const bool near = a.k_stride <= (1 << 24) && a.v_stride <= (1 << 24);  // a tile's offsets stay in 32 bits
   const uint32_t lds = lds_addr_of(sm) + (uint32_t)wid * 1024u;

@@ -668,25 +668,29 @@ __global__ void __launch_bounds__(kSampleThreads, 8) sample_part_kernel(SampleAr
 
 // The question inside one bin with more elements than the list holds. All threads; the list is overwritten.
 template <bool BF>
-__device__ __forceinline__ Found in_large_bin(const Row& r, int b, bool by_count, u64 t, u64 above, uint32_t before, FullShared& sh) {
+__device__ __forceinline__ Found in_large_bin(const Row& r, int b, bool by_count, u64 t, u64 above, FullShared& sh) {
   const int tid = threadIdx.x;
   constexpr int PARTS = 1024;
   uint32_t* cnt = reinterpret_cast<uint32_t*>(sh.sum);
   u64* mass = sh.list;
   static_assert(PARTS <= kList, "counts and sums of the parts lie in the list's memory");
   // the values that are left, in order_key's terms
+  uint32_t before = 0;  // elements above them
   uint32_t klo = order_key(fmaxf(r.floor_of(b), -3.4028234663852886e38f)), khi = order_key(r.M);
 #pragma unroll 1
   for (bool whole = true;; whole = false) {  // the whole bin at first
     // the range that they really take
     __syncthreads();
-    if (tid == 0) sh.lo = 0xFFFFFFFFu, sh.hi = 0, sh.n = 0;
+    if (tid == 0) sh.lo = 0xFFFFFFFFu, sh.hi = 0, sh.n = 0, sh.above = 0;
     __syncthreads();
-    uint32_t lo = 0xFFFFFFFFu, hi = 0, n = 0;
+    uint32_t lo = 0xFFFFFFFFu, hi = 0, n = 0, higher = 0;
     each_from<BF>(r, key_value(klo), [&](float x, int) {
       const uint32_t k = order_key(x);
-      if (whole ? r.bin(x) == b : k <= khi) lo = min(lo, k), hi = max(hi, k), ++n;
+      const int at = whole ? r.bin(x) : k <= khi ? b : b - 1;
+      if (at == b) lo = min(lo, k), hi = max(hi, k), ++n;
+      higher += at < b;
     });
+    if (whole && higher) atomicAdd(&sh.above, higher);
     if (n) {
       atomicMin(&sh.lo, lo);
       atomicMax(&sh.hi, hi);
@@ -696,6 +700,7 @@ __device__ __forceinline__ Found in_large_bin(const Row& r, int b, bool by_count
     klo = sh.lo;
     khi = sh.hi;
     const int left = sh.n;
+    if (whole) before = sh.above;
     __syncthreads();
     if (klo == khi) {  // equal values: element j of them, by arithmetic; its id by counting in order
       const u64 w = r.mass(key_value(klo));
@@ -929,22 +934,24 @@ __global__ void __launch_bounds__(kSampleThreads, 4) sample_full_kernel(SampleAr
     const u64 above = sums && list_lo <= list_hi ? sh.mass[list_lo] : 0;
     if (fresh) order_list(r, above, sh);
     if (whole || list_lo <= list_hi) f = in_list(q == 0, t, above, list_before, sh);
-    else f = in_large_bin<BF>(r, b, q == 0, t, sh.mass[b], list_before, sh);
+    else f = in_large_bin<BF>(r, b, q == 0, t, sh.mass[b], sh);
     if (q == 0) count = (uint32_t)how.k, total = k_total = f.incl;
     if (q == 1 && (uint32_t)f.count < count) count = (uint32_t)f.count, total = f.incl;
   }
   answer(a, row, f.id, (double)f.weight / (double)total, (int)count);
 }
 
-// Workgroups that share a row: a power of two, up to about two a CU and at least 4096 ids each.
+// Workgroups that share a row: a power of two, together up to one a CU, and at least 4096 ids each.
+constexpr int kShares = 256, kShare = 4096;
 static int sample_parts(int n, int V) {
   int parts = 1;
-  while (parts < kMaxParts && (long)n * parts * 2 <= 256 && V / (parts * 2) >= 4096) parts *= 2;
+  while (parts < kMaxParts && (long)n * parts * 2 <= kShares && V / (parts * 2) >= kShare) parts *= 2;
   return parts;
 }
 
-size_t sample_ws_bytes(int n, int V) {
-  return (size_t)n * (sizeof(RowState) + (sample_parts(n, V) > 1 ? sizeof(SplitRow) : 0));
+size_t sample_ws_bytes(int n, int V) {  // enough for fewer rows and ids too
+  const size_t shared = V >= 2 * kShare ? (n < kShares / 2 ? n : kShares / 2) : 0;
+  return (size_t)n * sizeof(RowState) + shared * sizeof(SplitRow);
 }
 
 template <bool BF>
@@ -962,8 +969,17 @@ static void run_sample(const SampleArgs& a, hipStream_t s) {
 }
 
 void launch_sample(const SampleArgs& a, hipStream_t s) {
-  if (a.n == 0) return;
-  a.bf16 ? run_sample<true>(a, s) : run_sample<false>(a, s);
+  constexpr int MOST = 1 << 21;  // rows of a launch: 2^32 threads are too many
+  for (int first = 0; first < a.n; first += MOST) {
+    SampleArgs b = a;
+    b.n = a.n - first < MOST ? a.n - first : MOST;
+    b.logits = static_cast<const char*>(a.logits) + (size_t)first * a.stride * (a.bf16 ? 2 : 4);
+    auto from = [&](auto*& p) {
+      if (p) p += first;
+    };
+    from(b.temperature), from(b.top_k), from(b.top_p), from(b.min_p), from(b.uniform), from(b.token), from(b.conf), from(b.kept);
+    a.bf16 ? run_sample<true>(b, s) : run_sample<false>(b, s);  // in turn, over the same workspace
+  }
 }
 
 }  // namespace dcl

@@ -239,3 +239,61 @@ def test_replays_and_streams(dcl):
     go(0)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) and torch.equal(c, b) for a, b, c in zip(bufs[0], ref, bufs[1]))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("V", [8191, 8192, 16384 + 5, 70001])
+def test_few_rows_are_drawn_as_many_are(dcl, V, bf16):
+    """Workgroups share the rows of small calls: the same rows, special ones among them, in calls of 300 and of 1 to 90."""
+    n = 300
+    x, g = logits(n, V, V)
+    x[1] = -math.inf
+    x[2] = math.nan
+    x[3, [7, 100, V - 1]] = math.inf
+    x[4] = 3.25
+    x[5] = torch.finfo(torch.float32).min
+    x[5, V - 1] = 0
+    x[6, V // 2:] = -math.inf
+    x[7] = 20 + torch.arange(V) * 2.0 ** -19                      # one bin, and in bfloat16 few values
+    x[8, :V - 600] = math.nan
+    x[9] *= 0.01
+    x[10, :] = -40
+    x[10, 3] = 0
+    x[11] = torch.arange(V).float() * -1e-3
+    x[12, :] = -math.inf
+    x[12, V - 3:] = -2.5
+    x = (x.to(torch.bfloat16) if bf16 else x).cuda()
+    r = np.random.default_rng(V)
+    how = dict(temperature=r.choice([0.0, 0.2, 0.6, 1.0, 1.0, 1.4], n), top_k=r.choice([0, 0, 0, 1, 20, 512, 513, 1500, 5000], n),
+               top_p=r.choice([1.0, 0.5, 0.9, 0.999], n), min_p=r.choice([0.0, 0.0, 0.05, 1e-4], n))
+    u = torch.rand(n, generator=g).numpy()
+    for settings in (how, {}, {"top_k": 40}, {"top_p": 0.9}):
+        def part(rows):
+            return {k: (v[rows] if isinstance(v, np.ndarray) else v) for k, v in settings.items()}
+        whole = draw(dcl, x, u, **settings)
+        check(x[:16], [w[:16] for w in whole], u[:16], **part(slice(0, 16)))
+        first = 0
+        for m in (1, 2, 5, 14, 33, 90):
+            rows = slice(first, first + m)
+            got = draw(dcl, x[rows], u[rows], **part(rows))
+            for a, b in zip(got, whole):
+                assert np.array_equal(a, b[rows], equal_nan=True), (m, np.nonzero(a != b[rows])[0][:5] + first)
+            first += m
+
+
+def test_more_rows_than_a_launch_has(dcl):
+    n, V = (1 << 21) + 3, 2
+    x = torch.zeros(n, V, device="cuda")
+    x[::3, 1] = 1.0
+    u = torch.zeros(n, device="cuda")
+    u[5::7] = 0.999
+    need = dcl.dcl_sample_workspace_bytes(n, V)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    token, kept = (torch.full((n,), -9, dtype=torch.int32, device="cuda") for _ in range(2))
+    top_k = torch.zeros(n, dtype=torch.int32, device="cuda")
+    top_k[n - 1] = 1
+    dcl.dcl_sample_tokens(x, n, V, None, top_k, None, None, u, token, None, kept, ws, need)
+    best = (x[:, 1] > 0).int()
+    want = torch.where(u > 0.5, 1 - best, best)                   # the less likely id has a quarter or a half
+    want[n - 1] = best[n - 1]
+    assert torch.equal(token, want) and int(kept[n - 1]) == 1 and bool((kept[:n - 1] == 2).all())

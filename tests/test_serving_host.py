@@ -94,6 +94,17 @@ def test_pages_attention_refusals(dcl, change, status, word):
     assert r == status and word in msg, (r, msg)
 
 
+def test_pages_calls_of_too_many_workgroups(dcl):
+    g = pool(dcl, n_kv_heads=1024)
+    copy, attn = (256, 1 << 16, 256, 1 << 16, None), (256, 1 << 16, 1024, 0.125, 1, 256, 0, 256, 1 << 60, None)
+    for name, tail, kw in (("dcl_pages_write", copy, dict(B=8192, max_new=0)), ("dcl_pages_read", copy, dict(max_new=1 << 22)),
+                           ("dcl_pages_attention", attn, dict(B=1 << 14)),
+                           ("dcl_pages_attention", attn, dict(max_new=1 << 20, T=1 << 20))):
+        r, msg = call(dcl, name, g, tail, **kw)
+        assert r == 2 and "too many" in msg, (name, kw, r, msg)
+    assert dcl.load_library().dcl_pages_attention_workspace_bytes(ctypes.byref(g), 1024, 1 << 14, 4, 4, 2) == 0
+
+
 def test_pages_workspace_sizes(dcl):
     f = dcl.load_library().dcl_pages_attention_workspace_bytes
     g = pool(dcl)
@@ -175,7 +186,7 @@ PROMPT = (256, 256, 256, 128, 256, 128, 256, 1, 4, 4, 4, 2, 64, 0.125, 1, 256, 0
     ({4: 8}, 1, "aligned"), ({5: 120}, 1, "stride"), ({6: 0}, 1, "cu"), ({7: 0}, 1, "B=0"), ({8: -1}, 1, "T="),
     ({9: -1}, 1, "max_len"), ({10: 3}, 2, "n_heads"), ({11: 0}, 2, "n_heads"), ({12: 80}, 2, "head_dim"),
     ({13: float("inf")}, 1, "scale"), ({14: 5}, 1, "causal"), ({15: 0}, 1, "out"),
-    ({7: 60000, 9: 1 << 22, 8: 1 << 22}, 2, "too many"),
+    ({7: 60000, 9: 1 << 22, 8: 1 << 22}, 2, "too many"), ({7: 1 << 16, 8: 1 << 22, 9: 128 * 63}, 2, "too many"),
 ])
 def test_prompt_refusals(dcl, change, status, word):
     r = dcl.load_library().dcl_prompt_attention(*[change.get(i, x) for i, x in enumerate(PROMPT)])
@@ -207,6 +218,8 @@ def test_sample_needs_random_numbers_and_sizes(dcl):
     r, msg = sample_call(dcl, how=dcl.DclSampling(256, 256, 256, 256, 0))
     assert r == 1 and "uniform" in msg
     f = dcl.load_library().dcl_sample_workspace_bytes
+    assert all(f(n, v) <= f(m, w) for n, m in ((1, 2), (4, 128), (128, 129), (128, 512), (512, 1 << 22))
+               for v, w in ((1, 8191), (8191, 8192), (50000, 1 << 20), (1 << 20, 1 << 20)))
     assert f(1, 1) > 0 and f(0, 10) > 0 and f(-1, 10) == 0 and f(1, 0) == 0 and f(1, (1 << 20) + 1) == 0
 
 
