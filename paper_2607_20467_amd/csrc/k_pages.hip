@@ -65,7 +65,9 @@ __device__ __forceinline__ uint32_t amax8(const uint4& x) {
 // ---------------------------------------------------------------- write
 // One workgroup takes 64 positions (aligned to 64 in the sequence) of one KV head. Rows arrive with the dimension
 // innermost; keys go out the same way, values through LDS with the position innermost, in chunks of 16 positions that
-// never straddle a page. Memory-bound: each row is read once and each byte of the pages written once.
+// never straddle a page. Memory-bound: each row is read once and each byte of the pages written once. Nine prompts of 500 to
+// 7000 tokens x 32 heads into 8-bit pages, 592 MB: 128 us, 4.6 TB/s (a copy reaches 5.1); one token of each of 64 sequences
+// x 8 heads: 7.7 us, the chain of border, length, page number and row, one load after the other.
 constexpr int kGroup = 64;
 
 template <int DH, bool E4>
@@ -74,7 +76,7 @@ __global__ void __launch_bounds__(256) pages_write_kernel(Pages p, const bf16_t*
   constexpr int ES = E4 ? 1 : 2, L = DH / 8, TPR = 256 / L, R = kGroup / TPR;
   constexpr int PITCH = DH * ES + 4;  // four chunks of 16 rows apart: other banks
   __shared__ __attribute__((aligned(16))) uint8_t sv[kGroup * PITCH];
-  const int grp = blockIdx.x % groups, bh = blockIdx.x / groups, h = bh % p.Hkv, b = bh / p.Hkv;
+  const int h = blockIdx.x % p.Hkv, gb = blockIdx.x / p.Hkv, grp = gb % groups, b = gb / groups;
   const SeqRows r = seq_rows(p.cu, b, p.T);
   const int n = min(r.n, p.max_new), start = seq_len(p.len, b) - r.n;  // position of the first row
   const int g0 = (start & ~(kGroup - 1)) + grp * kGroup;
@@ -161,20 +163,37 @@ __global__ void __launch_bounds__(256) pages_write_kernel(Pages p, const bf16_t*
 
 // ---------------------------------------------------------------- read
 // The reverse, in the same groups: values come in by rows of positions and leave by rows of dimensions. A row whose
-// position no page holds is zeros.
+// position no page holds is zeros. Seven sequences of 300 to 5000 positions x 8 heads of 8 bits, 96 MB: 24 us, 4.0 TB/s (28 with
+// the heads of a group in workgroups far apart and the keys read after the values).
 template <int DH, bool E4>
 __global__ void __launch_bounds__(256) pages_read_kernel(Pages p, bf16_t* __restrict__ k, long kst,
                                                         bf16_t* __restrict__ v, long vst, int groups) {
   constexpr int ES = E4 ? 1 : 2, L = DH / 8, TPR = 256 / L, R = kGroup / TPR;
   constexpr int PITCH = kGroup * ES + 4;
   __shared__ __attribute__((aligned(16))) uint8_t sv[DH * PITCH];
-  const int grp = blockIdx.x % groups, bh = blockIdx.x / groups, h = bh % p.Hkv, b = bh / p.Hkv;
+  const int h = blockIdx.x % p.Hkv, gb = blockIdx.x / p.Hkv, grp = gb % groups, b = gb / groups;
   const SeqRows r = seq_rows(p.cu, b, p.T);
   const int n = min(r.n, p.max_new), start = seq_len(p.len, b) - r.n;
   const int g0 = (start & ~(kGroup - 1)) + grp * kGroup;
   if (g0 >= start + n) return;
   const int32_t* row = p.table + (size_t)b * p.max_pages;
   const int plen = 1 << p.shift, tid = threadIdx.x, c = tid % L;
+  typedef std::conditional_t<E4, uint2, uint4> Piece;
+  Piece xk[R];
+  uint32_t held = 0, ks[R], vs[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int local = i * TPR + tid / L, t = g0 + local - start;
+    const int page = t >= 0 && t < n ? page_of(row, p.max_pages, p.n_pages, p.shift, (g0 + local) >> 4) : -1;
+    const size_t slot = ((size_t)max(page, 0) * p.Hkv + h) * plen + ((g0 + local) & (plen - 1));
+    xk[i] = Piece{};
+    ks[i] = vs[i] = 0;
+    if (page >= 0) {
+      held |= 1u << i;
+      xk[i] = *reinterpret_cast<const Piece*>(p.k + (slot * DH + 8 * c) * ES);
+      if constexpr (E4) ks[i] = p.ks[slot], vs[i] = p.vs[slot];
+    }
+  }
 #pragma unroll
   for (int i = 0; i < DH * 4 / 256; ++i) {
     const int u = tid + 256 * i, ch = u & 3, d = u >> 2, p0 = g0 + 16 * ch;
@@ -197,14 +216,12 @@ __global__ void __launch_bounds__(256) pages_read_kernel(Pages p, bf16_t* __rest
   for (int i = 0; i < R; ++i) {
     const int local = i * TPR + tid / L, t = g0 + local - start;
     if (t < 0 || t >= n) continue;
-    const int page = page_of(row, p.max_pages, p.n_pages, p.shift, (g0 + local) >> 4);
-    const int off = (g0 + local) & (plen - 1);
-    const size_t slot = ((size_t)max(page, 0) * p.Hkv + h) * plen + off, at = (size_t)(r.first + t);
+    const size_t at = (size_t)(r.first + t);
     uint4 ok = make_uint4(0, 0, 0, 0), ov = ok;
-    if (page >= 0) {
+    if (held >> i & 1) {
       if constexpr (E4) {
-        const uint2 x = *reinterpret_cast<const uint2*>(p.k + slot * DH + 8 * c);
-        const float fk = scale_of(p.ks[slot]), fv = scale_of(p.vs[slot]);
+        const uint2 x = xk[i];
+        const float fk = scale_of(ks[i]), fv = scale_of(vs[i]);
         uint32_t y[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -218,7 +235,7 @@ __global__ void __launch_bounds__(256) pages_read_kernel(Pages p, bf16_t* __rest
         ok = make_uint4(pair(x.x, false, fk), pair(x.x, true, fk), pair(x.y, false, fk), pair(x.y, true, fk));
         ov = make_uint4(pair(y[0], false, fv), pair(y[0], true, fv), pair(y[1], false, fv), pair(y[1], true, fv));
       } else {
-        ok = *reinterpret_cast<const uint4*>(p.k + (slot * DH + 8 * c) * 2);
+        ok = xk[i];
         uint32_t y[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -273,6 +290,12 @@ void launch_pages_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, h
 // a value without, since its piece is many keys; that scale multiplies the key's probability in float32. The probability
 // is then rounded to bfloat16 once, 2^-9 of itself, while the sum that divides takes it unrounded: over many keys these
 // roundings average out, far below the rounding of the output.
+//
+// With one token it is bound by HBM: two sequences of 90000 to 131072 keys, 28 / 4 heads, bfloat16, 516 MB: 102 us with the
+// join, 5.05 TB/s; 64 sequences of 200 to 8000 8-bit keys, 32 / 8 heads, 323 MB: 78 us, 4.1 TB/s, the rest being the first
+// loads and the ragged end. Four sequences of 90 to 700 keys x 32 heads take 13 us, two launches and their loads' latency. Under
+// a block of 64 tokens (8 sequences, 1280 8-bit keys, 32 heads: 32 us) a key's conversion, its products and the
+// exponentials share a SIMD's issue slots with little overlap: 2.9 TB/s, 1.35 of the time that the loads alone would take.
 __device__ __forceinline__ f32x4_t mfma16p(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }

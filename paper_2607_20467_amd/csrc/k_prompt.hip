@@ -9,6 +9,11 @@
 // rows that one read touches lie in different banks.
 //
 // The probabilities are rounded to bfloat16 once, 2^-9 of each, the sum that divides takes them unrounded.
+//
+// Bound by the matrix and vector pipes together: one causal prompt of 8192 tokens x 32 heads of 128 takes 513 to 533 us, 1.03 to
+// 1.07 PFLOP/s of the 1.21 that a large matrix product reaches. Eight prompts of 78 to 1531 tokens, 28 / 4 heads: 90 us, 0.59
+// PFLOP/s: the two tiles on the diagonal are half masked, and a workgroup of seven tiles starts and ends three times as
+// often as it would in the long prompt.
 #include <type_traits>
 
 #include "dcl_internal.h"

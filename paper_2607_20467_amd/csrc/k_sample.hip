@@ -3,9 +3,9 @@
 // The ids of a row in order of (logit descending, id ascending) have weights w = exp((x - M) / T), M the row's maximum.
 // Every filter keeps a prefix of that order, and the draw asks for the element at which the running sum passes
 // u * total, so all of them are one question: at which element does the running count or the running sum of weights
-// pass a value? It is answered without sorting the row: a histogram of 2048 bins over (M - x) / T (count and sum per bin)
-// says in which bin, and only that bin's elements (or, where they are few, all up to it) are collected into LDS, sorted and
-// summed. A bin with more elements than fit is split again by value; equal values are answered by arithmetic.
+// pass a value? It is answered without sorting the row: a histogram over the weights (32 bins per factor of 2, their sums, and
+// their counts where top-k asks) says in which bin, and only that bin's elements (or, where they are few, all up to it) are
+// collected into LDS, put in order and summed. A bin with more elements than fit is split again by value; equal values are answered by arithmetic.
 //
 // Weights are exponentials to 1e-13, held as whole numbers of 2^-shift, so every sum is exact in any order: results do not
 // depend on timing, and a border falls as exact arithmetic on the weights has it (a float32 sum's error of 1e-7 would move
@@ -15,6 +15,12 @@
 // or little more (top-k with the ids down to its border in LDS: nothing else of the row needs a weight), the second answers
 // the others from the histogram. Few rows are shared by several workgroups, in three kernels: maxima, then the parts'
 // elements or histograms, then one workgroup a row for the answer.
+//
+// 512 rows of 152064 bfloat16 logits, each row with its own settings: 170 us. The first kernel (52) is bound by memory: 156 MB,
+// and the rows with a top-k once more, mostly from the last cache; the second (124) by the additions to the histogram in
+// LDS (35 us of a row's 57 without a filter, one row a CU) and its passes one behind the other. 4 rows of 126464 float32, top-k 50
+// and top-p 0.95: 25 us, three kernels of 6, 9 and 11 us: chains of dependent loads, barriers and instruction fetches. Without
+// sharing they took 35, rows without a filter 85 instead of 38.
 #include <limits.h>
 
 #include "dcl_internal.h"
@@ -635,7 +641,7 @@ __global__ void __launch_bounds__(kSampleThreads, 8) sample_top_kernel(SampleArg
   if (tid == 0) left->M = best;
 }
 
-// Rows that `parts` workgroups share (few rows: one CU reads 30 GB/s, a row of 126464 float32 16 us). First the parts'
+// Rows that `parts` workgroups share (few rows: one CU reads 30 GB/s, a row of 126464 float32 in 16 us). First the parts'
 // maxima and those of 1024 groups of threads, and zeros where the next kernel counts.
 template <bool BF>
 __global__ void __launch_bounds__(kSampleThreads, 8) sample_part_kernel(SampleArgs a, int parts) {
