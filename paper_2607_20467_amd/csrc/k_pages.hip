@@ -62,11 +62,26 @@ __device__ __forceinline__ uint32_t amax8(const uint4& x) {
   return m;
 }
 
+// Streams that pass the caches by, where it measured faster: stores of whole rows and pages (the read measured below 23.5 -> 16.9
+// us, write 127 -> 122.5) and the rows that are written to pages (119.3). Pages are read through the caches: their lines are
+// asked for in pieces (read 21.7 otherwise, attention over two long sequences 111 instead of 102).
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void store_past(void* p, const uint4& x) {
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, x), static_cast<u32x4_t*>(p));
+}
+__device__ __forceinline__ uint4 load_past(const void* p) {
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(static_cast<const u32x4_t*>(p)));
+}
+__device__ __forceinline__ void store_past(void* p, const uint2& x) {
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x2_t, x), static_cast<u32x2_t*>(p));
+}
+
 // ---------------------------------------------------------------- write
 // One workgroup takes 64 positions (aligned to 64 in the sequence) of one KV head. Rows arrive with the dimension
 // innermost; keys go out the same way, values through LDS with the position innermost, in chunks of 16 positions that
 // never straddle a page. Memory-bound: each row is read once and each byte of the pages written once. Nine prompts of 500 to
-// 7000 tokens x 32 heads into 8-bit pages, 592 MB: 128 us, 4.6 TB/s (a copy reaches 5.1); one token of each of 64 sequences
+// 7000 tokens x 32 heads into 8-bit pages, 592 MB: 119 us, 5.0 TB/s (a copy reaches 5.1); one token of each of 64 sequences
 // x 8 heads: 7.7 us, the chain of border, length, page number and row, one load after the other.
 constexpr int kGroup = 64;
 
@@ -90,8 +105,8 @@ __global__ void __launch_bounds__(256) pages_write_kernel(Pages p, const bf16_t*
     xk[i] = xv[i] = make_uint4(0, 0, 0, 0);
     if (t >= 0 && t < n) {
       const size_t at = (size_t)(r.first + t);
-      xk[i] = *reinterpret_cast<const uint4*>(k + at * kst + (size_t)h * DH + 8 * c);
-      xv[i] = *reinterpret_cast<const uint4*>(v + at * vst + (size_t)h * DH + 8 * c);
+      xk[i] = load_past(k + at * kst + (size_t)h * DH + 8 * c);
+      xv[i] = load_past(v + at * vst + (size_t)h * DH + 8 * c);
     }
   }
 #pragma unroll
@@ -113,7 +128,7 @@ __global__ void __launch_bounds__(256) pages_write_kernel(Pages p, const bf16_t*
       d[0] = qv.x;
       d[1] = qv.y;
       if (page >= 0) {
-        *reinterpret_cast<uint2*>(p.k + slot * DH + 8 * c) = qk;
+        store_past(p.k + slot * DH + 8 * c, qk);
         if (c == 0) {
           p.ks[slot] = (uint8_t)ek;
           p.vs[slot] = (uint8_t)ev;
@@ -125,7 +140,7 @@ __global__ void __launch_bounds__(256) pages_write_kernel(Pages p, const bf16_t*
       d[1] = xv[i].y;
       d[2] = xv[i].z;
       d[3] = xv[i].w;
-      if (page >= 0) *reinterpret_cast<uint4*>(p.k + (slot * DH + 8 * c) * 2) = xk[i];
+      if (page >= 0) store_past(p.k + (slot * DH + 8 * c) * 2, xk[i]);
     }
   }
   __syncthreads();
@@ -151,7 +166,7 @@ __global__ void __launch_bounds__(256) pages_write_kernel(Pages p, const bf16_t*
       }
 #pragma unroll
       for (int j = 0; j < ES; ++j)
-        reinterpret_cast<uint4*>(dst)[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+        store_past(dst + 16 * j, make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]));
     } else {
       for (int j = lo; j < hi; ++j) {
         if constexpr (E4) dst[j] = src[j * PITCH];
@@ -163,8 +178,8 @@ __global__ void __launch_bounds__(256) pages_write_kernel(Pages p, const bf16_t*
 
 // ---------------------------------------------------------------- read
 // The reverse, in the same groups: values come in by rows of positions and leave by rows of dimensions. A row whose
-// position no page holds is zeros. Seven sequences of 300 to 5000 positions x 8 heads of 8 bits, 96 MB: 24 us, 4.0 TB/s (28 with
-// the heads of a group in workgroups far apart and the keys read after the values).
+// position no page holds is zeros. Seven sequences of 300 to 5000 positions x 8 heads of 8 bits, 96 MB: 17 us, 5.7 TB/s
+// (28 with the heads of a group in workgroups far apart, the keys read after the values and stores that stay in the caches).
 template <int DH, bool E4>
 __global__ void __launch_bounds__(256) pages_read_kernel(Pages p, bf16_t* __restrict__ k, long kst,
                                                         bf16_t* __restrict__ v, long vst, int groups) {
@@ -245,8 +260,8 @@ __global__ void __launch_bounds__(256) pages_read_kernel(Pages p, bf16_t* __rest
         ov = make_uint4(y[0], y[1], y[2], y[3]);
       }
     }
-    *reinterpret_cast<uint4*>(k + at * kst + (size_t)h * DH + 8 * c) = ok;
-    *reinterpret_cast<uint4*>(v + at * vst + (size_t)h * DH + 8 * c) = ov;
+    store_past(k + at * kst + (size_t)h * DH + 8 * c, ok);
+    store_past(v + at * vst + (size_t)h * DH + 8 * c, ov);
   }
 }
 
@@ -294,8 +309,8 @@ void launch_pages_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, h
 // With one token it is bound by HBM: two sequences of 90000 to 131072 keys, 28 / 4 heads, bfloat16, 516 MB: 102 us with the
 // join, 5.05 TB/s; 64 sequences of 200 to 8000 8-bit keys, 32 / 8 heads, 323 MB: 78 us, 4.1 TB/s, the rest being the first
 // loads and the ragged end. Four sequences of 90 to 700 keys x 32 heads take 13 us, two launches and their loads' latency. Under
-// a block of 64 tokens (8 sequences, 1280 8-bit keys, 32 heads: 32 us) a key's conversion, its products and the
-// exponentials share a SIMD's issue slots with little overlap: 2.9 TB/s, 1.35 of the time that the loads alone would take.
+// a block of 64 tokens (8 sequences, 1280 8-bit keys, 32 heads: 32 us, 2.9 TB/s) the vector pipes are busy half of the time with
+// conversions and exponentials, the matrix pipes a seventh, and a wave has one tile of keys on its way at a time.
 __device__ __forceinline__ f32x4_t mfma16p(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
