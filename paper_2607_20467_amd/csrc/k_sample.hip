@@ -864,19 +864,25 @@ __global__ void __launch_bounds__(kSampleThreads, 4) sample_full_kernel(SampleAr
   Row r = row_of<BF>(a, row, sh.table);
   const How how(a, row);
   fill_table(sh.table, a.shift);
+  const SplitRow* split = reinterpret_cast<const SplitRow*>(static_cast<const RowState*>(a.ws) + a.n) + row;
+  if (SHARED && takes_bound(how) && state.M < INFINITY && state.n_list <= kList) {  // the list is in the workspace
+    r.set(state.M, how.T);
+    for (int i = tid; i < (int)state.n_list; i += kSampleThreads) sh.list[i] = split->list[i];
+    if (tid == 0) sh.n = (int)state.n_list;
+    __syncthreads();
+    return answer_from_list(a, row, r, how, sh);
+  }
   clear_histogram(sh);
   __syncthreads();
   if (SHARED && state.M == INFINITY) return infinite_row<BF>(a, row, r, how, sh);
   r.set(state.M, how.T);
-  const SplitRow* split = reinterpret_cast<const SplitRow*>(static_cast<const RowState*>(a.ws) + a.n) + row;
-  const bool gathered = SHARED && takes_bound(how) && state.n_list <= kList;  // the list is in the workspace
-  const bool summed = SHARED && !takes_bound(how);                            // the histogram is
+  const bool summed = SHARED && !takes_bound(how);  // the histogram is in the workspace
   if (summed) {
     for (int i = tid; i <= kFar; i += kSampleThreads) sh.cnt[i] = split->cnt[i], sh.mass[i] = split->mass[i];
     if (tid == 0) sh.m_cnt = state.m_cnt, sh.m_mass = state.m_mass, sh.dead = state.dead;
     __syncthreads();
   }
-  if (how.k > 0 && !gathered) {
+  if (how.k > 0) {
     if (!summed) count_bins<BF>(r, sh);
     scan_bins(sh.cnt, sh.red32);
   }
@@ -892,16 +898,9 @@ __global__ void __launch_bounds__(kSampleThreads, 4) sample_full_kernel(SampleAr
     int b = kFar;
     bool fresh = false;  // the list was collected just now
     if (q == 0) {
-      if (how.k <= 0 || (!gathered && (uint32_t)how.k >= sh.cnt[kBins])) continue;
-      if (gathered) {
-        for (int i = tid; i < (int)state.n_list; i += kSampleThreads) sh.list[i] = split->list[i];
-        if (tid == 0) sh.n = (int)state.n_list;
-        __syncthreads();
-        whole = fresh = true;
-      } else {
-        b = bin_of(sh.cnt, (uint32_t)(how.k - 1), sh);
-        whole = b < kFar && sh.cnt[b + 2] <= kList;  // fits with all that `collect` looks at
-      }
+      if (how.k <= 0 || (uint32_t)how.k >= sh.cnt[kBins]) continue;
+      b = bin_of(sh.cnt, (uint32_t)(how.k - 1), sh);
+      whole = b < kFar && sh.cnt[b + 2] <= kList;  // fits with all that `collect` looks at
     }
     if (!whole && !sums) {
       if (!summed) sum_bins<BF>(r, how, sh);
@@ -928,7 +927,7 @@ __global__ void __launch_bounds__(kSampleThreads, 4) sample_full_kernel(SampleAr
     }
     const u64 t = q == 0 ? (u64)(how.k - 1) : q == 1 ? how.p_target(k_total) : how.u_target(total);
     if (q > 0 && !whole) b = bin_of(sh.mass, t, sh);
-    if (!fresh && (q == 0 || (!whole && (b < list_lo || b > list_hi)))) {
+    if (q == 0 || (!whole && (b < list_lo || b > list_hi))) {
       list_hi = b;
       for (list_lo = sh.cnt[b + 2] <= kList ? 0 : b;; list_lo = b) {
         fresh = collect_bins<BF>(r, list_lo, b, sh);
