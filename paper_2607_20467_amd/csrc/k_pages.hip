@@ -308,7 +308,7 @@ void launch_pages_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, h
 //
 // With one token it is bound by HBM: two sequences of 90000 to 131072 keys, 28 / 4 heads, bfloat16, 516 MB: 102 us with the
 // join, 5.05 TB/s; 64 sequences of 200 to 8000 8-bit keys, 32 / 8 heads, 323 MB: 78 us, 4.1 TB/s, the rest being the first
-// loads and the ragged end. Four sequences of 90 to 700 keys x 32 heads take 13 us, two launches and their loads' latency. Under
+// loads and the ragged end. Four sequences of 90 to 700 keys x 32 heads take 12 us, the latency of their loads. Under
 // a block of 64 tokens (8 sequences, 1280 8-bit keys, 32 heads: 32 us, 2.9 TB/s) the vector pipes are busy half of the time with
 // conversions and exponentials, the matrix pipes a seventh, and a wave has one tile of keys on its way at a time.
 __device__ __forceinline__ f32x4_t mfma16p(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
@@ -728,11 +728,14 @@ static int query_fragments(int Hkv, int g, int B, int max_new) {
 // Keys of a part: about 2048 workgroups if every sequence filled its row of the table (fewer leave CUs idle and the longest
 // sequence's parts last; more spend their time on their first loads: one token of 64 sequences of 200 to 8000, 2048 / 4096 /
 // 8192 workgroups 81 / 85 / 90 us), at most 128 parts. A part's output costs 8 bytes an element of memory traffic: at most
-// a sixteenth of the part's keys and values, unless there are too few workgroups for that to matter.
+// a sixteenth of the part's keys and values, unless there are too few workgroups for that to matter. Up to 768 keys under one
+// fragment stay whole: a join costs more than three parts save (4 x 1 token, 32 heads, 500 / 700 bfloat16 keys: 14.4 / 15.9 us in
+// parts of 256, 12.3 / 14.2 whole; 32 / 8 heads, 8 bits: 12.7 / 12.8 and 12.0 / 12.3).
 int pages_attention_span(int Hkv, int g, int B, int max_new, int capacity, int e4m3) {
   const int qf = query_fragments(Hkv, g, B, max_new);
   const long rows = (long)g * max_new, units = ((rows + 16 * qf - 1) / (16 * qf)) * Hkv * B;
   if (units < 1) return 64;
+  if (qf == 1 && capacity <= 768) return (capacity + 63) / 64 * 64;
   const long tile = rows < 16 * qf ? rows : 16 * qf, cheap = 64 * tile / (e4m3 ? 1 : 2);
   long span = ((long)capacity * units + 2047) / 2048;
   if (span < cheap && units * ((capacity + span - 1) / span) > 256) span = cheap;

@@ -19,8 +19,8 @@
 // 512 rows of 152064 bfloat16 logits, each row with its own settings: 170 us. The first kernel (52) is bound by memory: 156 MB,
 // and the rows with a top-k once more, mostly from the last cache; the second (124) by the additions to the histogram in
 // LDS (35 us of a row's 57 without a filter, one row a CU) and its passes one behind the other. 4 rows of 126464 float32, top-k 50
-// and top-p 0.95: 25 us, three kernels of 6, 9 and 11 us: chains of dependent loads, barriers and instruction fetches. Without
-// sharing they took 35, rows without a filter 85 instead of 38.
+// and top-p 0.95: 22 us, three kernels of 6 to 9 us: chains of dependent loads, barriers and instruction fetches. Without
+// sharing they took 35, rows without a filter 55 instead of 38.
 #include <limits.h>
 
 #include "dcl_internal.h"
