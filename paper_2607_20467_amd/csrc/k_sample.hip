@@ -464,43 +464,76 @@ __device__ __forceinline__ Found in_list(bool by_count, u64 t, u64 above, uint32
   return {sh.sum[i], sh.sum[i] - prev, (int)before + i + 1, (int)(uint32_t)sh.list[i]};
 }
 
-// Id of the j-th of the elements equal to the value of `k`, in order of ids: a range of ids is cut into one part per wave,
-// the waves count, and the part that holds it is cut again. All threads.
+// Id of the j-th of the elements equal to v, in order of ids: the pieces are cut into one range per wave, the waves count, and
+// the range that holds it is cut again. `red`: a word a wave. All threads, of which each gets it.
 template <bool BF>
-__device__ __forceinline__ int equal_id(const Row& r, uint32_t k, u64 j, ListShared& sh) {
+__device__ __forceinline__ int equal_id(const Row& r, float v, u64 j, uint32_t* red) {
+  constexpr int ES = BF ? 2 : 4, VEC = 16 / ES, U = 4;
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  auto hit = [&](int id) {
-    const float x = logit<BF>(r, id);
-    return x > -INFINITY && order_key(x) == k;
+  const uint4* src = reinterpret_cast<const uint4*>(r.base + (size_t)r.head * ES);
+  const int pieces = (r.V - r.head) / VEC;
+  auto count = [&](const uint4& w) {
+    float x[VEC];
+    unpack<BF>(w, x);
+    int n = 0;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) n += x[e] == v;
+    return n;
   };
-  int lo = 0, len = r.V;
+  auto edge = [&](int first, int n) {  // of the n elements from `first` on, every wave alike; j counts on where it is not there
+    u64 m = __builtin_amdgcn_ballot_w64(lane < n && logit<BF>(r, lane < n ? first + lane : 0) == v);
+    for (; m && j; m &= m - 1) --j;
+    return m ? first + (int)__builtin_ctzll(m) : -1;
+  };
+  const int before = edge(0, r.head);
+  if (before >= 0) return before;
+  int lo = 0, len = pieces;
 #pragma unroll 1
   while (len > 64) {
-    const int part = (len + kWaves - 1) / kWaves, from = lo + wid * part, to = min(from + part, lo + len);
+    const int part = (len + kWaves - 1) / kWaves, to = min(lo + (wid + 1) * part, lo + len);
     int n = 0;
-    constexpr int U = 8;
 #pragma unroll 1
-    for (int i = from + lane; i < to; i += 64 * U) {
-      bool h[U];
+    for (int i = lo + wid * part + lane; i < to; i += 64 * U) {
+      uint4 w[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) h[u] = i + 64 * u < to && hit(i + 64 * u);
+      for (int u = 0; u < U; ++u) {
+        w[u] = make_uint4(~0u, ~0u, ~0u, ~0u);
+        if (i + 64 * u < to) w[u] = src[i + 64 * u];
+      }
 #pragma unroll
-      for (int u = 0; u < U; ++u) n += h[u];
+      for (int u = 0; u < U; ++u) n += count(w[u]);
     }
     for (int o = 32; o >= 1; o >>= 1) n += __shfl_xor(n, o, 64);
     __syncthreads();
-    if (lane == 0) sh.red32[wid] = (uint32_t)n;
+    if (lane == 0) red[wid] = (uint32_t)n;
     __syncthreads();
     int w = 0;
-    while (w < kWaves - 1 && j >= sh.red32[w]) j -= sh.red32[w++];
+    while (w < kWaves && j >= red[w]) j -= red[w++];
     const int end = lo + len;
-    lo += w * part;
-    len = min(part, end - lo);
-    if (len <= 0) return -1;  // fewer than j + 1 such elements: not reached
+    lo = min(lo + w * part, end);
+    len = w < kWaves ? min(part, end - lo) : 0;  // in none of them: behind the pieces
   }
-  u64 m = __builtin_amdgcn_ballot_w64(lane < len && hit(lo + lane));  // every wave alike
-  for (u64 i = 0; i < j && m; ++i) m &= m - 1;
-  return m ? lo + (int)__builtin_ctzll(m) : -1;
+  // a piece a lane, every wave alike
+  const uint4 last = lane < len ? src[lo + lane] : make_uint4(~0u, ~0u, ~0u, ~0u);
+  const int own = count(last);
+  int upto = own;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += u;
+  }
+  const u64 past = __builtin_amdgcn_ballot_w64((u64)upto > j);
+  if (!past) {
+    j -= (u64)__shfl(upto, 63, 64);
+    return edge(r.head + pieces * VEC, r.V - r.head - pieces * VEC);
+  }
+  const int at = (int)__builtin_ctzll(past);
+  float x[VEC];
+  unpack<BF>(last, x);
+  int left = (int)j - (upto - own), id = -1;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e)
+    if (x[e] == v && left-- == 0) id = r.head + (lo + lane) * VEC + e;
+  return __shfl(id, at, 64);
 }
 
 // What a row's kernels leave for the next ones (in the workspace).
@@ -542,7 +575,7 @@ __device__ __forceinline__ void infinite_row(const SampleArgs& a, int row, const
   if (how.by_p) count = min(count, (uint32_t)how.p_target(in_k) + 1);  // weight 1 each: a sum is a count
   if (how.by_m) count = min(count, top);
   const uint32_t total = min(count, top);
-  const int id = equal_id<BF>(r, order_key(INFINITY), how.u_target(total), sh);
+  const int id = equal_id<BF>(r, INFINITY, how.u_target(total), sh.red32);
   answer(a, row, id, 1.0 / (double)total, (int)count);
 }
 
@@ -711,7 +744,7 @@ __device__ __forceinline__ Found in_large_bin(const Row& r, int b, bool by_count
     if (klo == khi) {  // equal values: element j of them, by arithmetic; its id by counting in order
       const u64 w = r.mass(key_value(klo));
       const u64 j = by_count ? (uint32_t)t - before : w ? (t - above) / w : 0;
-      const int id = equal_id<BF>(r, klo, j, sh);
+      const int id = equal_id<BF>(r, key_value(klo), j, sh.red32);
       return {above + (j + 1) * w, w, (int)(before + (uint32_t)j + 1), id};
     }
     if (left <= kList) {
@@ -854,6 +887,169 @@ __global__ void __launch_bounds__(kSampleThreads, 8) sample_gather_kernel(Sample
   if (sh.dead) atomicAdd(&state->dead, sh.dead);
 }
 
+// bfloat16 rows that are not answered yet: their values are few enough for a count of each, between the maximum and 47
+// factors of 2 below it, so that no element needs an exponential or a place in a list. Thread t has values 37 t .. 37 t + 36
+// from the top (an odd number: other banks). Rows whose values reach further (their biased exponents would have to sum to more than
+// 290: magnitudes of 2^17 and more, of either sign) are left to the next kernel.
+constexpr int kPer = 37, kValues = kPer * kSampleThreads;
+struct ValueShared {
+  alignas(16) uint32_t cnt[kValues];
+  double table[kTable];
+  u64 red64[kWaves];
+  uint32_t red32[kWaves];
+  u64 m_mass, above;
+  uint32_t m_cnt, dead, before;
+  int owner;
+};
+__global__ void __launch_bounds__(kSampleThreads, 4) sample_values_kernel(SampleArgs a) {
+  __shared__ ValueShared sh;
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, row = blockIdx.x;
+  RowState* left = static_cast<RowState*>(a.ws) + row;
+  const float M = left->M;
+  if (!(M > -INFINITY)) return;  // answered
+  Row r = row_of<true>(a, row, sh.table);
+  const How how(a, row);
+  r.set(M, how.T);
+  // a value by its place: order_key has 16 bits of it
+  const uint32_t top = order_key(M) >> 16;
+  const uint32_t limit = top - (order_key(fmaxf(r.floor_of(kFar - 1), -3.4028234663852886e38f)) >> 16) + 1;
+  if (limit > (uint32_t)kValues) return;
+  auto value = [&](int i) { return key_value((top - (uint32_t)i) << 16 | ((top - (uint32_t)i) & 0x8000u ? 0u : 0xFFFFu)); };
+  fill_table(sh.table, a.shift);
+  if (tid == 0) sh.m_mass = 0, sh.m_cnt = 0, sh.dead = 0;
+  for (uint32_t i = 4 * tid; i < limit; i += 4 * kSampleThreads) *reinterpret_cast<uint4*>(sh.cnt + i) = make_uint4(0, 0, 0, 0);
+  __syncthreads();
+
+  const uint32_t lowest = top - 0x80u;  // the place of the least finite value; -inf and NaN are past it, modulo 2^16
+  uint32_t dead = 0;
+  auto add = [&](uint32_t i) {
+    if (i < limit) atomicAdd(&sh.cnt[i], 1u);
+    else dead += i > lowest;
+  };
+  {
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    const u16x2 tops = {(unsigned short)top, (unsigned short)top}, flip = {0x8000, 0x8000};
+    auto places = [&](uint32_t two) {
+      const u16x2 w = __builtin_bit_cast(u16x2, two);
+      const u16x2 sign = __builtin_bit_cast(u16x2, __builtin_bit_cast(s16x2, two) >> 15);
+      return __builtin_bit_cast(uint32_t, (u16x2)(tops - (w ^ (sign | flip))));
+    };
+    constexpr int U = 4;
+    const int tail = r.head + (r.V - r.head) / 8 * 8, edge = tid < r.head ? tid : tail + tid - r.head;
+    if (edge < r.V && tid < 16) add(places(reinterpret_cast<const bf16_t*>(r.base)[edge]) & 0xFFFFu);
+    const uint4* src = reinterpret_cast<const uint4*>(r.base + (size_t)r.head * 2);
+#pragma unroll 1
+    for (int p = tid; p < r.p1; p += kSampleThreads * U) {
+      uint4 w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) w[u] = src[min(p + u * kSampleThreads, r.p1 - 1)];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (p + u * kSampleThreads >= r.p1) break;
+        const uint32_t two[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t i = places(two[e]);
+          add(i & 0xFFFFu);
+          add(i >> 16);
+        }
+      }
+    }
+  }
+  if (dead) atomicAdd(&sh.dead, dead);
+  __syncthreads();
+  if (tid == 0 && top >= 0x8000u && top - 0x7FFFu < limit) {  // -0 is +0
+    sh.cnt[top - 0x8000u] += sh.cnt[top - 0x7FFFu];
+    sh.cnt[top - 0x7FFFu] = 0;
+  }
+  __syncthreads();
+
+  uint32_t c = 0, m_cnt = 0;
+  u64 mass = 0, m_mass = 0;
+  const int first = kPer * tid, end = min(first + kPer, (int)limit);
+#pragma unroll 1
+  for (int i0 = first; i0 < end; i0 += 8) {
+    uint32_t n[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) n[e] = i0 + e < end ? sh.cnt[i0 + e] : 0;
+#pragma unroll 1
+    for (int e = 0; e < 8; ++e) {
+      if (n[0]) {
+        const float x = value(i0 + e);
+        const u64 w = n[0] * r.mass(x);
+        c += n[0];
+        mass += w;
+        if (how.by_m && r.weight(x) >= how.m_least) m_cnt += n[0], m_mass += w;
+      }
+#pragma unroll
+      for (int z = 0; z < 7; ++z) n[z] = n[z + 1];
+    }
+  }
+  if (m_cnt) atomicAdd(&sh.m_cnt, m_cnt), atomicAdd(&sh.m_mass, m_mass);
+  // sums up to the thread's values
+  uint32_t cs = c;
+  u64 ms = mass;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t u = __shfl_up(cs, o, 64);
+    const u64 v = __shfl_up(ms, o, 64);
+    if (lane >= o) cs += u, ms += v;
+  }
+  if (lane == 63) sh.red32[wid] = cs, sh.red64[wid] = ms;
+  __syncthreads();
+  cs -= c;
+  ms -= mass;
+  uint32_t near = 0;
+  u64 total = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wid) cs += sh.red32[w], ms += sh.red64[w];
+    near += sh.red32[w];
+    total += sh.red64[w];
+  }
+  uint32_t count = (uint32_t)r.V - sh.dead;
+  u64 k_total = total;
+  Found f{};
+  u64 j = 0;  // which of the elements of the found value
+#pragma unroll 1
+  for (int q = 0; q < 3; ++q) {  // the border of top-k, that of top-p, the draw
+    if (q == 0 ? how.k <= 0 || (uint32_t)how.k >= count : q == 1 && !how.by_p) continue;
+    if (q == 0 && (uint32_t)how.k > near) {  // past every id with a weight: the sum is all there is
+      count = (uint32_t)how.k;
+      continue;
+    }
+    if (q == 2 && how.by_m && sh.m_cnt < count) count = sh.m_cnt, total = sh.m_mass;
+    const u64 t = q == 0 ? (u64)(how.k - 1) : q == 1 ? how.p_target(k_total) : how.u_target(total);
+    if (q == 0 ? cs <= t && t < cs + c : ms <= t && t < ms + mass) sh.owner = first, sh.before = cs, sh.above = ms;
+    __syncthreads();
+    // that thread's values, one a lane, every wave alike
+    const int i = sh.owner + lane;
+    const uint32_t n = lane < kPer && i < (int)limit ? sh.cnt[i] : 0;
+    const u64 w = n ? r.mass(value(i)) : 0;
+    uint32_t upto = n;
+    u64 sum = n * w;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t u = __shfl_up(upto, o, 64);
+      const u64 v = __shfl_up(sum, o, 64);
+      if (lane >= o) upto += u, sum += v;
+    }
+    upto += sh.before;
+    sum += sh.above;
+    const int at = (int)__builtin_ctzll(__builtin_amdgcn_ballot_w64(q == 0 ? upto > t : sum > t));
+    const uint32_t before = (uint32_t)__shfl((int)(upto - n), at, 64);
+    const u64 above = __shfl(sum - n * w, at, 64), weight = __shfl(w, at, 64);
+    j = q == 0 ? t - before : (t - above) / weight;
+    f = {above + (j + 1) * weight, weight, (int)(before + (uint32_t)j + 1), __shfl(i, at, 64)};
+    __syncthreads();
+    if (q == 0) count = (uint32_t)how.k, total = k_total = f.incl;
+    if (q == 1 && (uint32_t)f.count < count) count = (uint32_t)f.count, total = f.incl;
+  }
+  const int id = equal_id<true>(r, value(f.id), j, sh.red32);
+  answer(a, row, id, (double)f.weight / (double)total, (int)count);
+  if (tid == 0) left->M = __uint_as_float(0x7FC00000u);
+}
+
 // The rows that are not answered yet, one workgroup each; of shared rows the list or the histogram is there.
 template <bool BF, bool SHARED>
 __global__ void __launch_bounds__(kSampleThreads, 4) sample_full_kernel(SampleArgs a) {
@@ -969,6 +1165,7 @@ static void run_sample(const SampleArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((sample_full_kernel<BF, true>), rows, threads, 0, s, a);
   } else {
     hipLaunchKernelGGL(sample_top_kernel<BF>, rows, threads, 0, s, a);
+    if (BF) hipLaunchKernelGGL(sample_values_kernel, rows, threads, 0, s, a);
     hipLaunchKernelGGL((sample_full_kernel<BF, false>), rows, threads, 0, s, a);
   }
 }
