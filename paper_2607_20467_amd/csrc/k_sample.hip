@@ -536,10 +536,11 @@ __device__ __forceinline__ int equal_id(const Row& r, float v, u64 j, uint32_t* 
   return __shfl(id, at, 64);
 }
 
-// What a row's kernels leave for the next ones (in the workspace).
+// What a row's kernels leave for the next ones, in the workspace: of rows that are not shared their maximum, NaN where the row
+// is answered, for the next kernel (n floats) and the one after it (n more); of shared rows all this.
 struct RowState {
-  float M;             // the row's maximum, NaN where the row is answered
-  uint32_t n_list;     // split rows: elements that reach top-k's bound, collected if they fit; ~0: no bound was set
+  float M;             // as above
+  uint32_t n_list;     // elements that reach top-k's bound, collected if they fit; ~0: no bound was set
   uint32_t m_cnt;      // elements that min-p keeps
   uint32_t dead;       // elements that are -inf or NaN
   u64 m_mass;          // the sum of those that min-p keeps
@@ -554,6 +555,22 @@ struct SplitRow {
   u64 mass[kBins];
   uint32_t cnt[kBins];
 };
+
+// The open rows of 1024 go to the first of their 1024 workgroups, so that they spread over the XCDs and CUs whichever rows
+// they are (512 rows, 213 of them open: 74 us with a row to its own workgroup, 51 so). The row of this one, or -1. All threads.
+__device__ __forceinline__ int open_row(const float* M, int n, uint32_t* red, int* found) {
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, i = (int)(blockIdx.x & ~(kSampleThreads - 1u)) + (int)threadIdx.x;
+  const bool open = i < n && M[i] > -INFINITY;
+  const u64 b = __builtin_amdgcn_ballot_w64(open);
+  if (lane == 0) red[wid] = (uint32_t)__builtin_popcountll(b);
+  if (threadIdx.x == 0) *found = -1;
+  __syncthreads();
+  uint32_t before = (uint32_t)__builtin_popcountll(b & ((1ull << lane) - 1));
+  for (int w = 0; w < wid; ++w) before += red[w];
+  if (open && before == (blockIdx.x & (kSampleThreads - 1u))) *found = i;
+  __syncthreads();
+  return *found;
+}
 
 // Rows whose logits are +inf somewhere: those ids share the weight alike, all others have none.
 template <bool BF>
@@ -645,7 +662,7 @@ __global__ void __launch_bounds__(kSampleThreads, 8) sample_top_kernel(SampleArg
   __shared__ float red_least[kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, row = blockIdx.x;
   Row r = row_of<BF>(a, row, sh.table);
-  RowState* left = static_cast<RowState*>(a.ws) + row;
+  float* left = static_cast<float*>(a.ws) + row;
   float best;
   int best_id;
   thread_max<BF>(r, best, best_id);
@@ -663,7 +680,7 @@ __global__ void __launch_bounds__(kSampleThreads, 8) sample_top_kernel(SampleArg
   __syncthreads();
   for (int w = 0; w < kWaves; ++w) lower_id(sh.red_x[w], red_id[w], best, best_id), least = fminf(least, red_least[w]);
   const How how(a, row);
-  if (tid == 0) left->M = __uint_as_float(0x7FC00000u);
+  if (tid == 0) left[0] = left[a.n] = __uint_as_float(0x7FC00000u);
   if (best == -INFINITY) return answer(a, row, -1, 0.0, 0);  // nothing but -inf and NaN
   if (!(how.T > 0.f) || how.k == 1) return answer(a, row, best_id, 1.0, 1);
   if (best == INFINITY) return infinite_row<BF>(a, row, r, how, sh);
@@ -671,7 +688,7 @@ __global__ void __launch_bounds__(kSampleThreads, 8) sample_top_kernel(SampleArg
   float lo;
   if (takes_bound(how) && bound_of(r, how.k, own, least, cnt, sh, lo) && collect<BF>(r, lo, INFINITY, sh, [](float) { return 0; }))
     return answer_from_list(a, row, r, how, sh);
-  if (tid == 0) left->M = best;
+  if (tid == 0) left[0] = left[a.n] = best;
 }
 
 // Rows that `parts` workgroups share (few rows: one CU reads 30 GB/s, a row of 126464 float32 in 16 us). First the parts'
@@ -903,10 +920,11 @@ struct ValueShared {
 };
 __global__ void __launch_bounds__(kSampleThreads, 4) sample_values_kernel(SampleArgs a) {
   __shared__ ValueShared sh;
-  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, row = blockIdx.x;
-  RowState* left = static_cast<RowState*>(a.ws) + row;
-  const float M = left->M;
-  if (!(M > -INFINITY)) return;  // answered
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  float* left = static_cast<float*>(a.ws);
+  const int row = open_row(left, a.n, sh.red32, &sh.owner);
+  if (row < 0) return;
+  const float M = left[row];
   Row r = row_of<true>(a, row, sh.table);
   const How how(a, row);
   r.set(M, how.T);
@@ -1047,15 +1065,20 @@ __global__ void __launch_bounds__(kSampleThreads, 4) sample_values_kernel(Sample
   }
   const int id = equal_id<true>(r, value(f.id), j, sh.red32);
   answer(a, row, id, (double)f.weight / (double)total, (int)count);
-  if (tid == 0) left->M = __uint_as_float(0x7FC00000u);
+  if (tid == 0) left[a.n + row] = __uint_as_float(0x7FC00000u);
 }
 
 // The rows that are not answered yet, one workgroup each; of shared rows the list or the histogram is there.
 template <bool BF, bool SHARED>
 __global__ void __launch_bounds__(kSampleThreads, 4) sample_full_kernel(SampleArgs a) {
   __shared__ FullShared sh;
-  const int tid = threadIdx.x, row = blockIdx.x;
-  const RowState state = static_cast<const RowState*>(a.ws)[row];
+  const int tid = threadIdx.x;
+  const float* left = static_cast<const float*>(a.ws) + a.n;
+  const int row = SHARED ? (int)blockIdx.x : open_row(left, a.n, sh.red32, &sh.found);
+  if (row < 0) return;
+  RowState state{};
+  if (SHARED) state = static_cast<const RowState*>(a.ws)[row];
+  else state.M = left[row];
   if (!(state.M > -INFINITY)) return;  // answered
   Row r = row_of<BF>(a, row, sh.table);
   const How how(a, row);
