@@ -11,14 +11,15 @@
 // depend on timing, and a border falls as exact arithmetic on the weights has it (a float32 sum's error of 1e-7 would move
 // one border in a hundred rows of a flat distribution over 10^5 ids).
 //
-// Two kernels, a workgroup per row. The first finds the row's maximum and answers rows that need no more (the top-1 alone)
-// or little more (top-k with the ids down to its border in LDS: nothing else of the row needs a weight), the second answers
-// the others from the histogram. Few rows are shared by several workgroups, in three kernels: maxima, then the parts'
-// elements or histograms, then one workgroup a row for the answer.
+// A workgroup per row: one kernel finds the row's maximum and answers rows that need no more (the top-1 alone) or little
+// more (top-k with the ids down to its border in LDS: nothing else of the row needs a weight), one answers bfloat16 rows by a
+// count of each value, and one the others from the histogram. Few rows are shared by several workgroups, in three kernels:
+// maxima, then the parts' elements or histograms, then one workgroup a row for the answer.
 //
-// 512 rows of 152064 bfloat16 logits, each row with its own settings: 170 us. The first kernel (52) is bound by memory: 156 MB,
-// and the rows with a top-k once more, mostly from the last cache; the second (124) by the additions to the histogram in
-// LDS (35 us of a row's 57 without a filter, one row a CU) and its passes one behind the other. 4 rows of 126464 float32, top-k 50
+// 512 rows of 152064 bfloat16 logits, each row with its own settings: 100 us. The first kernel (52) is bound by memory: 156 MB,
+// and the rows with a top-k once more, mostly from the last cache; the second (45) by two passes over a row by one CU. The
+// same in float32 without a filter: 200 us, 57 of a row's time in the last kernel, 35 of them additions to the histogram in
+// LDS (with the arithmetic of four elements interleaved 32, and low temperatures slower). 4 rows of 126464 float32, top-k 50
 // and top-p 0.95: 22 us, three kernels of 6 to 9 us: chains of dependent loads, barriers and instruction fetches. Without
 // sharing they took 35, rows without a filter 55 instead of 38.
 #include <limits.h>
@@ -557,7 +558,7 @@ struct SplitRow {
 };
 
 // The open rows of 1024 go to the first of their 1024 workgroups, so that they spread over the XCDs and CUs whichever rows
-// they are (512 rows, 213 of them open: 74 us with a row to its own workgroup, 51 so). The row of this one, or -1. All threads.
+// they are (512 rows, 213 of them open: 74 us with a row to its own workgroup, 45 so). The row of this one, or -1. All threads.
 __device__ __forceinline__ int open_row(const float* M, int n, uint32_t* red, int* found) {
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, i = (int)(blockIdx.x & ~(kSampleThreads - 1u)) + (int)threadIdx.x;
   const bool open = i < n && M[i] > -INFINITY;
@@ -905,13 +906,17 @@ __global__ void __launch_bounds__(kSampleThreads, 8) sample_gather_kernel(Sample
 }
 
 // bfloat16 rows that are not answered yet: their values are few enough for a count of each, between the maximum and 47
-// factors of 2 below it, so that no element needs an exponential or a place in a list. Thread t has values 37 t .. 37 t + 36
-// from the top (an odd number: other banks). Rows whose values reach further (their biased exponents would have to sum to more than
-// 290: magnitudes of 2^17 and more, of either sign) are left to the next kernel.
-constexpr int kPer = 37, kValues = kPer * kSampleThreads;
+// factors of 2 below it, so that no element needs an exponential or a place in a list: 42 us a row of 152064 (one row a CU), of
+// which the two passes over it take 12 and 13, near a CU's share of the memory's rate. Slabs of 64 values go round the waves. Rows
+// whose values reach further (the biased exponents of the first and the last would have to sum to more than 290: magnitudes
+// of 2^18 and more, of either sign) are left to the next kernel.
+constexpr int kSlabs = 592, kValues = 64 * kSlabs;
+static_assert(kSlabs % kWaves == 0 && kSlabs <= kSampleThreads, "a slab a thread in the sums");
 struct ValueShared {
   alignas(16) uint32_t cnt[kValues];
   double table[kTable];
+  u64 slab_mass[kSlabs];
+  uint32_t slab_cnt[kSlabs];
   u64 red64[kWaves];
   uint32_t red32[kWaves];
   u64 m_mass, above;
@@ -935,6 +940,7 @@ __global__ void __launch_bounds__(kSampleThreads, 4) sample_values_kernel(Sample
   auto value = [&](int i) { return key_value((top - (uint32_t)i) << 16 | ((top - (uint32_t)i) & 0x8000u ? 0u : 0xFFFFu)); };
   fill_table(sh.table, a.shift);
   if (tid == 0) sh.m_mass = 0, sh.m_cnt = 0, sh.dead = 0;
+  if (tid < kSlabs) sh.slab_cnt[tid] = 0, sh.slab_mass[tid] = 0;
   for (uint32_t i = 4 * tid; i < limit; i += 4 * kSampleThreads) *reinterpret_cast<uint4*>(sh.cnt + i) = make_uint4(0, 0, 0, 0);
   __syncthreads();
 
@@ -983,29 +989,37 @@ __global__ void __launch_bounds__(kSampleThreads, 4) sample_values_kernel(Sample
   }
   __syncthreads();
 
-  uint32_t c = 0, m_cnt = 0;
-  u64 mass = 0, m_mass = 0;
-  const int first = kPer * tid, end = min(first + kPer, (int)limit);
+  uint32_t m_cnt = 0;
+  u64 m_mass = 0;
+  constexpr int G = 8;  // slabs looked at together: most are empty
 #pragma unroll 1
-  for (int i0 = first; i0 < end; i0 += 8) {
-    uint32_t n[8];
+  for (int s0 = wid; s0 < kSlabs; s0 += G * kWaves) {
+    uint32_t n[G], all = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) n[e] = i0 + e < end ? sh.cnt[i0 + e] : 0;
+    for (int e = 0; e < G; ++e) {
+      const int i = 64 * (s0 + e * kWaves) + lane;
+      n[e] = i < (int)limit ? sh.cnt[i] : 0;
+      all |= n[e];
+    }
+    if (!__any(all != 0)) continue;
 #pragma unroll 1
-    for (int e = 0; e < 8; ++e) {
-      if (n[0]) {
-        const float x = value(i0 + e);
-        const u64 w = n[0] * r.mass(x);
-        c += n[0];
-        mass += w;
-        if (how.by_m && r.weight(x) >= how.m_least) m_cnt += n[0], m_mass += w;
-      }
+    for (int slab = s0; slab < kSlabs && slab < s0 + G * kWaves; slab += kWaves) {
+      const uint32_t c = n[0];
 #pragma unroll
-      for (int z = 0; z < 7; ++z) n[z] = n[z + 1];
+      for (int e = 0; e + 1 < G; ++e) n[e] = n[e + 1];
+      if (c == 0) continue;
+      const float x = value(64 * slab + lane);
+      const u64 mass = c * r.mass(x);
+      if (how.by_m && r.weight(x) >= how.m_least) m_cnt += c, m_mass += mass;
+      atomicAdd(&sh.slab_cnt[slab], c);
+      atomicAdd(&sh.slab_mass[slab], mass);
     }
   }
   if (m_cnt) atomicAdd(&sh.m_cnt, m_cnt), atomicAdd(&sh.m_mass, m_mass);
-  // sums up to the thread's values
+  __syncthreads();
+  const uint32_t c = tid < kSlabs ? sh.slab_cnt[tid] : 0;
+  const u64 mass = tid < kSlabs ? sh.slab_mass[tid] : 0;
+  // sums up to the thread's slab
   uint32_t cs = c;
   u64 ms = mass;
 #pragma unroll
@@ -1038,11 +1052,11 @@ __global__ void __launch_bounds__(kSampleThreads, 4) sample_values_kernel(Sample
     }
     if (q == 2 && how.by_m && sh.m_cnt < count) count = sh.m_cnt, total = sh.m_mass;
     const u64 t = q == 0 ? (u64)(how.k - 1) : q == 1 ? how.p_target(k_total) : how.u_target(total);
-    if (q == 0 ? cs <= t && t < cs + c : ms <= t && t < ms + mass) sh.owner = first, sh.before = cs, sh.above = ms;
+    if (q == 0 ? cs <= t && t < cs + c : ms <= t && t < ms + mass) sh.owner = 64 * tid, sh.before = cs, sh.above = ms;
     __syncthreads();
-    // that thread's values, one a lane, every wave alike
+    // that slab's values, one a lane, every wave alike
     const int i = sh.owner + lane;
-    const uint32_t n = lane < kPer && i < (int)limit ? sh.cnt[i] : 0;
+    const uint32_t n = i < (int)limit ? sh.cnt[i] : 0;
     const u64 w = n ? r.mass(value(i)) : 0;
     uint32_t upto = n;
     u64 sum = n * w;

@@ -172,6 +172,30 @@ def test_settings_at_and_past_their_ends(dcl):
         check(x, got, u, **ref)
 
 
+def test_bfloat16_values_of_every_size(dcl):
+    """Magnitudes from the least to the largest in one row, both zeros, few and many counts of a value; temperatures under
+    which little or all of the type's range counts."""
+    V, n = 6001, 6
+    g = torch.Generator().manual_seed(77)
+    x = torch.zeros(n, V)
+    x[0] = torch.randn(V, generator=g) * 2.0 ** torch.randint(-130, 127, (V,), generator=g)
+    x[1] = torch.randint(-2, 3, (V,), generator=g).float() * 0.5
+    x[1][x[1] == 0] = -0.0
+    x[1][::3] = 0.0
+    x[2] = torch.randn(V, generator=g) * 1e30
+    x[3, ::2] = -0.0
+    x[4] = -torch.rand(V, generator=g) * 2.0 ** -120
+    x[5] = torch.randn(V, generator=g) * 1e5
+    x[5, 4000:] = -math.inf
+    x = x.to(torch.bfloat16)
+    assert bool(torch.isfinite(x[:5]).all())
+    x = x.cuda()
+    for T in (0.01, 1.0, 1e4, 1e30, 3e38):
+        for how in ({}, {"top_p": 0.7}, {"top_k": 700}, {"top_k": 5000, "top_p": 0.9}, {"min_p": 0.6}):
+            u = torch.rand(n, generator=g).numpy()
+            check(x, draw(dcl, x, u, temperature=T, **how), u, temperature=T, **how)
+
+
 def test_rows_apart_and_not_aligned(dcl):
     for dt in (torch.float32, torch.bfloat16):
         for V, extra, first in ((1001, 3, 1), (64, 7, 3), (4097, 1, 2)):
