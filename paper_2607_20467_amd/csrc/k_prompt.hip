@@ -67,16 +67,6 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
   const int wkeys = qw >= n ? 0 : a.causal ? min(n, qw + 32) : n;
   const int tiles = (nkeys + KT - 1) / KT;
 
-  bf16x8_t qf[DH / 16];
-  {
-    const bf16_t* qp = a.q + (size_t)(r.first + min(query, n - 1)) * a.q_stride + (size_t)h * DH + 8 * hi;
-#pragma unroll
-    for (int ks = 0; ks < DH / 16; ++ks) {
-      uint4 x = *reinterpret_cast<const uint4*>(qp + 16 * ks);
-      x.x ^= a.q_sign, x.y ^= a.q_sign, x.z ^= a.q_sign, x.w ^= a.q_sign;  // a negative scale is a sign of the query
-      qf[ks] = __builtin_bit_cast(bf16x8_t, x);
-    }
-  }
   const bf16_t* kbase = a.k + (size_t)r.first * a.k_stride + (size_t)g * DH;
   const bf16_t* vbase = a.v + (size_t)r.first * a.v_stride + (size_t)g * DH;
 
@@ -114,6 +104,17 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
       }
     }
   };
+  issue(0, 0);  // first of all: the queries arrive beside it
+  bf16x8_t qf[DH / 16];
+  {
+    const bf16_t* qp = a.q + (size_t)(r.first + min(query, n - 1)) * a.q_stride + (size_t)h * DH + 8 * hi;
+#pragma unroll
+    for (int ks = 0; ks < DH / 16; ++ks) {
+      uint4 x = *reinterpret_cast<const uint4*>(qp + 16 * ks);
+      x.x ^= a.q_sign, x.y ^= a.q_sign, x.z ^= a.q_sign, x.w ^= a.q_sign;  // a negative scale is a sign of the query
+      qf[ks] = __builtin_bit_cast(bf16x8_t, x);
+    }
+  }
   // where the lane's fragments lie in a stage (see the reads below)
   const int key_at = lq * KC * 16 + ((hi ^ key_swizzle(lq)) * 16);
   int value_at[DH / 32];
@@ -247,7 +248,6 @@ __global__ void __launch_bounds__(256, 2) prompt_attn_kernel(PromptAttn a) {
       }
     }
   };
-  issue(0, 0);
   const int open = (a.causal ? min(n, q0 + 1) : n) / KT;  // tiles that every query of the workgroup sees whole
   int t = 0;
   for (; t + 1 < open; t += 2) {
