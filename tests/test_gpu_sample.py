@@ -321,3 +321,40 @@ def test_more_rows_than_a_launch_has(dcl):
     want = torch.where(u > 0.5, 1 - best, best)                   # the less likely id has a quarter or a half
     want[n - 1] = best[n - 1]
     assert torch.equal(token, want) and int(kept[n - 1]) == 1 and bool((kept[:n - 1] == 2).all())
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_more_rows_than_a_window_of_workgroups_and_replays(dcl, bf16):
+    """1500 rows, open and answered ones mixed; then the same call captured and replayed with other numbers."""
+    n, V = 1500, 300
+    x, g = logits(n, V, 41)
+    x[::7] = -math.inf
+    x = (x.to(torch.bfloat16) if bf16 else x).cuda()
+    r = np.random.default_rng(5)
+    how = dict(temperature=r.choice([0.0, 0.7, 1.0], n), top_k=r.choice([0, 0, 1, 5], n), top_p=r.choice([1.0, 0.9], n))
+    u = torch.rand(n, generator=g)
+    check(x, draw(dcl, x, u.numpy(), **how), u.numpy(), **how)
+
+    T, k, p = (torch.tensor(how[name], dtype=dt).cuda() for name, dt in
+               (("temperature", torch.float32), ("top_k", torch.int32), ("top_p", torch.float32)))
+    ud = u.cuda()
+    token, kept = (torch.empty(n, dtype=torch.int32, device="cuda") for _ in range(2))
+    conf = torch.empty(n, device="cuda")
+    need = dcl.dcl_sample_workspace_bytes(n, V)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+
+    def go():
+        dcl.dcl_sample_tokens(x, n, V, T, k, p, None, ud, token, conf, kept, ws, need)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        go()
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        u = torch.rand(n, generator=g)
+        ud.copy_(u)
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = draw(dcl, x, u.numpy(), **how)
+        assert all(np.array_equal(a.cpu().numpy(), b) for a, b in zip((token, conf, kept), want))
