@@ -14,7 +14,8 @@
 // A workgroup per row: one kernel finds the row's maximum and answers rows that need no more (the top-1 alone) or little
 // more (top-k with the ids down to its border in LDS: nothing else of the row needs a weight), one answers bfloat16 rows by a
 // count of each value, and one the others from the histogram. Few rows are shared by several workgroups, in three kernels:
-// maxima, then the parts' elements or histograms, then one workgroup a row for the answer.
+// maxima, then the parts' elements or histograms, then one workgroup a row for the answer. Rows of up to 2048 ids are lists as
+// a whole, in one kernel.
 //
 // 512 rows of 152064 bfloat16 logits, each row with its own settings: 100 us. The first kernel (52) is bound by memory: 156 MB,
 // and the rows with a top-k once more, mostly from the last cache; the second (45) by two passes over a row by one CU. The
@@ -1179,6 +1180,158 @@ __global__ void __launch_bounds__(kSampleThreads, 4) sample_full_kernel(SampleAr
   answer(a, row, f.id, (double)f.weight / (double)total, (int)count);
 }
 
+// Rows of up to CAP ids: all of them are the list, in one kernel, several rows a CU. 1500 rows of 1000 float32 logits without a
+// filter: 95 us by the kernels above, whose passes and barriers wait for each other, 17 so; 1500 rows of 2000: 99 and 31 (37 with
+// 256 threads); 1000 rows of 4000, with a top-k of 50: 78 and 71, 39 and 71, so that longer rows are left to those.
+template <int CAP, int NT>
+struct SmallShared {
+  double table[kTable];
+  u64 list[CAP], sum[CAP];
+  uint32_t start[CAP + 1];
+  u64 red64[NT / 64];
+  uint32_t red32[NT / 64], red_hi[NT / 64];
+  float red_x[NT / 64];
+  int red_id[NT / 64];
+  int found, kept;
+};
+template <bool BF, int CAP, int NT>
+__global__ void __launch_bounds__(NT) sample_small_kernel(SampleArgs a) {
+  constexpr int WAVES = NT / 64, E = CAP / NT;
+  __shared__ SmallShared<CAP, NT> sh;
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, row = blockIdx.x;
+  Row r = row_of<BF>(a, row, sh.table);
+  const How how(a, row);
+  float x[E], best = -INFINITY;
+  int best_id = INT_MAX;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int id = e * NT + tid;
+    x[e] = id < r.V ? logit<BF>(r, id) : -INFINITY;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (x[e] > best) best = x[e], best_id = e * NT + tid;
+  uint32_t lo = 0xFFFFFFFFu, hi = 0;  // of the complements of the keys, smallest first
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (x[e] > -INFINITY) lo = min(lo, ~order_key(x[e])), hi = max(hi, ~order_key(x[e]));
+  for (int o = 32; o >= 1; o >>= 1) {
+    const float y = __shfl_xor(best, o, 64);
+    const int id = __shfl_xor(best_id, o, 64);
+    lower_id(y, id, best, best_id);
+    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
+    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
+  }
+  if (lane == 0) sh.red_x[wid] = best, sh.red_id[wid] = best_id, sh.red32[wid] = lo, sh.red_hi[wid] = hi;
+  fill_table(sh.table, a.shift);
+  for (int i = tid; i <= CAP; i += NT) sh.start[i] = 0;
+  if (tid == 0) sh.kept = 0;
+  __syncthreads();
+  for (int w = 0; w < WAVES; ++w) {
+    lower_id(sh.red_x[w], sh.red_id[w], best, best_id);
+    lo = min(lo, sh.red32[w]);
+    hi = max(hi, sh.red_hi[w]);
+  }
+  if (best == -INFINITY) return answer(a, row, -1, 0.0, 0);
+  if (!(how.T > 0.f) || how.k == 1) return answer(a, row, best_id, 1.0, 1);
+  const bool infinite = best == INFINITY;  // those ids share the weight alike, all others have none
+  r.set(infinite ? 0.f : best, how.T);
+
+  // in order, as order_list has it, but half of the groups lie evenly over the values: a whole row's keys are dense around 0
+  const double ids = (double)r.V, scale = (CAP / 2 - 0.25) / ((double)((hi - lo) >> r.drop) * ids + ids);
+  const float range = best - key_value(~hi);  // its quotient stays finite, and its products below CAP / 2
+  const float even = range > 0.f && range < INFINITY ? fminf((CAP / 2 - 0.25f) / range, 1e30f) : 0.f;
+  u64 v[E];
+  int at[E], slot[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    at[e] = -1;
+    if (!(x[e] > -INFINITY)) continue;
+    const uint32_t key = ~order_key(x[e]), id = (uint32_t)(e * NT + tid);
+    v[e] = (u64)key << 32 | id;
+    at[e] = (int)(fma((double)((key - lo) >> r.drop), ids, (double)id) * scale);
+    if (even > 0.f) at[e] += (int)((best - x[e]) * even);
+    slot[e] = (int)atomicAdd(&sh.start[at[e]], 1u);
+  }
+  __syncthreads();
+  uint32_t c[E], all = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) c[e] = sh.start[E * tid + e], all += c[e];
+  uint32_t cs = all;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t u = __shfl_up(cs, o, 64);
+    if (lane >= o) cs += u;
+  }
+  if (lane == 63) sh.red32[wid] = cs;
+  __syncthreads();
+  int n = 0;
+  cs -= all;
+  for (int w = 0; w < WAVES; ++w) {
+    if (w < wid) cs += sh.red32[w];
+    n += (int)sh.red32[w];
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) sh.start[E * tid + e] = cs, cs += c[e];
+  if (tid == NT - 1) sh.start[CAP] = cs;
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (at[e] >= 0) sh.sum[sh.start[at[e]] + slot[e]] = v[e];
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (at[e] < 0) continue;
+    const int from = (int)sh.start[at[e]], to = (int)sh.start[at[e] + 1];
+    int rank = from;
+    for (int i = from; i < to; ++i) rank += sh.sum[i] < v[e];
+    sh.list[rank] = v[e];
+  }
+  __syncthreads();
+  // running sums, and how many min-p keeps
+  u64 w[E], mine = 0;
+  int kept = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    w[e] = 0;
+    if (E * tid + e < n) {
+      const float y = key_value(~(uint32_t)(sh.list[E * tid + e] >> 32));
+      w[e] = infinite ? (u64)(y == INFINITY) : r.mass(y);
+      if (how.by_m) kept += infinite ? y == INFINITY : r.weight(y) >= how.m_least;
+    }
+    mine += w[e];
+  }
+  u64 ms = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const u64 u = __shfl_up(ms, o, 64);
+    if (lane >= o) ms += u;
+  }
+  if (lane == 63) sh.red64[wid] = ms;
+  if (kept) atomicAdd(&sh.kept, kept);
+  __syncthreads();
+  ms -= mine;
+  for (int i = 0; i < wid; ++i) ms += sh.red64[i];
+#pragma unroll
+  for (int e = 0; e < E; ++e) sh.sum[E * tid + e] = ms += w[e];
+  __syncthreads();
+  auto find = [&](u64 t) {  // the place at which the running sum passes t, below the last one
+#pragma unroll
+    for (int i = tid; i < CAP; i += NT)
+      if (i < n && sh.sum[i] > t && (i == 0 || sh.sum[i - 1] <= t)) sh.found = i;
+    __syncthreads();
+    const int i = sh.found;
+    __syncthreads();
+    return i;
+  };
+  int count = how.k > 0 && how.k < n ? how.k : n;
+  if (how.by_p) count = min(count, find(how.p_target(sh.sum[count - 1])) + 1);
+  if (how.by_m) count = min(count, sh.kept);
+  const u64 total = sh.sum[count - 1];
+  const int i = find(how.u_target(total));
+  answer(a, row, (int)(uint32_t)sh.list[i], (double)(sh.sum[i] - (i > 0 ? sh.sum[i - 1] : 0)) / (double)total, count);
+}
+
 // Workgroups that share a row: a power of two, together up to one a CU, and at least 4096 ids each.
 constexpr int kShares = 256, kShare = 4096;
 static int sample_parts(int n, int V) {
@@ -1196,7 +1349,11 @@ template <bool BF>
 static void run_sample(const SampleArgs& a, hipStream_t s) {
   const int parts = sample_parts(a.n, a.V);
   const dim3 rows(a.n), shares((unsigned)a.n * parts), threads(kSampleThreads);
-  if (parts > 1) {
+  if (a.V <= 1024) {
+    hipLaunchKernelGGL((sample_small_kernel<BF, 1024, 256>), rows, dim3(256), 0, s, a);
+  } else if (a.V <= 2048) {
+    hipLaunchKernelGGL((sample_small_kernel<BF, 2048, 512>), rows, dim3(512), 0, s, a);
+  } else if (parts > 1) {
     hipLaunchKernelGGL(sample_part_kernel<BF>, shares, threads, 0, s, a, parts);
     hipLaunchKernelGGL(sample_gather_kernel<BF>, shares, threads, 0, s, a, parts);
     hipLaunchKernelGGL((sample_full_kernel<BF, true>), rows, threads, 0, s, a);

@@ -70,7 +70,7 @@ SETTINGS = [
 
 
 @pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("V", [1, 2, 3, 17, 433, 4096, 40010])
+@pytest.mark.parametrize("V", [1, 2, 3, 17, 433, 1024, 1025, 2048, 2049, 4096, 40010])
 def test_matches_sorted_rows(dcl, V, bf16):
     n = 8 if V < 5000 else 4
     for i, how in enumerate(SETTINGS):
@@ -133,14 +133,14 @@ def test_many_nearly_equal_values_in_one_bin(dcl):
         check(x, draw(dcl, x, u, **how), u, **how)
 
 
-def test_masked_infinite_and_nan_logits(dcl):
-    V = 3001
+@pytest.mark.parametrize("V", [3001, 1801, 1000])
+def test_masked_infinite_and_nan_logits(dcl, V):
     x, g = logits(8, V, 9)
     x[0] = -math.inf
     x[1] = math.nan
     x[2] = -math.inf
-    x[2, 2999] = -5e30
-    x[3, [7, 1000]] = math.inf
+    x[2, V - 2] = -5e30
+    x[3, [7, V - 1]] = math.inf
     x[4] = torch.finfo(torch.float32).min
     x[4, 5:9] = 0.0
     x[5, ::2] = math.nan
@@ -150,11 +150,11 @@ def test_masked_infinite_and_nan_logits(dcl):
     for bf16 in (False, True):
         xd = (x.to(torch.bfloat16) if bf16 else x).cuda()
         u = torch.rand(8, generator=g).numpy()
-        for how in ({}, {"top_k": 4}, {"top_p": 0.6}, {"min_p": 0.1}, {"top_k": 2500}):
+        for how in ({}, {"top_k": 4}, {"top_p": 0.6}, {"min_p": 0.1}, {"top_k": V - 500}):
             got = draw(dcl, xd, u, **how)
             check(xd, got, u, **how)
             assert got[0][0] == got[0][1] == -1 and got[1][0] == 0 and got[2][1] == 0
-            assert got[0][2] == 2999 and got[0][3] in (7, 1000)
+            assert got[0][2] == V - 2 and got[0][3] in (7, V - 1)
 
 
 def test_settings_at_and_past_their_ends(dcl):
@@ -172,10 +172,11 @@ def test_settings_at_and_past_their_ends(dcl):
         check(x, got, u, **ref)
 
 
-def test_bfloat16_values_of_every_size(dcl):
+@pytest.mark.parametrize("V", [6001, 2000])
+def test_bfloat16_values_of_every_size(dcl, V):
     """Magnitudes from the least to the largest in one row, both zeros, few and many counts of a value; temperatures under
     which little or all of the type's range counts."""
-    V, n = 6001, 6
+    n = 6
     g = torch.Generator().manual_seed(77)
     x = torch.zeros(n, V)
     x[0] = torch.randn(V, generator=g) * 2.0 ** torch.randint(-130, 127, (V,), generator=g)
@@ -186,7 +187,7 @@ def test_bfloat16_values_of_every_size(dcl):
     x[3, ::2] = -0.0
     x[4] = -torch.rand(V, generator=g) * 2.0 ** -120
     x[5] = torch.randn(V, generator=g) * 1e5
-    x[5, 4000:] = -math.inf
+    x[5, V // 3 * 2:] = -math.inf
     x = x.to(torch.bfloat16)
     assert bool(torch.isfinite(x[:5]).all())
     x = x.cuda()
