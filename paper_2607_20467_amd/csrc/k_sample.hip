@@ -1332,16 +1332,18 @@ __global__ void __launch_bounds__(NT) sample_small_kernel(SampleArgs a) {
   answer(a, row, (int)(uint32_t)sh.list[i], (double)(sh.sum[i] - (i > 0 ? sh.sum[i - 1] : 0)) / (double)total, count);
 }
 
-// Workgroups that share a row: a power of two, together up to one a CU, and at least 4096 ids each.
-constexpr int kShares = 256, kShare = 4096;
+// Workgroups that share a row: a power of two, together up to one a CU, and at least 4096 ids each. Rows of fewer than 20000 ids
+// stay whole (us shared and whole, 3 rows of float32 without a filter and with a top-k of 1000: 9000 ids 23 / 27 and 20 / 23,
+// 17000 25 / 29 and 24 / 26, 31000 27 / 30 and 29 / 28, 60000 31 / 34 and, in two parts, 36 / 40).
+constexpr int kShares = 256, kShare = 4096, kSharedFrom = 20000;
 static int sample_parts(int n, int V) {
   int parts = 1;
-  while (parts < kMaxParts && (long)n * parts * 2 <= kShares && V / (parts * 2) >= kShare) parts *= 2;
+  while (V >= kSharedFrom && parts < kMaxParts && (long)n * parts * 2 <= kShares && V / (parts * 2) >= kShare) parts *= 2;
   return parts;
 }
 
 size_t sample_ws_bytes(int n, int V) {  // enough for fewer rows and ids too
-  const size_t shared = V >= 2 * kShare ? (n < kShares / 2 ? n : kShares / 2) : 0;
+  const size_t shared = V >= kSharedFrom ? (n < kShares / 2 ? n : kShares / 2) : 0;
   return (size_t)n * sizeof(RowState) + shared * sizeof(SplitRow);
 }
 

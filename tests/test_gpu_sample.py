@@ -267,7 +267,7 @@ def test_replays_and_streams(dcl):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("V", [8191, 8192, 16384 + 5, 70001])
+@pytest.mark.parametrize("V", [16384 + 5, 20000, 70001])
 def test_few_rows_are_drawn_as_many_are(dcl, V, bf16):
     """Workgroups share the rows of small calls: the same rows, special ones among them, in calls of 300 and of 1 to 90."""
     n = 300
