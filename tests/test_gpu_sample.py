@@ -157,10 +157,11 @@ def test_masked_infinite_and_nan_logits(dcl, V):
             assert got[0][2] == V - 2 and got[0][3] in (7, V - 1)
 
 
-def test_settings_at_and_past_their_ends(dcl):
-    V = 1000
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("V", [1000, 5000, 24000])
+def test_settings_at_and_past_their_ends(dcl, V, bf16):
     x, _ = logits(12, V, 10)
-    x = x.cuda()
+    x = (x.to(torch.bfloat16) if bf16 else x).cuda()
     nan, inf = math.nan, math.inf
     u = np.array([0, 0, 0.5, 1.0, 2.0, nan, -1.0, 0.9, 0.3, 0.99, 0.4, 0.6], dtype=np.float32)
     for how in ({}, {"temperature": [nan, -1, 0, inf, 1e-40, 1e30, 1e-6, 1, 5, 0.01, -inf, 2]},
@@ -199,7 +200,7 @@ def test_bfloat16_values_of_every_size(dcl, V):
 
 def test_rows_apart_and_not_aligned(dcl):
     for dt in (torch.float32, torch.bfloat16):
-        for V, extra, first in ((1001, 3, 1), (64, 7, 3), (4097, 1, 2)):
+        for V, extra, first in ((1001, 3, 1), (64, 7, 3), (4097, 1, 1), (4099, 13, 6), (20011, 5, 3)):
             wide = torch.full((5, V + extra), 99.0, dtype=dt, device="cuda")
             x, g = logits(5, V, V)
             view = wide[:, first:first + V] if first + V <= V + extra else wide[:, :V]
