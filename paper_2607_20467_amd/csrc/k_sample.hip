@@ -1121,7 +1121,9 @@ __global__ void __launch_bounds__(kSampleThreads, 4) sample_full_kernel(SampleAr
     scan_bins(sh.cnt, sh.red32);
   }
 
-  bool sums = false, whole = false;  // the bins' sums are there; the list holds all that top-k keeps
+  // The bins' sums are there; the list holds all that top-k keeps (while it is asked for: all that it has to); a list of
+  // several bins is worth asking for.
+  bool sums = false, whole = false, several = true;
   int list_lo = 1, list_hi = 0;      // bins that the list holds
   uint32_t list_before = 0;          // elements above them
   uint32_t count = 0;
@@ -1134,7 +1136,7 @@ __global__ void __launch_bounds__(kSampleThreads, 4) sample_full_kernel(SampleAr
     if (q == 0) {
       if (how.k <= 0 || (uint32_t)how.k >= sh.cnt[kBins]) continue;
       b = bin_of(sh.cnt, (uint32_t)(how.k - 1), sh);
-      whole = b < kFar && sh.cnt[b + 2] <= kList;  // fits with all that `collect` looks at
+      whole = several && b < kFar && sh.cnt[b + 2] <= kList;  // all that `collect` looks at should fit
     }
     if (!whole && !sums) {
       if (!summed) sum_bins<BF>(r, how, sh);
@@ -1163,12 +1165,19 @@ __global__ void __launch_bounds__(kSampleThreads, 4) sample_full_kernel(SampleAr
     if (q > 0 && !whole) b = bin_of(sh.mass, t, sh);
     if (q == 0 || (!whole && (b < list_lo || b > list_hi))) {
       list_hi = b;
-      for (list_lo = sh.cnt[b + 2] <= kList ? 0 : b;; list_lo = b) {
+      for (list_lo = several && sh.cnt[b + 2] <= kList ? 0 : b;; list_lo = b) {
         fresh = collect_bins<BF>(r, list_lo, b, sh);
-        if (fresh || list_lo == b) break;
+        if (fresh || whole || list_lo == b) break;
       }
       list_before = sh.above;
       if (!fresh) list_lo = 1, list_hi = 0;
+      // Where the next float below a logit lies more than a bin away (low temperatures, logits far from 0), more elements than
+      // the bins up to b + 1 have can reach floor_of(b). Then the sums are needed: once more, without that list.
+      if (whole && !fresh) {
+        whole = several = false;
+        q = -1;
+        continue;
+      }
     }
     const u64 above = sums && list_lo <= list_hi ? sh.mass[list_lo] : 0;
     if (fresh) order_list(r, above, sh);

@@ -360,3 +360,49 @@ def test_more_rows_than_a_window_of_workgroups_and_replays(dcl, bf16):
         torch.cuda.synchronize()
         want = draw(dcl, x, u.numpy(), **how)
         assert all(np.array_equal(a.cpu().numpy(), b) for a, b in zip((token, conf, kept), want))
+
+
+def beside(V, groups, rest, g):
+    """Row of V float32 logits: groups of (count, value), the rest below, ids in no order."""
+    x = torch.full((V,), rest)
+    at = 0
+    for count, value in groups:
+        x[at:at + count] = value
+        at += count
+    return x[torch.randperm(V, generator=g)]
+
+
+@pytest.mark.parametrize("n", [2, 140])
+@pytest.mark.parametrize("V", [9001, 30000])
+def test_top_k_among_neighbouring_floats_far_apart_in_weight(dcl, V, n):
+    """The next float below a logit is many bins of the histogram away: what is looked at for the border's bin is more than the
+    list holds though the bins up to it are few. Few rows are shared, many are not."""
+    g = torch.Generator().manual_seed(V + n)
+    f = [12.0]
+    for _ in range(2):
+        f.append(float(np.nextafter(np.float32(f[-1]), np.float32(0))))
+    few = [(10, f[0]), (30, f[1]), (5000, f[2])]            # the border below the first ones, all others past the list
+    many = [(1500, f[0]), (200, f[1]), (400, f[2])]         # the border's bin alone fits it
+    for groups, ks in ((few, (20, 40, 600)), (many, (1501, 1600, 1700))):
+        x = torch.stack([beside(V, groups, -5.0, g) for _ in range(2)]).repeat(n // 2, 1).cuda()
+        u = torch.rand(n, generator=g).numpy()
+        for k in ks:
+            for T in (1e-6, 3e-6, 1e-5):
+                for how in ({}, {"top_p": 0.6}, {"min_p": 0.5}, {"top_p": 0.9, "min_p": 1e-3}):
+                    got = draw(dcl, x, u, temperature=T, top_k=k, **how)
+                    check(x[:4], [a[:4] for a in got], u[:4], temperature=T, top_k=k, **how)
+
+
+@pytest.mark.parametrize("V,n", [(152064, 2), (9001, 3), (152064, 130)])
+def test_top_k_of_logits_with_a_large_offset(dcl, V, n):
+    """Steps of a sixteenth (of 1 and 2) between the logits, temperature 1: a bin is a third of a step or less."""
+    g = torch.Generator().manual_seed(V)
+    x = (1e6 + 2 * torch.randn(2, V, generator=g)).repeat((n + 1) // 2, 1)[:n]
+    big = torch.stack([beside(V, [(600, 12582912.0), (600, 12582911.0), (V // 2, 12582910.0)], 12582000.0, g)] * n)
+    for x, ks in ((x, (300, 1850, 1900, 1945, 2040)), (big, (1000, 1200, 1201))):
+        x = x.cuda()
+        u = torch.rand(n, generator=g).numpy()
+        for k in ks:
+            for how in ({}, {"top_p": 0.7}, {"top_p": 0.95, "min_p": 0.02}):
+                got = draw(dcl, x, u, top_k=k, **how)
+                check(x[:3], [a[:3] for a in got], u[:3], top_k=k, **how)
