@@ -10,6 +10,7 @@ ids and positions, float32 statistics and residuals, 16-bit bfloat16 patterns), 
 least the elements the sizes imply. A failed check raises ``DclError`` (DCL_E_ARG) before the
 library is called. Plain integers are taken as raw device addresses and passed unchecked.
 """
+import contextlib
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -675,6 +676,14 @@ class Runner:
         self.ws = None
         self.ws_key = None
 
+    def _memory(self, stream):
+        """Where a call on ``stream`` allocates: in that stream's memory. A buffer that is dropped when the call returns is
+        then handed out again behind the call's kernels, not to the current stream beside them."""
+        if stream is None:
+            return contextlib.nullcontext()
+        cuda = self.torch.cuda
+        return cuda.stream(cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+
     def workspace(self, B, S, P=0):
         need = dcl_workspace_bytes(self.model, B, S, P)
         if self.ws is None or self.ws.numel() < need:
@@ -692,34 +701,38 @@ class Runner:
 
     def step(self, tokens, p, gen_end, stats=None, kv=None, flags=0, stream=None):
         B, S = tokens.shape
-        ws, n = self.workspace(B, S, 0 if kv is None else kv[2])
-        if stats is None:
-            stats = self.new_stats(B, S)
+        with self._memory(stream):
+            ws, n = self.workspace(B, S, 0 if kv is None else kv[2])
+            if stats is None:
+                stats = self.new_stats(B, S)
         dcl_denoise_step(self.model, tokens, B, S, p, gen_end, kv, flags, stats, ws, n, stream)
         return stats
 
     def logits(self, tokens, rows, kv=None, stream=None, with_hidden=False):
         """float32 logits [n_rows, V] (and, with_hidden, bf16-bit hidden states [n_rows, d] as int16)."""
         B, S = tokens.shape
-        ws, n = self.workspace(B, S, 0 if kv is None else kv[2])
-        out = self.torch.empty((rows.numel(), self.geom.vocab), dtype=self.torch.float32, device="cuda")
-        hid = self.torch.empty((rows.numel(), self.geom.d_model), dtype=self.torch.int16, device="cuda") \
-            if with_hidden else None
+        with self._memory(stream):
+            ws, n = self.workspace(B, S, 0 if kv is None else kv[2])
+            out = self.torch.empty((rows.numel(), self.geom.vocab), dtype=self.torch.float32, device="cuda")
+            hid = self.torch.empty((rows.numel(), self.geom.d_model), dtype=self.torch.int16, device="cuda") \
+                if with_hidden else None
         dcl_debug_logits(self.model, tokens, B, S, kv, rows, rows.numel(), out, hid, ws, n, stream)
         return (out, hid) if with_hidden else out
 
     def kv_append(self, tokens, kv, stream=None):
         """Write the keys/values of tokens [B, S] at positions kv[2] + i into the cache kv (see dcl_kv_append)."""
         B, S = tokens.shape
-        ws, n = self.workspace(B, S, kv[2])
+        with self._memory(stream):
+            ws, n = self.workspace(B, S, kv[2])
         dcl_kv_append(self.model, tokens, B, S, kv, ws, n, stream)
 
     def score_hidden(self, hidden, stream=None):
         """Statistics of given bf16 hidden rows (int16 bit patterns or torch.bfloat16, [n, d])."""
         n = hidden.shape[0]
         need = dcl_score_workspace_bytes(self.model, n)
-        ws = self.torch.empty(need, dtype=self.torch.uint8, device="cuda")
-        st = self.new_stats(1, n)
+        with self._memory(stream):
+            ws = self.torch.empty(need, dtype=self.torch.uint8, device="cuda")
+            st = self.new_stats(1, n)
         dcl_score_hidden(self.model, hidden, n, st, ws, need, stream)
         return {k: v.view(n) for k, v in st.items()}
 
@@ -727,9 +740,10 @@ class Runner:
         """Tokens drawn from the head's distribution at given hidden rows: {"token", "conf", "kept"} (each [n])."""
         n, t = hidden.shape[0], self.torch
         need = dcl_sample_hidden_workspace_bytes(self.model, n)
-        ws = t.empty(need, dtype=t.uint8, device="cuda")
-        out = {"token": t.empty(n, dtype=t.int32, device="cuda"), "conf": t.empty(n, device="cuda"),
-               "kept": t.empty(n, dtype=t.int32, device="cuda")}
+        with self._memory(stream):
+            ws = t.empty(need, dtype=t.uint8, device="cuda")
+            out = {"token": t.empty(n, dtype=t.int32, device="cuda"), "conf": t.empty(n, device="cuda"),
+                   "kept": t.empty(n, dtype=t.int32, device="cuda")}
         dcl_sample_hidden(self.model, hidden, n, temperature, top_k, top_p, min_p, uniform, out["token"], out["conf"],
                           out["kept"], ws, need, stream)
         return out

@@ -184,3 +184,30 @@ def test_a_captured_iteration_of_all_of_them(dcl):
         graphs[i].replay()
         torch.cuda.synchronize()
         assert all(torch.equal(state[i][n], w) for n, w in zip(("out", "tok", "conf"), want[i]))
+
+
+def test_drawing_on_another_stream_than_the_current_one(dcl):
+    """The call's buffers belong to its stream: what the current stream allocates and fills beside it touches none of them."""
+    w = CASES["c1s"]
+    g = w.geom
+    run = runner_for(w, synth.make_weights(g))
+    n, gen = 64, torch.Generator().manual_seed(5)
+    hid = torch.randn(n, g.d_model, generator=gen).to(torch.bfloat16).cuda()
+    u = torch.rand(n, generator=gen).cuda()
+    want = run.sample_hidden(hid, u)
+    scored = run.score_hidden(hid)
+    need = dcl.dcl_sample_hidden_workspace_bytes(run.model, n)
+    busy = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                torch.mm(busy, busy)                     # the call waits behind these
+        got = run.sample_hidden(hid, u, stream=stream)
+        again = run.score_hidden(hid, stream=stream)
+        for size in (need, n * 4, n * 4, n * 4, dcl.dcl_score_workspace_bytes(run.model, n)):
+            torch.empty(size, dtype=torch.uint8, device="cuda").fill_(0xFF)
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[k], want[k]) for k in want)
+        assert all(torch.equal(again[k], scored[k]) for k in scored)
