@@ -734,7 +734,6 @@ static int query_fragments(int Hkv, int g, int B, int max_new) {
 int pages_attention_span(int Hkv, int g, int B, int max_new, int capacity, int e4m3) {
   const int qf = query_fragments(Hkv, g, B, max_new);
   const long rows = (long)g * max_new, units = ((rows + 16 * qf - 1) / (16 * qf)) * Hkv * B;
-  if (units < 1) return 64;
   if (qf == 1 && capacity <= 768) return (capacity + 63) / 64 * 64;
   const long tile = rows < 16 * qf ? rows : 16 * qf, cheap = 64 * tile / (e4m3 ? 1 : 2);
   long span = ((long)capacity * units + 2047) / 2048;
@@ -763,8 +762,7 @@ static void run_pages_attention(PagesAttn& a, hipStream_t s) {
   }
 }
 
-void launch_pages_attention(PagesAttn a, hipStream_t s) {
-  if (a.p.T == 0 || a.p.max_new == 0) return;
+void launch_pages_attention(PagesAttn a, hipStream_t s) {  // T and max_new above 0
   if (a.p.dh == 128) a.p.e4m3 ? run_pages_attention<128, true>(a, s) : run_pages_attention<128, false>(a, s);
   else a.p.e4m3 ? run_pages_attention<64, true>(a, s) : run_pages_attention<64, false>(a, s);
 }

@@ -277,3 +277,17 @@ def test_a_runner_allocates_where_its_call_runs(dcl, monkeypatch, given):
             go()
             assert made and set(made) == {where}, (called[-1], made)
             assert called[-1][1] is stream and now == ["current"]
+
+
+def test_attention_calls_without_rows_need_no_workspace(dcl):
+    """No tokens, or none that a call may take: accepted whatever the table and the batch, with the least workspace."""
+    lib = dcl.load_library()
+    for dtype, kw in ((1, {}), (2, dict(k_scale=256, v_scale=256))):
+        for hkv, heads, B, max_pages in ((2, 4, 1, 2), (4, 32, 64, 1 << 14), (1024, 1024, 1 << 16, 1 << 22)):
+            g = pool(dcl, dtype=dtype, n_kv_heads=hkv, head_dim=64, page_len=64, **kw)
+            for T, max_new in ((0, 0), (0, 1), (0, 1 << 22), (64, 0), (1 << 22, 0)):
+                assert lib.dcl_pages_attention_workspace_bytes(ctypes.byref(g), heads, B, T, max_new, max_pages) == 256
+                r, msg = call(dcl, "dcl_pages_attention", g,
+                              (256, heads * 64, heads, 0.125, 1, 256, 0, 256, 256, None), B=B, T=T, max_new=max_new,
+                              max_pages=max_pages)
+                assert r == 0, (dtype, hkv, T, max_new, msg)
