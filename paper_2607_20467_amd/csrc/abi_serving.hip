@@ -116,30 +116,37 @@ dcl_status check_heads(int32_t n_heads, int32_t n_kv_heads) {
   return DCL_OK;
 }
 
+dcl_status check_attention_size(const dcl_pages* g, int32_t n_heads, int32_t B, int32_t max_new, int nsplit) {
+  const int64_t rows = (int64_t)(n_heads / g->n_kv_heads) * max_new, tiles = rows <= 16 ? 1 : (rows + 31) / 32;
+  const int64_t joined = nsplit > 16 ? n_heads : n_heads / 8 + 1;
+  if (too_many(((int64_t)nsplit * B * g->n_kv_heads + 8) * tiles) || (nsplit > 1 && too_many(joined * max_new * B)))
+    return fail(DCL_E_UNSUPPORTED, "B=%d sequences of %d new tokens x %d heads: too many for one call", B, max_new, n_heads);
+  return DCL_OK;
+}
+
 // Workspace of an attention call over pages: the parts' outputs and their (reference, sum). A call without rows has one
 // part.
 struct PartLayout {
   int nsplit, span;
   size_t ml, total;
 };
-PartLayout part_layout(const dcl_pages* g, int32_t n_heads, int32_t B, int32_t T, int32_t max_new, int32_t max_pages) {
-  PartLayout L;
+dcl_status part_layout(const dcl_pages* g, int32_t n_heads, int32_t B, int32_t T, int32_t max_new, int32_t max_pages,
+                       PartLayout* L) {
   const int capacity = max_pages * g->page_len;
-  L.span = T == 0 || max_new == 0 ? capacity : pages_attention_span(g->n_kv_heads, n_heads / g->n_kv_heads, B, max_new, capacity,
-                                                                    g->dtype == DCL_DTYPE_E4M3);
-  L.nsplit = (capacity + L.span - 1) / L.span;
-  const size_t rows = (size_t)L.nsplit * T * n_heads;
-  L.ml = L.nsplit > 1 ? rows * g->head_dim * 4 : 0;
-  L.total = L.nsplit > 1 ? L.ml + rows * 8 : 256;
-  return L;
-}
-
-dcl_status check_attention_size(const dcl_pages* g, int32_t n_heads, int32_t B, int32_t T, int32_t max_new, int nsplit) {
-  if (T == 0 || max_new == 0) return DCL_OK;  // nothing is launched
-  const int64_t rows = (int64_t)(n_heads / g->n_kv_heads) * max_new, tiles = rows <= 16 ? 1 : (rows + 31) / 32;
-  const int64_t joined = nsplit > 16 ? n_heads : n_heads / 8 + 1;
-  if (too_many(((int64_t)nsplit * B * g->n_kv_heads + 8) * tiles) || (nsplit > 1 && too_many(joined * max_new * B)))
-    return fail(DCL_E_UNSUPPORTED, "B=%d sequences of %d new tokens x %d heads: too many for one call", B, max_new, n_heads);
+  L->nsplit = 1;
+  L->span = capacity;
+  if (T > 0 && max_new > 0) {
+    // in one part first: what passes keeps the partition's products in 64 bits
+    dcl_status st = check_attention_size(g, n_heads, B, max_new, 1);
+    if (st != DCL_OK) return st;
+    L->span = pages_attention_span(g->n_kv_heads, n_heads / g->n_kv_heads, B, max_new, capacity, g->dtype == DCL_DTYPE_E4M3);
+    L->nsplit = (capacity + L->span - 1) / L->span;
+    st = check_attention_size(g, n_heads, B, max_new, L->nsplit);
+    if (st != DCL_OK) return st;
+  }
+  const size_t rows = (size_t)L->nsplit * T * n_heads;
+  L->ml = L->nsplit > 1 ? rows * g->head_dim * 4 : 0;
+  L->total = L->nsplit > 1 ? L->ml + rows * 8 : 256;
   return DCL_OK;
 }
 
@@ -220,8 +227,8 @@ size_t dcl_pages_attention_workspace_bytes(const dcl_pages* pages, int32_t n_hea
   if (check_pool(pages, max_pages) != DCL_OK || check_heads(n_heads, pages->n_kv_heads) != DCL_OK || B < 1 ||
       B > (1 << 16) || T < 0 || T > (1 << 22) || max_new < 0 || max_new > (1 << 22))
     return 0;
-  const PartLayout L = part_layout(pages, n_heads, B, T, max_new, max_pages);
-  return check_attention_size(pages, n_heads, B, T, max_new, L.nsplit) == DCL_OK ? L.total : 0;
+  PartLayout L;
+  return part_layout(pages, n_heads, B, T, max_new, max_pages, &L) == DCL_OK ? L.total : 0;
 }
 
 dcl_status dcl_pages_attention(const dcl_pages* pages, const int32_t* table, int32_t max_pages, const int32_t* len,
@@ -235,8 +242,8 @@ dcl_status dcl_pages_attention(const dcl_pages* pages, const int32_t* table, int
   if (st != DCL_OK) return st;
   if (!isfinite(scale)) return fail(DCL_E_ARG, "scale must be finite");
   if (causal != 0 && causal != 1) return fail(DCL_E_ARG, "causal must be 0 or 1");
-  const PartLayout L = part_layout(pages, n_heads, B, T, max_new, max_pages);
-  st = check_attention_size(pages, n_heads, B, T, max_new, L.nsplit);
+  PartLayout L;
+  st = part_layout(pages, n_heads, B, T, max_new, max_pages, &L);
   if (st != DCL_OK) return st;
   if (!ws) return fail(DCL_E_ARG, "workspace is NULL");
   if (misaligned(ws, 256)) return fail(DCL_E_ARG, "workspace must be 256-byte aligned");

@@ -3,6 +3,7 @@ import ctypes
 import os
 import shutil
 import subprocess
+import sys
 
 import pytest
 import torch
@@ -291,3 +292,25 @@ def test_attention_calls_without_rows_need_no_workspace(dcl):
                               (256, heads * 64, heads, 0.125, 1, 256, 0, 256, 256, None), B=B, T=T, max_new=max_new,
                               max_pages=max_pages)
                 assert r == 0, (dtype, hkv, T, max_new, msg)
+
+
+@pytest.mark.parametrize("hkv,heads,B,max_new,max_pages", [
+    (1024, 1024, 1 << 16, 1 << 16, 1 << 22),                       # units x capacity is 2^64
+    (1024, 1024, 1 << 16, 1 << 22, 1 << 22), (1, 1 << 16, 1 << 16, 1 << 22, 1 << 22), (1, 1 << 16, 1, 1 << 22, 1),
+    (1024, 1 << 16, 1 << 16, 1 << 22, 1), (512, 512, 1 << 16, 1 << 17, 1 << 22),
+])
+def test_the_largest_sizes_are_refused_not_computed_with(dcl, hkv, heads, B, max_new, max_pages):
+    """Run apart: a division by a product that wrapped to 0 ends the process."""
+    code = f"""
+import ctypes, sys
+sys.path.insert(0, {ROOT!r})
+import paper_2607_20467_amd as dcl
+lib = dcl.load_library()
+g = dcl.DclPages(256, 256, 0, 0, 4, 64, {hkv}, 64, 1)
+assert lib.dcl_pages_attention_workspace_bytes(ctypes.byref(g), {heads}, {B}, 1 << 22, {max_new}, {max_pages}) == 0
+r = lib.dcl_pages_attention(ctypes.byref(g), 256, {max_pages}, 256, 256, {B}, 1 << 22, {max_new}, 256, {heads} * 64, {heads}, 0.125,
+                            1, 256, 0, 256, (1 << 63) - 1, None)
+assert r == 2 and "too many" in dcl.dcl_last_error(), r
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, (r.returncode, r.stderr[-500:])
