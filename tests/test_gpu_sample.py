@@ -406,3 +406,48 @@ def test_top_k_of_logits_with_a_large_offset(dcl, V, n):
             for how in ({}, {"top_p": 0.7}, {"top_p": 0.95, "min_p": 0.02}):
                 got = draw(dcl, x, u, top_k=k, **how)
                 check(x[:3], [a[:3] for a in got], u[:3], top_k=k, **how)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_more_rows_than_a_window_of_the_kernels_by_rows(dcl, bf16):
+    """1500 rows too long for one list: open and answered rows mixed over two windows of 1024 workgroups, windows without an open
+    row and full of them; then captured and replayed over a workspace of other bits."""
+    n, V = 1500, 2500
+    x, g = logits(n, V, 43)
+    x[::7] = -math.inf
+    x[5::11, ::3] = math.nan
+    x = (x.to(torch.bfloat16) if bf16 else x).cuda()
+    r = np.random.default_rng(6)
+    how = dict(temperature=r.choice([0.0, 0.7, 1.0], n), top_k=r.choice([0, 0, 1, 5, 700], n), top_p=r.choice([1.0, 0.9], n))
+    u = torch.rand(n, generator=g)
+    check(x, draw(dcl, x, u.numpy(), **how), u.numpy(), **how)
+    answered = np.arange(n) < 1024
+    for rows in (answered, ~answered, answered | True):
+        some = dict(temperature=np.where(rows, 0.0, 0.9))
+        check(x, draw(dcl, x, u.numpy(), **some), u.numpy(), **some)
+    check(x, draw(dcl, x, u.numpy()), u.numpy())
+
+    T, k, p = (torch.tensor(how[name], dtype=dt).cuda() for name, dt in
+               (("temperature", torch.float32), ("top_k", torch.int32), ("top_p", torch.float32)))
+    ud = u.cuda()
+    token, kept = (torch.empty(n, dtype=torch.int32, device="cuda") for _ in range(2))
+    conf = torch.empty(n, device="cuda")
+    need = dcl.dcl_sample_workspace_bytes(n, V)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+
+    def go():
+        dcl.dcl_sample_tokens(x, n, V, T, k, p, None, ud, token, conf, kept, ws, need)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        go()
+    torch.cuda.current_stream().wait_stream(side)
+    for fill in (0xFF, 0, 0x7F):
+        u = torch.rand(n, generator=g)
+        ud.copy_(u)
+        ws.fill_(fill)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [a.cpu().numpy() for a in (token, conf, kept)]
+        check(x, got, u.numpy(), **how)
+        assert all(np.array_equal(a, b) for a, b in zip(got, draw(dcl, x, u.numpy(), **how)))
