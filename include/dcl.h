@@ -346,8 +346,11 @@ size_t dcl_sample_workspace_bytes(int32_t n, int32_t vocab);
  * sum, 0 without a token) and kept[n] (may be NULL: ids kept; those whose weight is 0 count). The top-1 alone (temperature
  * not > 0, or top_k 1): token the lowest best id, conf 1, kept 1. Sums are exact in fixed point (42 bits and more below
  * the row's largest weight), so a border falls as exact arithmetic has it and results are bitwise reproducible.
- * token and conf can stand for dcl_row_stats' top1 and conf in dcl_select_contiguous. 0 <= n <= 2^22, 1 <= vocab <=
- * 2^20; ws: device, 256-byte aligned, ws_bytes >= dcl_sample_workspace_bytes; calls that overlap in time need their own. */
+ * In dcl_select_contiguous token can stand for dcl_row_stats' top1. conf is not the conf there, the softmax's share at
+ * temperature 1 over all ids: it is the share of what is kept, which low temperatures and filters raise, up to 1 for a row of
+ * the top-1 alone, which passes any threshold below 1. Thresholds meant for the model's own confidence take the conf of
+ * dcl_denoise_step or dcl_score_hidden. 0 <= n <= 2^22, 1 <= vocab <= 2^20; ws: device, 256-byte aligned, ws_bytes >=
+ * dcl_sample_workspace_bytes; calls that overlap in time need their own. */
 dcl_status dcl_sample_tokens(const void* logits, int32_t dtype, int64_t row_stride, int32_t n, int32_t vocab,
                              const dcl_sampling* how, int32_t* token, float* conf, int32_t* kept, void* ws,
                              size_t ws_bytes, hipStream_t stream);
@@ -356,8 +359,8 @@ dcl_status dcl_sample_tokens(const void* logits, int32_t dtype, int64_t row_stri
 size_t dcl_sample_hidden_workspace_bytes(dcl_model_t model, int32_t n);
 
 /* The same on given final hidden states (bf16 [n, d_model], device, 16-byte aligned, already final-normalised, as for
- * dcl_score_hidden): the model's LM head into float32 logits in ws, then dcl_sample_tokens. n * vocab < 2^31 and
- * n * d_model < 2^31. */
+ * dcl_score_hidden): the model's LM head into float32 logits in ws, then dcl_sample_tokens. Over the whole vocabulary, as
+ * dcl_score_hidden: the [MASK] id can be drawn. n * vocab < 2^31 and n * d_model < 2^31. */
 dcl_status dcl_sample_hidden(dcl_model_t model, const void* hidden, int32_t n, const dcl_sampling* how, int32_t* token,
                              float* conf, int32_t* kept, void* ws, size_t ws_bytes, hipStream_t stream);
 

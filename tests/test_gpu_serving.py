@@ -211,3 +211,35 @@ def test_drawing_on_another_stream_than_the_current_one(dcl):
         torch.cuda.synchronize()
         assert all(torch.equal(got[k], want[k]) for k in want)
         assert all(torch.equal(again[k], scored[k]) for k in scored)
+
+
+def test_a_greedy_rows_conf_is_its_share_of_what_is_kept(dcl):
+    """conf 1 passes every threshold below 1, so that a window of greedy rows commits as a whole; with the confidences that
+    dcl_score_hidden gives for the same rows the drawn tokens commit as the step's own do."""
+    w = CASES["c1s"]
+    g = w.geom
+    run = runner_for(w, synth.make_weights(g))
+    tok_h, p_h = synth.initial_state(w)
+    B, S = tok_h.shape
+    st = run.step(to_dev(tok_h), to_dev(p_h), w.gen_end)
+    scored = (st["top1"].view(-1) >= 0).nonzero()[:, 0].to(torch.int32)
+    _, hid = run.logits(to_dev(tok_h), scored, with_hidden=True)
+    n, at = scored.numel(), scored.long()
+    u = torch.rand(n, generator=torch.Generator().manual_seed(3)).cuda()
+    drawn = run.sample_hidden(hid, u, temperature=torch.zeros(n, device="cuda"))
+    own = run.score_hidden(hid)
+    # at least half of the rows of a window lie below the threshold, some above
+    tau = float(own["conf"].median())
+
+    def select(token, conf):
+        tok, p, k = to_dev(tok_h), to_dev(p_h), torch.zeros(B, dtype=torch.int32, device="cuda")
+        s = {name: a.clone() for name, a in st.items()}
+        s["top1"].view(-1)[at], s["conf"].view(-1)[at] = token, conf
+        dcl.dcl_select_contiguous(tok, B, S, p, w.gen_end, w.window, tau, 2.0, g.mask_id, s, None, k)
+        return tok.cpu(), p.cpu(), k.cpu()
+    share, model, step = select(drawn["token"], drawn["conf"]), select(drawn["token"], own["conf"]), \
+        select(st["top1"].view(-1)[at], own["conf"])
+    assert bool((drawn["conf"] == 1).all()) and bool((drawn["kept"] == 1).all())
+    whole = torch.tensor([min(w.window, w.gen_end - int(x)) for x in p_h])
+    assert torch.equal(share[2].long(), whole)
+    assert all(torch.equal(a, b) for a, b in zip(model, step)) and bool((model[2].long() < whole).any())
