@@ -302,14 +302,17 @@ void launch_pages_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, h
 // would spill.
 //
 // 8-bit rows become bfloat16, exactly: a key with its scale (the conversion takes one; all of a lane's piece is one key),
-// a value without, since its piece is many keys; that scale multiplies the key's probability in float32. The probability
-// is then rounded to bfloat16 once, 2^-9 of itself, while the sum that divides takes it unrounded: over many keys these
-// roundings average out, far below the rounding of the output.
+// a value without, since its piece is many keys; that scale multiplies the key's probability in float32. That product goes
+// to the matrix instructions as two bfloat16, the nearest and the nearest to what it leaves, which keep it to 2^-16 of itself;
+// the sum that divides takes the probability unrounded. With the first alone (2^-8) the error against 64 bits was 1.8e-3 to
+// 2.3e-3 where the output's own rounding gives 1.6e-3 to 1.7e-3, on 90000 keys as on 90: where values of both signs cancel,
+// their roundings do no better. The second costs least where memory bounds (one / two parts: 64 x 1 token 78.1 / 78.7 us, 2 x
+// 1 long 102.6 / 102.5, 8 x 64 tokens x 32 heads 31.8 / 34.0, x 28 / 4 heads in bfloat16 32.8 / 35.2).
 //
 // With one token it is bound by HBM: two sequences of 90000 to 131072 keys, 28 / 4 heads, bfloat16, 516 MB: 102 us with the
 // join, 5.05 TB/s; 64 sequences of 200 to 8000 8-bit keys, 32 / 8 heads, 323 MB: 78 us, 4.1 TB/s, the rest being the first
 // loads and the ragged end. Four sequences of 90 to 700 keys x 32 heads take 12 us, the latency of their loads. Under
-// a block of 64 tokens (8 sequences, 1280 8-bit keys, 32 heads: 32 us, 2.9 TB/s) the vector pipes are busy half of the time with
+// a block of 64 tokens (8 sequences, 1280 8-bit keys, 32 heads: 34 us, 2.7 TB/s) the vector pipes are busy half of the time with
 // conversions and exponentials, the matrix pipes a seventh, and a wave has one tile of keys on its way at a time.
 __device__ __forceinline__ f32x4_t mfma16p(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -525,7 +528,7 @@ __global__ void __launch_bounds__(256, QF <= 2 ? 2 : 1) pages_attn_kernel(PagesA
         m[f] = mn;
       }
     }
-    bf16x8_t pf[QF][S2];
+    bf16x8_t pf[QF][S2], rest[QF][S2];  // the probabilities as bfloat16, and what that leaves
 #pragma unroll
     for (int f = 0; f < QF; ++f) {
       const float mr = -finite_ref(m[f]);
@@ -544,8 +547,13 @@ __global__ void __launch_bounds__(256, QF <= 2 ? 2 : 1) pages_attn_kernel(PagesA
 #pragma unroll
       for (int s2 = 0; s2 < S2; ++s2) {
         const f32x4_t &x = sc[f][2 * s2], &y = sc[f][2 * s2 + 1];
-        pf[f][s2] = __builtin_bit_cast(bf16x8_t, make_uint4(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(y[0], y[1]),
-                                                            f2bf2(y[2], y[3])));
+        const uint4 w = make_uint4(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(y[0], y[1]), f2bf2(y[2], y[3]));
+        auto left = [](uint32_t two, float p0, float p1) {
+          return f2bf2(p0 - __uint_as_float(two << 16), p1 - __uint_as_float(two & 0xFFFF0000u));
+        };
+        pf[f][s2] = __builtin_bit_cast(bf16x8_t, w);
+        rest[f][s2] = __builtin_bit_cast(bf16x8_t, make_uint4(left(w.x, x[0], x[1]), left(w.y, x[2], x[3]),
+                                                              left(w.z, y[0], y[1]), left(w.w, y[2], y[3])));
       }
     }
     // Values. In a tile that some row does not see whole, a probability of 0 must meet no infinity or NaN: what lies in
@@ -607,7 +615,10 @@ __global__ void __launch_bounds__(256, QF <= 2 ? 2 : 1) pages_attn_kernel(PagesA
       for (int s2 = 0; s2 < S2; ++s2) {
         const bf16x8_t vf = value_fragment(dt, s2);
 #pragma unroll
-        for (int f = 0; f < QF; ++f) o[f][dt] = mfma16p(vf, pf[f][s2], o[f][dt]);
+        for (int f = 0; f < QF; ++f) {
+          o[f][dt] = mfma16p(vf, pf[f][s2], o[f][dt]);
+          o[f][dt] = mfma16p(vf, rest[f][s2], o[f][dt]);
+        }
       }
     if (t + 4 < t1) load_values(t + 4, pv);
   }

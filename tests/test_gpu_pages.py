@@ -383,3 +383,43 @@ def test_offsets_past_32_bits(dcl):
         o, _, eo, _ = attention_rows(q[0, h].double()[None], k[:, h].double(), v[:, h].double(), 0.09,
                                      torch.ones(1, 150, dtype=torch.bool))
         assert bool(((out[0, h].double().cpu() - o[0]).abs() <= eo[0]).all())
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("dh,heads,hkv,lens,new", [
+    (64, 4, 4, [64, 900, 2000], 1), (128, 8, 2, [64, 1500], 1), (128, 4, 4, [640, 2000], 8), (64, 8, 4, [512], 16),
+    (128, 16, 4, [256] * 12, 32),
+])
+def test_probabilities_keep_sixteen_bits(dcl, e4m3, dh, heads, hkv, lens, new):
+    """Half of the keys have the probability 1/2 (1 + 0.87 * 2^-8) of a reference's, half of them 1/2, with values 1 and -1: in
+    bfloat16 the two are the same number, and rounded so they cancel. o is the difference, some 2^-10; two parts keep each
+    probability to 2^-16, the scores to 2^-20 (four roundings of sums below 2) and the sums of m terms to m * 2^-23."""
+    x = 1.25 * 2.0 ** -8                                     # a bfloat16 number, and with -1 a row of e4m3 at the scale 2^-8
+    pool = Pool(dcl, lens, 64, hkv, dh, e4m3, seed=11)
+    for t in (pool.k, pool.v):
+        t.zero_()
+
+    def put(t, at, byte, number):
+        t[at] = byte if e4m3 else number
+    if e4m3:
+        pool.ks.fill_(119)
+        pool.vs.fill_(127)
+    byte = {float(v): i for i, v in enumerate(E4M3.tolist()) if v == v}
+    slot = torch.arange(64) % 16                             # sixteen positions: a reference, a pair of each kind, ...
+    kind = torch.where(slot < 2, 0, 1 + slot % 2)            # 0 reference, 1 and 2 the halves
+    put(pool.k.movedim(3, 0), (0, slice(None), slice(None), kind > 0), byte[-256.0], -1.0)
+    put(pool.k.movedim(3, 0), (1, slice(None), slice(None), kind == 1), byte[x * 256], x)
+    put(pool.v.movedim(3, 0), (kind == 1,), byte[1.0], 1.0)
+    put(pool.v.movedim(3, 0), (kind == 2,), byte[-1.0], -1.0)
+    counts = [new] * len(lens)
+    q = torch.zeros(sum(counts), heads, dh, dtype=torch.bfloat16)
+    q[:, :, :2] = 1
+    out, lse, *_ = attend(dcl, pool, counts, heads, False, math.log(2.0), q=q)
+    for b, n in enumerate(lens):
+        k, v = pool.rows(b)
+        p = torch.exp2(k[:, 0, :2].sum(1))
+        want = float((p * v[:, 0, 0]).sum() / p.sum())
+        assert 2.0 ** -11 < want < 2.0 ** -9
+        got = out[b * new:(b + 1) * new]
+        assert float((got - want).abs().max()) <= want * 2.0 ** -8 + 2.0 ** -16 + 2.0 ** -20 + n * 2.0 ** -23, (b, want)
+        assert float((lse[b * new:(b + 1) * new] - math.log(float(p.sum()))).abs().max()) <= (n + 64) * 2.0 ** -23
