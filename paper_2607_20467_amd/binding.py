@@ -448,7 +448,7 @@ def _space(ws, where, nbytes, dev):
 
 def _packed(x, name, where, T, heads, dim, dev):
     """Address and row stride of a packed operand [>= T, heads, dim] of bfloat16, whose rows may be apart."""
-    if isinstance(x, int):
+    if x is None or isinstance(x, int):
         return x, heads * dim
     if x.dim() == 3:
         n, h, d = x.shape
@@ -594,9 +594,9 @@ def dcl_sample_tokens(logits, n: int, vocab: int, temperature, top_k, top_p, min
     """logits [n, vocab] float32 or bfloat16 (rows may be apart); temperature, top_p, min_p, uniform float32 [n], top_k
     int32 [n] (all but uniform may be None); token, kept int32 [n], conf float32 [n] (conf and kept may be None)."""
     w, dev = "dcl_sample_tokens", _device()
-    f32 = logits.dtype is _torch.float32
+    f32 = getattr(logits, "dtype", None) is _torch.float32
     bad = None
-    if not logits.is_cuda:
+    if not getattr(logits, "is_cuda", False):
         bad = "must be a device (cuda) tensor"
     elif not f32 and logits.dtype not in _dtypes[_B16]:
         bad = f"has dtype {logits.dtype}, expected float32 or bfloat16"

@@ -314,3 +314,17 @@ assert r == 2 and "too many" in dcl.dcl_last_error(), r
 """
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0, (r.returncode, r.stderr[-500:])
+
+
+def test_missing_operands_are_refused_as_every_other_argument(dcl):
+    """None goes to the library, which names what is missing; logits, whose type decides the call, have to be a tensor."""
+    ws = dict(ws=256, ws_bytes=1 << 40)
+    with pytest.raises(dcl.DclError, match="q is NULL"):
+        dcl.dcl_prompt_attention(None, 256, 256, 256, 1, 4, 4, 4, 2, 64, 0.125, True, 256, stream=0)
+    with pytest.raises(dcl.DclError, match="v is NULL"):
+        dcl.dcl_prompt_attention(256, 256, None, 256, 1, 4, 4, 4, 2, 64, 0.125, True, 256, stream=0)
+    with pytest.raises(dcl.DclError, match="out is NULL"):
+        dcl.dcl_prompt_attention(256, 256, 256, 256, 1, 4, 4, 4, 2, 64, 0.125, True, None, stream=0)
+    for logits in (None, 256, torch.zeros(2, 10)):
+        with pytest.raises(dcl.DclError, match="logits"):
+            dcl.dcl_sample_tokens(logits, 2, 10, None, None, None, None, 256, 256, None, None, **ws, stream=0)
