@@ -439,8 +439,9 @@ __global__ void __launch_bounds__(256, QF <= 2 ? 2 : 1) pages_attn_kernel(PagesA
   auto page_at = [&](int t, int grp) { return page_of(row, p.max_pages, p.n_pages, p.shift, (KT * t + PK * grp) >> 4); };
 
   // Pages of the 64 chunks of 16 keys from `base` on, one a lane, and of the 64 after those: a look-up is then an exchange
-  // between lanes. Loaded tile by tile they came back in order with the values before them, so that the next keys were
-  // asked for only when this tile's values had arrived (8 x 64 tokens x 28 / 4 heads over 1280 keys 53.6 us, so 48.8).
+  // between lanes. Loaded tile by tile they come back in order with the values before them, so that the next keys are
+  // asked for only when this tile's values have arrived (8 x 64 tokens over 1280 keys, 28 / 4 heads, bfloat16: 36.4 us, so
+  // 33.2; 32 heads, 8 bits: 41 and 37).
   int base = t0 * (KT / 16);
   int ids = page_of(row, p.max_pages, p.n_pages, p.shift, base + lane);
   int ids_next = page_of(row, p.max_pages, p.n_pages, p.shift, base + 64 + lane);
@@ -727,13 +728,15 @@ __global__ void __launch_bounds__(256) pages_join_kernel(PagesAttn a, int head_b
   if (a.lse && c == 0) a.lse[at] = lt == 0.f ? -INFINITY : mm * 0.6931471805599453f + logf(lt);
 }
 
-// Query fragments (16 rows each) per wave. Two let two workgroups share a CU, four read a KV head's cache once for 64 rows
-// and pay for it where the rows are more and the workgroups enough: us with 1 / 2 / 4, over 1280 keys, 8 x 64 tokens x
-// 32 / 32 heads (64 rows, 8 bits) 56 / 31 / 44; 28 / 4 heads, bfloat16: 8 x 64 (448 rows, 224 workgroups of 64) 88 / 57 / 49,
-// 8 x 32 (112) 51 / 37 / 33, 8 x 16 (64) 33 / 24 / 35.
-static int query_fragments(int Hkv, int g, int B, int max_new) {
+// Query fragments (16 rows each) per wave. With two, two workgroups share a CU; four read a KV head's bfloat16 cache once for
+// 64 rows, which pays where the rows are more and the workgroups of two would not all have a CU of their own. us with 1 / 2 /
+// 4 over 1280 keys, three sets of operands in turn: 28 / 4 heads, bfloat16: 8 x 64 tokens (224 workgroups of four) 76 / 43 /
+// 33, 5 x 64 (140) - / 43 / 33, 8 x 32 (128) 49 / 25 / 32, 8 x 16 (64) 29 / 25 / 32. 8-bit rows are bound by their conversions,
+// for which one workgroup a CU is too few: 8 x 64 tokens x 32 / 32 heads 44 / 37 / 49, 28 / 4 heads - / 32 / 45, over 6000 keys
+// - / 127 / 158.
+static int query_fragments(int Hkv, int g, int B, int max_new, int e4m3) {
   const long rows = (long)g * max_new;
-  return rows <= 16 ? 1 : rows <= 64 || (rows + 63) / 64 * Hkv * B < 96 ? 2 : 4;
+  return rows <= 16 ? 1 : e4m3 || rows <= 64 || (rows + 63) / 64 * Hkv * B <= 128 ? 2 : 4;
 }
 
 // Keys of a part: about 2048 workgroups if every sequence filled its row of the table (fewer leave CUs idle and the longest
@@ -743,7 +746,7 @@ static int query_fragments(int Hkv, int g, int B, int max_new) {
 // fragment stay whole: a join costs more than three parts save (4 x 1 token, 32 heads, 500 / 700 bfloat16 keys: 14.4 / 15.9 us in
 // parts of 256, 12.3 / 14.2 whole; 32 / 8 heads, 8 bits: 12.7 / 12.8 and 12.0 / 12.3).
 int pages_attention_span(int Hkv, int g, int B, int max_new, int capacity, int e4m3) {
-  const int qf = query_fragments(Hkv, g, B, max_new);
+  const int qf = query_fragments(Hkv, g, B, max_new, e4m3);
   const long rows = (long)g * max_new, units = ((rows + 16 * qf - 1) / (16 * qf)) * Hkv * B;
   if (qf == 1 && capacity <= 768) return (capacity + 63) / 64 * 64;
   const long tile = rows < 16 * qf ? rows : 16 * qf, cheap = 64 * tile / (e4m3 ? 1 : 2);
@@ -757,13 +760,13 @@ int pages_attention_span(int Hkv, int g, int B, int max_new, int capacity, int e
 
 template <int DH, bool E4>
 static void run_pages_attention(PagesAttn& a, hipStream_t s) {
-  const int qf = query_fragments(a.p.Hkv, a.g, a.p.B, a.p.max_new);
+  const int qf = query_fragments(a.p.Hkv, a.g, a.p.B, a.p.max_new, E4);
   a.row_tiles = (int)(((long)a.g * a.p.max_new + 16 * qf - 1) / (16 * qf));
   const long items = (long)a.nsplit * a.p.B * a.p.Hkv;
   const dim3 grid((unsigned)((items + 7) / 8 * 8 * a.row_tiles));
   if (qf == 1) hipLaunchKernelGGL((pages_attn_kernel<DH, E4, 1>), grid, dim3(256), 0, s, a);
-  else if (qf == 2) hipLaunchKernelGGL((pages_attn_kernel<DH, E4, 2>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((pages_attn_kernel<DH, E4, 4>), grid, dim3(256), 0, s, a);
+  else if (E4 || qf == 2) hipLaunchKernelGGL((pages_attn_kernel<DH, E4, 2>), grid, dim3(256), 0, s, a);
+  else if constexpr (!E4) hipLaunchKernelGGL((pages_attn_kernel<DH, false, 4>), grid, dim3(256), 0, s, a);
   if (a.nsplit > 1) {
     const bool wide = a.nsplit > 16;
     const int blocks = wide ? a.H : (a.H + 1024 / DH - 1) / (1024 / DH);

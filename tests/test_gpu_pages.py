@@ -388,7 +388,7 @@ def test_offsets_past_32_bits(dcl):
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("dh,heads,hkv,lens,new", [
     (64, 4, 4, [64, 900, 2000], 1), (128, 8, 2, [64, 1500], 1), (128, 4, 4, [640, 2000], 8), (64, 8, 4, [512], 16),
-    (128, 16, 4, [256] * 12, 32),
+    (128, 16, 4, [256] * 12, 32), (128, 16, 4, [128] * 17, 32),
 ])
 def test_probabilities_keep_sixteen_bits(dcl, e4m3, dh, heads, hkv, lens, new):
     """Half of the keys have the probability 1/2 (1 + 0.87 * 2^-8) of a reference's, half of them 1/2, with values 1 and -1: in
@@ -423,3 +423,26 @@ def test_probabilities_keep_sixteen_bits(dcl, e4m3, dh, heads, hkv, lens, new):
         got = out[b * new:(b + 1) * new]
         assert float((got - want).abs().max()) <= want * 2.0 ** -8 + 2.0 ** -16 + 2.0 ** -20 + n * 2.0 ** -23, (b, want)
         assert float((lse[b * new:(b + 1) * new] - math.log(float(p.sum()))).abs().max()) <= (n + 64) * 2.0 ** -23
+
+
+@pytest.mark.parametrize("dh,page", [(64, 16), (128, 32)])
+def test_rows_of_more_than_128_workgroups_of_sixty_four(dcl, dh, page):
+    """Enough of them for the layout of 64 rows whatever the sequences' lengths: bfloat16 pages, partial last tiles of rows and
+    keys, NaN behind every end, an infinity that only the last token sees, a missing page, sequences without new tokens."""
+    lens = [70, 33, 20, 64, 65, 21, 40, 100, 1, 300, 24]
+    counts = [20, 20, 20, 7, 20, 20, 3, 20, 0, 20, 19]
+    pool = Pool(dcl, lens, page, 4, dh, False, seed=14, fill=0x7F)
+    pg, off = pool.places(0)
+    pool.v[pg[69], 1, 5, off[69]] = math.inf
+    pool.v[pg[69], 1, dh - 1, off[69]] = -math.inf
+    gone = pool.table[7, 2].clone()
+    pool.table[7, 2] = -1
+    heads = 28
+    assert (heads // 4 * 20 + 63) // 64 * 4 * len(lens) > 128
+    out, lse, q, cu, _ = attend(dcl, pool, counts, heads, True, 0.11)
+    pool.table[7, 2] = gone
+
+    def seen(b, n):
+        return torch.arange(n) // page != 2 if b == 7 else torch.ones(n, dtype=torch.bool)
+    check(pool, out, lse, q, cu, counts, heads, True, 0.11, seen=seen)
+    assert not torch.isfinite(out[19, 7:14, 5]).any() and torch.isfinite(out[:19]).all()
