@@ -269,7 +269,8 @@ dcl_status dcl_score_hidden(dcl_model_t model, const void* hidden, int32_t n, dc
  * sequence, with causal = 1 those up to t. q: [T, n_heads, head_dim], k and v: [T, n_kv_heads, head_dim], head h reads
  * KV head h / (n_heads / n_kv_heads). out: bf16 [T, n_heads, head_dim]; lse (NULL: not written): float32 [T, n_heads],
  * the natural logarithm of the sum of exponentials. A key that a row does not see has no effect on it, whatever it
- * holds. Needs no workspace; results are bitwise reproducible. */
+ * holds. The probabilities are rounded to bf16 (2^-8 of each) for the product with v; sums are float32. Needs no
+ * workspace; results are bitwise reproducible. */
 dcl_status dcl_prompt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                 int64_t v_stride, const int32_t* cu, int32_t B, int32_t T, int32_t max_len,
                                 int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float scale, int32_t causal,
@@ -318,8 +319,10 @@ size_t dcl_pages_attention_workspace_bytes(const dcl_pages* pages, int32_t n_hea
  * no part. out: bf16 [T, n_heads, head_dim]; lse (NULL: not written): float32 [T, n_heads], the natural logarithm of
  * the sum of exponentials. A token that sees no position gets zeros and -inf. Work is split over the length where few
  * rows would leave CUs idle; the parts go through ws (device, 256-byte aligned, ws_bytes >=
- * dcl_pages_attention_workspace_bytes) and are joined in order: results are bitwise reproducible. Calls that overlap
- * in time need their own workspaces. */
+ * dcl_pages_attention_workspace_bytes) and are joined in order: results are bitwise reproducible. The probabilities
+ * keep 16 bits in the product with v; sums are float32. The parts are cut from max_pages, since the host does not know
+ * the lengths: a table much wider than the sequences need costs time and workspace. Calls that overlap in time need their
+ * own workspaces. */
 dcl_status dcl_pages_attention(const dcl_pages* pages, const int32_t* table, int32_t max_pages, const int32_t* len,
                                const int32_t* cu, int32_t B, int32_t T, int32_t max_new, const void* q,
                                int64_t q_stride, int32_t n_heads, float scale, int32_t causal, void* out, float* lse,

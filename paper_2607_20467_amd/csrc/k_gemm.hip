@@ -1209,8 +1209,8 @@ static bool run_pp(const bf16_t* W, const bf16_t* X, int Nw, int T, int K, const
 
 static_assert(kNumCfgs == 20, "run_plan dispatches every configuration of kCfgs");
 
-// Whether the epilogue has a kernel for configuration CI: the LM head runs only the layouts of lm_ok, the debug
-// logits (test support) one tile, and the 128 x 192 ring serves residual GEMMs and the LM head.
+// Whether the epilogue has a kernel for configuration CI: the LM head runs only the layouts of lm_ok, float32
+// logits (the debug call, the head before a draw) one tile, and the 128 x 192 ring serves residual GEMMs and the LM head.
 template <class Epi, int CI>
 constexpr bool has_cfg() {
   if (Epi::kKind == kEpiLm) return (CI >= 3 && CI <= 6) || CI == 11 || CI == 13 || CI == 14 || CI == 19;

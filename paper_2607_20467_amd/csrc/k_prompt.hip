@@ -8,12 +8,16 @@
 // 8 bytes, four rows of 16 elements, lane i gets column i). Both tiles are XOR-swizzled in 16-byte chunks so that the
 // rows that one read touches lie in different banks.
 //
-// The probabilities are rounded to bfloat16 once, 2^-9 of each, the sum that divides takes them unrounded.
+// The probabilities are rounded to bfloat16 once, 2^-8 of each at most; the sum that divides takes them unrounded. That rounding
+// is about as large as the output's own: the error against 64 bits is 1.9e-3 to 2.1e-3 where the output alone gives 1.6e-3. A
+// second part for what it leaves, as the attention over pages has, takes that away and costs half as many matrix
+// instructions again, here where they bound: 8192 tokens 506 / 684 us, the eight prompts below 90 / 119.
 //
-// Bound by the matrix and vector pipes together: one causal prompt of 8192 tokens x 32 heads of 128 takes 513 to 533 us, 1.03 to
-// 1.07 PFLOP/s of the 1.21 that a large matrix product reaches. Eight prompts of 78 to 1531 tokens, 28 / 4 heads: 90 us, 0.59
-// PFLOP/s: the two tiles on the diagonal are half masked, and a workgroup of seven tiles starts and ends three times as
-// often as it would in the long prompt.
+// Bound by the matrix and vector pipes together: one causal prompt of 8192 tokens x 32 heads of 128 takes 506 to 533 us, 1.03 to
+// 1.09 PFLOP/s of the 1.21 that a large matrix product reaches (520 to 620 each where nothing but such calls runs, at the clock
+// that the power leaves). Eight prompts of 78 to 1531 tokens, 28 / 4 heads: 90 us, 0.59 PFLOP/s: the two tiles on the diagonal
+// are half masked, and a workgroup of seven tiles starts and ends three times as often as it would in the long prompt.
+// Bidirectional, 32 heads: 8 prompts of 512 tokens 67 us, of 1024 190, one of 4096 263 (1.04 PFLOP/s).
 #include <type_traits>
 
 #include "dcl_internal.h"

@@ -19,7 +19,7 @@
 //
 // 512 rows of 152064 bfloat16 logits, each row with its own settings: 100 us. The first kernel (52) is bound by memory: 156 MB,
 // and the rows with a top-k once more, mostly from the last cache; the second (45) by two passes over a row by one CU. The
-// same in float32 without a filter: 200 us, 57 of a row's time in the last kernel, 35 of them additions to the histogram in
+// same in float32 without a filter: 200 us (211 with logits not in the caches), 57 of a row's time in the last kernel, 35 of them additions to the histogram in
 // LDS (with the arithmetic of four elements interleaved 32, and low temperatures slower). 4 rows of 126464 float32, top-k 50
 // and top-p 0.95: 22 us, three kernels of 6 to 9 us: chains of dependent loads, barriers and instruction fetches. Without
 // sharing they took 35, rows without a filter 55 instead of 38.
