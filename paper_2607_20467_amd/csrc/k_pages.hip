@@ -310,7 +310,7 @@ void launch_pages_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, h
 // 1 long 102.6 / 102.5, 8 x 64 tokens x 32 heads 31.8 / 34.0, x 28 / 4 heads in bfloat16 32.8 / 35.2).
 //
 // With one token it is bound by HBM: two sequences of 90000 to 131072 keys, 28 / 4 heads, bfloat16, 516 MB: 102 us with the
-// join, 5.05 TB/s; 64 sequences of 200 to 8000 8-bit keys, 32 / 8 heads, 323 MB: 78 us, 4.1 TB/s, the rest being the first
+// join, 5.05 TB/s; 64 sequences of 200 to 8000 8-bit keys, 32 / 8 heads, 323 MB: 79 us, 4.1 TB/s, the rest being the first
 // loads and the ragged end. Four sequences of 90 to 700 keys x 32 heads take 12 us, the latency of their loads. Under
 // a block of 64 tokens (8 sequences, 1280 8-bit keys, 32 heads: 34 us, 2.7 TB/s) the vector pipes are busy half of the time with
 // conversions and exponentials, the matrix pipes a seventh, and a wave has one tile of keys on its way at a time.
