@@ -682,7 +682,9 @@ class Runner:
         if stream is None:
             return contextlib.nullcontext()
         cuda = self.torch.cuda
-        return cuda.stream(cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+        if isinstance(stream, int):  # an ExternalStream of 0 would be a stream of torch's own
+            stream = cuda.ExternalStream(stream) if stream else cuda.default_stream()
+        return cuda.stream(stream)
 
     def workspace(self, B, S, P=0):
         need = dcl_workspace_bytes(self.model, B, S, P)

@@ -241,8 +241,8 @@ def test_sample_hidden_refusals(dcl):
         dcl.dcl_model_destroy(m)
 
 
-@pytest.mark.parametrize("given", ["side", 0x50])
-def test_a_runner_allocates_where_its_call_runs(dcl, monkeypatch, given):
+@pytest.mark.parametrize("given,place", [("side", "side"), (0x50, ("external", 0x50)), (0, "default")])
+def test_a_runner_allocates_where_its_call_runs(dcl, monkeypatch, given, place):
     """Buffers of a call on another stream than the current one come from that stream's memory: the allocator hands them out
     again as soon as the call returns. A torch that writes down the stream under which it allocates stands for the device."""
     import contextlib
@@ -260,7 +260,8 @@ def test_a_runner_allocates_where_its_call_runs(dcl, monkeypatch, given):
         return torch.empty(shape, dtype=dtype)
     m, called = dcl.binding, []
     fake = types.SimpleNamespace(empty=empty, uint8=torch.uint8, int16=torch.int16, int32=torch.int32, float32=torch.float32,
-                                 cuda=types.SimpleNamespace(stream=on, ExternalStream=lambda h: ("external", h)))
+                                 cuda=types.SimpleNamespace(stream=on, ExternalStream=lambda h: ("external", h),
+                                                            default_stream=lambda: "default"))
     run = object.__new__(m.Runner)
     run.torch, run.model, run.ws, run.geom = fake, None, None, types.SimpleNamespace(vocab=8, d_model=4)
     for name in ("dcl_sample_hidden", "dcl_score_hidden", "dcl_debug_logits", "dcl_denoise_step", "dcl_kv_append"):
@@ -268,7 +269,7 @@ def test_a_runner_allocates_where_its_call_runs(dcl, monkeypatch, given):
     for name in ("dcl_sample_hidden_workspace_bytes", "dcl_score_workspace_bytes", "dcl_workspace_bytes"):
         monkeypatch.setattr(m, name, lambda *a: 64)
     rows, tokens = torch.zeros(3, 4, dtype=torch.int16), torch.zeros(1, 4, dtype=torch.int32)
-    for stream, where in ((None, "current"), (given, given if given == "side" else ("external", given))):
+    for stream, where in ((None, "current"), (given, place)):
         for go in (lambda: run.sample_hidden(rows, None, stream=stream), lambda: run.score_hidden(rows, stream=stream),
                    lambda: run.logits(tokens, tokens, stream=stream, with_hidden=True),
                    lambda: run.step(tokens, None, 4, stream=stream),
