@@ -313,7 +313,7 @@ void launch_pages_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, h
 // join, 5.05 TB/s; 64 sequences of 200 to 8000 8-bit keys, 32 / 8 heads, 323 MB: 79 us, 4.1 TB/s, the rest being the first
 // loads and the ragged end. Four sequences of 90 to 700 keys x 32 heads take 12 us, the latency of their loads. Under
 // a block of 64 tokens (8 sequences, 1280 8-bit keys, 32 heads: 34 us, 2.7 TB/s) the vector pipes are busy half of the time with
-// conversions and exponentials, the matrix pipes a seventh, and a wave has one tile of keys on its way at a time.
+// conversions and exponentials, the matrix pipes a fifth, and a wave has one tile of keys on its way at a time.
 __device__ __forceinline__ f32x4_t mfma16p(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
