@@ -94,7 +94,7 @@ typedef struct {
   int32_t capacity;
 } dcl_kv;
 
-enum { DCL_DTYPE_F32 = 0, DCL_DTYPE_BF16 = 1, DCL_DTYPE_E4M3 = 2 };
+enum { DCL_DTYPE_F32 = 0, DCL_DTYPE_BF16 = 1, DCL_DTYPE_E4M3 = 2, DCL_DTYPE_E2M1 = 3 };
 
 /* dcl_denoise_step flags */
 #define DCL_SCORE_ALL_UNCOMMITTED 0x1u  /* score every position p <= i < gen_end, not only masks */
@@ -276,17 +276,64 @@ dcl_status dcl_prompt_attention(const void* q, int64_t q_stride, const void* k, 
                                 int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float scale, int32_t causal,
                                 void* out, float* lse, hipStream_t stream);
 
+/* Queries and keys on their way from the projection to the cache: each head's RMSNorm and rotate-half RoPE in one pass.
+ * Of every row t with pos[t] >= 0 (pos: device int32 [T]) and every head x [head_dim] of q and k
+ *   y = x / sqrt(mean(x^2) + eps) * g   (g_q for q, g_k for k: device float32 [head_dim], NULL: y = x),
+ *   (y_i, y_{i + r/2}) -> (y_i cos a - y_{i + r/2} sin a, y_{i + r/2} cos a + y_i sin a), a = pos[t] base^(-2i/r), i < r/2,
+ * with r = rot_dim, a multiple of 16 up to head_dim (0: no rotation); dimensions from r on keep y. Sums and products are
+ * float32, the angle's turns float64 (exact to 2^-24 of a turn at any position), each element is rounded once, at the end.
+ * q: bf16 [T, n_heads, head_dim], k: [T, n_kv_heads, head_dim], rows apart as above; outputs likewise. An output may be its
+ * own input (same address, same stride), otherwise no two of the four may overlap. Rows with pos[t] < 0 are neither read nor
+ * written. n_heads or n_kv_heads may be 0: those pointers are not used. eps >= 0, rope_base > 1. */
+dcl_status dcl_heads_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const int32_t* pos,
+                               int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, const float* g_q,
+                               const float* g_k, float eps, float rope_base, int32_t rot_dim, void* q_out,
+                               int64_t q_out_stride, void* k_out, int64_t k_out_stride, hipStream_t stream);
+
 /* A pool of pages for keys (after RoPE) and values of many sequences: page_len (a power of two, 16 to 1024) positions
  * each. dtype DCL_DTYPE_BF16: bf16 elements, scales NULL. DCL_DTYPE_E4M3: elements are 8-bit floats (sign, 4 exponent
  * bits, 3 fraction bits, no infinity) times one power-of-two scale 2^(byte - 127) per (position, KV head), the byte
- * in [1, 254]. All arrays 16-byte aligned, device memory, the caller's. */
+ * in [1, 254]. DCL_DTYPE_E2M1: elements are 4-bit floats (sign, 2 exponent bits, 1 fraction bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6)
+ * times one such scale per (position, KV head, 32 dimensions), byte 255 making all 32 NaN. Two share a byte, the first
+ * named in the low half: dimensions 2 i and 2 i + 1 of a key; 32 g + i and 32 g + 16 + i (i < 16) of a value, in row 16 g + i,
+ * so that a position owns its bytes. All arrays 16-byte aligned, device memory, the caller's. */
 typedef struct {
-  void* k;          /* [n_pages, n_kv_heads, page_len, head_dim] */
-  void* v;          /* [n_pages, n_kv_heads, head_dim, page_len] (position contiguous) */
-  uint8_t* k_scale; /* [n_pages, n_kv_heads, page_len], E4M3 only */
+  void* k;          /* [n_pages, n_kv_heads, page_len, head_dim]; E2M1: bytes [.., page_len, head_dim / 2] */
+  void* v;          /* [n_pages, n_kv_heads, head_dim, page_len] (position contiguous); E2M1: bytes [.., head_dim / 2, page_len] */
+  uint8_t* k_scale; /* E4M3: [n_pages, n_kv_heads, page_len]; E2M1: [n_pages, n_kv_heads, head_dim / 32, page_len] */
   uint8_t* v_scale;
   int32_t n_pages, page_len, n_kv_heads, head_dim, dtype;
 } dcl_pages;
+
+/* Workspace bytes of dcl_pages_extend and of dcl_pages_shrink for B sequences; 0 if B is invalid. */
+size_t dcl_pages_turn_workspace_bytes(int32_t B);
+
+/* Room for new tokens, assigned on the device: sequence b has len[b] positions in the pages that its row of `table` (device
+ * int32 [B, max_pages], updated) names, and asks for count[b] more (device int32 [B]; NULL: one each). Free pages are a
+ * list in device memory: the first *n_free entries of free_pages (int32 [n_pages]), taken from its end; *n_free is updated.
+ * With P = page_len, sequences in order b = 0, 1, ..: one gets all of its tokens or none. It gets them if
+ *   0 <= len[b], 0 <= count[b], len[b] + count[b] <= max_pages * P;
+ *   its tokens and those of the sequences before it that pass this are at most T;
+ *   it needs no page, or the pages ceil((len + count) / P) - ceil(len / P) that it needs and those needed by the sequences before
+ *   it that pass both are at most *n_free.
+ * Then its new pages are in its row of the table and len[b] += count[b]; otherwise all of its state stays. cu (int32 [B + 1],
+ * out) receives the borders of the granted tokens as packed rows, which is what the calls below take with len and table;
+ * pos (int32 [T], may be NULL) each row's position, slot (int64 [T], may be NULL) its place in the pool, page * P + position %
+ * P, -1 where no page holds it; both are -1 for the rows from cu[B] to T. For the pool's n_pages (at most 2^30 here) and page_len
+ * only: layers whose pools have the same shape share table, lengths and list. ws: device, 256-byte aligned, ws_bytes >=
+ * dcl_pages_turn_workspace_bytes(B); calls that overlap in time need their own. 1 <= B <= 2^16, B * max_pages < 2^31, 0 <= T <= 2^22. */
+dcl_status dcl_pages_extend(const dcl_pages* pages, int32_t* table, int32_t max_pages, int32_t* len, const int32_t* count,
+                            int32_t B, int32_t T, const int32_t* free_pages, int32_t* n_free, int32_t* cu, int32_t* pos,
+                            int64_t* slot, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* The reverse (rejected drafts, ended sequences): a sequence with 0 <= keep[b] < len[b] (keep: device int32 [B]) is cut to keep[b]
+ * positions; other sequences stay. Pages of which nothing is kept go back to the list, their entries become -1 (entries
+ * outside [0, n_pages) become -1 alone), the last page of the last sequence first, so that cutting what an extend has just
+ * brought leaves the list as it was. Pages that several sequences share must be cut from one of them only. What would pass
+ * n_pages entries is dropped. A sequence with len[b] > max_pages * P stays. */
+dcl_status dcl_pages_shrink(const dcl_pages* pages, int32_t* table, int32_t max_pages, int32_t* len, const int32_t* keep,
+                            int32_t B, int32_t* free_pages, int32_t* n_free, void* ws, size_t ws_bytes,
+                            hipStream_t stream);
 
 /* In the three calls below position x of sequence b lies in page table[b][x / page_len] (device int32 [B, max_pages],
  * max_pages * page_len <= 2^28); entries outside [0, n_pages) name no page. len[b] (device int32 [B]) counts the
@@ -296,13 +343,13 @@ typedef struct {
 /* Keys and values of the tokens into their pages. Tokens whose position no page holds are skipped. E4M3: with amax
  * the largest finite magnitude of the (token, head)'s row, the scale is the least power of two with amax <= 448 *
  * scale (2^-126 for a row of zeros) and elements are x / scale rounded to nearest even; infinities and NaN become
- * NaN. No two positions of one call may share a place (a page listed twice): which one stays there is not defined.
+ * NaN. E2M1: the same for every 32 dimensions, with 6 in the place of 448; 32 that hold an infinity or NaN become NaN. No two positions of one call may share a place (a page listed twice): which one stays there is not defined.
  * Pages that several sequences share are fine as long as no token is written to them. */
 dcl_status dcl_pages_write(const dcl_pages* pages, const int32_t* table, int32_t max_pages, const int32_t* len,
                            const int32_t* cu, int32_t B, int32_t T, int32_t max_new, const void* k, int64_t k_stride,
                            const void* v, int64_t v_stride, hipStream_t stream);
 
-/* The reverse: keys and values of those positions into rows of bf16 (E4M3: the values they stand for, which are bf16
+/* The reverse: keys and values of those positions into rows of bf16 (E4M3, E2M1: the values they stand for, which are bf16
  * numbers but for subnormals below 2^-133 and a value rounded up to 2^128, read as infinity).
  * A row whose position no page holds becomes zeros. */
 dcl_status dcl_pages_read(const dcl_pages* pages, const int32_t* table, int32_t max_pages, const int32_t* len,

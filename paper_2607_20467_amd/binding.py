@@ -16,7 +16,7 @@ import os
 from typing import Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-DCL_DTYPE_F32, DCL_DTYPE_BF16, DCL_DTYPE_E4M3 = 0, 1, 2
+DCL_DTYPE_F32, DCL_DTYPE_BF16, DCL_DTYPE_E4M3, DCL_DTYPE_E2M1 = 0, 1, 2, 3
 DCL_SCORE_ALL_UNCOMMITTED = 0x1
 DCL_SCORE_SUPPRESS_MASK = 0x2
 DCL_SEL_NO_PROGRESS_GUARD = 0x1
@@ -121,6 +121,11 @@ def load_library():
         "dcl_pages_read": (ctypes.c_int, batch + [vp, i64, vp, i64, vp]),
         "dcl_pages_attention_workspace_bytes": (sz, [pages, i32, i32, i32, i32, i32]),
         "dcl_pages_attention": (ctypes.c_int, batch + [vp, i64, i32, f32, i32, vp, vp, vp, sz, vp]),
+        "dcl_pages_turn_workspace_bytes": (sz, [i32]),
+        "dcl_pages_extend": (ctypes.c_int, [pages, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "dcl_pages_shrink": (ctypes.c_int, [pages, vp, i32, vp, vp, i32, vp, vp, vp, sz, vp]),
+        "dcl_heads_norm_rope": (ctypes.c_int, [vp, i64, vp, i64, vp, i32, i32, i32, i32, vp, vp, f32, f32, i32, vp, i64,
+                                               vp, i64, vp]),
         "dcl_sample_workspace_bytes": (sz, [i32, i32]),
         "dcl_sample_tokens": (ctypes.c_int, [vp, i32, i64, i32, i32, how, vp, vp, vp, vp, sz, vp]),
         "dcl_sample_hidden_workspace_bytes": (sz, [vp, i32]),
@@ -151,6 +156,7 @@ def _ptr(x) -> Optional[int]:
 _I32 = ("int32",)
 _F32 = ("float32",)
 _B16 = ("int16", "bfloat16", "uint16")       # bfloat16 bit patterns
+_I64 = ("int64",)
 _ANY = None
 
 
@@ -409,7 +415,7 @@ def _device():
     if _torch is None:
         import torch
         _dtypes.update({kinds: frozenset(getattr(torch, k) for k in kinds if hasattr(torch, k))
-                        for kinds in (_I32, _F32, _B16)})
+                        for kinds in (_I32, _F32, _B16, _I64)})
         _torch = torch
     return _torch.cuda.current_device() if _torch.cuda.is_initialized() else -2
 
@@ -501,8 +507,9 @@ def dcl_prompt_attention(q, k, v, cu, B: int, T: int, max_len: int, n_heads: int
 
 
 class KVPages:
-    """A pool of cache pages (``dcl_pages``): owns the tensors, or takes the caller's. dtype: DCL_DTYPE_BF16 or
-    DCL_DTYPE_E4M3 (8-bit values, one power-of-two scale per position and KV head)."""
+    """A pool of cache pages (``dcl_pages``): owns the tensors, or takes the caller's. dtype: DCL_DTYPE_BF16,
+    DCL_DTYPE_E4M3 (8-bit values, one power-of-two scale per position and KV head) or DCL_DTYPE_E2M1 (4-bit values, two in a
+    byte, one scale per position, KV head and 32 dimensions)."""
 
     def __init__(self, n_pages: int, page_len: int, n_kv_heads: int, head_dim: int, dtype: int = DCL_DTYPE_BF16,
                  k=None, v=None, k_scale=None, v_scale=None, device=None):
@@ -510,10 +517,15 @@ class KVPages:
         w = "KVPages"
         if min(n_pages, page_len, n_kv_heads, head_dim) < 1:
             raise DclError(1, w, "sizes must be positive")
-        if dtype not in (DCL_DTYPE_BF16, DCL_DTYPE_E4M3):
-            raise DclError(2, w, f"dtype {dtype}: DCL_DTYPE_BF16 or DCL_DTYPE_E4M3")
-        e4m3 = dtype == DCL_DTYPE_E4M3
-        shape_k, shape_v = (n_pages, n_kv_heads, page_len, head_dim), (n_pages, n_kv_heads, head_dim, page_len)
+        if dtype not in (DCL_DTYPE_BF16, DCL_DTYPE_E4M3, DCL_DTYPE_E2M1):
+            raise DclError(2, w, f"dtype {dtype}: DCL_DTYPE_BF16, DCL_DTYPE_E4M3 or DCL_DTYPE_E2M1")
+        scaled, width = dtype != DCL_DTYPE_BF16, head_dim
+        shape_s = (n_pages, n_kv_heads, page_len)
+        if dtype == DCL_DTYPE_E2M1:
+            if head_dim % 32:
+                raise DclError(2, w, f"head_dim {head_dim}: kernels exist for 64 and 128")
+            width, shape_s = head_dim // 2, (n_pages, n_kv_heads, head_dim // 32, page_len)
+        shape_k, shape_v = (n_pages, n_kv_heads, page_len, width), (n_pages, n_kv_heads, width, page_len)
         if device is None:
             device = next((t.device for t in (k, v, k_scale, v_scale) if t is not None), "cuda")
 
@@ -524,14 +536,14 @@ class KVPages:
                 raise DclError(1, w, f"{name} has shape {tuple(t.shape)}, expected {shape}")
             _arg(t, name, w, kinds)
             return t
-        b8 = ("uint8", "int8", "float8_e4m3fn")
-        kinds, new = (b8, torch.uint8) if e4m3 else (_B16, torch.bfloat16)
+        b8 = ("uint8", "int8") + (("float8_e4m3fn",) if dtype == DCL_DTYPE_E4M3 else ("float4_e2m1fn_x2",))
+        kinds, new = (b8, torch.uint8) if scaled else (_B16, torch.bfloat16)
         self.k = take(k, "k", shape_k, kinds, new)
         self.v = take(v, "v", shape_v, kinds, new)
-        if not e4m3 and (k_scale is not None or v_scale is not None):
+        if not scaled and (k_scale is not None or v_scale is not None):
             raise DclError(1, w, "bfloat16 pages have no scales")
-        self.k_scale = take(k_scale, "k_scale", shape_k[:3], ("uint8",), torch.uint8) if e4m3 else None
-        self.v_scale = take(v_scale, "v_scale", shape_k[:3], ("uint8",), torch.uint8) if e4m3 else None
+        self.k_scale = take(k_scale, "k_scale", shape_s, ("uint8",), torch.uint8) if scaled else None
+        self.v_scale = take(v_scale, "v_scale", shape_s, ("uint8",), torch.uint8) if scaled else None
         self.device = self.k.get_device()
         if any(t is not None and t.get_device() != self.device for t in (self.v, self.k_scale, self.v_scale)):
             raise DclError(1, w, "the pool's tensors are on different devices")
@@ -558,6 +570,59 @@ def dcl_pages_read(pages: KVPages, table, length, cu, B: int, T: int, max_new: i
     kp, ks = _packed(k, "k", w, T, pages.n_kv_heads, pages.head_dim, dev)
     vp, vs = _packed(v, "v", w, T, pages.n_kv_heads, pages.head_dim, dev)
     _check(load_library().dcl_pages_read(*a, kp, ks, vp, vs, _queue(stream, dev)), w)
+
+
+def dcl_pages_turn_workspace_bytes(B: int) -> int:
+    return load_library().dcl_pages_turn_workspace_bytes(B)
+
+
+def _turn(pages, table, length, ask, name, B, free_pages, n_free, where, dev):
+    """The leading arguments of the calls that hand pages out and take them back."""
+    if not isinstance(pages, KVPages):
+        raise DclError(1, where, "pages must be a KVPages")
+    if getattr(table, "dim", int)() != 2:
+        raise DclError(1, where, "table must be a [B, max_pages] tensor")
+    width, n = table.shape[1], max(B, 0)
+    return ((pages.ref, _here(table, "table", where, _I32, n * width, dev), width,
+             _here(length, "len", where, _I32, n, dev), _here(ask, name, where, _I32, n, dev), B),
+            (_here(free_pages, "free_pages", where, _I32, pages.n_pages, dev),
+             _here(n_free, "n_free", where, _I32, 1, dev)))
+
+
+def dcl_pages_extend(pages: KVPages, table, length, count, B: int, T: int, free_pages, n_free, cu, pos, slot, ws,
+                     ws_bytes: int, stream=None) -> None:
+    """Room for count [B] new tokens (None: one each) behind length [B] in ``table`` [B, max_pages], pages from the list
+    free_pages [n_pages] of which n_free [1] are free; cu [B + 1], pos [T] (or None) and slot [T] (int64, or None) are outputs."""
+    w, dev = "dcl_pages_extend", _device()
+    lead, free = _turn(pages, table, length, count, "count", B, free_pages, n_free, w, dev)
+    n = max(T, 0)
+    _check(load_library().dcl_pages_extend(*lead, T, *free, _here(cu, "cu", w, _I32, max(B, 0) + 1, dev),
+                                           _here(pos, "pos", w, _I32, n, dev), _here(slot, "slot", w, _I64, n, dev),
+                                           _space(ws, w, ws_bytes, dev), ws_bytes, _queue(stream, dev)), w)
+
+
+def dcl_pages_shrink(pages: KVPages, table, length, keep, B: int, free_pages, n_free, ws, ws_bytes: int,
+                     stream=None) -> None:
+    """Sequences cut to keep [B] positions (where 0 <= keep < length), their pages back on the list."""
+    w, dev = "dcl_pages_shrink", _device()
+    lead, free = _turn(pages, table, length, keep, "keep", B, free_pages, n_free, w, dev)
+    _check(load_library().dcl_pages_shrink(*lead, *free, _space(ws, w, ws_bytes, dev), ws_bytes, _queue(stream, dev)), w)
+
+
+def dcl_heads_norm_rope(q, k, pos, T: int, n_heads: int, n_kv_heads: int, head_dim: int, g_q, g_k, eps: float,
+                        rope_base: float, rot_dim: int, q_out, k_out, stream=None) -> None:
+    """q [T, n_heads, head_dim], k [T, n_kv_heads, head_dim] (rows may be apart; None where there are no heads) normalised
+    head by head with gains g_q, g_k [head_dim] (float32, or None) and rotated by pos [T]; outputs like them (rows may be
+    apart), or the inputs themselves."""
+    w, dev = "dcl_heads_norm_rope", _device()
+    (qp, qs), (qo, qos) = (_packed(x, name, w, T, n_heads, head_dim, dev) if n_heads > 0 else (None, 0)
+                           for x, name in ((q, "q"), (q_out, "q_out")))
+    (kp, ks), (ko, kos) = (_packed(x, name, w, T, n_kv_heads, head_dim, dev) if n_kv_heads > 0 else (None, 0)
+                           for x, name in ((k, "k"), (k_out, "k_out")))
+    _check(load_library().dcl_heads_norm_rope(qp, qs, kp, ks, _here(pos, "pos", w, _I32, max(T, 0), dev), T, n_heads,
+                                              n_kv_heads, head_dim, _here(g_q, "g_q", w, _F32, head_dim, dev),
+                                              _here(g_k, "g_k", w, _F32, head_dim, dev), eps, rope_base, rot_dim, qo, qos,
+                                              ko, kos, _queue(stream, dev)), w)
 
 
 def dcl_pages_attention_workspace_bytes(pages: KVPages, n_heads: int, B: int, T: int, max_new: int,

@@ -11,11 +11,12 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdcl.so")
 SOURCES = ["abi.hip", "abi_serving.hip", "k_small.hip", "k_gemm.hip", "k_attn.hip", "k_pages.hip",
-           "k_prompt.hip", "k_sample.hip"]
+           "k_pages4.hip", "k_turn.hip", "k_heads.hip", "k_prompt.hip", "k_sample.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # (source, extra flags) of each object; the GEMM family's instantiations are spread over three of them
 OBJECTS = [("k_gemm.hip", ["-DDCL_GEMM_PART=1"]), ("k_gemm.hip", ["-DDCL_GEMM_PART=2"]),
-           ("k_gemm.hip", ["-DDCL_GEMM_PART=3"]), ("k_attn.hip", []), ("k_pages.hip", []), ("k_prompt.hip", []),
+           ("k_gemm.hip", ["-DDCL_GEMM_PART=3"]), ("k_attn.hip", []), ("k_pages.hip", []), ("k_pages4.hip", []),
+           ("k_turn.hip", []), ("k_heads.hip", []), ("k_prompt.hip", []),
            ("k_sample.hip", []), ("k_small.hip", []),
            ("abi.hip", []), ("abi_serving.hip", [])]
 FLAGS = [

@@ -47,8 +47,8 @@ dcl_status check_head_dim(int32_t dh) {
 // Shapes of a pool and a batch's table, without its pointers.
 dcl_status check_pool(const dcl_pages* g, int32_t max_pages) {
   if (!g) return fail(DCL_E_ARG, "pages is NULL");
-  if (g->dtype != DCL_DTYPE_BF16 && g->dtype != DCL_DTYPE_E4M3)
-    return fail(DCL_E_UNSUPPORTED, "pages dtype %d: bfloat16 or e4m3", g->dtype);
+  if (g->dtype != DCL_DTYPE_BF16 && g->dtype != DCL_DTYPE_E4M3 && g->dtype != DCL_DTYPE_E2M1)
+    return fail(DCL_E_UNSUPPORTED, "pages dtype %d: bfloat16, e4m3 or e2m1", g->dtype);
   dcl_status st = check_head_dim(g->head_dim);
   if (st != DCL_OK) return st;
   if (g->n_kv_heads < 1 || g->n_kv_heads > 1024) return fail(DCL_E_ARG, "n_kv_heads %d outside [1, 1024]", g->n_kv_heads);
@@ -67,8 +67,8 @@ dcl_status check_pages(const dcl_pages* g, const int32_t* table, int32_t max_pag
   if (st != DCL_OK) return st;
   if (!g->k || !g->v) return fail(DCL_E_ARG, "pages: k / v is NULL");
   if (misaligned(g->k, 16) || misaligned(g->v, 16)) return fail(DCL_E_ARG, "pages: k / v must be 16-byte aligned");
-  if (g->dtype == DCL_DTYPE_E4M3) {
-    if (!g->k_scale || !g->v_scale) return fail(DCL_E_ARG, "pages: e4m3 needs k_scale and v_scale");
+  if (g->dtype != DCL_DTYPE_BF16) {
+    if (!g->k_scale || !g->v_scale) return fail(DCL_E_ARG, "pages: e4m3 and e2m1 need k_scale and v_scale");
     if (misaligned(g->k_scale, 16) || misaligned(g->v_scale, 16))
       return fail(DCL_E_ARG, "pages: k_scale / v_scale must be 16-byte aligned");
   }
@@ -92,6 +92,7 @@ Pages view(const dcl_pages* g, const int32_t* table, int32_t max_pages, const in
   p.Hkv = g->n_kv_heads;
   p.dh = g->head_dim;
   p.e4m3 = g->dtype == DCL_DTYPE_E4M3;
+  p.e2m1 = g->dtype == DCL_DTYPE_E2M1;
   p.B = B;
   p.T = T;
   p.max_new = max_new;
@@ -124,6 +125,39 @@ dcl_status check_attention_size(const dcl_pages* g, int32_t n_heads, int32_t B, 
   return DCL_OK;
 }
 
+// Sequences of a turn and the pool's shape.
+dcl_status check_turn(const dcl_pages* g, const int32_t* table, int32_t max_pages, const int32_t* len, int32_t B,
+                      const int32_t* free_pages, const int32_t* n_free, const void* ws, size_t ws_bytes) {
+  dcl_status st = check_pool(g, max_pages);
+  if (st != DCL_OK) return st;
+  if (g->n_pages > (1 << 30)) return fail(DCL_E_UNSUPPORTED, "n_pages %d: at most 2^30 are handed out", g->n_pages);
+  if (B < 1 || B > (1 << 16)) return fail(DCL_E_ARG, "B=%d outside [1, 2^16]", B);
+  if ((int64_t)B * max_pages >= ((int64_t)1 << 31)) return fail(DCL_E_UNSUPPORTED, "B=%d rows of %d pages: a table of 2^31 entries", B, max_pages);
+  if (!table || !len) return fail(DCL_E_ARG, "table / len is NULL");
+  if (!free_pages || !n_free) return fail(DCL_E_ARG, "free_pages / n_free is NULL");
+  if (!ws) return fail(DCL_E_ARG, "workspace is NULL");
+  if (misaligned(ws, 256)) return fail(DCL_E_ARG, "workspace must be 256-byte aligned");
+  const size_t need = dcl_pages_turn_workspace_bytes(B);
+  if (ws_bytes < need) return fail(DCL_E_WORKSPACE, "workspace %zu bytes < required %zu", ws_bytes, need);
+  return DCL_OK;
+}
+
+PagesTurn turn_args(const dcl_pages* g, int32_t* table, int32_t max_pages, int32_t* len, const int32_t* ask, int32_t B,
+                    int32_t* free_pages, int32_t* n_free, void* ws) {
+  PagesTurn a = {};
+  a.table = table;
+  a.len = len;
+  a.ask = ask;
+  a.free_pages = free_pages;
+  a.n_free = n_free;
+  a.ws = static_cast<int32_t*>(ws);
+  a.B = B;
+  a.n_pages = g->n_pages;
+  a.shift = __builtin_ctz((unsigned)g->page_len);
+  a.max_pages = max_pages;
+  return a;
+}
+
 // Workspace of an attention call over pages: the parts' outputs and their (reference, sum). A call without rows has one
 // part.
 struct PartLayout {
@@ -139,7 +173,10 @@ dcl_status part_layout(const dcl_pages* g, int32_t n_heads, int32_t B, int32_t T
     // in one part first: what passes keeps the partition's products in 64 bits
     dcl_status st = check_attention_size(g, n_heads, B, max_new, 1);
     if (st != DCL_OK) return st;
-    L->span = pages_attention_span(g->n_kv_heads, n_heads / g->n_kv_heads, B, max_new, capacity, g->dtype == DCL_DTYPE_E4M3);
+    const int group = n_heads / g->n_kv_heads;
+    L->span = g->dtype == DCL_DTYPE_E2M1
+                  ? pages4_attention_span(g->n_kv_heads, group, B, max_new, capacity)
+                  : pages_attention_span(g->n_kv_heads, group, B, max_new, capacity, g->dtype == DCL_DTYPE_E4M3);
     L->nsplit = (capacity + L->span - 1) / L->span;
     st = check_attention_size(g, n_heads, B, max_new, L->nsplit);
     if (st != DCL_OK) return st;
@@ -206,8 +243,9 @@ dcl_status dcl_pages_write(const dcl_pages* pages, const int32_t* table, int32_t
   dcl_status st = check_pages_copy(pages, table, max_pages, len, cu, B, T, max_new, k, k_stride, v, v_stride);
   if (st != DCL_OK) return st;
   (void)hipGetLastError();
-  launch_pages_write(view(pages, table, max_pages, len, cu, B, T, max_new), static_cast<const bf16_t*>(k), (long)k_stride,
-                     static_cast<const bf16_t*>(v), (long)v_stride, stream);
+  (pages->dtype == DCL_DTYPE_E2M1 ? launch_pages4_write : launch_pages_write)(
+      view(pages, table, max_pages, len, cu, B, T, max_new), static_cast<const bf16_t*>(k), (long)k_stride,
+      static_cast<const bf16_t*>(v), (long)v_stride, stream);
   return hip_check(hipGetLastError(), "pages_write launch");
 }
 
@@ -217,9 +255,92 @@ dcl_status dcl_pages_read(const dcl_pages* pages, const int32_t* table, int32_t 
   dcl_status st = check_pages_copy(pages, table, max_pages, len, cu, B, T, max_new, k, k_stride, v, v_stride);
   if (st != DCL_OK) return st;
   (void)hipGetLastError();
-  launch_pages_read(view(pages, table, max_pages, len, cu, B, T, max_new), static_cast<bf16_t*>(k), (long)k_stride,
-                    static_cast<bf16_t*>(v), (long)v_stride, stream);
+  (pages->dtype == DCL_DTYPE_E2M1 ? launch_pages4_read : launch_pages_read)(
+      view(pages, table, max_pages, len, cu, B, T, max_new), static_cast<bf16_t*>(k), (long)k_stride,
+      static_cast<bf16_t*>(v), (long)v_stride, stream);
   return hip_check(hipGetLastError(), "pages_read launch");
+}
+
+size_t dcl_pages_turn_workspace_bytes(int32_t B) {
+  return B < 1 || B > (1 << 16) ? 0 : align256(pages_turn_ws_ints(B) * 4);
+}
+
+dcl_status dcl_pages_extend(const dcl_pages* pages, int32_t* table, int32_t max_pages, int32_t* len, const int32_t* count,
+                            int32_t B, int32_t T, const int32_t* free_pages, int32_t* n_free, int32_t* cu, int32_t* pos,
+                            int64_t* slot, void* ws, size_t ws_bytes, hipStream_t stream) {
+  dcl_status st = check_turn(pages, table, max_pages, len, B, free_pages, n_free, ws, ws_bytes);
+  if (st != DCL_OK) return st;
+  if (T < 0 || T > (1 << 22)) return fail(DCL_E_ARG, "T=%d outside [0, 2^22]", T);
+  if (!cu) return fail(DCL_E_ARG, "cu is NULL");
+  PagesTurn a = turn_args(pages, table, max_pages, len, count, B, const_cast<int32_t*>(free_pages), n_free, ws);
+  a.T = T;
+  a.cu = cu;
+  a.pos = pos;
+  a.slot = slot;
+  (void)hipGetLastError();
+  launch_pages_extend(a, stream);
+  return hip_check(hipGetLastError(), "pages_extend launch");
+}
+
+dcl_status dcl_pages_shrink(const dcl_pages* pages, int32_t* table, int32_t max_pages, int32_t* len, const int32_t* keep,
+                            int32_t B, int32_t* free_pages, int32_t* n_free, void* ws, size_t ws_bytes,
+                            hipStream_t stream) {
+  dcl_status st = check_turn(pages, table, max_pages, len, B, free_pages, n_free, ws, ws_bytes);
+  if (st != DCL_OK) return st;
+  if (!keep) return fail(DCL_E_ARG, "keep is NULL");
+  (void)hipGetLastError();
+  launch_pages_shrink(turn_args(pages, table, max_pages, len, keep, B, free_pages, n_free, ws), stream);
+  return hip_check(hipGetLastError(), "pages_shrink launch");
+}
+
+dcl_status dcl_heads_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const int32_t* pos,
+                               int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, const float* g_q,
+                               const float* g_k, float eps, float rope_base, int32_t rot_dim, void* q_out,
+                               int64_t q_out_stride, void* k_out, int64_t k_out_stride, hipStream_t stream) {
+  if (T < 0 || T > (1 << 22)) return fail(DCL_E_ARG, "T=%d outside [0, 2^22]", T);
+  dcl_status st = check_head_dim(head_dim);
+  if (st != DCL_OK) return st;
+  if (n_heads < 0 || n_kv_heads < 0 || n_heads > (1 << 16) || n_kv_heads > (1 << 16) || n_heads + n_kv_heads < 1)
+    return fail(DCL_E_ARG, "n_heads %d, n_kv_heads %d: each in [0, 2^16], not both 0", n_heads, n_kv_heads);
+  if (n_heads > 0) st = check_rows("q", q, q_stride, T, n_heads, head_dim);
+  if (st == DCL_OK && n_heads > 0) st = check_rows("q_out", q_out, q_out_stride, T, n_heads, head_dim);
+  if (st == DCL_OK && n_kv_heads > 0) st = check_rows("k", k, k_stride, T, n_kv_heads, head_dim);
+  if (st == DCL_OK && n_kv_heads > 0) st = check_rows("k_out", k_out, k_out_stride, T, n_kv_heads, head_dim);
+  if (st != DCL_OK) return st;
+  if (T > 0 && !pos) return fail(DCL_E_ARG, "pos is NULL");
+  if (misaligned(g_q, 16) || misaligned(g_k, 16)) return fail(DCL_E_ARG, "g_q / g_k must be 16-byte aligned");
+  if (!(eps >= 0.f) || !isfinite(eps)) return fail(DCL_E_ARG, "eps must be >= 0");
+  if (!(rope_base > 1.f) || !isfinite(rope_base)) return fail(DCL_E_ARG, "rope_base must be > 1");
+  if (rot_dim < 0 || rot_dim > head_dim || rot_dim % 16 != 0)
+    return fail(DCL_E_ARG, "rot_dim %d must be a multiple of 16 in [0, head_dim]", rot_dim);
+  if (T == 0) return DCL_OK;
+  HeadsArgs a = {};
+  a.q = static_cast<const bf16_t*>(q);
+  a.k = static_cast<const bf16_t*>(k);
+  a.q_out = static_cast<bf16_t*>(q_out);
+  a.k_out = static_cast<bf16_t*>(k_out);
+  a.q_stride = (long)q_stride;
+  a.k_stride = (long)k_stride;
+  a.q_out_stride = (long)q_out_stride;
+  a.k_out_stride = (long)k_out_stride;
+  a.pos = pos;
+  a.g_q = g_q;
+  a.g_k = g_k;
+  a.T = T;
+  a.H = n_heads;
+  a.Hkv = n_kv_heads;
+  a.dh = head_dim;
+  a.rot = rot_dim;
+  a.eps = eps;
+  // powers in turn in 64 fraction bits: the last of 64 is off by less than 2^-56 of itself
+  if (rot_dim > 0) {
+    const long double step = powl((long double)rope_base, -2.0L / rot_dim);
+    long double f = 0.15915494309189533576888376337251436L;  // 1 / (2 pi)
+    for (int i = 0; i < rot_dim / 2; ++i, f *= step) a.turns[i] = (double)f;
+  }
+  (void)hipGetLastError();
+  launch_heads_norm_rope(a, stream);
+  return hip_check(hipGetLastError(), "heads_norm_rope launch");
 }
 
 size_t dcl_pages_attention_workspace_bytes(const dcl_pages* pages, int32_t n_heads, int32_t B, int32_t T,
@@ -266,7 +387,7 @@ dcl_status dcl_pages_attention(const dcl_pages* pages, const int32_t* table, int
   a.q_sign = scale < 0.f ? 0x80008000u : 0u;
   a.scale_log2 = scale_log2(scale);
   (void)hipGetLastError();
-  launch_pages_attention(a, stream);
+  (pages->dtype == DCL_DTYPE_E2M1 ? launch_pages4_attention : launch_pages_attention)(a, stream);
   return hip_check(hipGetLastError(), "pages_attention launch");
 }
 

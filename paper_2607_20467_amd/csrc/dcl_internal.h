@@ -186,16 +186,19 @@ dcl_status hip_check(hipError_t e, const char* what);
 
 // A pool of pages with the batch's table and lengths, as the kernels take them.
 struct Pages {
-  uint8_t *k, *v;                // [n_pages, Hkv, page, dh], [n_pages, Hkv, dh, page]
-  uint8_t *ks, *vs;              // [n_pages, Hkv, page] exponents of the scales (E4M3)
+  uint8_t *k, *v;                // [n_pages, Hkv, page, dh], [n_pages, Hkv, dh, page] (E2M1: dh / 2 bytes)
+  uint8_t *ks, *vs;              // [n_pages, Hkv, page] exponents of the scales (E4M3), [n_pages, Hkv, dh / 32, page] (E2M1)
   const int32_t *table, *len;    // [B, max_pages], [B]
   const int32_t* cu;             // [B + 1]
-  int n_pages, shift, max_pages, Hkv, dh, e4m3;  // pages of 2^shift positions
+  int n_pages, shift, max_pages, Hkv, dh, e4m3, e2m1;  // pages of 2^shift positions
   int B, T, max_new;
 };
 // Rows k, v [T, Hkv, dh] (row strides in elements) into the pages, or out of them.
 void launch_pages_write(const Pages& p, const bf16_t* k, long ks, const bf16_t* v, long vs, hipStream_t s);
 void launch_pages_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, hipStream_t s);
+// The same for pages of 4 bits.
+void launch_pages4_write(const Pages& p, const bf16_t* k, long ks, const bf16_t* v, long vs, hipStream_t s);
+void launch_pages4_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, hipStream_t s);
 
 struct PagesAttn {
   Pages p;
@@ -212,6 +215,38 @@ struct PagesAttn {
 // Keys of one part: from sizes that the host knows (capacity: positions that a row of the table can name).
 int pages_attention_span(int Hkv, int g, int B, int max_new, int capacity, int e4m3);
 void launch_pages_attention(PagesAttn a, hipStream_t s);
+// The parts of an attention over pages joined (nsplit > 1).
+void launch_pages_join(const PagesAttn& a, hipStream_t s);
+int pages4_attention_span(int Hkv, int g, int B, int max_new, int capacity);
+void launch_pages4_attention(PagesAttn a, hipStream_t s);
+
+// Pages handed out and taken back.
+struct PagesTurn {
+  int32_t* table;                // [B, max_pages]
+  int32_t* len;                  // [B]
+  const int32_t* ask;            // [B] tokens to add (null: one each) or lengths to keep
+  int32_t* free_pages;           // [n_pages], the first *n_free of them a stack
+  int32_t* n_free;
+  int32_t *cu, *pos;             // [B + 1], [T] (pos may be null)
+  int64_t* slot;                 // [T] or null
+  int32_t* ws;                   // pages_turn_ws_ints(B)
+  int B, T, n_pages, shift, max_pages;
+};
+size_t pages_turn_ws_ints(int B);
+void launch_pages_extend(const PagesTurn& a, hipStream_t s);
+void launch_pages_shrink(const PagesTurn& a, hipStream_t s);
+
+struct HeadsArgs {
+  const bf16_t *q, *k;           // [T, H, dh], [T, Hkv, dh] with row strides
+  bf16_t *q_out, *k_out;
+  long q_stride, k_stride, q_out_stride, k_out_stride;
+  const int32_t* pos;            // [T]
+  const float *g_q, *g_k;        // [dh] or null
+  int T, H, Hkv, dh, rot;
+  float eps;
+  double turns[64];              // base^(-2i/rot) / (2 pi): turns a position adds to pair i
+};
+void launch_heads_norm_rope(const HeadsArgs& a, hipStream_t s);
 
 struct PromptAttn {
   const bf16_t *q, *k, *v;       // [T, H, dh], [T, Hkv, dh] with row strides

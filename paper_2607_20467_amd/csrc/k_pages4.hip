@@ -1,0 +1,584 @@
+// Pages of 4 bits: keys and values of packed tokens into them and back, and attention from a sequence's newest tokens.
+#include "dcl_internal.h"
+#include "pages_index.h"
+
+namespace dcl {
+
+// ---------------------------------------------------------------- 4-bit rows
+// 32 dimensions of a row are stored as e2m1 values (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) times one scale 2^(e - 127):
+// the least power of two with amax <= 6 * scale. As with 8 bits, a power of two makes x / scale exact and keeps every stored
+// value a bfloat16 number. 32 values share a scale because 12 to 1 is all that the format spans: keys after the rotation have a
+// few large dimensions, which cost only their own group its precision. The format has no infinity and no NaN: a group that
+// holds one has scale byte 255, for which gfx950's conversions and scaled matrix products give NaN (checked there for every
+// byte under every scale).
+__device__ __forceinline__ int e2m1_exponent(uint32_t amax_bits) {  // bfloat16 bits of amax, sign cleared
+  // amax = 1.f * 2^(E - 127), 6 = 1.5 * 2^2
+  const int e = (int)(amax_bits >> 7) - 2 + ((amax_bits & 127) > 64 ? 1 : 0);
+  return e < 1 ? 1 : e;  // at most 253
+}
+__device__ __forceinline__ float scale4(uint32_t e) { return __uint_as_float(e << 23); }  // 255: no finite number
+
+// Largest magnitude of eight bfloat16, as bits: 0x7F80 and more for infinities and NaN.
+__device__ __forceinline__ uint32_t magnitude8(const uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = max(m, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+  return m;
+}
+// Eight bfloat16 over `scale` (a power of two) to eight codes, the first in the lowest bits.
+__device__ __forceinline__ uint32_t codes8(const uint4& x, float scale) {
+  uint32_t o = 0;
+  o = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, __builtin_bit_cast(bf16x2_t, x.x), scale, 0);
+  o = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, __builtin_bit_cast(bf16x2_t, x.y), scale, 1);
+  o = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, __builtin_bit_cast(bf16x2_t, x.z), scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, __builtin_bit_cast(bf16x2_t, x.w), scale, 3);
+}
+// The reverse.
+__device__ __forceinline__ uint4 widen_codes8(uint32_t w, float scale) {
+  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)));
+}
+// Four codes to the low halves of four bytes, and back.
+__device__ __forceinline__ uint32_t spread4(uint32_t x) {
+  x = (x | x << 8) & 0x00FF00FFu;
+  return (x | x << 4) & 0x0F0F0F0Fu;
+}
+
+// Streams that pass the caches by.
+typedef uint32_t u32x4p_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void stream_store(void* p, const uint4& x) {
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4p_t, x), static_cast<u32x4p_t*>(p));
+}
+__device__ __forceinline__ void stream_store(void* p, uint32_t x) {
+  __builtin_nontemporal_store(x, static_cast<uint32_t*>(p));
+}
+__device__ __forceinline__ uint4 stream_load(const void* p) {
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(static_cast<const u32x4p_t*>(p)));
+}
+
+// ---------------------------------------------------------------- write
+// One workgroup takes 64 positions (aligned to 64 in the sequence) of one KV head, eight dimensions a lane. Keys go out as they
+// come; a value's dimensions i and i + 16 of a group, which share a byte, are two lanes apart, and values and scales turn
+// position-innermost in LDS, in chunks of 16 positions that never straddle a page.
+constexpr int kGroup4 = 64;
+
+template <int DH>
+__global__ void __launch_bounds__(256) pages4_write_kernel(Pages p, const bf16_t* __restrict__ k, long kst,
+                                                          const bf16_t* __restrict__ v, long vst, int groups) {
+  constexpr int L = DH / 8, TPR = 256 / L, R = kGroup4 / TPR, G = DH / 32, HB = DH / 2;
+  constexpr int PITCH = HB + 4;
+  __shared__ __attribute__((aligned(16))) uint8_t sv[kGroup4 * PITCH], ss[2][G][kGroup4];
+  const int h = blockIdx.x % p.Hkv, gb = blockIdx.x / p.Hkv, grp = gb % groups, b = gb / groups;
+  const SeqRows r = seq_rows(p.cu, b, p.T);
+  const int n = min(r.n, p.max_new), start = seq_len(p.len, b) - r.n;  // position of the first row
+  const int g0 = (start & ~(kGroup4 - 1)) + grp * kGroup4;
+  if (g0 >= start + n) return;
+  const int32_t* row = p.table + (size_t)b * p.max_pages;
+  const int plen = 1 << p.shift, tid = threadIdx.x, c = tid % L;
+  uint4 xk[R], xv[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int t = g0 + i * TPR + tid / L - start;
+    xk[i] = xv[i] = make_uint4(0, 0, 0, 0);
+    if (t >= 0 && t < n) {
+      const size_t at = (size_t)(r.first + t);
+      xk[i] = stream_load(k + at * kst + (size_t)h * DH + 8 * c);
+      xv[i] = stream_load(v + at * vst + (size_t)h * DH + 8 * c);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int local = i * TPR + tid / L, t = g0 + local - start;
+    const int page = t >= 0 && t < n ? page_of(row, p.max_pages, p.n_pages, p.shift, (g0 + local) >> 4) : -1;
+    const size_t slot = ((size_t)max(page, 0) * p.Hkv + h) * plen + ((g0 + local) & (plen - 1));
+    uint32_t ak = magnitude8(xk[i]), av = magnitude8(xv[i]);
+#pragma unroll
+    for (int o = 2; o >= 1; o >>= 1) {  // four lanes hold a group
+      ak = max(ak, (uint32_t)__shfl_xor((int)ak, o, 64));
+      av = max(av, (uint32_t)__shfl_xor((int)av, o, 64));
+    }
+    const bool odd_k = ak >= 0x7F80u, odd_v = av >= 0x7F80u;
+    const int ek = odd_k ? 255 : e2m1_exponent(ak), ev = odd_v ? 255 : e2m1_exponent(av);
+    const uint32_t qk = odd_k ? 0u : codes8(xk[i], scale4(ek)), qv = odd_v ? 0u : codes8(xv[i], scale4(ev));
+    if (page >= 0) stream_store(p.k + slot * HB + 4 * c, qk);
+    const uint32_t other = (uint32_t)__shfl_xor((int)qv, 2, 64);
+    const bool upper = (c & 2) != 0;
+    // the lower lane makes the bytes of its first four dimensions, the upper one those of its last four
+    const uint32_t lo = upper ? other >> 16 : qv & 0xFFFFu, hi = upper ? qv >> 16 : other & 0xFFFFu;
+    *reinterpret_cast<uint32_t*>(sv + local * PITCH + 16 * (c >> 2) + 8 * (c & 1) + (upper ? 4 : 0)) = spread4(lo) | spread4(hi) << 4;
+    if ((c & 3) == 0) {
+      ss[0][c >> 2][local] = (uint8_t)ek;
+      ss[1][c >> 2][local] = (uint8_t)ev;
+    }
+  }
+  __syncthreads();
+  // rows of positions: HB of values, 2 G of scales
+  for (int u = tid; u < (HB + 2 * G) * 4; u += 256) {
+    const int ch = u & 3, d = u >> 2, p0 = g0 + 16 * ch;
+    const int lo = max(0, start - p0), hi = min(16, start + n - p0);
+    if (lo >= hi) continue;
+    const int page = page_of(row, p.max_pages, p.n_pages, p.shift, p0 >> 4);
+    if (page < 0) continue;
+    const size_t ph = (size_t)page * p.Hkv + h;
+    const int off = p0 & (plen - 1);
+    uint8_t* dst;
+    const uint8_t* src;
+    int step;
+    if (d < HB) {
+      dst = p.v + (ph * HB + d) * plen + off;
+      src = sv + 16 * ch * PITCH + d;
+      step = PITCH;
+    } else {
+      const int which = (d - HB) / G, g = (d - HB) % G;
+      dst = (which ? p.vs : p.ks) + (ph * G + g) * plen + off;
+      src = &ss[which][g][16 * ch];
+      step = 1;
+    }
+    if (hi - lo == 16) {
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        w[j] = src[4 * j * step] | src[(4 * j + 1) * step] << 8 | src[(4 * j + 2) * step] << 16 |
+               (uint32_t)src[(4 * j + 3) * step] << 24;
+      stream_store(dst, make_uint4(w[0], w[1], w[2], w[3]));
+    } else {
+      for (int j = lo; j < hi; ++j) dst[j] = src[j * step];
+    }
+  }
+}
+
+// ---------------------------------------------------------------- read
+// The reverse, in the same groups. A row whose position no page holds is zeros.
+template <int DH>
+__global__ void __launch_bounds__(256) pages4_read_kernel(Pages p, bf16_t* __restrict__ k, long kst, bf16_t* __restrict__ v,
+                                                         long vst, int groups) {
+  constexpr int L = DH / 8, TPR = 256 / L, R = kGroup4 / TPR, G = DH / 32, HB = DH / 2;
+  constexpr int PITCH = kGroup4 + 4;
+  __shared__ __attribute__((aligned(16))) uint8_t sv[HB * PITCH];
+  const int h = blockIdx.x % p.Hkv, gb = blockIdx.x / p.Hkv, grp = gb % groups, b = gb / groups;
+  const SeqRows r = seq_rows(p.cu, b, p.T);
+  const int n = min(r.n, p.max_new), start = seq_len(p.len, b) - r.n;
+  const int g0 = (start & ~(kGroup4 - 1)) + grp * kGroup4;
+  if (g0 >= start + n) return;
+  const int32_t* row = p.table + (size_t)b * p.max_pages;
+  const int plen = 1 << p.shift, tid = threadIdx.x, c = tid % L;
+  uint32_t xk[R], ks[R], vs[R], held = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int local = i * TPR + tid / L, t = g0 + local - start;
+    const int page = t >= 0 && t < n ? page_of(row, p.max_pages, p.n_pages, p.shift, (g0 + local) >> 4) : -1;
+    const size_t ph = (size_t)max(page, 0) * p.Hkv + h;
+    const int off = (g0 + local) & (plen - 1);
+    xk[i] = ks[i] = vs[i] = 0;
+    if (page >= 0) {
+      held |= 1u << i;
+      xk[i] = *reinterpret_cast<const uint32_t*>(p.k + (ph * plen + off) * HB + 4 * c);
+      ks[i] = p.ks[(ph * G + (c >> 2)) * plen + off];
+      vs[i] = p.vs[(ph * G + (c >> 2)) * plen + off];
+    }
+  }
+#pragma unroll
+  for (int u = tid; u < HB * 4; u += 256) {
+    const int ch = u & 3, d = u >> 2, p0 = g0 + 16 * ch;
+    const int page = p0 < start + n && p0 + 16 > start ? page_of(row, p.max_pages, p.n_pages, p.shift, p0 >> 4) : -1;
+    if (page < 0) continue;
+    const uint4 x = *reinterpret_cast<const uint4*>(p.v + (((size_t)page * p.Hkv + h) * HB + d) * plen + (p0 & (plen - 1)));
+    uint32_t* dst = reinterpret_cast<uint32_t*>(sv + d * PITCH + 16 * ch);
+    dst[0] = x.x;
+    dst[1] = x.y;
+    dst[2] = x.z;
+    dst[3] = x.w;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int local = i * TPR + tid / L, t = g0 + local - start;
+    if (t < 0 || t >= n) continue;
+    const size_t at = (size_t)(r.first + t);
+    uint4 ok = make_uint4(0, 0, 0, 0), ov = ok;
+    if (held >> i & 1) {
+      const uint8_t* s = sv + (16 * (c >> 2) + 8 * (c & 1)) * PITCH + local;
+      const int half = c & 2 ? 4 : 0;  // which half of the bytes the lane's dimensions have
+      uint32_t w = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w |= ((uint32_t)(s[e * PITCH] >> half) & 15u) << (4 * e);
+      ok = widen_codes8(xk[i], scale4(ks[i]));
+      ov = widen_codes8(w, scale4(vs[i]));
+    }
+    stream_store(k + at * kst + (size_t)h * DH + 8 * c, ok);
+    stream_store(v + at * vst + (size_t)h * DH + 8 * c, ov);
+  }
+}
+
+// Groups of kGroup4 positions that `n` consecutive positions can touch.
+static int groups4_of(int n) { return (n + kGroup4 - 2) / kGroup4 + 1; }
+
+void launch_pages4_write(const Pages& p, const bf16_t* k, long ks, const bf16_t* v, long vs, hipStream_t s) {
+  if (p.T == 0 || p.max_new == 0) return;
+  const int groups = groups4_of(p.max_new);
+  const dim3 grid((unsigned)groups * p.Hkv * p.B);
+  if (p.dh == 128) hipLaunchKernelGGL((pages4_write_kernel<128>), grid, dim3(256), 0, s, p, k, ks, v, vs, groups);
+  else hipLaunchKernelGGL((pages4_write_kernel<64>), grid, dim3(256), 0, s, p, k, ks, v, vs, groups);
+}
+
+void launch_pages4_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, hipStream_t s) {
+  if (p.T == 0 || p.max_new == 0) return;
+  const int groups = groups4_of(p.max_new);
+  const dim3 grid((unsigned)groups * p.Hkv * p.B);
+  if (p.dh == 128) hipLaunchKernelGGL((pages4_read_kernel<128>), grid, dim3(256), 0, s, p, k, ks, v, vs, groups);
+  else hipLaunchKernelGGL((pages4_read_kernel<64>), grid, dim3(256), 0, s, p, k, ks, v, vs, groups);
+}
+
+// ---------------------------------------------------------------- attention over pages
+// o = sum_j softmax_j(scale q.k_j) v_j, split and joined as over the other pages: a workgroup takes one tile of 16 QF rows of one
+// KV head (its g = H / Hkv query heads times the new tokens) and `span` keys, its four waves every fourth tile of 64 keys, which
+// come straight from memory into the registers of the matrix instructions.
+//
+// Row 4 a + r of score step kt is key 16 a + 4 kt + r of the tile, so that lane group a (= lane / 16) ends up with the
+// probabilities of 16 adjacent keys, which lie in one page, and loads their values as one 16-byte piece of each row of two
+// dimensions.
+__device__ __forceinline__ f32x4_t mfma16q(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float max_over_groups(float v) {  // over the lanes l, l ^ 16, l ^ 32, l ^ 48
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float sum_over_groups(float v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+__device__ __forceinline__ float reference_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+template <int DH, int QF>
+__global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages4_attn_kernel(PagesAttn a) {
+  constexpr int KT = 64, NKT = 4, HB = DH / 2, G = DH / 32, KS = DH / 32, DT = DH / 16;
+  constexpr int KW = DH / 32;  // words of a lane's dimensions of one key
+  __shared__ f32x4_t xo[3][DT][64];
+  __shared__ float2 xml[3][64];
+  const Pages& p = a.p;
+  // units: row tiles of one (part, sequence, KV head) follow each other on one XCD and share its L2
+  const int u = blockIdx.x, item = (u / (8 * a.row_tiles)) * 8 + (u & 7), tile = (u >> 3) % a.row_tiles;
+  if (item >= a.nsplit * p.B * p.Hkv) return;
+  const int h = item % p.Hkv, b = (item / p.Hkv) % p.B, part = item / (p.Hkv * p.B);
+  const SeqRows r = seq_rows(p.cu, b, p.T);
+  const int n = min(r.n, p.max_new), rows = n * a.g, row0 = tile * 16 * QF;
+  if (row0 >= rows) return;
+  const int len = seq_len(p.len, b), plen = 1 << p.shift;
+  const int kend = min(len, p.max_pages << p.shift);  // keys that the table can name
+  const int t0 = part * (a.span / KT), t1 = min(t0 + a.span / KT, (kend + KT - 1) / KT);
+  if (part > 0 && t0 >= t1) return;  // part 0 always answers
+  const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 15, lg = lane >> 4, la = lq >> 2, lr = lq & 3;
+  const int32_t* row = p.table + (size_t)b * p.max_pages;
+
+  // the wave's queries, and how many keys each may see (rows past the last one: like any other, never written)
+  bf16x8_t qf[QF][KS];
+  int lim[QF], lim_min = kend;
+#pragma unroll
+  for (int f = 0; f < QF; ++f) {
+    const int rr = min(row0 + 16 * f + lq, rows - 1), i = rr / a.g, head = h * a.g + rr % a.g;
+    const bf16_t* qp = a.q + (size_t)(r.first + i) * a.q_stride + (size_t)head * DH + (DH / 4) * lg;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      uint4 x = *reinterpret_cast<const uint4*>(qp + 8 * ks);
+      x.x ^= a.q_sign, x.y ^= a.q_sign, x.z ^= a.q_sign, x.w ^= a.q_sign;  // a negative scale is a sign of the query
+      qf[f][ks] = __builtin_bit_cast(bf16x8_t, x);
+    }
+    lim[f] = a.causal ? min(kend, max(0, len - r.n + i + 1)) : kend;
+  }
+  if (a.causal) lim_min = min(kend, max(0, len - r.n + row0 / a.g + 1));
+
+  const float scale = a.scale_log2;
+  f32x4_t o[QF][DT];
+  float m[QF], l[QF];
+#pragma unroll
+  for (int f = 0; f < QF; ++f) {
+    m[f] = -INFINITY;
+    l[f] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[f][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  typedef uint32_t words_t __attribute__((ext_vector_type(KW)));
+  typedef uint32_t u32x4q_t __attribute__((ext_vector_type(4)));
+  words_t kr[NKT];           // the tile's keys, values and scales, as loaded
+  u32x4q_t vr[G], vsr[G], ksr;
+  int pid_v = -1;            // page of the lane group's 16 keys of the tile whose values are in vr
+  auto load_keys = [&](int t, int pid) {  // pid: page of keys 64 t + 16 la ..
+    const int off = (KT * t + 16 * la) & (plen - 1);
+    const size_t ph = (size_t)max(pid, 0) * p.Hkv + h;
+    const uint8_t* base = p.k + (ph * plen + off + lr) * HB + lg * (HB / 4);
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt) kr[kt] = *reinterpret_cast<const words_t*>(base + 4 * kt * HB);
+    ksr = *reinterpret_cast<const u32x4q_t*>(p.ks + (ph * G + lg * G / 4) * plen + off);  // byte lr of word kt
+  };
+  auto load_values = [&](int t, int pid) {  // pid: page of keys 64 t + 16 lg ..
+    const int off = (KT * t + 16 * lg) & (plen - 1);
+    const size_t ph = (size_t)max(pid, 0) * p.Hkv + h;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      vr[g] = *reinterpret_cast<const u32x4q_t*>(p.v + (ph * HB + 16 * g + lq) * plen + off);
+      vsr[g] = *reinterpret_cast<const u32x4q_t*>(p.vs + (ph * G + g) * plen + off);
+    }
+    pid_v = pid;
+  };
+
+  // Pages of the 64 chunks of 16 keys from `base` on, one a lane, and of the 64 after those.
+  int base = t0 * (KT / 16);
+  int ids = page_of(row, p.max_pages, p.n_pages, p.shift, base + lane);
+  int ids_next = page_of(row, p.max_pages, p.n_pages, p.shift, base + 64 + lane);
+  int pk = -1, pv = -1;
+  auto find_pages = [&](int t) {  // of tile t, at most four further than the last one asked for
+    if (t * (KT / 16) - base >= 64) {
+      base += 64;
+      ids = ids_next;
+      ids_next = page_of(row, p.max_pages, p.n_pages, p.shift, base + 64 + lane);
+    }
+    pk = __shfl(ids, 4 * t + la - base, 64);
+    pv = __shfl(ids, 4 * t + lg - base, 64);
+  };
+
+  int t = t0 + wid;
+  if (t < t1) {
+    find_pages(t);
+    load_keys(t, pk);
+    load_values(t, pv);
+  }
+  for (; t < t1; t += 4) {
+    const int k0 = KT * t + 16 * lg;  // the lane group's first key
+    f32x4_t sc[QF][NKT];
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt) {
+      const float key_scale = scale4((ksr[kt] >> (8 * lr)) & 255u);
+      bf16x8_t kf[KS];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) kf[ks] = __builtin_bit_cast(bf16x8_t, widen_codes8(kr[kt][ks], key_scale));
+#pragma unroll
+      for (int f = 0; f < QF; ++f) {
+        sc[f][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sc[f][kt] = mfma16q(kf[ks], qf[f][ks], sc[f][kt]);
+      }
+    }
+    if (t + 4 < t1) {
+      find_pages(t + 4);
+      load_keys(t + 4, pk);
+    }
+
+    // the keys that a row does not see: past its limit, past the last key, in no page
+    const bool whole = KT * t + KT <= lim_min && __builtin_amdgcn_ballot_w64(pid_v < 0) == 0;
+    if (!whole) {
+#pragma unroll
+      for (int f = 0; f < QF; ++f)
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+          for (int rr = 0; rr < 4; ++rr)
+            if (pid_v < 0 || k0 + 4 * kt + rr >= lim[f]) sc[f][kt][rr] = -INFINITY;
+    }
+    // The reference point m (log2 units) moves only when a score passes it by more than 2^8 (any reference gives the same
+    // quotient), so that most tiles need no maximum across the lanes and no rescaling.
+    float tmax[QF];
+    bool move = false;
+#pragma unroll
+    for (int f = 0; f < QF; ++f) {
+      tmax[f] = -INFINITY;
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) tmax[f] = fmaxf(tmax[f], sc[f][kt][rr]);
+      move |= tmax[f] * scale > m[f] + 8.f;
+    }
+    if (__builtin_amdgcn_ballot_w64(move)) {
+#pragma unroll
+      for (int f = 0; f < QF; ++f) {
+        const float ts = max_over_groups(tmax[f]) * scale;
+        const float mn = ts > m[f] + 8.f ? ts : m[f];
+        const float alpha = mn == m[f] ? 1.f : __builtin_amdgcn_exp2f(m[f] - mn);
+        l[f] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[f][dt] *= alpha;
+        m[f] = mn;
+      }
+    }
+    // The probabilities enter the product as two bfloat16 parts, the nearest and the nearest to what it leaves (2^-16 of each
+    // together); the sum that divides takes them unrounded.
+    bf16x8_t pf[QF][2], rest[QF][2];
+#pragma unroll
+    for (int f = 0; f < QF; ++f) {
+      const float mr = -reference_of(m[f]);
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) {
+          sc[f][kt][rr] = __builtin_amdgcn_exp2f(fmaf(sc[f][kt][rr], scale, mr));
+          l[f] += sc[f][kt][rr];
+        }
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        const f32x4_t &x = sc[f][2 * s2], &y = sc[f][2 * s2 + 1];
+        const uint4 w = make_uint4(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(y[0], y[1]), f2bf2(y[2], y[3]));
+        auto left = [](uint32_t two, float p0, float p1) {
+          return f2bf2(p0 - __uint_as_float(two << 16), p1 - __uint_as_float(two & 0xFFFF0000u));
+        };
+        pf[f][s2] = __builtin_bit_cast(bf16x8_t, w);
+        rest[f][s2] = __builtin_bit_cast(bf16x8_t, make_uint4(left(w.x, x[0], x[1]), left(w.y, x[2], x[3]),
+                                                              left(w.z, y[0], y[1]), left(w.w, y[2], y[3])));
+      }
+    }
+    // Values. In a tile that some row does not see whole, a probability of 0 must meet no NaN: the scales of slots past the last
+    // key become 1 (any code is then a number), and a group of NaN that only some rows see is given to just those.
+    if (!whole) {
+      const int nv = pid_v < 0 ? 0 : kend - k0;  // the lane group's keys that are there
+      uint32_t odd = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int bits = 8 * (nv - 4 * j);
+        const uint32_t keep = bits >= 32 ? ~0u : bits <= 0 ? 0u : (1u << bits) - 1u;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const uint32_t s = (vsr[g][j] & keep) | (0x7F7F7F7Fu & ~keep);
+          vsr[g][j] = s;
+          odd |= ((s & 0x7F7F7F7Fu) + 0x01010101u) & s & 0x80808080u;  // a byte of 255
+        }
+      }
+      if (__builtin_amdgcn_ballot_w64(odd != 0)) {
+        // rare: such groups leave the product and are added key by key
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const uint32_t s = vsr[g][j], bad = (((s & 0x7F7F7F7Fu) + 0x01010101u) & s & 0x80808080u) >> 7;
+            vsr[g][j] = s ^ (bad << 7);  // 255 -> 127
+          }
+#pragma unroll 1
+        for (int y = 0; y < KT; ++y) {
+          const int key = KT * t + y, pid = page_of(row, p.max_pages, p.n_pages, p.shift, key >> 4);
+          if (pid < 0 || key >= kend) continue;
+          const uint8_t* at = p.vs + ((size_t)pid * p.Hkv + h) * G * plen + (key & (plen - 1));
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            if (at[g * plen] != 255) continue;
+#pragma unroll
+            for (int f = 0; f < QF; ++f)
+              if (key < lim[f]) {
+                o[f][2 * g] += __uint_as_float(0x7FC00000u);
+                o[f][2 * g + 1] += __uint_as_float(0x7FC00000u);
+              }
+          }
+        }
+      }
+    }
+    // A byte is two dimensions, 16 apart, of one key: converted under that key's scale, then two keys of a dimension side by side.
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        uint32_t lo[4], hi[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w = vr[g][2 * s2 + j / 2], e = vsr[g][2 * s2 + j / 2];
+          const uint32_t x = __builtin_bit_cast(uint32_t, j % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale4((e >> 16) & 255u), 2)
+                                                                : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale4(e & 255u), 0));
+          const uint32_t y = __builtin_bit_cast(uint32_t, j % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale4(e >> 24), 3)
+                                                                : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale4((e >> 8) & 255u), 1));
+          lo[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+          hi[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        }
+        const bf16x8_t vl = __builtin_bit_cast(bf16x8_t, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+        const bf16x8_t vh = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+#pragma unroll
+        for (int f = 0; f < QF; ++f) {
+          o[f][2 * g] = mfma16q(vl, pf[f][s2], o[f][2 * g]);
+          o[f][2 * g] = mfma16q(vl, rest[f][s2], o[f][2 * g]);
+          o[f][2 * g + 1] = mfma16q(vh, pf[f][s2], o[f][2 * g + 1]);
+          o[f][2 * g + 1] = mfma16q(vh, rest[f][s2], o[f][2 * g + 1]);
+        }
+      }
+    if (t + 4 < t1) load_values(t + 4, pv);
+  }
+
+  // the waves' (m, l, o) joined in wave order, query fragment by query fragment
+#pragma unroll
+  for (int f = 0; f < QF; ++f) {
+    if (f) __syncthreads();
+    l[f] = sum_over_groups(l[f]);
+    if (wid > 0) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) xo[wid - 1][dt][lane] = o[f][dt];
+      xml[wid - 1][lane] = make_float2(m[f], l[f]);
+    }
+    __syncthreads();
+    if (wid > 0) continue;
+    float mm = m[f];
+#pragma unroll
+    for (int w = 0; w < 3; ++w) mm = fmaxf(mm, xml[w][lane].x);
+    const float ref = reference_of(mm), e0 = __builtin_amdgcn_exp2f(m[f] - ref);
+    float lt = l[f] * e0;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[f][dt] *= e0;
+#pragma unroll
+    for (int w = 0; w < 3; ++w) {
+      const float2 ml = xml[w][lane];
+      if (ml.x == -INFINITY && ml.y == 0.f) continue;  // a wave without keys
+      const float e = __builtin_amdgcn_exp2f(ml.x - ref);
+      lt += ml.y * e;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[f][dt] += xo[w][dt][lane] * e;
+    }
+    const int rr = row0 + 16 * f + lq;
+    if (rr >= rows) continue;
+    const size_t at = (size_t)(r.first + rr / a.g) * a.H + h * a.g + rr % a.g;
+    if (a.nsplit > 1) {  // uniform: the join reads all of them
+      float* dst = a.po + ((size_t)part * p.T * a.H + at) * DH + 4 * lg;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = o[f][dt];
+      if (lg == 0) a.pml[(size_t)part * p.T * a.H + at] = make_float2(mm, lt);
+    } else {
+      const float inv = lt == 0.f ? 0.f : 1.0f / lt;  // a row without keys is zeros
+      bf16_t* dst = a.out + at * DH + 4 * lg;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        *reinterpret_cast<uint2*>(dst + 16 * dt) =
+            make_uint2(f2bf2(o[f][dt][0] * inv, o[f][dt][1] * inv), f2bf2(o[f][dt][2] * inv, o[f][dt][3] * inv));
+      if (a.lse && lg == 0) a.lse[at] = lt == 0.f ? -INFINITY : mm * 0.6931471805599453f + logf(lt);
+    }
+  }
+}
+
+static int query_fragments4(int g, int max_new) { return (long)g * max_new <= 16 ? 1 : 2; }
+
+// Keys of a part.
+int pages4_attention_span(int Hkv, int g, int B, int max_new, int capacity) {
+  const int qf = query_fragments4(g, max_new);
+  const long rows = (long)g * max_new, units = ((rows + 16 * qf - 1) / (16 * qf)) * Hkv * B;
+  if (qf == 1 && capacity <= 768) return (capacity + 63) / 64 * 64;
+  const long tile = rows < 16 * qf ? rows : 16 * qf, cheap = 128 * tile;
+  long span = ((long)capacity * units + 2047) / 2048;
+  if (span < cheap && units * ((capacity + span - 1) / span) > 256) span = cheap;
+  if (span < 256) span = 256;
+  long parts = (capacity + span / 2) / span;
+  parts = parts < 1 ? 1 : parts > 128 ? 128 : parts;
+  return (int)(((capacity + parts - 1) / parts + 63) / 64 * 64);
+}
+
+template <int DH>
+static void run_pages4_attention(PagesAttn& a, hipStream_t s) {
+  const int qf = query_fragments4(a.g, a.p.max_new);
+  a.row_tiles = (int)(((long)a.g * a.p.max_new + 16 * qf - 1) / (16 * qf));
+  const long items = (long)a.nsplit * a.p.B * a.p.Hkv;
+  const dim3 grid((unsigned)((items + 7) / 8 * 8 * a.row_tiles));
+  if (qf == 1) hipLaunchKernelGGL((pages4_attn_kernel<DH, 1>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((pages4_attn_kernel<DH, 2>), grid, dim3(256), 0, s, a);
+  if (a.nsplit > 1) launch_pages_join(a, s);
+}
+
+void launch_pages4_attention(PagesAttn a, hipStream_t s) {  // T and max_new above 0
+  a.p.dh == 128 ? run_pages4_attention<128>(a, s) : run_pages4_attention<64>(a, s);
+}
+
+}  // namespace dcl
