@@ -1,4 +1,6 @@
 // Pages of 4 bits: keys and values of packed tokens into them and back, and attention from a sequence's newest tokens.
+#include <type_traits>
+
 #include "dcl_internal.h"
 #include "pages_index.h"
 
@@ -253,8 +255,134 @@ __device__ __forceinline__ float sum_over_groups(float v) {
 }
 __device__ __forceinline__ float reference_of(float m) { return m == -INFINITY ? 0.f : m; }
 
+// A query against keys that stay in their 4 bits: gfx950's scaled product takes 128 dimensions of e2m1 times e4m3, every 32 of either
+// side under a power-of-two scale of their own, which is how the keys lie in their pages. The query enters as two e4m3 parts,
+// the nearest and the nearest to what it leaves under a 16th of its scale. Their eight significant bits are a bfloat16's, down
+// to 2^-14 of the group's largest; what is smaller keeps a step of 2^-22 of it. (e4m3 reaches from 2^-9 to 448; the scale is the
+// least power of two with the group's largest at most 448 times it.)
+//
+// The product's own order (found by one-hot operands): lane group g holds dimensions 32 g .. of the e2m1 operand, 16 g .. and 64 +
+// 16 g .. of the e4m3 one; a scale operand's lane group g is that of dimensions 32 g .. on both sides.
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+struct QueryParts {
+  i32x8_t part[2];
+  int scale;  // bytes 0 and 1: the parts' scales of the lane's logical group; 255 where the query is no number
+};
+__device__ __forceinline__ QueryParts query_parts(const bf16_t* q, int lq, int lg, uint32_t sign) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = max(m, magnitude8(*reinterpret_cast<const uint4*>(q + 32 * lg + 8 * i)));
+  int e = (int)(m >> 7) - 8 + ((m & 127) > 96 ? 1 : 0);  // m = 1.f * 2^(E - 127), 448 = 1.75 * 2^8
+  e = m >= 0x7F80u ? 255 : max(e, 5);                    // the second part's is 4 less
+  QueryParts r;
+  r.scale = e == 255 ? 0xFFFF : e | (e - 4) << 8;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int es = __shfl(e, lq + 16 * (2 * half + (lg >> 1)), 64);
+    const float inv = es == 255 ? 0.f : scale4(254 - es);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint4 x = *reinterpret_cast<const uint4*>(q + 64 * half + 16 * lg + 8 * i);
+      const uint32_t w[4] = {x.x ^ sign, x.y ^ sign, x.z ^ sign, x.w ^ sign};
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        int p1 = 0, p2 = 0;
+        float v[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const uint32_t u = w[2 * j + y / 2];
+          v[y] = es == 255 ? 0.f : __uint_as_float(y & 1 ? u & 0xFFFF0000u : u << 16) * inv;
+        }
+        p1 = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], p1, false);
+        p1 = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], p1, true);
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(p1, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(p1, true);
+        p2 = __builtin_amdgcn_cvt_pk_fp8_f32((v[0] - lo[0]) * 16.f, (v[1] - lo[1]) * 16.f, p2, false);
+        p2 = __builtin_amdgcn_cvt_pk_fp8_f32((v[2] - hi[0]) * 16.f, (v[3] - hi[1]) * 16.f, p2, true);
+        r.part[0][4 * half + 2 * i + j] = p1;
+        r.part[1][4 * half + 2 * i + j] = p2;
+      }
+    }
+  }
+  return r;
+}
+
+// One fragment's scores of a tile (C layout: key 16 lg + 4 kt + r, query lq). The reference point m (log2 units) moves only when a
+// score passes it by more than 2^8 (any reference gives the same quotient), so that most tiles need no maximum across the lanes
+// and no rescaling. Returns whether it moved for some lane; then alpha is what the row's sum and output are worth.
+__device__ __forceinline__ bool move_reference(const f32x4_t (&sc)[4], float scale, float& m, float& alpha) {
+  float top = -INFINITY;
+#pragma unroll
+  for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+    for (int rr = 0; rr < 4; ++rr) top = fmaxf(top, sc[kt][rr]);
+  if (__builtin_amdgcn_ballot_w64(top * scale > m + 8.f) == 0) return false;
+  const float ts = max_over_groups(top) * scale;
+  const float mn = ts > m + 8.f ? ts : m;
+  alpha = mn == m ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+  m = mn;
+  return true;
+}
+// The probabilities, as two bfloat16 parts: the nearest and the nearest to what it leaves (2^-16 of each together); the sum l that
+// divides takes them unrounded.
+__device__ __forceinline__ void probabilities(f32x4_t (&sc)[4], float scale, float m, float& l, bf16x8_t (&pf)[2], bf16x8_t (&rest)[2]) {
+  const float mr = -reference_of(m);
+#pragma unroll
+  for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+    for (int rr = 0; rr < 4; ++rr) {
+      sc[kt][rr] = __builtin_amdgcn_exp2f(fmaf(sc[kt][rr], scale, mr));
+      l += sc[kt][rr];
+    }
+#pragma unroll
+  for (int s2 = 0; s2 < 2; ++s2) {
+    const f32x4_t &x = sc[2 * s2], &y = sc[2 * s2 + 1];
+    const uint4 w = make_uint4(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(y[0], y[1]), f2bf2(y[2], y[3]));
+    auto left = [](uint32_t two, float p0, float p1) {
+      return f2bf2(p0 - __uint_as_float(two << 16), p1 - __uint_as_float(two & 0xFFFF0000u));
+    };
+    pf[s2] = __builtin_bit_cast(bf16x8_t, w);
+    rest[s2] = __builtin_bit_cast(bf16x8_t, make_uint4(left(w.x, x[0], x[1]), left(w.y, x[2], x[3]),
+                                                       left(w.z, y[0], y[1]), left(w.w, y[2], y[3])));
+  }
+}
+
+// Eight keys of the two dimensions that share a byte: converted under each key's scale, then two keys of a dimension side by side.
+// w, e: two words of bytes and of scale bytes. A conversion takes its scale's exponent bits alone (found so for all of them): the
+// byte is shifted there, with what comes along.
+__device__ __forceinline__ void widen_values8(const uint32_t (&w)[2], const uint32_t (&e)[2], uint4& lo, uint4& hi) {
+  uint32_t l[4], h[4];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], __uint_as_float(e[j] << 23), 0));
+    const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], __uint_as_float(e[j] << 15), 1));
+    const uint32_t c = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], __uint_as_float(e[j] << 7), 2));
+    const uint32_t d = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], __uint_as_float(e[j] >> 1), 3));
+    l[2 * j] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+    h[2 * j] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    l[2 * j + 1] = __builtin_amdgcn_perm(d, c, 0x05040100u);
+    h[2 * j + 1] = __builtin_amdgcn_perm(d, c, 0x07060302u);
+  }
+  lo = make_uint4(l[0], l[1], l[2], l[3]);
+  hi = make_uint4(h[0], h[1], h[2], h[3]);
+}
+
+// Scale bytes of four keys: those that are not there (`keep` masks the ones that are) become 1, so that any code is a number. Where
+// a group of NaN is left, it becomes 1 too and the return value is not 0: the rows that see it are given NaN apart.
+__device__ __forceinline__ uint32_t sane_scales(uint32_t& s, uint32_t keep) {
+  s = (s & keep) | (0x7F7F7F7Fu & ~keep);
+  const uint32_t odd = ((s & 0x7F7F7F7Fu) + 0x01010101u) & s & 0x80808080u;  // a byte of 255
+  s ^= odd;                                                                   // 255 -> 127
+  return odd;
+}
+__device__ __forceinline__ uint32_t first_bytes(int n) {  // a mask of the first n bytes of a word
+  return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+}
+
 template <int DH, int QF>
-__global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages4_attn_kernel(PagesAttn a) {
+__global__ void __launch_bounds__(256, QF == 1 ? 3 : 2) pages4_attn_kernel(PagesAttn a) {
+  // heads of 64 would leave half of the scaled product empty: their keys are converted to bfloat16
+  constexpr bool SCALED = DH == 128;
   constexpr int KT = 64, NKT = 4, HB = DH / 2, G = DH / 32, KS = DH / 32, DT = DH / 16;
   constexpr int KW = DH / 32;  // words of a lane's dimensions of one key
   __shared__ f32x4_t xo[3][DT][64];
@@ -276,17 +404,23 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages4_attn_kernel(Pages
   const int32_t* row = p.table + (size_t)b * p.max_pages;
 
   // the wave's queries, and how many keys each may see (rows past the last one: like any other, never written)
-  bf16x8_t qf[QF][KS];
+  bf16x8_t qf[SCALED ? 1 : QF][KS];
+  QueryParts qp[SCALED ? QF : 1];
   int lim[QF], lim_min = kend;
 #pragma unroll
   for (int f = 0; f < QF; ++f) {
     const int rr = min(row0 + 16 * f + lq, rows - 1), i = rr / a.g, head = h * a.g + rr % a.g;
-    const bf16_t* qp = a.q + (size_t)(r.first + i) * a.q_stride + (size_t)head * DH + (DH / 4) * lg;
+    const bf16_t* q = a.q + (size_t)(r.first + i) * a.q_stride + (size_t)head * DH;
+    // a negative scale is a sign of the query
+    if constexpr (SCALED) {
+      qp[f] = query_parts(q, lq, lg, a.q_sign);
+    } else {
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      uint4 x = *reinterpret_cast<const uint4*>(qp + 8 * ks);
-      x.x ^= a.q_sign, x.y ^= a.q_sign, x.z ^= a.q_sign, x.w ^= a.q_sign;  // a negative scale is a sign of the query
-      qf[f][ks] = __builtin_bit_cast(bf16x8_t, x);
+      for (int ks = 0; ks < KS; ++ks) {
+        uint4 x = *reinterpret_cast<const uint4*>(q + (DH / 4) * lg + 8 * ks);
+        x.x ^= a.q_sign, x.y ^= a.q_sign, x.z ^= a.q_sign, x.w ^= a.q_sign;
+        qf[f][ks] = __builtin_bit_cast(bf16x8_t, x);
+      }
     }
     lim[f] = a.causal ? min(kend, max(0, len - r.n + i + 1)) : kend;
   }
@@ -310,19 +444,20 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages4_attn_kernel(Pages
   int pid_v = -1;            // page of the lane group's 16 keys of the tile whose values are in vr
   auto load_keys = [&](int t, int pid) {  // pid: page of keys 64 t + 16 la ..
     const int off = (KT * t + 16 * la) & (plen - 1);
-    const size_t ph = (size_t)max(pid, 0) * p.Hkv + h;
-    const uint8_t* base = p.k + (ph * plen + off + lr) * HB + lg * (HB / 4);
+    const size_t ph = (size_t)((unsigned)max(pid, 0)) * p.Hkv + h;
+    const uint8_t* base = p.k + ((ph << p.shift) + (off + lr)) * HB + lg * (HB / 4);
 #pragma unroll
     for (int kt = 0; kt < NKT; ++kt) kr[kt] = *reinterpret_cast<const words_t*>(base + 4 * kt * HB);
-    ksr = *reinterpret_cast<const u32x4q_t*>(p.ks + (ph * G + lg * G / 4) * plen + off);  // byte lr of word kt
+    ksr = *reinterpret_cast<const u32x4q_t*>(p.ks + ((ph * G + lg * G / 4) << p.shift) + off);  // byte lr of word kt
   };
   auto load_values = [&](int t, int pid) {  // pid: page of keys 64 t + 16 lg ..
     const int off = (KT * t + 16 * lg) & (plen - 1);
-    const size_t ph = (size_t)max(pid, 0) * p.Hkv + h;
+    const size_t ph = (size_t)((unsigned)max(pid, 0)) * p.Hkv + h;
+    const uint8_t *vb = p.v + ((ph * HB + lq) << p.shift) + off, *sb = p.vs + ((ph * G) << p.shift) + off;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      vr[g] = *reinterpret_cast<const u32x4q_t*>(p.v + (ph * HB + 16 * g + lq) * plen + off);
-      vsr[g] = *reinterpret_cast<const u32x4q_t*>(p.vs + (ph * G + g) * plen + off);
+      vr[g] = *reinterpret_cast<const u32x4q_t*>(vb + ((size_t)(16 * g) << p.shift));
+      vsr[g] = *reinterpret_cast<const u32x4q_t*>(sb + ((size_t)g << p.shift));
     }
     pid_v = pid;
   };
@@ -348,23 +483,38 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages4_attn_kernel(Pages
     load_keys(t, pk);
     load_values(t, pv);
   }
-  for (; t < t1; t += 4) {
+  // MORE: a tile of this wave follows, whose loads are issued here. The last tile is a call of its own: behind a branch around the
+  // loads, the waits for older ones are counted as if they had not been issued, and wait for them too.
+  auto one_tile = [&](auto more) {
+    constexpr bool MORE = decltype(more)::value;
     const int k0 = KT * t + 16 * lg;  // the lane group's first key
     f32x4_t sc[QF][NKT];
 #pragma unroll
     for (int kt = 0; kt < NKT; ++kt) {
-      const float key_scale = scale4((ksr[kt] >> (8 * lr)) & 255u);
-      bf16x8_t kf[KS];
+      const uint32_t key_scale = ksr[kt] >> (8 * lr);  // in the lowest byte
+      if constexpr (SCALED) {
+        i32x8_t kf = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) kf[ks] = __builtin_bit_cast(bf16x8_t, widen_codes8(kr[kt][ks], key_scale));
+        for (int x = 0; x < KW; ++x) kf[x] = (int)kr[kt][x];
 #pragma unroll
-      for (int f = 0; f < QF; ++f) {
-        sc[f][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int f = 0; f < QF; ++f) {
+          sc[f][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+          sc[f][kt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qp[f].part[0], sc[f][kt], 4, 0, 0, (int)key_scale, 0, qp[f].scale);
+          sc[f][kt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qp[f].part[1], sc[f][kt], 4, 0, 0, (int)key_scale, 1, qp[f].scale);
+        }
+      } else {
+        bf16x8_t kf[KS];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) sc[f][kt] = mfma16q(kf[ks], qf[f][ks], sc[f][kt]);
+        for (int ks = 0; ks < KS; ++ks) kf[ks] = __builtin_bit_cast(bf16x8_t, widen_codes8(kr[kt][ks], __uint_as_float(key_scale << 23)));
+#pragma unroll
+        for (int f = 0; f < QF; ++f) {
+          sc[f][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) sc[f][kt] = mfma16q(kf[ks], qf[f][ks], sc[f][kt]);
+        }
       }
     }
-    if (t + 4 < t1) {
+    if constexpr (MORE) {
       find_pages(t + 4);
       load_keys(t + 4, pk);
     }
@@ -373,88 +523,38 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages4_attn_kernel(Pages
     const bool whole = KT * t + KT <= lim_min && __builtin_amdgcn_ballot_w64(pid_v < 0) == 0;
     if (!whole) {
 #pragma unroll
-      for (int f = 0; f < QF; ++f)
+      for (int f = 0; f < QF; ++f) {
+        const int seen = pid_v < 0 ? 0 : lim[f] - k0;  // of the lane group's keys
 #pragma unroll
         for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
-          for (int rr = 0; rr < 4; ++rr)
-            if (pid_v < 0 || k0 + 4 * kt + rr >= lim[f]) sc[f][kt][rr] = -INFINITY;
-    }
-    // The reference point m (log2 units) moves only when a score passes it by more than 2^8 (any reference gives the same
-    // quotient), so that most tiles need no maximum across the lanes and no rescaling.
-    float tmax[QF];
-    bool move = false;
-#pragma unroll
-    for (int f = 0; f < QF; ++f) {
-      tmax[f] = -INFINITY;
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-        for (int rr = 0; rr < 4; ++rr) tmax[f] = fmaxf(tmax[f], sc[f][kt][rr]);
-      move |= tmax[f] * scale > m[f] + 8.f;
-    }
-    if (__builtin_amdgcn_ballot_w64(move)) {
-#pragma unroll
-      for (int f = 0; f < QF; ++f) {
-        const float ts = max_over_groups(tmax[f]) * scale;
-        const float mn = ts > m[f] + 8.f ? ts : m[f];
-        const float alpha = mn == m[f] ? 1.f : __builtin_amdgcn_exp2f(m[f] - mn);
-        l[f] *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[f][dt] *= alpha;
-        m[f] = mn;
+          for (int rr = 0; rr < 4; ++rr) sc[f][kt][rr] = 4 * kt + rr < seen ? sc[f][kt][rr] : -INFINITY;
       }
     }
-    // The probabilities enter the product as two bfloat16 parts, the nearest and the nearest to what it leaves (2^-16 of each
-    // together); the sum that divides takes them unrounded.
     bf16x8_t pf[QF][2], rest[QF][2];
 #pragma unroll
     for (int f = 0; f < QF; ++f) {
-      const float mr = -reference_of(m[f]);
+      float alpha;
+      if (move_reference(sc[f], scale, m[f], alpha)) {
+        l[f] *= alpha;
 #pragma unroll
-      for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-        for (int rr = 0; rr < 4; ++rr) {
-          sc[f][kt][rr] = __builtin_amdgcn_exp2f(fmaf(sc[f][kt][rr], scale, mr));
-          l[f] += sc[f][kt][rr];
-        }
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) {
-        const f32x4_t &x = sc[f][2 * s2], &y = sc[f][2 * s2 + 1];
-        const uint4 w = make_uint4(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(y[0], y[1]), f2bf2(y[2], y[3]));
-        auto left = [](uint32_t two, float p0, float p1) {
-          return f2bf2(p0 - __uint_as_float(two << 16), p1 - __uint_as_float(two & 0xFFFF0000u));
-        };
-        pf[f][s2] = __builtin_bit_cast(bf16x8_t, w);
-        rest[f][s2] = __builtin_bit_cast(bf16x8_t, make_uint4(left(w.x, x[0], x[1]), left(w.y, x[2], x[3]),
-                                                              left(w.z, y[0], y[1]), left(w.w, y[2], y[3])));
+        for (int dt = 0; dt < DT; ++dt) o[f][dt] *= alpha;
       }
+      probabilities(sc[f], scale, m[f], l[f], pf[f], rest[f]);
     }
-    // Values. In a tile that some row does not see whole, a probability of 0 must meet no NaN: the scales of slots past the last
-    // key become 1 (any code is then a number), and a group of NaN that only some rows see is given to just those.
+    // values: in a tile that some row does not see whole, a probability of 0 must meet no NaN
     if (!whole) {
       const int nv = pid_v < 0 ? 0 : kend - k0;  // the lane group's keys that are there
       uint32_t odd = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int bits = 8 * (nv - 4 * j);
-        const uint32_t keep = bits >= 32 ? ~0u : bits <= 0 ? 0u : (1u << bits) - 1u;
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          const uint32_t s = (vsr[g][j] & keep) | (0x7F7F7F7Fu & ~keep);
-          vsr[g][j] = s;
-          odd |= ((s & 0x7F7F7F7Fu) + 0x01010101u) & s & 0x80808080u;  // a byte of 255
+          uint32_t e = vsr[g][j];
+          odd |= sane_scales(e, first_bytes(nv - 4 * j));
+          vsr[g][j] = e;
         }
-      }
-      if (__builtin_amdgcn_ballot_w64(odd != 0)) {
-        // rare: such groups leave the product and are added key by key
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            const uint32_t s = vsr[g][j], bad = (((s & 0x7F7F7F7Fu) + 0x01010101u) & s & 0x80808080u) >> 7;
-            vsr[g][j] = s ^ (bad << 7);  // 255 -> 127
-          }
+      if (__builtin_amdgcn_ballot_w64(odd != 0)) {  // rare
 #pragma unroll 1
         for (int y = 0; y < KT; ++y) {
           const int key = KT * t + y, pid = page_of(row, p.max_pages, p.n_pages, p.shift, key >> 4);
@@ -473,24 +573,14 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages4_attn_kernel(Pages
         }
       }
     }
-    // A byte is two dimensions, 16 apart, of one key: converted under that key's scale, then two keys of a dimension side by side.
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
-        uint32_t lo[4], hi[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t w = vr[g][2 * s2 + j / 2], e = vsr[g][2 * s2 + j / 2];
-          const uint32_t x = __builtin_bit_cast(uint32_t, j % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale4((e >> 16) & 255u), 2)
-                                                                : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale4(e & 255u), 0));
-          const uint32_t y = __builtin_bit_cast(uint32_t, j % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale4(e >> 24), 3)
-                                                                : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale4((e >> 8) & 255u), 1));
-          lo[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-          hi[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-        }
-        const bf16x8_t vl = __builtin_bit_cast(bf16x8_t, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-        const bf16x8_t vh = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+        uint4 lo, hi;
+        widen_values8({vr[g][2 * s2], vr[g][2 * s2 + 1]}, {vsr[g][2 * s2], vsr[g][2 * s2 + 1]}, lo, hi);
+        const bf16x8_t vl = __builtin_bit_cast(bf16x8_t, lo), vh = __builtin_bit_cast(bf16x8_t, hi);
 #pragma unroll
         for (int f = 0; f < QF; ++f) {
           o[f][2 * g] = mfma16q(vl, pf[f][s2], o[f][2 * g]);
@@ -499,8 +589,19 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages4_attn_kernel(Pages
           o[f][2 * g + 1] = mfma16q(vh, rest[f][s2], o[f][2 * g + 1]);
         }
       }
-    if (t + 4 < t1) load_values(t + 4, pv);
-  }
+    // the conversions of the next eight keys between the products of these (left to itself the compiler groups each kind)
+    __builtin_amdgcn_sched_group_barrier(0x002, 24, 0);
+#pragma unroll
+    for (int i = 0; i < (2 * G - 1) * 4 * QF; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 6 / QF, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 4 * QF, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (MORE) load_values(t + 4, pv);
+  };
+  for (; t + 4 < t1; t += 4) one_tile(std::true_type());
+  if (t < t1) one_tile(std::false_type());
 
   // the waves' (m, l, o) joined in wave order, query fragment by query fragment
 #pragma unroll
@@ -552,16 +653,21 @@ __global__ void __launch_bounds__(256, QF == 1 ? 2 : 1) pages4_attn_kernel(Pages
 
 static int query_fragments4(int g, int max_new) { return (long)g * max_new <= 16 ? 1 : 2; }
 
-// Keys of a part.
+// Keys of a part. Few workgroups: two a CU, or one, as long as they keep 768 or 512 keys, since each starts with a chain of
+// loads; whole multiples of the CUs, since the rest of a round lasts as long as the round. From one a CU on, the parts of about 1536
+// even out the sequences' lengths where a part's output is small beside its keys (one fragment). us by keys of a part, 28 / 4
+// heads, 2 x 1 token over 131072: 1024 38.6, 1536 38.1, 2048 (512 workgroups) 34.3, 4096 (256) 35.0, 5632 41.5; 32 / 8 heads, 80 x 1 over 250
+// to 9000: 512 71.5, 1024 58.0, 1536 56.7, 3072 59.0, 5632 61.6, 16 x 1 over 2000 to 6000: 768 26.3, 1024 24.2, 1536 (512 workgroups) 23.3, 3072
+// 25.5; 4 x 512 tokens over 4096: whole 209, 1536 282.
 int pages4_attention_span(int Hkv, int g, int B, int max_new, int capacity) {
   const int qf = query_fragments4(g, max_new);
   const long rows = (long)g * max_new, units = ((rows + 16 * qf - 1) / (16 * qf)) * Hkv * B;
-  if (qf == 1 && capacity <= 768) return (capacity + 63) / 64 * 64;
-  const long tile = rows < 16 * qf ? rows : 16 * qf, cheap = 128 * tile;
-  long span = ((long)capacity * units + 2047) / 2048;
-  if (span < cheap && units * ((capacity + span - 1) / span) > 256) span = cheap;
-  if (span < 256) span = 256;
-  long parts = (capacity + span / 2) / span;
+  const long most = qf == 1 ? 1536 : 16384;
+  long parts;
+  if (units >= 256) parts = (capacity + most - 1) / most;
+  else if (capacity >= 768 * (512 / units)) parts = 512 / units;
+  else if (capacity >= 512 * (256 / units)) parts = 256 / units;
+  else parts = capacity / 512;
   parts = parts < 1 ? 1 : parts > 128 ? 128 : parts;
   return (int)(((capacity + parts - 1) / parts + 63) / 64 * 64);
 }

@@ -177,14 +177,29 @@ class Turn:
 
 
 def attention_rows4(q, k, v, scale, sees):
-    """attention_rows for values of which some are exactly 0, so that an output may consist of the least probabilities alone: a
-    probability below 2^-126 of the reference point (which some key of the row has reached, so that they sum to 1 at least) may
-    be flushed to 0, and with it 2^-126 of its value."""
+    """attention_rows with what 4-bit pages add to its bounds.
+
+    Values may be exactly 0, so that an output may consist of the least probabilities alone: a probability below 2^-126 of the
+    reference point (which some key of the row has reached, so that they sum to 1 at least) may be flushed to 0, and with it
+    2^-126 of its value.
+
+    Heads of 128: the query is held as two e4m3 parts with scales s and s / 16 for every 32 dimensions, the largest of which is in (224 s,
+    448 s]. The first part leaves at most half of its step, 16 s at most; the second is e4m3 of that over s / 16, at most
+    256, to half a step: exact where eight significant bits of the element end above 2^-9 s / 16, otherwise within half of
+    that step, 2^-14 s, below 2^-21 of the largest. A score moves by that times the sum of the group's |k|, a
+    probability by twice the largest move of a score relative to itself, the lse by once."""
     o, lse, eo, el = attention_rows(q, k, v, scale, sees)
     for i in range(len(sees)):
         j = sees[i].nonzero()[:, 0]
-        if len(j):
-            eo[i] += v[j].abs().nan_to_num(0, 0, 0).sum(0) * 2.0 ** -126
+        if len(j) == 0:
+            continue
+        eo[i] += v[j].abs().nan_to_num(0, 0, 0).sum(0) * 2.0 ** -126
+        if q.shape[1] == 128:
+            top = q[i].abs().nan_to_num(0, 0, 0).unflatten(0, (4, 32)).amax(-1)
+            move = (k[j].abs().nan_to_num(0, 0, 0).unflatten(1, (4, 32)).sum(-1) @ top) * abs(scale) * 2.0 ** -21
+            p = torch.exp((k[j] @ q[i]) * scale - lse[i])
+            eo[i] += (p @ v[j].abs()).nan_to_num(0, 0, 0) * 2 * float(move.max())
+            el[i] += float(move.max())
     return o, lse, eo, el
 
 

@@ -147,7 +147,7 @@ def test_many_rows(dcl, dh):
 
 def test_many_parts(dcl):
     """More parts than one group of lanes joins, most of them empty for the short sequence, and a page missing from each."""
-    pool = Pool4(dcl, [6000, 300, 0], 32, 1, 128, seed=13)
+    pool = Pool4(dcl, [12000, 300, 0], 32, 1, 128, seed=13)
     missing = pool.table[:2, 3].clone()
     pool.table[:2, 3] = -1
     out, lse, q, cu, _ = attend(dcl, pool, [2, 1, 1], 3, True, 0.09)
@@ -331,3 +331,87 @@ def test_offsets_past_32_bits(dcl):
         o, _, eo, _ = attention_rows4(q[0, h].double()[None], want[0][:, h], want[1][:, h], 0.09,
                                      torch.ones(1, 150, dtype=torch.bool))
         assert bool(((out[0, h].double().cpu() - o[0]).abs() <= eo[0]).all())
+
+
+@pytest.mark.parametrize("dh,heads,hkv,page,lens,counts,causal", [
+    (128, 4, 4, 64, [1280, 700], [64, 64], False),
+    (128, 28, 4, 16, [130, 64, 1], [11, 64, 1], True),
+    (64, 8, 2, 32, [40, 64, 65, 200], [40, 20, 9, 33], True),
+    (64, 3, 1, 128, [129, 900], [12, 100], False),
+    (128, 8, 1, 1024, [1100, 0, 63], [5, 0, 63], True),
+])
+def test_blocks_of_more_than_32_rows(dcl, dh, heads, hkv, page, lens, counts, causal):
+    pool = Pool4(dcl, lens, page, hkv, dh, seed=31, fill=0xA7)
+    out, lse, q, cu, _ = attend(dcl, pool, counts, heads, causal, 0.1, pad=1)
+    check4(pool, out, lse, q, cu, counts, heads, causal, 0.1)
+    assert bool((out[int(cu[-1]):] == 7).all())
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+def test_blocks_with_odd_groups_and_missing_pages(dcl, dh):
+    """In several tiles, seen by all rows, by some and by none."""
+    lens, counts, heads = [400, 190], [60, 64], 4
+    pool = Pool4(dcl, lens, 16, 2, dh, seed=32, fill=0x7F)
+
+    def put(scales, b, x, h, g):
+        scales[pool.table[b, x // 16].long(), h, g, x % 16] = 255
+    for x in (345, 370, 399):
+        put(pool.vs, 0, x, 0, x % (dh // 32))
+    put(pool.vs, 1, 10, 1, 1)
+    put(pool.ks, 1, 150, 0, 0)
+    gone = pool.table[:, 4].clone()
+    pool.table[:, 4] = torch.tensor([-1, pool.n_pages])
+    out, lse, q, cu, _ = attend(dcl, pool, counts, heads, True, 0.1)
+    pool.table[:, 4] = gone
+    check4(pool, out, lse, q, cu, counts, heads, True, 0.1, seen=lambda b, n: torch.arange(n) // 16 != 4)
+    assert torch.isfinite(out[:5]).all() and torch.isnan(out[59, 0]).any() and torch.isfinite(out[59, 2:]).all()
+    again = attend(dcl, pool, counts, heads, True, 0.1)[0]
+    assert torch.equal(attend(dcl, pool, counts, heads, True, 0.1)[0].nan_to_num(3), again.nan_to_num(3))
+
+
+def test_blocks_in_parts(dcl):
+    """Few rows' tiles over a long cache: parts, the last of them short, and a sequence that ends in the first."""
+    pool = Pool4(dcl, [5000, 100], 32, 1, 128, seed=33)
+    out, lse, q, cu, args = attend(dcl, pool, [40, 10], 1, True, 0.09)
+    assert args[-1] > 256                                # the workspace of parts
+    rows = [0, 7, 39, 40, 49]
+    for t in rows:
+        b, i = (0, t) if t < 40 else (1, t - 40)
+        k, v = pool.rows(b)
+        sees = (torch.arange(pool.lens[b]) <= pool.lens[b] - (40, 10)[b] + i)[None]
+        o, s, eo, es = attention_rows4(q[t, 0].double()[None], k[:, 0], v[:, 0], 0.09, sees)
+        assert bool(((out[t, 0] - o[0]).abs() <= eo[0]).all()) and abs(float(lse[t, 0] - s[0])) <= float(es[0]), t
+
+
+@pytest.mark.parametrize("dh,heads,hkv,lens,new", [(64, 4, 4, [64, 900], 1), (128, 8, 2, [64, 1500], 1), (128, 4, 4, [640], 20),
+                                                  (64, 8, 4, [512], 30), (128, 16, 4, [256] * 3, 32)])
+def test_probabilities_keep_sixteen_bits(dcl, dh, heads, hkv, lens, new):
+    """Half of the keys have the probability 1/2 (1 + 0.69 * 2^-7) of a reference's, half of them 1/2, with values 1 and -1: in
+    bfloat16 the first is 1/2 (1 + 2^-7) or 1/2, and rounded so they differ by 2^-8 too much or not at all. o is the difference, some 2^-9;
+    two parts keep each probability to 2^-16, the scores to 2^-20 (four roundings of sums below 2), and the sums of m terms to m *
+    2^-23."""
+    pool = Pool4(dcl, lens, 64, hkv, dh, seed=11)
+    slot = torch.arange(64) % 16
+    kind = torch.where(slot < 2, 0, 1 + slot % 2)
+    code = torch.zeros(64, dh, dtype=torch.int64)
+    code[kind > 0, 0] = 8 + 2                            # -1 in the first 32 dimensions
+    code[kind == 1, 32] = 2                              # 1 under a scale of 2^-7 in the next
+    pool.k[:] = key_bytes(code)
+    pool.ks.fill_(127)
+    pool.ks[:, :, 1] = 120
+    val = torch.zeros(64, dh, dtype=torch.int64)
+    val[kind == 1], val[kind == 2] = 2, 10
+    pool.v[:] = value_bytes(val).T
+    pool.vs.fill_(127)
+    counts = [new] * len(lens)
+    q = torch.zeros(sum(counts), heads, dh, dtype=torch.bfloat16)
+    q[:, :, 0] = q[:, :, 32] = 1
+    out, lse, *_ = attend(dcl, pool, counts, heads, False, math.log(2.0), q=q)
+    for b, n in enumerate(lens):
+        k, v = pool.rows(b)
+        p = torch.exp2(k[:, 0, 0] + k[:, 0, 32])
+        want = float((p * v[:, 0, 0]).sum() / p.sum())
+        assert 2.0 ** -11 < want < 2.0 ** -8
+        got = out[b * new:(b + 1) * new]
+        assert float((got - want).abs().max()) <= want * 2.0 ** -8 + 2.0 ** -16 + 2.0 ** -20 + n * 2.0 ** -23, (b, want)
+        assert float((lse[b * new:(b + 1) * new] - math.log(float(p.sum()))).abs().max()) <= (n + 64) * 2.0 ** -23
