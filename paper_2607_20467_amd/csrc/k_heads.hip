@@ -3,85 +3,123 @@
 
 namespace dcl {
 
-// dh / 8 lanes hold a head, eight dimensions each, so that a wave takes 64 / (dh / 8) heads of a row at a time; the squares are
-// summed over those lanes, and the partner of a rotated dimension, r / 2 further, comes from the lane that holds it. A wave
-// stays with its row, so that angles are worked out once for all of its heads.
+// dh / 8 lanes hold a head, so that a wave takes 64 / (dh / 8) heads of a row at a time. A lane has both dimensions of its four
+// pairs, 4 c .. and r / 2 + 4 c .. (behind the rotated ones, eight that follow each other): nothing is exchanged but the sum
+// of squares, and a wave, which stays with its row, works each angle out once for all of its heads.
 //
 // The angle: pos * turns[i] in float64 is exact to 2^-52 of itself, at most 2^31 / (2 pi) turns, so that its fraction is exact to
-// 2^-23 of a turn at the farthest position and to 2^-24 below 2^28; as float32 in [-0.5, 0.5] it keeps 2^-25.
+// 2^-23 of a turn at the farthest position and to 2^-24 below 2^28; as float32 in [-0.5, 0.5] it keeps 2^-26.
+//
+// Gains and angles meet before the heads do: with x and z a pair's elements times 1 / sqrt(mean + eps), the outputs are
+// x (g_x cos) - z (g_z sin) and z (g_z cos) + x (g_x sin).
+
+// Sum over the L lanes (8 or 16, aligned) of a head, by exchanges inside a row of 16 lanes.
+template <int CTRL>
+__device__ __forceinline__ float plus_lane(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+template <int L>
+__device__ __forceinline__ float sum_head(float v) {
+  v = plus_lane<0xB1>(v);                          // quads 1 0 3 2
+  v = plus_lane<0x4E>(v);                          // quads 2 3 0 1
+  v = plus_lane<0x141>(v);                         // lane 7 - i of eight
+  return L == 16 ? plus_lane<0x140>(v) : v;        // lane 15 - i of sixteen
+}
+
 template <int DH>
-__global__ void __launch_bounds__(256) heads_kernel(HeadsArgs a, int chunks, int per) {
+__global__ void __launch_bounds__(256) heads_kernel(HeadsArgs a, int groups_q, int groups, int per) {
   constexpr int L = DH / 8, HW = 64 / L;  // lanes of a head, heads of a wave
   const int lane = threadIdx.x & 63, c = lane % L, sub = lane / L;
-  const long unit = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int t = (int)(unit / chunks), chunk = (int)(unit % chunks);
+  const int t = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (t >= a.T) return;
   const int pos = a.pos[t];
   if (pos < 0) return;
-  const int half = a.rot / 2, d0 = 8 * c;
-  const bool turned = d0 < a.rot, upper = d0 >= half;
-  float cs[8], sn[8];
+  const bool turned = c < a.rot / 8;
+  const int dx = turned ? 4 * c : a.rot + 8 * (c - a.rot / 8), dz = turned ? a.rot / 2 + 4 * c : dx + 4;
+  float cs[4], sn[4];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int e = 0; e < 4; ++e) {
     cs[e] = 1.f;
     sn[e] = 0.f;
   }
   if (turned) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const double turns = (double)pos * a.turns[(upper ? d0 - half : d0) + e];
+    for (int e = 0; e < 4; ++e) {
+      const double turns = (double)pos * a.turns[dx + e];
       sincospif(2.0f * (float)(turns - rint(turns)), &sn[e], &cs[e]);
-      if (!upper) sn[e] = -sn[e];
     }
   }
-  const int partner = turned ? sub * L + c + (upper ? -half / 8 : half / 8) : lane;
-  const int total = a.H + a.Hkv, h1 = min((chunk + 1) * per * HW, total);
-  for (int h0 = chunk * per * HW; h0 < h1; h0 += HW) {
-    const int h = h0 + sub;
-    const bool mine = h < h1, key = h >= a.H;
-    const int hh = key ? h - a.H : h;
-    const float* gain = key ? a.g_k : a.g_q;
-    uint4 w = make_uint4(0, 0, 0, 0);
-    if (mine) w = *reinterpret_cast<const uint4*>((key ? a.k + t * a.k_stride : a.q + t * a.q_stride) + (size_t)hh * DH + d0);
-    float x[8];
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+  // groups of HW heads: those of the queries, then those of the keys
+  auto some = [&](const bf16_t* in, bf16_t* out, int heads, const float* gain, int g0, int g1) {
+    if (g0 >= g1) return;
+    float gx[4], gz[4], xs[4], zs[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(u[i] << 16);
-      x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    for (int e = 0; e < 4; ++e) gx[e] = gz[e] = 1.f;
+    if (gain) {
+      const float4 p = *reinterpret_cast<const float4*>(gain + dx), q = *reinterpret_cast<const float4*>(gain + dz);
+      gx[0] = p.x, gx[1] = p.y, gx[2] = p.z, gx[3] = p.w;
+      gz[0] = q.x, gz[1] = q.y, gz[2] = q.z, gz[3] = q.w;
     }
-    float ss = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-#pragma unroll
-    for (int o = L / 2; o >= 1; o >>= 1) ss += __shfl_xor(ss, o, 64);
-    if (mine && gain) {
-      const float inv = 1.0f / sqrtf(ss * (1.0f / DH) + a.eps);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * gain[d0 + e];
+    for (int e = 0; e < 4; ++e) {
+      xs[e] = gx[e] * sn[e];
+      zs[e] = gz[e] * sn[e];
+      gx[e] *= cs[e];
+      gz[e] *= cs[e];
     }
-    float y[8];
+    for (int g = g0; g < g1; ++g) {
+      const int h = g * HW + sub;
+      if (h >= heads) continue;  // a head's lanes together
+      const bf16_t* src = in + (size_t)h * DH;
+      const uint2 ux = *reinterpret_cast<const uint2*>(src + dx), uz = *reinterpret_cast<const uint2*>(src + dz);
+      float x[4] = {__uint_as_float(ux.x << 16), __uint_as_float(ux.x & 0xFFFF0000u), __uint_as_float(ux.y << 16),
+                    __uint_as_float(ux.y & 0xFFFF0000u)};
+      float z[4] = {__uint_as_float(uz.x << 16), __uint_as_float(uz.x & 0xFFFF0000u), __uint_as_float(uz.y << 16),
+                    __uint_as_float(uz.y & 0xFFFF0000u)};
+      if (gain) {
+        float ss = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float other = __shfl(x[e], partner, 64);
-      y[e] = turned ? fmaf(other, sn[e], x[e] * cs[e]) : x[e];
+        for (int e = 0; e < 4; ++e) ss = fmaf(x[e], x[e], fmaf(z[e], z[e], ss));
+        const float inv = rsqrtf(sum_head<L>(ss) * (1.0f / DH) + a.eps);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] *= inv;
+          z[e] *= inv;
+        }
+      }
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        y[e] = fmaf(x[e], gx[e], -(z[e] * zs[e]));
+        y[4 + e] = fmaf(z[e], gz[e], x[e] * xs[e]);
+      }
+      if (!turned) {  // an infinity of the one is nothing to the other
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          y[e] = x[e] * gx[e];
+          y[4 + e] = z[e] * gz[e];
+        }
+      }
+      bf16_t* dst = out + (size_t)h * DH;
+      *reinterpret_cast<uint2*>(dst + dx) = make_uint2(f2bf2(y[0], y[1]), f2bf2(y[2], y[3]));
+      *reinterpret_cast<uint2*>(dst + dz) = make_uint2(f2bf2(y[4], y[5]), f2bf2(y[6], y[7]));
     }
-    if (mine)
-      *reinterpret_cast<uint4*>((key ? a.k_out + t * a.k_out_stride : a.q_out + t * a.q_out_stride) + (size_t)hh * DH + d0) =
-          make_uint4(f2bf2(y[0], y[1]), f2bf2(y[2], y[3]), f2bf2(y[4], y[5]), f2bf2(y[6], y[7]));
-  }
+  };
+  const int g0 = blockIdx.y * per, g1 = min(g0 + per, groups);
+  some(a.q + t * a.q_stride, a.q_out + t * a.q_out_stride, a.H, a.g_q, g0, min(g1, groups_q));
+  some(a.k + t * a.k_stride, a.k_out + t * a.k_out_stride, a.Hkv, a.g_k, max(g0, groups_q) - groups_q, g1 - groups_q);
 }
 
 void launch_heads_norm_rope(const HeadsArgs& a, hipStream_t s) {  // T above 0
-  const int HW = 512 / a.dh, groups = (a.H + a.Hkv + HW - 1) / HW;
-  // a wave per group of heads while that leaves CUs idle, otherwise a wave per row
+  const int HW = 512 / a.dh, gq = (a.H + HW - 1) / HW, groups = gq + (a.Hkv + HW - 1) / HW;
+  // a wave per group of heads while that leaves CUs idle, otherwise about 16384 of them, that share a row evenly
   const long waves = (long)a.T * groups;
-  int per = 1;
-  while (per < groups && waves / (2 * per) >= 8192) per *= 2;
-  const int chunks = (groups + per - 1) / per;
-  const dim3 grid((unsigned)(((long)a.T * chunks + 3) / 4));
-  if (a.dh == 128) hipLaunchKernelGGL((heads_kernel<128>), grid, dim3(256), 0, s, a, chunks, per);
-  else hipLaunchKernelGGL((heads_kernel<64>), grid, dim3(256), 0, s, a, chunks, per);
+  int chunks = (int)(waves <= 16384 ? groups : 16384 / a.T);
+  chunks = chunks < 1 ? 1 : chunks;
+  const int per = (groups + chunks - 1) / chunks;
+  const dim3 grid((unsigned)((a.T + 3) / 4), (unsigned)((groups + per - 1) / per));
+  if (a.dh == 128) hipLaunchKernelGGL((heads_kernel<128>), grid, dim3(256), 0, s, a, gq, groups, per);
+  else hipLaunchKernelGGL((heads_kernel<64>), grid, dim3(256), 0, s, a, gq, groups, per);
 }
 
 }  // namespace dcl

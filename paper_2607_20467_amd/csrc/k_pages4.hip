@@ -54,9 +54,6 @@ typedef uint32_t u32x4p_t __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void stream_store(void* p, const uint4& x) {
   __builtin_nontemporal_store(__builtin_bit_cast(u32x4p_t, x), static_cast<u32x4p_t*>(p));
 }
-__device__ __forceinline__ void stream_store(void* p, uint32_t x) {
-  __builtin_nontemporal_store(x, static_cast<uint32_t*>(p));
-}
 __device__ __forceinline__ uint4 stream_load(const void* p) {
   return __builtin_bit_cast(uint4, __builtin_nontemporal_load(static_cast<const u32x4p_t*>(p)));
 }
@@ -72,7 +69,7 @@ __global__ void __launch_bounds__(256) pages4_write_kernel(Pages p, const bf16_t
                                                           const bf16_t* __restrict__ v, long vst, int groups) {
   constexpr int L = DH / 8, TPR = 256 / L, R = kGroup4 / TPR, G = DH / 32, HB = DH / 2;
   constexpr int PITCH = HB + 4;
-  __shared__ __attribute__((aligned(16))) uint8_t sv[kGroup4 * PITCH], ss[2][G][kGroup4];
+  __shared__ __attribute__((aligned(16))) uint8_t sv[kGroup4 * PITCH], sk[kGroup4 * HB], ss[2][G][kGroup4];
   const int h = blockIdx.x % p.Hkv, gb = blockIdx.x / p.Hkv, grp = gb % groups, b = gb / groups;
   const SeqRows r = seq_rows(p.cu, b, p.T);
   const int n = min(r.n, p.max_new), start = seq_len(p.len, b) - r.n;  // position of the first row
@@ -93,9 +90,7 @@ __global__ void __launch_bounds__(256) pages4_write_kernel(Pages p, const bf16_t
   }
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    const int local = i * TPR + tid / L, t = g0 + local - start;
-    const int page = t >= 0 && t < n ? page_of(row, p.max_pages, p.n_pages, p.shift, (g0 + local) >> 4) : -1;
-    const size_t slot = ((size_t)max(page, 0) * p.Hkv + h) * plen + ((g0 + local) & (plen - 1));
+    const int local = i * TPR + tid / L;
     uint32_t ak = magnitude8(xk[i]), av = magnitude8(xv[i]);
 #pragma unroll
     for (int o = 2; o >= 1; o >>= 1) {  // four lanes hold a group
@@ -105,7 +100,7 @@ __global__ void __launch_bounds__(256) pages4_write_kernel(Pages p, const bf16_t
     const bool odd_k = ak >= 0x7F80u, odd_v = av >= 0x7F80u;
     const int ek = odd_k ? 255 : e2m1_exponent(ak), ev = odd_v ? 255 : e2m1_exponent(av);
     const uint32_t qk = odd_k ? 0u : codes8(xk[i], scale4(ek)), qv = odd_v ? 0u : codes8(xv[i], scale4(ev));
-    if (page >= 0) stream_store(p.k + slot * HB + 4 * c, qk);
+    *reinterpret_cast<uint32_t*>(sk + local * HB + 4 * c) = qk;
     const uint32_t other = (uint32_t)__shfl_xor((int)qv, 2, 64);
     const bool upper = (c & 2) != 0;
     // the lower lane makes the bytes of its first four dimensions, the upper one those of its last four
@@ -117,6 +112,16 @@ __global__ void __launch_bounds__(256) pages4_write_kernel(Pages p, const bf16_t
     }
   }
   __syncthreads();
+  // keys in pieces of 16 bytes, those of a page one behind the other
+#pragma unroll
+  for (int u = tid; u < kGroup4 * (HB / 16); u += 256) {
+    const int local = u / (HB / 16), x = g0 + local;
+    if (x < start || x >= start + n) continue;
+    const int page = page_of(row, p.max_pages, p.n_pages, p.shift, x >> 4);
+    if (page >= 0)
+      stream_store(p.k + (((size_t)page * p.Hkv + h) * plen + (x & (plen - 1))) * HB + 16 * (u % (HB / 16)),
+                   *reinterpret_cast<const uint4*>(sk + 16 * u));
+  }
   // rows of positions: HB of values, 2 G of scales
   for (int u = tid; u < (HB + 2 * G) * 4; u += 256) {
     const int ch = u & 3, d = u >> 2, p0 = g0 + 16 * ch;
@@ -159,7 +164,7 @@ __global__ void __launch_bounds__(256) pages4_read_kernel(Pages p, bf16_t* __res
                                                          long vst, int groups) {
   constexpr int L = DH / 8, TPR = 256 / L, R = kGroup4 / TPR, G = DH / 32, HB = DH / 2;
   constexpr int PITCH = kGroup4 + 4;
-  __shared__ __attribute__((aligned(16))) uint8_t sv[HB * PITCH];
+  __shared__ __attribute__((aligned(16))) uint8_t sv[HB * PITCH], sk[kGroup4 * HB];
   const int h = blockIdx.x % p.Hkv, gb = blockIdx.x / p.Hkv, grp = gb % groups, b = gb / groups;
   const SeqRows r = seq_rows(p.cu, b, p.T);
   const int n = min(r.n, p.max_new), start = seq_len(p.len, b) - r.n;
@@ -167,20 +172,27 @@ __global__ void __launch_bounds__(256) pages4_read_kernel(Pages p, bf16_t* __res
   if (g0 >= start + n) return;
   const int32_t* row = p.table + (size_t)b * p.max_pages;
   const int plen = 1 << p.shift, tid = threadIdx.x, c = tid % L;
-  uint32_t xk[R], ks[R], vs[R], held = 0;
+  uint32_t ks[R], vs[R], held = 0;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int local = i * TPR + tid / L, t = g0 + local - start;
     const int page = t >= 0 && t < n ? page_of(row, p.max_pages, p.n_pages, p.shift, (g0 + local) >> 4) : -1;
     const size_t ph = (size_t)max(page, 0) * p.Hkv + h;
     const int off = (g0 + local) & (plen - 1);
-    xk[i] = ks[i] = vs[i] = 0;
+    ks[i] = vs[i] = 0;
     if (page >= 0) {
       held |= 1u << i;
-      xk[i] = *reinterpret_cast<const uint32_t*>(p.k + (ph * plen + off) * HB + 4 * c);
       ks[i] = p.ks[(ph * G + (c >> 2)) * plen + off];
       vs[i] = p.vs[(ph * G + (c >> 2)) * plen + off];
     }
+  }
+#pragma unroll
+  for (int u = tid; u < kGroup4 * (HB / 16); u += 256) {
+    const int x = g0 + u / (HB / 16);
+    const int page = x >= start && x < start + n ? page_of(row, p.max_pages, p.n_pages, p.shift, x >> 4) : -1;
+    if (page >= 0)
+      *reinterpret_cast<uint4*>(sk + 16 * u) =
+          *reinterpret_cast<const uint4*>(p.k + (((size_t)page * p.Hkv + h) * plen + (x & (plen - 1))) * HB + 16 * (u % (HB / 16)));
   }
 #pragma unroll
   for (int u = tid; u < HB * 4; u += 256) {
@@ -207,7 +219,7 @@ __global__ void __launch_bounds__(256) pages4_read_kernel(Pages p, bf16_t* __res
       uint32_t w = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) w |= ((uint32_t)(s[e * PITCH] >> half) & 15u) << (4 * e);
-      ok = widen_codes8(xk[i], scale4(ks[i]));
+      ok = widen_codes8(*reinterpret_cast<const uint32_t*>(sk + local * HB + 4 * c), scale4(ks[i]));
       ov = widen_codes8(w, scale4(vs[i]));
     }
     stream_store(k + at * kst + (size_t)h * DH + 8 * c, ok);

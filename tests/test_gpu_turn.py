@@ -74,10 +74,14 @@ def state(r, B, page, width, lo, hi, spare):
     (64, 64, 8, 400, 1, 64, 40),
     (200, 16, 5, 60, 20, 5000, 150),        # too few pages for the last ones
     (300, 32, 4, 100, 25, 2000, 4000),      # too few rows, and rows of the table that are full
+    (256, 16, 8, 100, 5, 1024, 300),        # a small workgroup's most
+    (257, 16, 8, 100, 5, 1024, 300),
     (1024, 16, 16, 200, 3, 4000, 1000),     # one launch's most
     (1025, 16, 6, 60, 3, 4000, 1000),       # and one more
     (700, 16, 40, 500, 60, 30000, 1700),    # more rows than one launch has
     (3000, 16, 3, 40, 5, 9000, 900),
+    (4097, 16, 3, 40, 2, 9000, 3000),       # more than one window
+    (65536, 16, 2, 30, 2, 60000, 20000),
 ])
 def test_many_turns_match_the_rules(dcl, B, page, width, hi, most, T, spare):
     r = random.Random(B)
