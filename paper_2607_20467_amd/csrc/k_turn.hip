@@ -16,36 +16,48 @@ constexpr uint32_t kMost = 0x7FFFFFFFu;
 
 __device__ __forceinline__ uint32_t add_up(uint32_t a, uint32_t b) { return min(a + b, kMost); }
 
-// Inclusive running sum over the workgroup's W threads, on top of `before`. `sh`: W / 64 words.
-template <int W>
-__device__ __forceinline__ uint32_t running_sum(uint32_t v, uint32_t before, uint32_t* sh) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t x = (uint32_t)__shfl_up((int)v, o, 64);
-    if (lane >= o) v = add_up(v, x);
-  }
-  __syncthreads();
-  if (lane == 63) sh[w] = v;
-  __syncthreads();
-  uint32_t base = before;
-#pragma unroll
-  for (int i = 0; i < W / 64; ++i)
-    if (i < w) base = add_up(base, sh[i]);
-  return add_up(base, v);
-}
-// What the last thread has, for all.
-template <int W>
-__device__ __forceinline__ uint32_t last_of(uint32_t v, uint32_t* sh) {
-  __syncthreads();
-  if (threadIdx.x == W - 1) sh[0] = v;
-  __syncthreads();
-  const uint32_t r = sh[0];
-  __syncthreads();
-  return r;
+// What these workgroups' threads exchange goes through LDS alone, so that a barrier need not wait for loads and stores on their way.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-__device__ __forceinline__ int pages_for(int n, int shift) { return (int)(((long)n + (1 << shift) - 1) >> shift); }
+// Inclusive running sum over the wave: inside rows of 16 lanes, then the rows' last lanes on the rows behind them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t plus_shifted(uint32_t v) {
+  return add_up(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
+  v = plus_shifted<0x111, 0xF>(v);
+  v = plus_shifted<0x112, 0xF>(v);
+  v = plus_shifted<0x114, 0xF>(v);
+  v = plus_shifted<0x118, 0xF>(v);
+  v = plus_shifted<0x142, 0xA>(v);
+  return plus_shifted<0x143, 0xC>(v);
+}
+
+// Inclusive running sum over the workgroup's W threads, on top of `all`, which becomes the sum of all. `sh`: W / 64 words, which
+// nothing before the last barrier reads.
+template <int W>
+__device__ __forceinline__ uint32_t running_sum(uint32_t v, uint32_t& all, uint32_t* sh) {
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  v = wave_sum(v);
+  if (lane == 63) sh[w] = v;
+  lds_barrier();
+  // the waves' sums again in a row of 16 lanes
+  uint32_t x = (lane & 15) < W / 64 ? sh[lane & 15] : 0;
+  x = plus_shifted<0x111, 0xF>(x);
+  x = plus_shifted<0x112, 0xF>(x);
+  x = plus_shifted<0x114, 0xF>(x);
+  x = plus_shifted<0x118, 0xF>(x);
+  const uint32_t before = all;
+  all = add_up(all, (uint32_t)__builtin_amdgcn_readlane((int)x, 15));
+  const uint32_t base = w ? add_up(before, (uint32_t)__builtin_amdgcn_readlane((int)x, w - 1)) : before;
+  return add_up(base, v);
+}
+
+__device__ __forceinline__ int pages_for(int n, int shift) { return (n + (1 << shift) - 1) >> shift; }  // n <= 2^28
 
 // Largest b in [lo, hi) with at[b] <= x (at[lo] <= x).
 __device__ __forceinline__ int find_last(const int32_t* at, int lo, int hi, int x) {
@@ -61,6 +73,25 @@ __device__ __forceinline__ int find_last(const int32_t* at, int lo, int hi, int 
 // [2 + B + b] its first page that goes back, [2 + 2 B + g] pages that come back through workgroup g.
 constexpr int kBackGroups = 64;
 size_t pages_turn_ws_ints(int B) { return 2 + 2 * (size_t)B + kBackGroups; }
+
+// The same for the values x, not falling, of a wave's lanes, by all lanes together: 64 borders a look, the first lane's and the last
+// one's place (three looks for 2^16 sequences, where a lane alone waits for sixteen loads one after the other), then each
+// lane between the two.
+__device__ __forceinline__ int wave_find(const int32_t* at, int hi, int x) {
+  int lo = 0;
+  const int lane = threadIdx.x & 63;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) >> 6, i = lo + step * lane;
+    const int n = __popcll(__builtin_amdgcn_ballot_w64(i < hi && at[min(i, hi - 1)] <= x));
+    lo += step * (n - 1);
+    hi = min(lo + step, hi);
+  }
+  return lo;
+}
+__device__ __forceinline__ int find_rising(const int32_t* at, int n, int x) {
+  const int lo = wave_find(at, n, __builtin_amdgcn_readfirstlane(x)), hi = wave_find(at, n, __builtin_amdgcn_readlane(x, 63));
+  return find_last(at, lo, hi + 1, x);
+}
 
 // ---------------------------------------------------------------- extend
 // One packed row: its position, its place, and, where it is a new page's first, the page into the table. start: pages that the
@@ -83,33 +114,36 @@ __device__ __forceinline__ void no_row(const PagesTurn& a, int t) {
 template <int W, bool ROWS>
 __global__ void __launch_bounds__(W) extend_kernel(PagesTurn a) {
   constexpr int IT = ROWS ? 1 : kItems;
-  __shared__ uint32_t sh[W / 64];
+  __shared__ uint32_t sh[3][W / 64];
   __shared__ int32_t s_cu[ROWS ? W + 1 : 1], s_n[ROWS ? W : 1], s_start[ROWS ? W : 1];
   const int tid = threadIdx.x;
   const int list = max(0, min(*a.n_free, a.n_pages));
-  const long capacity = (long)a.max_pages << a.shift;
+  const int capacity = a.max_pages << a.shift;  // at most 2^28
   uint32_t asked = 0, wanted = 0, granted = 0, used = 0;
+  int n[IT], c[IT], n_next[IT], c_next[IT];
+  auto ahead = [&](int b0) {  // the window after this one
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      n_next[i] = b0 + i < a.B ? a.len[b0 + i] : -1;
+      c_next[i] = b0 + i < a.B && a.ask ? a.ask[b0 + i] : 1;
+    }
+  };
+  ahead(tid * IT);
   for (int w = 0; w < a.B; w += W * IT) {
     const int b0 = w + tid * IT;
-    int n[IT], c[IT];
     uint32_t need[IT], sum;
     bool ok[IT];
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const int b = b0 + i;
-      n[i] = c[i] = 0;
-      ok[i] = false;
-      if (b < a.B) {
-        n[i] = a.len[b];
-        c[i] = a.ask ? a.ask[b] : 1;
-        ok[i] = n[i] >= 0 && c[i] >= 0 && (long)n[i] + c[i] <= capacity;
-      }
+      n[i] = n_next[i];
+      c[i] = c_next[i];
+      ok[i] = n[i] >= 0 && n[i] <= capacity && c[i] >= 0 && c[i] <= capacity - n[i];
     }
+    if (!ROWS) ahead(b0 + W * IT);
     sum = 0;
 #pragma unroll
     for (int i = 0; i < IT; ++i) sum += ok[i] ? c[i] : 0;
-    const uint32_t rows = running_sum<W>(sum, asked, sh);
-    uint32_t upto = rows - sum;
+    uint32_t upto = running_sum<W>(sum, asked, sh[0]) - sum;
     sum = 0;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
@@ -118,8 +152,8 @@ __global__ void __launch_bounds__(W) extend_kernel(PagesTurn a) {
       need[i] = ok[i] ? pages_for(n[i] + c[i], a.shift) - pages_for(n[i], a.shift) : 0;
       sum += need[i];
     }
-    const uint32_t pages = running_sum<W>(sum, wanted, sh);
-    uint32_t start = pages - sum;
+    const uint32_t first = running_sum<W>(sum, wanted, sh[1]) - sum;
+    uint32_t start = first;
     sum = 0;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
@@ -128,11 +162,8 @@ __global__ void __launch_bounds__(W) extend_kernel(PagesTurn a) {
       if (ok[i] && need[i]) used = start;
       sum += ok[i] ? c[i] : 0;
     }
-    const uint32_t ends = running_sum<W>(sum, granted, sh);
-    uint32_t end = ends - sum;
-    start = pages;
-#pragma unroll
-    for (int i = 0; i < IT; ++i) start -= need[i];
+    uint32_t end = running_sum<W>(sum, granted, sh[2]) - sum;
+    start = first;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
       const int b = b0 + i;
@@ -150,21 +181,16 @@ __global__ void __launch_bounds__(W) extend_kernel(PagesTurn a) {
       }
       start += need[i];
     }
-    if (!ROWS) {
-      asked = last_of<W>(rows, sh);
-      wanted = last_of<W>(pages, sh);
-      granted = last_of<W>(ends, sh);
-    }
+    if (!ROWS) lds_barrier();  // before sh is written again
   }
   // the sequences that take pages are the first of those that need some: the last one's sum is what the list loses
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) used = max(used, (uint32_t)__shfl_xor((int)used, o, 64));
-  __syncthreads();
-  if ((tid & 63) == 0) sh[tid >> 6] = used;
+  if ((tid & 63) == 0) sh[0][tid >> 6] = used;  // read last before the third sum's barrier
   if (ROWS && tid == 0) s_cu[0] = 0;
-  __syncthreads();
+  lds_barrier();
   if (tid == 0) {
-    for (int i = 1; i < W / 64; ++i) used = max(used, sh[i]);
+    for (int i = 1; i < W / 64; ++i) used = max(used, sh[0][i]);
     a.cu[0] = 0;
     *a.n_free = list - (int)used;
     if (!ROWS) a.ws[0] = list;
@@ -183,14 +209,15 @@ __global__ void __launch_bounds__(W) extend_kernel(PagesTurn a) {
 }
 
 __global__ void __launch_bounds__(256) extend_rows_kernel(PagesTurn a) {
-  const int t = blockIdx.x * 256 + threadIdx.x;
+  const int t = blockIdx.x * 256 + threadIdx.x, end = a.cu[a.B], list = a.ws[0];
+  const int b = find_rising(a.cu, a.B, t);  // every lane of the wave takes part
   if (t >= a.T) return;
-  if (t >= a.cu[a.B]) {
+  if (t >= end) {
     no_row(a, t);
     return;
   }
-  const int b = find_last(a.cu, 0, a.B, t), first = a.cu[b];
-  extend_row(a, t, b, first, a.cu[b + 1] - first, a.len[b], a.ws[2 + b], a.ws[0]);
+  const int first = a.cu[b];
+  extend_row(a, t, b, first, a.cu[b + 1] - first, a.len[b], a.ws[2 + b], list);
 }
 
 void launch_pages_extend(const PagesTurn& a, hipStream_t s) {
@@ -209,69 +236,85 @@ void launch_pages_extend(const PagesTurn& a, hipStream_t s) {
 // ---------------------------------------------------------------- shrink
 // Entries that may go back are numbered through, sequence by sequence; those that name a page are counted, and the i-th of
 // `all` goes to place list + all - 1 - i.
+template <bool WHOLE>
 __device__ __forceinline__ int32_t* back_entry(const PagesTurn& a, const int32_t* start, const int32_t* first, int i) {
-  const int b = find_last(start, 0, a.B, i);
+  const int b = WHOLE ? find_last(start, 0, a.B, i) : find_rising(start, a.B, i);
   return a.table + (size_t)b * a.max_pages + first[b] + (i - start[b]);
 }
 __device__ __forceinline__ bool names_page(const PagesTurn& a, int page) { return page >= 0 && page < a.n_pages; }
 
-// Entries [from, to) of the numbering, in windows of the workgroup: how many name a page.
-template <int W>
+// Entries [from, to) of the numbering, in windows of the workgroup: how many name a page. WHOLE: start and first in LDS. What a
+// thread past the end would look at is the last entry.
+template <int W, bool WHOLE>
 __device__ uint32_t back_count(const PagesTurn& a, const int32_t* start, const int32_t* first, int from, int to, uint32_t* sh) {
-  uint32_t n = 0;
-  for (long i = (long)from + threadIdx.x; i < to; i += W) n += names_page(a, *back_entry(a, start, first, (int)i));
-  return last_of<W>(running_sum<W>(n, 0, sh), sh);
-}
-// The same entries onto the list, `before` of `all` being those of entries before them.
-template <int W>
-__device__ void back_write(const PagesTurn& a, const int32_t* start, const int32_t* first, int from, int to, uint32_t before,
-                           uint32_t all, int list, uint32_t* sh) {
+  uint32_t n = 0, all = 0;
   for (long w = from; w < to; w += W) {
     const long i = w + threadIdx.x;
+    const int32_t* entry = back_entry<WHOLE>(a, start, first, (int)min(i, (long)to - 1));
+    if (i < to) n += names_page(a, *entry);
+  }
+  running_sum<W>(n, all, sh);
+  return all;
+}
+// The same entries onto the list, `before` of `all` being those of entries before them. sh: two times W / 64 words.
+template <int W, bool WHOLE>
+__device__ void back_write(const PagesTurn& a, const int32_t* start, const int32_t* first, int from, int to, uint32_t before,
+                           uint32_t all, int list, uint32_t* sh) {
+  int turn = 0;
+  for (long w = from; w < to; w += W, turn ^= W / 64) {  // a barrier lies between a window's reads of sh and the next but one's writes
+    const long i = w + threadIdx.x;
+    int32_t* entry = back_entry<WHOLE>(a, start, first, (int)min(i, (long)to - 1));
     int page = -1;
     if (i < to) {
-      int32_t* entry = back_entry(a, start, first, (int)i);
       page = *entry;
       *entry = -1;
     }
     const bool real = names_page(a, page);
-    const uint32_t upto = running_sum<W>(real, before, sh);
-    const long place = (long)list + all - upto;
+    const long place = (long)list + all - running_sum<W>(real, before, sh + turn);
     if (real && place < a.n_pages) a.free_pages[place] = page;
-    before = last_of<W>(upto, sh);
   }
 }
 
 template <int W, bool WHOLE>
 __global__ void __launch_bounds__(W) shrink_kernel(PagesTurn a) {
   constexpr int IT = WHOLE ? 1 : kItems;
-  __shared__ uint32_t sh[W / 64];
+  __shared__ uint32_t sh[4][W / 64];
   __shared__ int32_t s_start[WHOLE ? W : 1], s_first[WHOLE ? W : 1];
   const int tid = threadIdx.x;
   const int list = max(0, min(*a.n_free, a.n_pages));
-  const long capacity = (long)a.max_pages << a.shift;
+  const int capacity = a.max_pages << a.shift;  // at most 2^28
   uint32_t total = 0;
+  int len_next[IT], keep_next[IT];
+  auto ahead = [&](int b0) {  // the window after this one
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      len_next[i] = b0 + i < a.B ? a.len[b0 + i] : 0;
+      keep_next[i] = b0 + i < a.B ? a.ask[b0 + i] : -1;
+    }
+  };
+  ahead(tid * IT);
   for (int w = 0; w < a.B; w += W * IT) {
     const int b0 = w + tid * IT;
     uint32_t n[IT], sum = 0;
-    int first[IT];
+    int first[IT], len[IT], keep[IT];
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const int b = b0 + i;
+      len[i] = len_next[i];
+      keep[i] = keep_next[i];
+    }
+    if (!WHOLE) ahead(b0 + W * IT);
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
       n[i] = 0;
       first[i] = 0;
-      if (b < a.B) {
-        const int len = a.len[b], keep = a.ask[b];
-        if (keep >= 0 && keep < len && len <= capacity) {
-          first[i] = pages_for(keep, a.shift);
-          n[i] = pages_for(len, a.shift) - first[i];
-          a.len[b] = keep;
-        }
+      if (keep[i] >= 0 && keep[i] < len[i] && len[i] <= capacity) {
+        first[i] = pages_for(keep[i], a.shift);
+        n[i] = pages_for(len[i], a.shift) - first[i];
+        a.len[b0 + i] = keep[i];
       }
       sum += n[i];
     }
-    const uint32_t upto = running_sum<W>(sum, total, sh);
-    uint32_t at = upto - sum;
+    uint32_t at = running_sum<W>(sum, total, sh[0]) - sum;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
       const int b = b0 + i;
@@ -281,11 +324,11 @@ __global__ void __launch_bounds__(W) shrink_kernel(PagesTurn a) {
       }
       at += n[i];
     }
-    total = last_of<W>(upto, sh);
+    lds_barrier();  // before sh is written again, and s_start read
   }
   if constexpr (WHOLE) {
-    const uint32_t all = back_count<W>(a, s_start, s_first, 0, (int)total, sh);
-    back_write<W>(a, s_start, s_first, 0, (int)total, 0, all, list, sh);
+    const uint32_t all = back_count<W, true>(a, s_start, s_first, 0, (int)total, sh[1]);
+    back_write<W, true>(a, s_start, s_first, 0, (int)total, 0, all, list, sh[2]);
     if (tid == 0) *a.n_free = (int)min((long)list + all, (long)a.n_pages);
   } else if (tid == 0) {
     a.ws[0] = list;
@@ -303,20 +346,22 @@ __global__ void __launch_bounds__(kWindow) back_count_kernel(PagesTurn a) {
   __shared__ uint32_t sh[kWindow / 64];
   int from, to;
   back_span(a, &from, &to);
-  const uint32_t n = back_count<kWindow>(a, a.ws + 2, a.ws + 2 + a.B, from, to, sh);
+  const uint32_t n = back_count<kWindow, false>(a, a.ws + 2, a.ws + 2 + a.B, from, to, sh);
   if (threadIdx.x == 0) a.ws[2 + 2 * a.B + blockIdx.x] = (int)n;
 }
 
 __global__ void __launch_bounds__(kWindow) back_write_kernel(PagesTurn a) {
-  __shared__ uint32_t sh[kWindow / 64];
+  __shared__ uint32_t sh[3][kWindow / 64];
   __shared__ uint32_t s_before;
   int from, to;
   back_span(a, &from, &to);
   const int tid = threadIdx.x, list = a.ws[0];
-  const uint32_t n = tid < kBackGroups ? (uint32_t)a.ws[2 + 2 * a.B + tid] : 0, upto = running_sum<kWindow>(n, 0, sh);
+  const uint32_t n = tid < kBackGroups ? (uint32_t)a.ws[2 + 2 * a.B + tid] : 0;
+  uint32_t all = 0;
+  const uint32_t upto = running_sum<kWindow>(n, all, sh[0]);
   if (tid == (int)blockIdx.x) s_before = upto - n;
-  const uint32_t all = last_of<kWindow>(upto, sh);
-  back_write<kWindow>(a, a.ws + 2, a.ws + 2 + a.B, from, to, s_before, all, list, sh);
+  lds_barrier();
+  back_write<kWindow, false>(a, a.ws + 2, a.ws + 2 + a.B, from, to, s_before, all, list, sh[1]);
   if (blockIdx.x == 0 && tid == 0) *a.n_free = (int)min((long)list + all, (long)a.n_pages);
 }
 
