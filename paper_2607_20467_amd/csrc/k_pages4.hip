@@ -254,6 +254,14 @@ void launch_pages4_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, 
 // Row 4 a + r of score step kt is key 16 a + 4 kt + r of the tile, so that lane group a (= lane / 16) ends up with the
 // probabilities of 16 adjacent keys, which lie in one page, and loads their values as one 16-byte piece of each row of two
 // dimensions.
+//
+// With one token it is bound by HBM behind its starts: 2 sequences of 100000 to 131072 keys, 28 / 4 heads, 133 MB: 30.5 us with the join
+// (5), 4.35 TB/s; 80 of 250 to 9000, 32 / 8 heads, 204 MB: 50 us, 4.1 TB/s. A tile of 64 keys under one fragment takes 400 vector
+// instructions (192 convert its values, 110 are the softmax's) and 40 matrix ones, 1.0 us of a SIMD where HBM brings one in 1.7.
+// Under blocks the two add up: 512 tokens of 4 sequences over 4096 keys, 32 / 8 heads: vector pipes busy 3/4 of the time, matrix pipes
+// 2/5 of it, 196 us, 0.65 PFLOP/s; 64 tokens of 8 over 1280, 32 heads: 25 us. Sharing the converted values between waves through LDS
+// saved a quarter of the vector instructions and lost it again to barriers and LDS reads (8 x 64 tokens 28 to 32 us, 4 x 512 205 to
+// 264); four fragments a wave spill (44 us).
 __device__ __forceinline__ f32x4_t mfma16q(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -281,21 +289,34 @@ struct QueryParts {
   i32x8_t part[2];
   int scale;  // bytes 0 and 1: the parts' scales of the lane's logical group; 255 where the query is no number
 };
-__device__ __forceinline__ QueryParts query_parts(const bf16_t* q, int lq, int lg, uint32_t sign) {
-  uint32_t m = 0;
+struct RawQuery {
+  uint4 x[4];  // the lane's elements as loaded: dimensions 16 lg .. and 64 + 16 lg ..
+};
+__device__ __forceinline__ RawQuery load_query(const bf16_t* q, int lg) {
+  RawQuery r;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) m = max(m, magnitude8(*reinterpret_cast<const uint4*>(q + 32 * lg + 8 * i)));
-  int e = (int)(m >> 7) - 8 + ((m & 127) > 96 ? 1 : 0);  // m = 1.f * 2^(E - 127), 448 = 1.75 * 2^8
-  e = m >= 0x7F80u ? 255 : max(e, 5);                    // the second part's is 4 less
-  QueryParts r;
-  r.scale = e == 255 ? 0xFFFF : e | (e - 4) << 8;
+  for (int i = 0; i < 4; ++i) r.x[i] = *reinterpret_cast<const uint4*>(q + 64 * (i >> 1) + 16 * lg + 8 * (i & 1));
+  return r;
+}
+__device__ __forceinline__ QueryParts query_parts(const RawQuery& q, int lq, int lg, uint32_t sign) {
+  int e[2];  // exponents of the groups that the lane's two halves belong to
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    const int es = __shfl(e, lq + 16 * (2 * half + (lg >> 1)), 64);
-    const float inv = es == 255 ? 0.f : scale4(254 - es);
+    uint32_t m = max(magnitude8(q.x[2 * half]), magnitude8(q.x[2 * half + 1]));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 16, 64));
+    const int b = (int)(m >> 7) - 8 + ((m & 127) > 96 ? 1 : 0);  // m = 1.f * 2^(E - 127), 448 = 1.75 * 2^8
+    e[half] = m >= 0x7F80u ? 255 : max(b, 5);                    // the second part's is 4 less
+  }
+  QueryParts r;
+  const int from = lq + 32 * (lg & 1), e0 = __shfl(e[0], from, 64), e1 = __shfl(e[1], from, 64), es = lg < 2 ? e0 : e1;
+  r.scale = es == 255 ? 0xFFFF : es | (es - 4) << 8;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const bool odd = e[half] == 255;
+    const float inv = odd ? 0.f : scale4(254 - e[half]);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const uint4 x = *reinterpret_cast<const uint4*>(q + 64 * half + 16 * lg + 8 * i);
+      const uint4 x = q.x[2 * half + i];
       const uint32_t w[4] = {x.x ^ sign, x.y ^ sign, x.z ^ sign, x.w ^ sign};
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -304,7 +325,7 @@ __device__ __forceinline__ QueryParts query_parts(const bf16_t* q, int lq, int l
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           const uint32_t u = w[2 * j + y / 2];
-          v[y] = es == 255 ? 0.f : __uint_as_float(y & 1 ? u & 0xFFFF0000u : u << 16) * inv;
+          v[y] = odd ? 0.f : __uint_as_float(y & 1 ? u & 0xFFFF0000u : u << 16) * inv;
         }
         p1 = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], p1, false);
         p1 = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], p1, true);
@@ -415,29 +436,6 @@ __global__ void __launch_bounds__(256, QF == 1 ? 3 : 2) pages4_attn_kernel(Pages
   const int lq = lane & 15, lg = lane >> 4, la = lq >> 2, lr = lq & 3;
   const int32_t* row = p.table + (size_t)b * p.max_pages;
 
-  // the wave's queries, and how many keys each may see (rows past the last one: like any other, never written)
-  bf16x8_t qf[SCALED ? 1 : QF][KS];
-  QueryParts qp[SCALED ? QF : 1];
-  int lim[QF], lim_min = kend;
-#pragma unroll
-  for (int f = 0; f < QF; ++f) {
-    const int rr = min(row0 + 16 * f + lq, rows - 1), i = rr / a.g, head = h * a.g + rr % a.g;
-    const bf16_t* q = a.q + (size_t)(r.first + i) * a.q_stride + (size_t)head * DH;
-    // a negative scale is a sign of the query
-    if constexpr (SCALED) {
-      qp[f] = query_parts(q, lq, lg, a.q_sign);
-    } else {
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        uint4 x = *reinterpret_cast<const uint4*>(q + (DH / 4) * lg + 8 * ks);
-        x.x ^= a.q_sign, x.y ^= a.q_sign, x.z ^= a.q_sign, x.w ^= a.q_sign;
-        qf[f][ks] = __builtin_bit_cast(bf16x8_t, x);
-      }
-    }
-    lim[f] = a.causal ? min(kend, max(0, len - r.n + i + 1)) : kend;
-  }
-  if (a.causal) lim_min = min(kend, max(0, len - r.n + row0 / a.g + 1));
-
   const float scale = a.scale_log2;
   f32x4_t o[QF][DT];
   float m[QF], l[QF];
@@ -454,12 +452,18 @@ __global__ void __launch_bounds__(256, QF == 1 ? 3 : 2) pages4_attn_kernel(Pages
   words_t kr[NKT];           // the tile's keys, values and scales, as loaded
   u32x4q_t vr[G], vsr[G], ksr;
   int pid_v = -1;            // page of the lane group's 16 keys of the tile whose values are in vr
+  // With one fragment a KV head's rows are one tile, and pages are read once: past the caches, so that they keep what is not (2 x 1
+  // token over 131072 keys 33.9 -> 30.5 us, 80 x 1 55.4 -> 50.4).
+  auto fetch = [](auto* src) {
+    if constexpr (QF == 1) return __builtin_nontemporal_load(src);
+    else return *src;
+  };
   auto load_keys = [&](int t, int pid) {  // pid: page of keys 64 t + 16 la ..
     const int off = (KT * t + 16 * la) & (plen - 1);
     const size_t ph = (size_t)((unsigned)max(pid, 0)) * p.Hkv + h;
     const uint8_t* base = p.k + ((ph << p.shift) + (off + lr)) * HB + lg * (HB / 4);
 #pragma unroll
-    for (int kt = 0; kt < NKT; ++kt) kr[kt] = *reinterpret_cast<const words_t*>(base + 4 * kt * HB);
+    for (int kt = 0; kt < NKT; ++kt) kr[kt] = fetch(reinterpret_cast<const words_t*>(base + 4 * kt * HB));
     ksr = *reinterpret_cast<const u32x4q_t*>(p.ks + ((ph * G + lg * G / 4) << p.shift) + off);  // byte lr of word kt
   };
   auto load_values = [&](int t, int pid) {  // pid: page of keys 64 t + 16 lg ..
@@ -468,7 +472,7 @@ __global__ void __launch_bounds__(256, QF == 1 ? 3 : 2) pages4_attn_kernel(Pages
     const uint8_t *vb = p.v + ((ph * HB + lq) << p.shift) + off, *sb = p.vs + ((ph * G) << p.shift) + off;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      vr[g] = *reinterpret_cast<const u32x4q_t*>(vb + ((size_t)(16 * g) << p.shift));
+      vr[g] = fetch(reinterpret_cast<const u32x4q_t*>(vb + ((size_t)(16 * g) << p.shift)));
       vsr[g] = *reinterpret_cast<const u32x4q_t*>(sb + ((size_t)g << p.shift));
     }
     pid_v = pid;
@@ -489,12 +493,40 @@ __global__ void __launch_bounds__(256, QF == 1 ? 3 : 2) pages4_attn_kernel(Pages
     pv = __shfl(ids, 4 * t + lg - base, 64);
   };
 
+  // The wave's queries, and how many keys each may see (rows past the last one: like any other, never written). They are asked for
+  // behind the pages' numbers and before the first tile, and made ready while that is on its way.
+  bf16x8_t qf[SCALED ? 1 : QF][KS];
+  QueryParts qp[SCALED ? QF : 1];
+  RawQuery raw[SCALED ? QF : 1];
+  int lim[QF], lim_min = kend;
+#pragma unroll
+  for (int f = 0; f < QF; ++f) {
+    const int rr = min(row0 + 16 * f + lq, rows - 1), i = rr / a.g, head = h * a.g + rr % a.g;
+    const bf16_t* q = a.q + (size_t)(r.first + i) * a.q_stride + (size_t)head * DH;
+    if constexpr (SCALED) {
+      raw[f] = load_query(q, lg);
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        uint4 x = *reinterpret_cast<const uint4*>(q + (DH / 4) * lg + 8 * ks);
+        x.x ^= a.q_sign, x.y ^= a.q_sign, x.z ^= a.q_sign, x.w ^= a.q_sign;  // a negative scale is a sign of the query
+        qf[f][ks] = __builtin_bit_cast(bf16x8_t, x);
+      }
+    }
+    lim[f] = a.causal ? min(kend, max(0, len - r.n + i + 1)) : kend;
+  }
+  if (a.causal) lim_min = min(kend, max(0, len - r.n + row0 / a.g + 1));
   int t = t0 + wid;
   if (t < t1) {
     find_pages(t);
     load_keys(t, pk);
     load_values(t, pv);
   }
+  if constexpr (SCALED) {
+#pragma unroll
+    for (int f = 0; f < QF; ++f) qp[f] = query_parts(raw[f], lq, lg, a.q_sign);
+  }
+
   // MORE: a tile of this wave follows, whose loads are issued here. The last tile is a call of its own: behind a branch around the
   // loads, the waits for older ones are counted as if they had not been issued, and wait for them too.
   auto one_tile = [&](auto more) {
@@ -667,10 +699,10 @@ static int query_fragments4(int g, int max_new) { return (long)g * max_new <= 16
 
 // Keys of a part. Few workgroups: two a CU, or one, as long as they keep 768 or 512 keys, since each starts with a chain of
 // loads; whole multiples of the CUs, since the rest of a round lasts as long as the round. From one a CU on, the parts of about 1536
-// even out the sequences' lengths where a part's output is small beside its keys (one fragment). us by keys of a part, 28 / 4
-// heads, 2 x 1 token over 131072: 1024 38.6, 1536 38.1, 2048 (512 workgroups) 34.3, 4096 (256) 35.0, 5632 41.5; 32 / 8 heads, 80 x 1 over 250
-// to 9000: 512 71.5, 1024 58.0, 1536 56.7, 3072 59.0, 5632 61.6, 16 x 1 over 2000 to 6000: 768 26.3, 1024 24.2, 1536 (512 workgroups) 23.3, 3072
-// 25.5; 4 x 512 tokens over 4096: whole 209, 1536 282.
+// even out the sequences' lengths where a part's output is small beside its keys (one fragment). us by keys of a part: 2 x 1 token
+// over 131072, 28 / 4 heads: 1024 33.6, 1536 34.0, 2048 (512 workgroups) 31.0, 3072 36.6, 4096 (256) 31.9; 32 / 8 heads, 80 x 1 over 250 to
+// 9000: 640 63, 1024 52.5, 1536 50.3, 3072 51.7; 16 x 1 over 2000 to 6000: 768 25.6, 1024 24.1, 1536 (512) 23.2, 3072 24.9; 4 x 512 tokens over
+// 4096: whole 198, 1536 282.
 int pages4_attention_span(int Hkv, int g, int B, int max_new, int capacity) {
   const int qf = query_fragments4(g, max_new);
   const long rows = (long)g * max_new, units = ((rows + 16 * qf - 1) / (16 * qf)) * Hkv * B;
