@@ -153,10 +153,15 @@ def _ptr(x) -> Optional[int]:
     return x.data_ptr()
 
 
-_I32 = ("int32",)
-_F32 = ("float32",)
-_B16 = ("int16", "bfloat16", "uint16")       # bfloat16 bit patterns
-_I64 = ("int64",)
+class _Kinds(tuple):
+    """Names of element types; ``types`` are torch's, once it is imported."""
+    types = frozenset()
+
+
+_I32 = _Kinds(("int32",))
+_F32 = _Kinds(("float32",))
+_B16 = _Kinds(("int16", "bfloat16", "uint16"))       # bfloat16 bit patterns
+_I64 = _Kinds(("int64",))
 _ANY = None
 
 
@@ -405,7 +410,6 @@ def dcl_debug_gemm_plan(Nw: int, T: int, K: int, lm_head: int = False, max_split
 # Latency counts in these calls, so that a sound argument passes in a few attribute reads; what is wrong with an
 # unsound one is worked out only then.
 _torch = None
-_dtypes = {}
 
 
 def _device():
@@ -414,18 +418,20 @@ def _device():
     global _torch
     if _torch is None:
         import torch
-        _dtypes.update({kinds: frozenset(getattr(torch, k) for k in kinds if hasattr(torch, k))
-                        for kinds in (_I32, _F32, _B16, _I64)})
+        for kinds in (_I32, _F32, _B16, _I64):
+            kinds.types = frozenset(getattr(torch, k) for k in kinds if hasattr(torch, k))
         _torch = torch
-    return _torch.cuda.current_device() if _torch.cuda.is_initialized() else -2
+    return _torch._C._cuda_getDevice() if _torch.cuda.is_initialized() else -2
 
 
 def _here(x, name, where, kinds, numel, dev):
     """``_arg`` for the serving operators, which also refuse a tensor of another device than the current one ``dev``."""
-    if x is None or isinstance(x, int):
-        return x
-    if x.get_device() == dev and x.dtype in _dtypes[kinds] and x.is_contiguous() and x.numel() >= numel:
-        return x.data_ptr()
+    try:
+        if x.get_device() == dev and x.dtype in kinds.types and x.is_contiguous() and x.numel() >= numel:
+            return x.data_ptr()
+    except AttributeError:                              # no tensor: None or an address, or refused below
+        if x is None or isinstance(x, int):
+            return x
     p = _arg(x, name, where, kinds, numel)
     _on_current(x, name, where, dev)
     return p
@@ -446,6 +452,11 @@ def _queue(stream, dev):
 
 
 def _space(ws, where, nbytes, dev):
+    try:
+        if ws.get_device() == dev and ws.is_contiguous() and ws.numel() * ws.element_size() >= nbytes:
+            return ws.data_ptr()
+    except AttributeError:
+        pass
     p = _arg(ws, "ws", where, _ANY, nbytes=nbytes)
     if ws is not None and not isinstance(ws, int):
         _on_current(ws, "ws", where, dev)
@@ -454,18 +465,19 @@ def _space(ws, where, nbytes, dev):
 
 def _packed(x, name, where, T, heads, dim, dev):
     """Address and row stride of a packed operand [>= T, heads, dim] of bfloat16, whose rows may be apart."""
-    if x is None or isinstance(x, int):
-        return x, heads * dim
-    if x.dim() == 3:
+    try:
         n, h, d = x.shape
         step, inner, one = x.stride()
         if (h == heads and d == dim and n >= T and one == 1 and (inner == dim or heads == 1) and x.get_device() == dev
-                and x.dtype in _dtypes[_B16]):
+                and x.dtype in _B16.types):
             return x.data_ptr(), step if T > 1 else heads * dim
+    except (AttributeError, ValueError):                # no tensor, or not of three dimensions
+        if x is None or isinstance(x, int):
+            return x, heads * dim
     bad = None
     if not x.is_cuda:
         bad = "must be a device (cuda) tensor"
-    elif x.dtype not in _dtypes[_B16]:
+    elif x.dtype not in _B16.types:
         bad = f"has dtype {x.dtype}, expected {' or '.join(_B16)}"
     elif x.dim() != 3 or x.shape[1] != heads or x.shape[2] != dim or x.shape[0] < T:
         bad = f"has shape {tuple(x.shape)}, expected ({T}, {heads}, {dim})"
@@ -615,12 +627,15 @@ def dcl_heads_norm_rope(q, k, pos, T: int, n_heads: int, n_kv_heads: int, head_d
     head by head with gains g_q, g_k [head_dim] (float32, or None) and rotated by pos [T]; outputs like them (rows may be
     apart), or the inputs themselves."""
     w, dev = "dcl_heads_norm_rope", _device()
-    (qp, qs), (qo, qos) = (_packed(x, name, w, T, n_heads, head_dim, dev) if n_heads > 0 else (None, 0)
-                           for x, name in ((q, "q"), (q_out, "q_out")))
-    (kp, ks), (ko, kos) = (_packed(x, name, w, T, n_kv_heads, head_dim, dev) if n_kv_heads > 0 else (None, 0)
-                           for x, name in ((k, "k"), (k_out, "k_out")))
-    _check(load_library().dcl_heads_norm_rope(qp, qs, kp, ks, _here(pos, "pos", w, _I32, max(T, 0), dev), T, n_heads,
-                                              n_kv_heads, head_dim, _here(g_q, "g_q", w, _F32, head_dim, dev),
+    qp = qs = qo = qos = kp = ks = ko = kos = 0
+    if n_heads > 0:
+        qp, qs = _packed(q, "q", w, T, n_heads, head_dim, dev)
+        qo, qos = _packed(q_out, "q_out", w, T, n_heads, head_dim, dev)
+    if n_kv_heads > 0:
+        kp, ks = _packed(k, "k", w, T, n_kv_heads, head_dim, dev)
+        ko, kos = _packed(k_out, "k_out", w, T, n_kv_heads, head_dim, dev)
+    _check(load_library().dcl_heads_norm_rope(qp, qs, kp, ks, _here(pos, "pos", w, _I32, T, dev), T, n_heads, n_kv_heads,
+                                              head_dim, _here(g_q, "g_q", w, _F32, head_dim, dev),
                                               _here(g_k, "g_k", w, _F32, head_dim, dev), eps, rope_base, rot_dim, qo, qos,
                                               ko, kos, _queue(stream, dev)), w)
 
@@ -663,7 +678,7 @@ def dcl_sample_tokens(logits, n: int, vocab: int, temperature, top_k, top_p, min
     bad = None
     if not getattr(logits, "is_cuda", False):
         bad = "must be a device (cuda) tensor"
-    elif not f32 and logits.dtype not in _dtypes[_B16]:
+    elif not f32 and logits.dtype not in _B16.types:
         bad = f"has dtype {logits.dtype}, expected float32 or bfloat16"
     elif logits.dim() != 2 or logits.shape[0] < n or logits.shape[1] < vocab:
         bad = f"has shape {tuple(logits.shape)}, the call needs ({n}, {vocab})"
