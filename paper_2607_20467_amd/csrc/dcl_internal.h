@@ -215,8 +215,6 @@ struct PagesAttn {
 // Keys of one part: from sizes that the host knows (capacity: positions that a row of the table can name).
 int pages_attention_span(int Hkv, int g, int B, int max_new, int capacity, int e4m3);
 void launch_pages_attention(PagesAttn a, hipStream_t s);
-// The parts of an attention over pages joined (nsplit > 1).
-void launch_pages_join(const PagesAttn& a, hipStream_t s);
 int pages4_attention_span(int Hkv, int g, int B, int max_new, int capacity);
 void launch_pages4_attention(PagesAttn a, hipStream_t s);
 

@@ -758,17 +758,6 @@ int pages_attention_span(int Hkv, int g, int B, int max_new, int capacity, int e
   return (int)(((capacity + parts - 1) / parts + 63) / 64 * 64);
 }
 
-template <int DH>
-static void run_pages_join(const PagesAttn& a, hipStream_t s) {
-  const bool wide = a.nsplit > 16;
-  const int blocks = wide ? a.H : (a.H + 1024 / DH - 1) / (1024 / DH);
-  const dim3 all((unsigned)blocks * a.p.max_new * a.p.B);
-  if (wide) hipLaunchKernelGGL((pages_join_kernel<DH, true>), all, dim3(256), 0, s, a, blocks);
-  else hipLaunchKernelGGL((pages_join_kernel<DH, false>), all, dim3(256), 0, s, a, blocks);
-}
-
-void launch_pages_join(const PagesAttn& a, hipStream_t s) { a.p.dh == 128 ? run_pages_join<128>(a, s) : run_pages_join<64>(a, s); }
-
 template <int DH, bool E4>
 static void run_pages_attention(PagesAttn& a, hipStream_t s) {
   const int qf = query_fragments(a.p.Hkv, a.g, a.p.B, a.p.max_new, E4);
@@ -778,7 +767,13 @@ static void run_pages_attention(PagesAttn& a, hipStream_t s) {
   if (qf == 1) hipLaunchKernelGGL((pages_attn_kernel<DH, E4, 1>), grid, dim3(256), 0, s, a);
   else if (E4 || qf == 2) hipLaunchKernelGGL((pages_attn_kernel<DH, E4, 2>), grid, dim3(256), 0, s, a);
   else if constexpr (!E4) hipLaunchKernelGGL((pages_attn_kernel<DH, false, 4>), grid, dim3(256), 0, s, a);
-  if (a.nsplit > 1) launch_pages_join(a, s);
+  if (a.nsplit > 1) {
+    const bool wide = a.nsplit > 16;
+    const int blocks = wide ? a.H : (a.H + 1024 / DH - 1) / (1024 / DH);
+    const dim3 all((unsigned)blocks * a.p.max_new * a.p.B);
+    if (wide) hipLaunchKernelGGL((pages_join_kernel<DH, true>), all, dim3(256), 0, s, a, blocks);
+    else hipLaunchKernelGGL((pages_join_kernel<DH, false>), all, dim3(256), 0, s, a, blocks);
+  }
 }
 
 void launch_pages_attention(PagesAttn a, hipStream_t s) {  // T and max_new above 0

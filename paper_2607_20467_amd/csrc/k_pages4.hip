@@ -695,6 +695,80 @@ __global__ void __launch_bounds__(256, QF == 1 ? 3 : 2) pages4_attn_kernel(Pages
   }
 }
 
+// The parts of a (row, head) joined: DH / 4 lanes take its dimensions, G such groups every G-th part, eight of them asked for at
+// once, with their references; then the groups in order. One pass, so that two loads follow each other, the lengths and the parts.
+template <int DH, int G>
+__global__ void __launch_bounds__(256) pages4_join_kernel(PagesAttn a, int head_blocks) {
+  constexpr int L = DH / 4, PER = 256 / L, AT = 8;
+  __shared__ float4 xo[PER][L];
+  __shared__ float2 xml[PER];
+  const Pages& p = a.p;
+  const int hb = blockIdx.x % head_blocks, bi = blockIdx.x / head_blocks, i = bi % p.max_new, b = bi / p.max_new;
+  const SeqRows r = seq_rows(p.cu, b, p.T);
+  const int len = seq_len(p.len, b);
+  const int grp = threadIdx.x / L, c = threadIdx.x % L, head = G > 1 ? hb : hb * PER + grp;
+  if (i >= r.n) return;
+  const bool mine = head < a.H;  // uniform over the workgroup where groups meet
+  const int kend = min(len, p.max_pages << p.shift);
+  const int parts = !mine ? 0 : kend == 0 ? 1 : (kend + a.span - 1) / a.span;
+  const size_t at = (size_t)(r.first + i) * a.H + head, step = (size_t)p.T * a.H;
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s0 = G > 1 ? grp : 0; s0 < parts; s0 += AT * G) {
+    float2 ml[AT];
+    float4 x[AT];
+#pragma unroll
+    for (int j = 0; j < AT; ++j) {
+      const int s = s0 + j * G;
+      ml[j] = make_float2(-INFINITY, 0.f);
+      x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (s < parts) {
+        ml[j] = a.pml[s * step + at];
+        x[j] = *reinterpret_cast<const float4*>(a.po + (s * step + at) * DH + 4 * c);
+      }
+    }
+    float mn = m;
+#pragma unroll
+    for (int j = 0; j < AT; ++j) mn = fmaxf(mn, ml[j].x);
+    const float ref = reference_of(mn), old = __builtin_amdgcn_exp2f(m - ref);
+    l *= old;
+    o.x *= old, o.y *= old, o.z *= old, o.w *= old;
+#pragma unroll
+    for (int j = 0; j < AT; ++j) {
+      // a part without keys that the row sees: (-inf, 0), and zeros for an output
+      const float e = __builtin_amdgcn_exp2f(ml[j].x - ref);
+      l += ml[j].y * e;
+      o.x += x[j].x * e, o.y += x[j].y * e, o.z += x[j].z * e, o.w += x[j].w * e;
+    }
+    m = mn;
+  }
+  if constexpr (G > 1) {
+    xo[grp][c] = o;
+    if (c == 0) xml[grp] = make_float2(m, l);
+    __syncthreads();
+    if (grp > 0) return;
+    float mn = m;
+#pragma unroll
+    for (int s = 1; s < G; ++s) mn = fmaxf(mn, xml[s].x);
+    const float ref = reference_of(mn);
+    l = 0.f;
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int s = 0; s < G; ++s) {
+      const float2 ml = xml[s];
+      const float e = __builtin_amdgcn_exp2f(ml.x - ref);
+      const float4 x = xo[s][c];
+      l += ml.y * e;
+      o.x += x.x * e, o.y += x.y * e, o.z += x.z * e, o.w += x.w * e;
+    }
+    m = mn;
+  }
+  if (!mine) return;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  *reinterpret_cast<uint2*>(a.out + at * DH + 4 * c) = make_uint2(f2bf2(o.x * inv, o.y * inv), f2bf2(o.z * inv, o.w * inv));
+  if (a.lse && c == 0) a.lse[at] = l == 0.f ? -INFINITY : m * 0.6931471805599453f + logf(l);
+}
+
 static int query_fragments4(int g, int max_new) { return (long)g * max_new <= 16 ? 1 : 2; }
 
 // Keys of a part. Few workgroups: two a CU, or one, as long as they keep 768 or 512 keys, since each starts with a chain of
@@ -724,7 +798,14 @@ static void run_pages4_attention(PagesAttn& a, hipStream_t s) {
   const dim3 grid((unsigned)((items + 7) / 8 * 8 * a.row_tiles));
   if (qf == 1) hipLaunchKernelGGL((pages4_attn_kernel<DH, 1>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((pages4_attn_kernel<DH, 2>), grid, dim3(256), 0, s, a);
-  if (a.nsplit > 1) launch_pages_join(a, s);
+  if (a.nsplit > 1) {
+    constexpr int PER = 1024 / DH;  // groups of lanes in a workgroup
+    const bool wide = a.nsplit > 16;
+    const int blocks = wide ? a.H : (a.H + PER - 1) / PER;
+    const dim3 all((unsigned)blocks * a.p.max_new * a.p.B);
+    if (wide) hipLaunchKernelGGL((pages4_join_kernel<DH, PER>), all, dim3(256), 0, s, a, blocks);
+    else hipLaunchKernelGGL((pages4_join_kernel<DH, 1>), all, dim3(256), 0, s, a, blocks);
+  }
 }
 
 void launch_pages4_attention(PagesAttn a, hipStream_t s) {  // T and max_new above 0
