@@ -308,6 +308,8 @@ dcl_status dcl_heads_norm_rope(const void* q, int64_t q_stride, const void* k, i
   if (st == DCL_OK && n_kv_heads > 0) st = check_rows("k_out", k_out, k_out_stride, T, n_kv_heads, head_dim);
   if (st != DCL_OK) return st;
   if (T > 0 && !pos) return fail(DCL_E_ARG, "pos is NULL");
+  if (T > 1 && ((n_heads > 0 && q_out == q && q_out_stride != q_stride) || (n_kv_heads > 0 && k_out == k && k_out_stride != k_stride)))
+    return fail(DCL_E_ARG, "an output over its input needs the input's row stride");
   if (misaligned(g_q, 16) || misaligned(g_k, 16)) return fail(DCL_E_ARG, "g_q / g_k must be 16-byte aligned");
   if (!(eps >= 0.f) || !isfinite(eps)) return fail(DCL_E_ARG, "eps must be >= 0");
   if (!(rope_base > 1.f) || !isfinite(rope_base)) return fail(DCL_E_ARG, "rope_base must be > 1");

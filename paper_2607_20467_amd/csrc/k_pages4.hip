@@ -425,16 +425,24 @@ __global__ void __launch_bounds__(256, QF == 1 ? 3 : 2) pages4_attn_kernel(Pages
   const int u = blockIdx.x, item = (u / (8 * a.row_tiles)) * 8 + (u & 7), tile = (u >> 3) % a.row_tiles;
   if (item >= a.nsplit * p.B * p.Hkv) return;
   const int h = item % p.Hkv, b = (item / p.Hkv) % p.B, part = item / (p.Hkv * p.B);
-  const SeqRows r = seq_rows(p.cu, b, p.T);
-  const int n = min(r.n, p.max_new), rows = n * a.g, row0 = tile * 16 * QF;
-  if (row0 >= rows) return;
-  const int len = seq_len(p.len, b), plen = 1 << p.shift;
-  const int kend = min(len, p.max_pages << p.shift);  // keys that the table can name
-  const int t0 = part * (a.span / KT), t1 = min(t0 + a.span / KT, (kend + KT - 1) / KT);
-  if (part > 0 && t0 >= t1) return;  // part 0 always answers
   const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lq = lane & 15, lg = lane >> 4, la = lq >> 2, lr = lq & 3;
   const int32_t* row = p.table + (size_t)b * p.max_pages;
+  const int t0 = part * (a.span / KT);
+  // Pages of the 64 chunks of 16 keys from `base` on, one a lane, and of the 64 after those: asked for together with the borders and the
+  // length, which they do not depend on (the empty assembly keeps the loads before the branch).
+  int base = t0 * (KT / 16);
+  auto entry = [&](int c) { return row[page_entry(p.max_pages, p.shift, c)]; };
+  auto page_in = [&](int found, int c) { return page_found(found, p.max_pages, p.n_pages, p.shift, c); };
+  int ids = entry(base + lane), ids_next = entry(base + 64 + lane);
+  const SeqRows r = seq_rows(p.cu, b, p.T);
+  const int len = __builtin_amdgcn_readfirstlane(seq_len(p.len, b));
+  asm volatile("" : "+v"(ids), "+v"(ids_next) : "s"(len));
+  const int n = min(r.n, p.max_new), rows = n * a.g, row0 = tile * 16 * QF, plen = 1 << p.shift;
+  const int kend = min(len, p.max_pages << p.shift);  // keys that the table can name
+  const int t1 = min(t0 + a.span / KT, (kend + KT - 1) / KT);
+  if (row0 >= rows || (part > 0 && t0 >= t1)) return;  // part 0 always answers
+  ids = page_in(ids, base + lane);
+  const int lq = lane & 15, lg = lane >> 4, la = lq >> 2, lr = lq & 3;
 
   const float scale = a.scale_log2;
   f32x4_t o[QF][DT];
@@ -478,16 +486,12 @@ __global__ void __launch_bounds__(256, QF == 1 ? 3 : 2) pages4_attn_kernel(Pages
     pid_v = pid;
   };
 
-  // Pages of the 64 chunks of 16 keys from `base` on, one a lane, and of the 64 after those.
-  int base = t0 * (KT / 16);
-  int ids = page_of(row, p.max_pages, p.n_pages, p.shift, base + lane);
-  int ids_next = page_of(row, p.max_pages, p.n_pages, p.shift, base + 64 + lane);
   int pk = -1, pv = -1;
   auto find_pages = [&](int t) {  // of tile t, at most four further than the last one asked for
     if (t * (KT / 16) - base >= 64) {
       base += 64;
-      ids = ids_next;
-      ids_next = page_of(row, p.max_pages, p.n_pages, p.shift, base + 64 + lane);
+      ids = page_in(ids_next, base + lane);
+      ids_next = entry(base + 64 + lane);
     }
     pk = __shfl(ids, 4 * t + la - base, 64);
     pv = __shfl(ids, 4 * t + lg - base, 64);

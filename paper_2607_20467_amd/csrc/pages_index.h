@@ -40,4 +40,14 @@ DCL_HD int page_of(const int32_t* row, int max_pages, int n_pages, int shift, in
   return page >= 0 && page < n_pages ? page : -1;
 }
 
+// The same in two steps, for a load that nothing waits for: the entry to look at (of a row of max_pages >= 1), and the page that
+// what was found there stands for.
+DCL_HD int page_entry(int max_pages, int shift, int c) {
+  const int slot = c >> (shift - 4);
+  return slot < 0 ? 0 : slot < max_pages ? slot : max_pages - 1;
+}
+DCL_HD int page_found(int page, int max_pages, int n_pages, int shift, int c) {
+  return c >= 0 && (c >> (shift - 4)) < max_pages && page >= 0 && page < n_pages ? page : -1;
+}
+
 }  // namespace dcl

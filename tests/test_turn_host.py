@@ -2,6 +2,8 @@
 import ctypes
 import os
 import re
+import shutil
+import subprocess
 
 import pytest
 import torch
@@ -95,7 +97,8 @@ HEADS = dict(q=256, q_stride=128, k=256, k_stride=128, pos=256, T=4, n_heads=2, 
     (dict(head_dim=96), 2, "head_dim"), (dict(g_q=8), 1, "g_q"), (dict(g_k=4), 1, "g_k"), (dict(eps=-1e-6), 1, "eps"),
     (dict(eps=float("nan")), 1, "eps"), (dict(eps=float("inf")), 1, "eps"), (dict(base=1.0), 1, "rope_base"),
     (dict(base=float("nan")), 1, "rope_base"), (dict(base=float("inf")), 1, "rope_base"), (dict(rot=-16), 1, "rot_dim"),
-    (dict(rot=80), 1, "rot_dim"), (dict(rot=24), 1, "rot_dim"),
+    (dict(rot=80), 1, "rot_dim"), (dict(rot=24), 1, "rot_dim"), (dict(q_out_stride=256), 1, "over its input"),
+    (dict(k_stride=192), 1, "over its input"),
 ])
 def test_heads_refusals(dcl, kw, status, word):
     r = dcl.load_library().dcl_heads_norm_rope(*{**HEADS, **kw}.values())
@@ -104,6 +107,41 @@ def test_heads_refusals(dcl, kw, status, word):
 
 def test_heads_without_rows_return_at_once(dcl):
     assert dcl.load_library().dcl_heads_norm_rope(*{**HEADS, **dict(T=0, q=0, pos=0)}.values()) == 0
+
+
+PROBE = r"""
+#include <cstdio>
+#include "pages_index.h"
+using namespace dcl;
+int main() {
+  unsigned s = 1;
+  auto rnd = [&]() { s = s * 1664525u + 1013904223u; return (int)s; };
+  const int odd[] = {0, 1, -1, 2147483647, -2147483647 - 1, 64, 63, 1 << 30, -(1 << 30)};
+  auto any = [&]() { int r = rnd(); return (r & 3) ? odd[(unsigned)r % 9] : r >> ((unsigned)r % 31); };
+  for (long i = 0; i < 2000000; ++i) {
+    int table[4] = {any(), any(), any(), any()};
+    const int n_pages = 1 + (unsigned)any() % 1000, shift = 4 + (unsigned)rnd() % 7, width = 1 + (unsigned)rnd() % 4, c = any();
+    const int at = page_entry(width, shift, c);
+    if (at < 0 || at >= width) return 1;
+    if (page_found(table[at], width, n_pages, shift, c) != page_of(table, width, n_pages, shift, c)) return 2;
+  }
+  std::puts("ok");
+  return 0;
+}
+"""
+
+
+def test_a_page_looked_up_in_two_steps_is_the_same(tmp_path):
+    """Compiled for the host with bounds checking: the entry is always inside the row, the page what page_of gives."""
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("g++ is not installed")
+    src, exe = tmp_path / "probe.cpp", tmp_path / "probe"
+    src.write_text(PROBE)
+    subprocess.run([cxx, "-O1", "-g", "-std=c++17", "-fsanitize=undefined,bounds", "-fno-sanitize-recover=all", "-I",
+                    os.path.join(ROOT, "paper_2607_20467_amd", "csrc"), str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "ok" in r.stdout, (r.returncode, r.stdout, r.stderr)
 
 
 def test_the_binding_checks_pools_and_operands(dcl):
