@@ -412,14 +412,14 @@ __device__ __forceinline__ uint32_t first_bytes(int n) {  // a mask of the first
   return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
 }
 
-template <int DH, int QF>
-__global__ void __launch_bounds__(256, QF == 1 ? 3 : 2) pages4_attn_kernel(PagesAttn a) {
+template <int DH, int QF, int NW>
+__global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_attn_kernel(PagesAttn a) {
   // heads of 64 would leave half of the scaled product empty: their keys are converted to bfloat16
   constexpr bool SCALED = DH == 128;
   constexpr int KT = 64, NKT = 4, HB = DH / 2, G = DH / 32, KS = DH / 32, DT = DH / 16;
   constexpr int KW = DH / 32;  // words of a lane's dimensions of one key
-  __shared__ f32x4_t xo[3][DT][64];
-  __shared__ float2 xml[3][64];
+  __shared__ f32x4_t xo[NW][DT][64];
+  __shared__ float2 xml[NW][64];
   const Pages& p = a.p;
   // units: row tiles of one (part, sequence, KV head) follow each other on one XCD and share its L2
   const int u = blockIdx.x, item = (u / (8 * a.row_tiles)) * 8 + (u & 7), tile = (u >> 3) % a.row_tiles;
@@ -487,7 +487,7 @@ __global__ void __launch_bounds__(256, QF == 1 ? 3 : 2) pages4_attn_kernel(Pages
   };
 
   int pk = -1, pv = -1;
-  auto find_pages = [&](int t) {  // of tile t, at most four further than the last one asked for
+  auto find_pages = [&](int t) {  // of tile t, at most sixteen further than the last one asked for
     if (t * (KT / 16) - base >= 64) {
       base += 64;
       ids = page_in(ids_next, base + lane);
@@ -563,8 +563,8 @@ __global__ void __launch_bounds__(256, QF == 1 ? 3 : 2) pages4_attn_kernel(Pages
       }
     }
     if constexpr (MORE) {
-      find_pages(t + 4);
-      load_keys(t + 4, pk);
+      find_pages(t + NW);
+      load_keys(t + NW, pk);
     }
 
     // the keys that a row does not see: past its limit, past the last key, in no page
@@ -646,55 +646,47 @@ __global__ void __launch_bounds__(256, QF == 1 ? 3 : 2) pages4_attn_kernel(Pages
     }
     __builtin_amdgcn_sched_group_barrier(0x008, 4 * QF, 0);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (MORE) load_values(t + 4, pv);
+    if constexpr (MORE) load_values(t + NW, pv);
   };
-  for (; t + 4 < t1; t += 4) one_tile(std::true_type());
+  for (; t + NW < t1; t += NW) one_tile(std::true_type());
   if (t < t1) one_tile(std::false_type());
 
-  // the waves' (m, l, o) joined in wave order, query fragment by query fragment
+  // The waves' (m, l, o) joined in wave order, query fragment by query fragment: each wave takes every NW-th group of dimensions.
 #pragma unroll
   for (int f = 0; f < QF; ++f) {
     if (f) __syncthreads();
     l[f] = sum_over_groups(l[f]);
-    if (wid > 0) {
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) xo[wid - 1][dt][lane] = o[f][dt];
-      xml[wid - 1][lane] = make_float2(m[f], l[f]);
-    }
+    for (int dt = 0; dt < DT; ++dt) xo[wid][dt][lane] = o[f][dt];
+    xml[wid][lane] = make_float2(m[f], l[f]);
     __syncthreads();
-    if (wid > 0) continue;
-    float mm = m[f];
-#pragma unroll
-    for (int w = 0; w < 3; ++w) mm = fmaxf(mm, xml[w][lane].x);
-    const float ref = reference_of(mm), e0 = __builtin_amdgcn_exp2f(m[f] - ref);
-    float lt = l[f] * e0;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[f][dt] *= e0;
-#pragma unroll
-    for (int w = 0; w < 3; ++w) {
-      const float2 ml = xml[w][lane];
-      if (ml.x == -INFINITY && ml.y == 0.f) continue;  // a wave without keys
-      const float e = __builtin_amdgcn_exp2f(ml.x - ref);
-      lt += ml.y * e;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[f][dt] += xo[w][dt][lane] * e;
-    }
     const int rr = row0 + 16 * f + lq;
-    if (rr >= rows) continue;
+    if (wid >= DT || rr >= rows) continue;
+    float e[NW], mm = -INFINITY, lt = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) mm = fmaxf(mm, xml[w][lane].x);
+    const float ref = reference_of(mm);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float2 ml = xml[w][lane];
+      e[w] = __builtin_amdgcn_exp2f(ml.x - ref);  // a wave without keys: (-inf, 0), and zeros for an output
+      lt += ml.y * e[w];
+    }
     const size_t at = (size_t)(r.first + rr / a.g) * a.H + h * a.g + rr % a.g;
-    if (a.nsplit > 1) {  // uniform: the join reads all of them
-      float* dst = a.po + ((size_t)part * p.T * a.H + at) * DH + 4 * lg;
+    const float inv = lt == 0.f ? 0.f : 1.0f / lt;  // a row without keys is zeros
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = o[f][dt];
-      if (lg == 0) a.pml[(size_t)part * p.T * a.H + at] = make_float2(mm, lt);
-    } else {
-      const float inv = lt == 0.f ? 0.f : 1.0f / lt;  // a row without keys is zeros
-      bf16_t* dst = a.out + at * DH + 4 * lg;
+    for (int dt = wid; dt < DT; dt += NW) {
+      f32x4_t x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-        *reinterpret_cast<uint2*>(dst + 16 * dt) =
-            make_uint2(f2bf2(o[f][dt][0] * inv, o[f][dt][1] * inv), f2bf2(o[f][dt][2] * inv, o[f][dt][3] * inv));
-      if (a.lse && lg == 0) a.lse[at] = lt == 0.f ? -INFINITY : mm * 0.6931471805599453f + logf(lt);
+      for (int w = 0; w < NW; ++w) x += xo[w][dt][lane] * e[w];
+      if (a.nsplit > 1)  // uniform: the join reads all of them
+        *reinterpret_cast<f32x4_t*>(a.po + ((size_t)part * p.T * a.H + at) * DH + 16 * dt + 4 * lg) = x;
+      else
+        *reinterpret_cast<uint2*>(a.out + at * DH + 16 * dt + 4 * lg) = make_uint2(f2bf2(x[0] * inv, x[1] * inv), f2bf2(x[2] * inv, x[3] * inv));
+    }
+    if (wid == 0 && lg == 0) {
+      if (a.nsplit > 1) a.pml[(size_t)part * p.T * a.H + at] = make_float2(mm, lt);
+      else if (a.lse) a.lse[at] = lt == 0.f ? -INFINITY : mm * 0.6931471805599453f + logf(lt);
     }
   }
 }
@@ -775,21 +767,27 @@ __global__ void __launch_bounds__(256) pages4_join_kernel(PagesAttn a, int head_
 
 static int query_fragments4(int g, int max_new) { return (long)g * max_new <= 16 ? 1 : 2; }
 
-// Keys of a part. Few workgroups: two a CU, or one, as long as they keep 768 or 512 keys, since each starts with a chain of
-// loads; whole multiples of the CUs, since the rest of a round lasts as long as the round. From one a CU on, the parts of about 1536
-// even out the sequences' lengths where a part's output is small beside its keys (one fragment). us by keys of a part: 2 x 1 token
-// over 131072, 28 / 4 heads: 1024 33.6, 1536 34.0, 2048 (512 workgroups) 31.0, 3072 36.6, 4096 (256) 31.9; 32 / 8 heads, 80 x 1 over 250 to
-// 9000: 640 63, 1024 52.5, 1536 50.3, 3072 51.7; 16 x 1 over 2000 to 6000: 768 25.6, 1024 24.1, 1536 (512) 23.2, 3072 24.9; 4 x 512 tokens over
-// 4096: whole 198, 1536 282.
+// Keys of a part. Where sequences and heads give fewer workgroups than there are CUs, as many parts as cost least: the workgroups of
+// the fullest CU, each its keys and 300 more for its start, and 900 for a join (a workgroup of eight waves takes about 5 ns a key), over one part and
+// the numbers from as many as all CUs take at once. us so, 28 / 4 heads, 2 x 1 token over 131072 keys, parts of 1536 / 2048 / 3072 / 4096
+// (256 workgroups): 32.4 / 29.7 / 34.7 / 28.7; 32 / 8 heads, 1 x 1 over 20000: 384 / 640 (256) / 1024 / 2048: 14.1 / 12.8 / 13.7 / 17.5, 16 x 1 over 2000 to 6000:
+// 768 / 1536 / 3072 (256): 24.6 / 21.9 / 21.5; 32 / 32 heads, 4 x 1 over 80 to 720: 384 / whole 12.1 / 8.9. From one a CU on, parts of about 1536
+// even out the sequences' lengths where a part's output is small beside its keys (one fragment): 80 x 1 over 250 to 9000: 640 63,
+// 1024 52.5, 1536 50.3, 3072 51.7; 4 x 512 tokens over 4096: whole 198, 1536 282.
 int pages4_attention_span(int Hkv, int g, int B, int max_new, int capacity) {
   const int qf = query_fragments4(g, max_new);
   const long rows = (long)g * max_new, units = ((rows + 16 * qf - 1) / (16 * qf)) * Hkv * B;
   const long most = qf == 1 ? 1536 : 16384;
-  long parts;
-  if (units >= 256) parts = (capacity + most - 1) / most;
-  else if (capacity >= 768 * (512 / units)) parts = 512 / units;
-  else if (capacity >= 512 * (256 / units)) parts = 256 / units;
-  else parts = capacity / 512;
+  long parts = 1;
+  if (units >= 256) {
+    parts = (capacity + most - 1) / most;
+  } else {
+    long best = capacity + 300;
+    for (long k = 256 / units, i = 0; i < 8; ++k, ++i) {
+      const long cost = (units * k + 255) / 256 * (capacity / k + 300) + 900;
+      if (k > 1 && cost < best) best = cost, parts = k;
+    }
+  }
   parts = parts < 1 ? 1 : parts > 128 ? 128 : parts;
   return (int)(((capacity + parts - 1) / parts + 63) / 64 * 64);
 }
@@ -800,8 +798,11 @@ static void run_pages4_attention(PagesAttn& a, hipStream_t s) {
   a.row_tiles = (int)(((long)a.g * a.p.max_new + 16 * qf - 1) / (16 * qf));
   const long items = (long)a.nsplit * a.p.B * a.p.Hkv;
   const dim3 grid((unsigned)((items + 7) / 8 * 8 * a.row_tiles));
-  if (qf == 1) hipLaunchKernelGGL((pages4_attn_kernel<DH, 1>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((pages4_attn_kernel<DH, 2>), grid, dim3(256), 0, s, a);
+  const bool wide_groups = items * a.row_tiles <= 256;  // one a CU: eight waves take its keys (1 x 1 token over 20000: 13.1 / 12.7 us with four / eight)
+  if (qf == 1 && wide_groups) hipLaunchKernelGGL((pages4_attn_kernel<DH, 1, 8>), grid, dim3(512), 0, s, a);
+  else if (qf == 1) hipLaunchKernelGGL((pages4_attn_kernel<DH, 1, 4>), grid, dim3(256), 0, s, a);
+  else if (wide_groups) hipLaunchKernelGGL((pages4_attn_kernel<DH, 2, 8>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((pages4_attn_kernel<DH, 2, 4>), grid, dim3(256), 0, s, a);
   if (a.nsplit > 1) {
     constexpr int PER = 1024 / DH;  // groups of lanes in a workgroup
     const bool wide = a.nsplit > 16;

@@ -415,3 +415,28 @@ def test_probabilities_keep_sixteen_bits(dcl, dh, heads, hkv, lens, new):
         got = out[b * new:(b + 1) * new]
         assert float((got - want).abs().max()) <= want * 2.0 ** -8 + 2.0 ** -16 + 2.0 ** -20 + n * 2.0 ** -23, (b, want)
         assert float((lse[b * new:(b + 1) * new] - math.log(float(p.sum()))).abs().max()) <= (n + 64) * 2.0 ** -23
+
+
+@pytest.mark.parametrize("dh,heads,hkv,page,n,lo,hi,new,causal", [
+    (128, 8, 8, 16, 40, 0, 150, 1, True), (64, 16, 8, 32, 40, 0, 120, 1, True), (128, 4, 4, 16, 24, 20, 120, 110, True),
+    (64, 4, 4, 16, 24, 60, 100, 105, False),
+])
+def test_more_workgroups_than_cus(dcl, dh, heads, hkv, page, n, lo, hi, new, causal):
+    """The kernels' form for many workgroups: one token or a block of each of many sequences, some of them empty, a missing page in
+    one, NaN behind every end and in a key that only the last row sees."""
+    lens = [lo + (37 * i) % (hi - lo + 1) for i in range(n)]
+    counts = [new if new == 1 else 1 + (i * 7) % new if i % 3 == 0 else 0 for i in range(n)]
+    counts = [min(c, max(1, x)) if new > 1 else c for c, x in zip(counts, lens)]
+    assert n * hkv * (1 if new == 1 else (heads // hkv * max(counts) + 31) // 32) > 256
+    pool = Pool4(dcl, lens, page, hkv, dh, seed=41, fill=0x7F)
+    at = next(b for b in range(n) if lens[b] > 3 * page and counts[b])
+    pool.vs[pool.table[at, (lens[at] - 1) // page].long(), 1, 0, (lens[at] - 1) % page] = 255
+    gone = pool.table[at, 1].clone()
+    pool.table[at, 1] = -1
+    out, lse, q, cu, _ = attend(dcl, pool, counts, heads, causal, 0.1, pad=3)
+    pool.table[at, 1] = gone
+
+    def seen(b, m):
+        return torch.arange(m) // page != 1 if b == at else torch.ones(m, dtype=torch.bool)
+    check4(pool, out, lse, q, cu, counts, heads, causal, 0.1, seen=seen)
+    assert bool((out[int(cu[-1]):] == 7).all())
