@@ -343,14 +343,16 @@ dcl_status dcl_pages_shrink(const dcl_pages* pages, int32_t* table, int32_t max_
 /* Keys and values of the tokens into their pages. Tokens whose position no page holds are skipped. E4M3: with amax
  * the largest finite magnitude of the (token, head)'s row, the scale is the least power of two with amax <= 448 *
  * scale (2^-126 for a row of zeros) and elements are x / scale rounded to nearest even; infinities and NaN become
- * NaN. E2M1: the same for every 32 dimensions, with 6 in the place of 448; 32 that hold an infinity or NaN become NaN. No two positions of one call may share a place (a page listed twice): which one stays there is not defined.
- * Pages that several sequences share are fine as long as no token is written to them. */
+ * NaN. E2M1: the same for every 32 dimensions, with 6 in the place of 448; 32 that hold an infinity or NaN become NaN, and a
+ * magnitude of 3.5 * 2^126 or more becomes 3 * 2^126 (the nearest would be 2^128, an infinity). No two positions of one call
+ * may share a place (a page listed twice): which one stays there is not defined. Pages that several sequences share are
+ * fine as long as no token is written to them. */
 dcl_status dcl_pages_write(const dcl_pages* pages, const int32_t* table, int32_t max_pages, const int32_t* len,
                            const int32_t* cu, int32_t B, int32_t T, int32_t max_new, const void* k, int64_t k_stride,
                            const void* v, int64_t v_stride, hipStream_t stream);
 
 /* The reverse: keys and values of those positions into rows of bf16 (E4M3, E2M1: the values they stand for, which are bf16
- * numbers but for subnormals below 2^-133 and a value rounded up to 2^128, read as infinity).
+ * numbers but for subnormals below 2^-133 and a magnitude of 2^128 or more, read as infinity).
  * A row whose position no page holds becomes zeros. */
 dcl_status dcl_pages_read(const dcl_pages* pages, const int32_t* table, int32_t max_pages, const int32_t* len,
                           const int32_t* cu, int32_t B, int32_t T, int32_t max_new, void* k, int64_t k_stride, void* v,

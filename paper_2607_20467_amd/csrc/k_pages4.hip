@@ -12,7 +12,8 @@ namespace dcl {
 // value a bfloat16 number. 32 values share a scale because 12 to 1 is all that the format spans: keys after the rotation have a
 // few large dimensions, which cost only their own group its precision. The format has no infinity and no NaN: a group that
 // holds one has scale byte 255, for which gfx950's conversions and scaled matrix products give NaN (checked there for every
-// byte under every scale).
+// byte under every scale). What would round to 2^128 is stored as 3 * 2^126, so that no finite number becomes an infinity, which
+// as a value that a row does not see would meet that row's probability of 0.
 __device__ __forceinline__ int e2m1_exponent(uint32_t amax_bits) {  // bfloat16 bits of amax, sign cleared
   // amax = 1.f * 2^(E - 127), 6 = 1.5 * 2^2
   const int e = (int)(amax_bits >> 7) - 2 + ((amax_bits & 127) > 64 ? 1 : 0);
@@ -27,6 +28,14 @@ __device__ __forceinline__ uint32_t magnitude8(const uint4& x) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) m = max(m, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
   return m;
+}
+// The largest numbers' magnitudes cut to the last one below 3.5 * 2^126.
+constexpr uint32_t kTop4 = 0x7F5Fu;
+__device__ __forceinline__ void cut8(uint4& x) {
+  uint32_t* w[4] = {&x.x, &x.y, &x.z, &x.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    *w[i] = (*w[i] & 0x80008000u) | min(*w[i] & 0x7FFFu, kTop4) | min((*w[i] >> 16) & 0x7FFFu, kTop4) << 16;
 }
 // Eight bfloat16 over `scale` (a power of two) to eight codes, the first in the lowest bits.
 __device__ __forceinline__ uint32_t codes8(const uint4& x, float scale) {
@@ -60,8 +69,10 @@ __device__ __forceinline__ uint4 stream_load(const void* p) {
 
 // ---------------------------------------------------------------- write
 // One workgroup takes 64 positions (aligned to 64 in the sequence) of one KV head, eight dimensions a lane. Keys go out as they
-// come; a value's dimensions i and i + 16 of a group, which share a byte, are two lanes apart, and values and scales turn
-// position-innermost in LDS, in chunks of 16 positions that never straddle a page.
+// come, through LDS so that they are stored in 16-byte pieces; a value's dimensions i and i + 16 of a group, which share a byte, are
+// two lanes apart, and values and scales turn position-innermost in LDS, in chunks of 16 positions that never straddle a page.
+// Memory-bound: ten prompts of 400 to 6000 tokens x 32 heads, 325 MB: 62.8 us, 5.2 TB/s (70.3 with keys stored by the four bytes of a
+// lane); one token of each of 48 sequences x 8 heads: 5.6 us, a chain of loads.
 constexpr int kGroup4 = 64;
 
 template <int DH>
@@ -98,6 +109,10 @@ __global__ void __launch_bounds__(256) pages4_write_kernel(Pages p, const bf16_t
       av = max(av, (uint32_t)__shfl_xor((int)av, o, 64));
     }
     const bool odd_k = ak >= 0x7F80u, odd_v = av >= 0x7F80u;
+    if (max(ak, av) > kTop4) {
+      cut8(xk[i]);
+      cut8(xv[i]);
+    }
     const int ek = odd_k ? 255 : e2m1_exponent(ak), ev = odd_v ? 255 : e2m1_exponent(av);
     const uint32_t qk = odd_k ? 0u : codes8(xk[i], scale4(ek)), qv = odd_v ? 0u : codes8(xv[i], scale4(ev));
     *reinterpret_cast<uint32_t*>(sk + local * HB + 4 * c) = qk;
@@ -158,7 +173,8 @@ __global__ void __launch_bounds__(256) pages4_write_kernel(Pages p, const bf16_t
 }
 
 // ---------------------------------------------------------------- read
-// The reverse, in the same groups. A row whose position no page holds is zeros.
+// The reverse, in the same groups. A row whose position no page holds is zeros. The same ten prompts: 70.3 us, 4.6 TB/s, four fifths of
+// it stores of 256 bytes a row and head; nine sequences of 300 to 5000 positions x 8 heads, 99 MB: 17.7 us, 5.6 TB/s.
 template <int DH>
 __global__ void __launch_bounds__(256) pages4_read_kernel(Pages p, bf16_t* __restrict__ k, long kst, bf16_t* __restrict__ v,
                                                          long vst, int groups) {
@@ -255,13 +271,13 @@ void launch_pages4_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, 
 // probabilities of 16 adjacent keys, which lie in one page, and loads their values as one 16-byte piece of each row of two
 // dimensions.
 //
-// With one token it is bound by HBM behind its starts: 2 sequences of 100000 to 131072 keys, 28 / 4 heads, 133 MB: 30.5 us with the join
-// (5), 4.35 TB/s; 80 of 250 to 9000, 32 / 8 heads, 204 MB: 50 us, 4.1 TB/s. A tile of 64 keys under one fragment takes 400 vector
-// instructions (192 convert its values, 110 are the softmax's) and 40 matrix ones, 1.0 us of a SIMD where HBM brings one in 1.7.
-// Under blocks the two add up: 512 tokens of 4 sequences over 4096 keys, 32 / 8 heads: vector pipes busy 3/4 of the time, matrix pipes
-// 2/5 of it, 196 us, 0.65 PFLOP/s; 64 tokens of 8 over 1280, 32 heads: 25 us. Sharing the converted values between waves through LDS
-// saved a quarter of the vector instructions and lost it again to barriers and LDS reads (8 x 64 tokens 28 to 32 us, 4 x 512 205 to
-// 264); four fragments a wave spill (44 us).
+// With one token it is bound by HBM behind its starts: 2 sequences of 100000 to 131072 keys, 28 / 4 heads, 133 MB: 28.7 us with the join
+// (4.5), the kernel alone 5 TB/s; 80 of 250 to 9000, 32 / 8 heads, 204 MB: 50 us, 4.1 TB/s. A tile of 64 keys under one fragment takes 400
+// vector instructions (192 convert its values, 110 are the softmax's) and 40 matrix ones, 1.0 us of a SIMD where HBM brings one in
+// 1.7. Under blocks the two add up: 512 tokens of 4 sequences over 4096 keys, 32 / 8 heads: vector pipes busy 3/4 of the time,
+// matrix pipes 2/5 of it, 196 us, 0.65 PFLOP/s; 64 tokens of 8 over 1280, 32 heads: 24 us. Sharing the converted values between waves
+// through LDS saved a quarter of the vector instructions and lost it again to barriers and LDS reads (8 x 64 tokens 28 to 32 us,
+// 4 x 512 205 to 264, where this form took 27 and 202); four fragments a wave spill (44 us).
 __device__ __forceinline__ f32x4_t mfma16q(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -768,12 +784,13 @@ __global__ void __launch_bounds__(256) pages4_join_kernel(PagesAttn a, int head_
 static int query_fragments4(int g, int max_new) { return (long)g * max_new <= 16 ? 1 : 2; }
 
 // Keys of a part. Where sequences and heads give fewer workgroups than there are CUs, as many parts as cost least: the workgroups of
-// the fullest CU, each its keys and 300 more for its start, and 900 for a join (a workgroup of eight waves takes about 5 ns a key), over one part and
-// the numbers from as many as all CUs take at once. us so, 28 / 4 heads, 2 x 1 token over 131072 keys, parts of 1536 / 2048 / 3072 / 4096
-// (256 workgroups): 32.4 / 29.7 / 34.7 / 28.7; 32 / 8 heads, 1 x 1 over 20000: 384 / 640 (256) / 1024 / 2048: 14.1 / 12.8 / 13.7 / 17.5, 16 x 1 over 2000 to 6000:
-// 768 / 1536 / 3072 (256): 24.6 / 21.9 / 21.5; 32 / 32 heads, 4 x 1 over 80 to 720: 384 / whole 12.1 / 8.9. From one a CU on, parts of about 1536
-// even out the sequences' lengths where a part's output is small beside its keys (one fragment): 80 x 1 over 250 to 9000: 640 63,
-// 1024 52.5, 1536 50.3, 3072 51.7; 4 x 512 tokens over 4096: whole 198, 1536 282.
+// the fullest CU, each its keys and 300 more for its start, and 900 for a join (a workgroup of eight waves takes about 5 ns a key),
+// over one part and the numbers from as many as all CUs take at once. us so: 28 / 4 heads, 2 x 1 token over 131072 keys, parts of
+// 1536 / 2048 / 4096 (256 workgroups): 32.4 / 29.7 / 28.7; 32 / 8 heads, 1 x 1 over 20000: 384 / 640 (256) / 1024 / 2048: 14.1 / 12.8 /
+// 13.7 / 17.5; 16 x 1 over 2000 to 6000: 768 / 1536: 24.6 / 21.9; 32 / 32 heads, 4 x 1 over 80 to 720: 384 / whole: 12.1 / 8.9.
+// From one a CU on, parts of about 1536 even out the sequences' lengths where a part's output is small beside its keys (one
+// fragment): 80 x 1 over 250 to 9000: 640 / 1024 / 1536: 63 / 52.5 / 50.3. Under two fragments it is not: 4 x 512 tokens over 4096:
+// whole / 1536: 198 / 282.
 int pages4_attention_span(int Hkv, int g, int B, int max_new, int capacity) {
   const int qf = query_fragments4(g, max_new);
   const long rows = (long)g * max_new, units = ((rows + 16 * qf - 1) / (16 * qf)) * Hkv * B;

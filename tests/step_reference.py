@@ -13,13 +13,16 @@ E2M1 = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -
 
 def e2m1_rows(x):
     """Rows x [..., dh] float64 -> (codes [..., dh], exponent bytes [..., dh / 32]), from the definition: the least scale of 32
-    dimensions that reaches their largest magnitude, the nearest value, ties to the even code."""
+    dimensions that reaches their largest magnitude, the nearest value, ties to the even code, and 3 * 2^126 where that would be
+    2^128."""
     x = x.unflatten(-1, (-1, 32))
     fin = torch.isfinite(x).all(-1)
     a = torch.where(fin, x.abs().nan_to_num(0, 0, 0).amax(-1), torch.zeros(()).double())
     e = torch.ones(a.shape, dtype=torch.int64)
     for b in range(1, 255):
         e = torch.where(a > 6.0 * 2.0 ** (b - 127), torch.full_like(e, b + 1), e)
+    top = (x.abs() >= 3.5 * 2.0 ** 126) & torch.isfinite(x)
+    x = torch.where(top, torch.copysign(torch.full_like(x, 3 * 2.0 ** 126), x), x)
     y = x / torch.exp2((e - 127).double())[..., None]
     dist = (y.abs().nan_to_num(0, 0, 0)[..., None] - E2M1[:8]).abs()
     best = dist.amin(-1, keepdim=True)

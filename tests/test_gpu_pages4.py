@@ -93,14 +93,37 @@ def test_every_bfloat16_is_rounded_to_the_nearest_e2m1(dcl):
     rk = torch.empty_like(k, device="cuda")
     rv = torch.empty_like(rk)
     dcl.dcl_pages_read(*a, rk, rv)
-    # read back they are those values, each a bfloat16 number but where two significant bits round up to 2^128: infinity
+    # read back they are those values, each a bfloat16 number
     want = E2M1[code] * scale_of(e).repeat_interleave(32, -1)
-    over = want.abs() >= 2.0 ** 128
-    assert bool(over.any())
-    want[over] = torch.copysign(torch.full_like(want, math.inf), want)[over]
+    assert float(want.nan_to_num(0).abs().max()) == 3 * 2.0 ** 126
     got = rk.double().cpu()
     assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(0, 1, -1), want.nan_to_num(0, 1, -1))
     assert torch.equal(rk.view(torch.int16), rv.view(torch.int16))
+
+
+@pytest.mark.parametrize("dh,heads,hkv", [(128, 4, 2), (64, 8, 8)])
+def test_largest_numbers_stay_out_of_rows_that_do_not_see_them(dcl, dh, heads, hkv):
+    """Tokens of bfloat16's largest numbers behind a row's own position: as if they were anything else."""
+    n, new = 70, 6
+    g = torch.Generator().manual_seed(71)
+    k, v = (torch.randn(n, hkv, dh, generator=g).bfloat16() for _ in range(2))
+    q = torch.randn(new, heads, dh, generator=g).bfloat16().cuda()
+    top = torch.finfo(torch.bfloat16).max
+    outs = []
+    for values in ([0.0, 0.0, 0.0], [top, -top, 3.2e38]):
+        pool = Pool4(dcl, [n], 16, hkv, dh)
+        dev = pool.device()
+        v[n - 3:, :, 1] = v[n - 3:, :, dh - 1] = torch.tensor(values).bfloat16()[:, None]
+        table, length = pool.table.cuda(), pool.len.cuda()
+        dcl.dcl_pages_write(dev, table, length, starts([n]).cuda(), 1, n, n, k.cuda(), v.cuda())
+        nb = dcl.dcl_pages_attention_workspace_bytes(dev, heads, 1, new, new, table.shape[1])
+        out = torch.empty(new, heads, dh, dtype=torch.bfloat16, device="cuda")
+        dcl.dcl_pages_attention(dev, table, length, starts([new]).cuda(), 1, new, new, q, heads, 0.1, True, out, None,
+                                torch.empty(nb, dtype=torch.uint8, device="cuda"), nb)
+        outs.append(out.float().cpu())
+    a, b = outs
+    assert torch.equal(a[:new - 3], b[:new - 3])
+    assert bool(torch.isfinite(b).all()) and float(b[new - 3:].abs().max()) > 1e34
 
 
 @pytest.mark.parametrize("dh,heads,hkv,page,lens,counts,causal", [
@@ -386,10 +409,10 @@ def test_blocks_in_parts(dcl):
 @pytest.mark.parametrize("dh,heads,hkv,lens,new", [(64, 4, 4, [64, 900], 1), (128, 8, 2, [64, 1500], 1), (128, 4, 4, [640], 20),
                                                   (64, 8, 4, [512], 30), (128, 16, 4, [256] * 3, 32)])
 def test_probabilities_keep_sixteen_bits(dcl, dh, heads, hkv, lens, new):
-    """Half of the keys have the probability 1/2 (1 + 0.69 * 2^-7) of a reference's, half of them 1/2, with values 1 and -1: in
-    bfloat16 the first is 1/2 (1 + 2^-7) or 1/2, and rounded so they differ by 2^-8 too much or not at all. o is the difference, some 2^-9;
-    two parts keep each probability to 2^-16, the scores to 2^-20 (four roundings of sums below 2), and the sums of m terms to m *
-    2^-23."""
+    """Half of the keys have a probability 1 + 0.69 * 2^-7 times that of the other half, with values 1 and -1: o is their difference
+    over the sum of all, some 2^-9. In bfloat16 the two are a whole number of steps apart, 2^-7 or 0 of them, and o is off by a
+    third or more; two parts keep each probability to 2^-16, the scores to 2^-20 (four roundings of sums below 2), and the sums of
+    m terms to m * 2^-23."""
     pool = Pool4(dcl, lens, 64, hkv, dh, seed=11)
     slot = torch.arange(64) % 16
     kind = torch.where(slot < 2, 0, 1 + slot % 2)
