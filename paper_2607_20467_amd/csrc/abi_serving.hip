@@ -161,7 +161,7 @@ PagesTurn turn_args(const dcl_pages* g, int32_t* table, int32_t max_pages, int32
 // Workspace of an attention call over pages: the parts' outputs and their (reference, sum). A call without rows has one
 // part.
 struct PartLayout {
-  int nsplit, span;
+  int nsplit, span, run;
   size_t ml, total;
 };
 dcl_status part_layout(const dcl_pages* g, int32_t n_heads, int32_t B, int32_t T, int32_t max_new, int32_t max_pages,
@@ -169,15 +169,18 @@ dcl_status part_layout(const dcl_pages* g, int32_t n_heads, int32_t B, int32_t T
   const int capacity = max_pages * g->page_len;
   L->nsplit = 1;
   L->span = capacity;
+  L->run = 0;
   if (T > 0 && max_new > 0) {
     // in one part first: what passes keeps the partition's products in 64 bits
     dcl_status st = check_attention_size(g, n_heads, B, max_new, 1);
     if (st != DCL_OK) return st;
     const int group = n_heads / g->n_kv_heads;
-    L->span = g->dtype == DCL_DTYPE_E2M1
-                  ? pages4_attention_span(g->n_kv_heads, group, B, max_new, capacity)
-                  : pages_attention_span(g->n_kv_heads, group, B, max_new, capacity, g->dtype == DCL_DTYPE_E4M3);
-    L->nsplit = (capacity + L->span - 1) / L->span;
+    if (g->dtype == DCL_DTYPE_E2M1) {
+      pages4_attention_parts(g->n_kv_heads, group, B, max_new, capacity, &L->nsplit, &L->run);
+    } else {
+      L->span = pages_attention_span(g->n_kv_heads, group, B, max_new, capacity, g->dtype == DCL_DTYPE_E4M3);
+      L->nsplit = (capacity + L->span - 1) / L->span;
+    }
     st = check_attention_size(g, n_heads, B, max_new, L->nsplit);
     if (st != DCL_OK) return st;
   }
@@ -385,6 +388,7 @@ dcl_status dcl_pages_attention(const dcl_pages* pages, const int32_t* table, int
   a.causal = causal;
   a.nsplit = L.nsplit;
   a.span = L.span;
+  a.run = L.run;
   a.row_tiles = 0;
   a.q_sign = scale < 0.f ? 0x80008000u : 0u;
   a.scale_log2 = scale_log2(scale);

@@ -209,13 +209,14 @@ struct PagesAttn {
   float* po;                     // partial outputs [nsplit, T, H, dh] (nsplit > 1)
   float2* pml;                   // their (reference, sum) [nsplit, T, H]
   int H, g, causal, nsplit, span, row_tiles;  // parts of `span` keys (a multiple of 64)
+  int run;                       // 4 bits: part i has the runs i, i + nsplit, .. of 2^run tiles of 64 keys
   uint32_t q_sign;               // the scale's sign, for both halves of a word of queries
   float scale_log2;              // its magnitude times log2(e), a normal number
 };
 // Keys of one part: from sizes that the host knows (capacity: positions that a row of the table can name).
 int pages_attention_span(int Hkv, int g, int B, int max_new, int capacity, int e4m3);
 void launch_pages_attention(PagesAttn a, hipStream_t s);
-int pages4_attention_span(int Hkv, int g, int B, int max_new, int capacity);
+void pages4_attention_parts(int Hkv, int g, int B, int max_new, int capacity, int* parts, int* run);
 void launch_pages4_attention(PagesAttn a, hipStream_t s);
 
 // Pages handed out and taken back.

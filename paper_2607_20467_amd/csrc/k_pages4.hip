@@ -263,16 +263,16 @@ void launch_pages4_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, 
 }
 
 // ---------------------------------------------------------------- attention over pages
-// o = sum_j softmax_j(scale q.k_j) v_j, split and joined as over the other pages: a workgroup takes one tile of 16 QF rows of one
-// KV head (its g = H / Hkv query heads times the new tokens) and `span` keys, its four waves every fourth tile of 64 keys, which
-// come straight from memory into the registers of the matrix instructions.
+// o = sum_j softmax_j(scale q.k_j) v_j. A workgroup takes one tile of 16 QF rows of one KV head (its g = H / Hkv query heads times the
+// new tokens) and one part of the sequence's keys, its NW waves every NW-th tile of 64 keys of those, which come straight from memory
+// into the registers of the matrix instructions. Where a sequence has more than one part they are joined in order.
 //
 // Row 4 a + r of score step kt is key 16 a + 4 kt + r of the tile, so that lane group a (= lane / 16) ends up with the
 // probabilities of 16 adjacent keys, which lie in one page, and loads their values as one 16-byte piece of each row of two
 // dimensions.
 //
-// With one token it is bound by HBM behind its starts: 2 sequences of 100000 to 131072 keys, 28 / 4 heads, 133 MB: 28.7 us with the join
-// (4.5), the kernel alone 5 TB/s; 80 of 250 to 9000, 32 / 8 heads, 204 MB: 50 us, 4.1 TB/s. A tile of 64 keys under one fragment takes 400
+// With one token it is bound by HBM behind its starts: 2 sequences of 100000 to 131072 keys, 28 / 4 heads, 133 MB: 29 us with the join
+// (4.5), the kernel alone 5 TB/s; 80 of 250 to 9000, 32 / 8 heads, 204 MB: 48 us, 4.2 TB/s. A tile of 64 keys under one fragment takes 400
 // vector instructions (192 convert its values, 110 are the softmax's) and 40 matrix ones, 1.0 us of a SIMD where HBM brings one in
 // 1.7. Under blocks the two add up: 512 tokens of 4 sequences over 4096 keys, 32 / 8 heads: vector pipes busy 3/4 of the time,
 // matrix pipes 2/5 of it, 196 us, 0.65 PFLOP/s; 64 tokens of 8 over 1280, 32 heads: 24 us. Sharing the converted values between waves
@@ -443,21 +443,26 @@ __global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_at
   const int h = item % p.Hkv, b = (item / p.Hkv) % p.B, part = item / (p.Hkv * p.B);
   const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* row = p.table + (size_t)b * p.max_pages;
-  const int t0 = part * (a.span / KT);
-  // Pages of the 64 chunks of 16 keys from `base` on, one a lane, and of the 64 after those: asked for together with the borders and the
-  // length, which they do not depend on (the empty assembly keeps the loads before the branch).
-  int base = t0 * (KT / 16);
-  auto entry = [&](int c) { return row[page_entry(p.max_pages, p.shift, c)]; };
-  auto page_in = [&](int found, int c) { return page_found(found, p.max_pages, p.n_pages, p.shift, c); };
-  int ids = entry(base + lane), ids_next = entry(base + 64 + lane);
+  // The part's i-th tile: every nsplit-th run of 2^run tiles is its own.
+  auto tile_of = [&](int i) { return (((i >> a.run) * a.nsplit + part) << a.run) + (i & ((1 << a.run) - 1)); };
+  // Pages of the 64 chunks of 16 keys from the part's tile `base` on, one a lane, and of the 64 after those: asked for together with the
+  // borders and the length, which they do not depend on (the empty assembly keeps the loads before the branch).
+  int base = 0;
+  auto chunk_of = [&](int i) { return 4 * tile_of(i + (lane >> 2)) + (lane & 3); };
+  auto entry = [&](int i) { return row[page_entry(p.max_pages, p.shift, chunk_of(i))]; };
+  auto page_in = [&](int found, int i) { return page_found(found, p.max_pages, p.n_pages, p.shift, chunk_of(i)); };
+  int ids = entry(0), ids_next = entry(16);
   const SeqRows r = seq_rows(p.cu, b, p.T);
   const int len = __builtin_amdgcn_readfirstlane(seq_len(p.len, b));
   asm volatile("" : "+v"(ids), "+v"(ids_next) : "s"(len));
   const int n = min(r.n, p.max_new), rows = n * a.g, row0 = tile * 16 * QF, plen = 1 << p.shift;
   const int kend = min(len, p.max_pages << p.shift);  // keys that the table can name
-  const int t1 = min(t0 + a.span / KT, (kend + KT - 1) / KT);
-  if (row0 >= rows || (part > 0 && t0 >= t1)) return;  // part 0 always answers
-  ids = page_in(ids, base + lane);
+  // the part's tiles: whole runs, and what the last run has of one
+  const int tiles = (kend + KT - 1) / KT, runs = tiles >> a.run, each = runs / a.nsplit, over = runs - each * a.nsplit;
+  const int t1 = ((each + (part < over)) << a.run) + (part == over ? tiles & ((1 << a.run) - 1) : 0);
+  if (row0 >= rows || (part > 0 && t1 == 0)) return;  // part 0 always answers
+  const bool kept = a.nsplit > 1 && tiles > 1 << a.run;  // more than this part: for the join
+  ids = page_in(ids, 0);
   const int lq = lane & 15, lg = lane >> 4, la = lq >> 2, lr = lq & 3;
 
   const float scale = a.scale_log2;
@@ -503,14 +508,14 @@ __global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_at
   };
 
   int pk = -1, pv = -1;
-  auto find_pages = [&](int t) {  // of tile t, at most sixteen further than the last one asked for
-    if (t * (KT / 16) - base >= 64) {
-      base += 64;
-      ids = page_in(ids_next, base + lane);
-      ids_next = entry(base + 64 + lane);
+  auto find_pages = [&](int i) {  // of the part's tile i, at most sixteen further than the last one asked for
+    if (i - base >= 16) {
+      base += 16;
+      ids = page_in(ids_next, base);
+      ids_next = entry(base + 16);
     }
-    pk = __shfl(ids, 4 * t + la - base, 64);
-    pv = __shfl(ids, 4 * t + lg - base, 64);
+    pk = __shfl(ids, 4 * (i - base) + la, 64);
+    pv = __shfl(ids, 4 * (i - base) + lg, 64);
   };
 
   // The wave's queries, and how many keys each may see (rows past the last one: like any other, never written). They are asked for
@@ -536,9 +541,9 @@ __global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_at
     lim[f] = a.causal ? min(kend, max(0, len - r.n + i + 1)) : kend;
   }
   if (a.causal) lim_min = min(kend, max(0, len - r.n + row0 / a.g + 1));
-  int t = t0 + wid;
-  if (t < t1) {
-    find_pages(t);
+  int i = wid, t = tile_of(i), t_next = t;  // the part's tile, and which of the sequence it is
+  if (i < t1) {
+    find_pages(i);
     load_keys(t, pk);
     load_values(t, pv);
   }
@@ -579,8 +584,9 @@ __global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_at
       }
     }
     if constexpr (MORE) {
-      find_pages(t + NW);
-      load_keys(t + NW, pk);
+      find_pages(i + NW);
+      t_next = tile_of(i + NW);
+      load_keys(t_next, pk);
     }
 
     // the keys that a row does not see: past its limit, past the last key, in no page
@@ -662,10 +668,13 @@ __global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_at
     }
     __builtin_amdgcn_sched_group_barrier(0x008, 4 * QF, 0);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (MORE) load_values(t + NW, pv);
+    if constexpr (MORE) {
+      load_values(t_next, pv);
+      t = t_next;
+    }
   };
-  for (; t + NW < t1; t += NW) one_tile(std::true_type());
-  if (t < t1) one_tile(std::false_type());
+  for (; i + NW < t1; i += NW) one_tile(std::true_type());
+  if (i < t1) one_tile(std::false_type());
 
   // The waves' (m, l, o) joined in wave order, query fragment by query fragment: each wave takes every NW-th group of dimensions.
 #pragma unroll
@@ -695,13 +704,13 @@ __global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_at
       f32x4_t x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < NW; ++w) x += xo[w][dt][lane] * e[w];
-      if (a.nsplit > 1)  // uniform: the join reads all of them
+      if (kept)
         *reinterpret_cast<f32x4_t*>(a.po + ((size_t)part * p.T * a.H + at) * DH + 16 * dt + 4 * lg) = x;
       else
         *reinterpret_cast<uint2*>(a.out + at * DH + 16 * dt + 4 * lg) = make_uint2(f2bf2(x[0] * inv, x[1] * inv), f2bf2(x[2] * inv, x[3] * inv));
     }
     if (wid == 0 && lg == 0) {
-      if (a.nsplit > 1) a.pml[(size_t)part * p.T * a.H + at] = make_float2(mm, lt);
+      if (kept) a.pml[(size_t)part * p.T * a.H + at] = make_float2(mm, lt);
       else if (a.lse) a.lse[at] = lt == 0.f ? -INFINITY : mm * 0.6931471805599453f + logf(lt);
     }
   }
@@ -722,7 +731,8 @@ __global__ void __launch_bounds__(256) pages4_join_kernel(PagesAttn a, int head_
   if (i >= r.n) return;
   const bool mine = head < a.H;  // uniform over the workgroup where groups meet
   const int kend = min(len, p.max_pages << p.shift);
-  const int parts = !mine ? 0 : kend == 0 ? 1 : (kend + a.span - 1) / a.span;
+  const int runs = (kend + (64 << a.run) - 1) >> (a.run + 6), parts = mine ? min(a.nsplit, runs) : 0;
+  if (runs < 2) return;  // answered by its only part
   const size_t at = (size_t)(r.first + i) * a.H + head, step = (size_t)p.T * a.H;
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -783,30 +793,42 @@ __global__ void __launch_bounds__(256) pages4_join_kernel(PagesAttn a, int head_
 
 static int query_fragments4(int g, int max_new) { return (long)g * max_new <= 16 ? 1 : 2; }
 
-// Keys of a part. Where sequences and heads give fewer workgroups than there are CUs, as many parts as cost least: the workgroups of
-// the fullest CU, each its keys and 300 more for its start, and 900 for a join (a workgroup of eight waves takes about 5 ns a key),
-// over one part and the numbers from as many as all CUs take at once. us so: 28 / 4 heads, 2 x 1 token over 131072 keys, parts of
-// 1536 / 2048 / 4096 (256 workgroups): 32.4 / 29.7 / 28.7; 32 / 8 heads, 1 x 1 over 20000: 384 / 640 (256) / 1024 / 2048: 14.1 / 12.8 /
-// 13.7 / 17.5; 16 x 1 over 2000 to 6000: 768 / 1536: 24.6 / 21.9; 32 / 32 heads, 4 x 1 over 80 to 720: 384 / whole: 12.1 / 8.9.
-// From one a CU on, parts of about 1536 even out the sequences' lengths where a part's output is small beside its keys (one
-// fragment): 80 x 1 over 250 to 9000: 640 / 1024 / 1536: 63 / 52.5 / 50.3. Under two fragments it is not: 4 x 512 tokens over 4096:
-// whole / 1536: 198 / 282.
-int pages4_attention_span(int Hkv, int g, int B, int max_new, int capacity) {
+// How many parts, and how long the runs of keys that they take in turn. The host knows no lengths, only what the table could name;
+// runs in turn give every part its share at any length, so that a wide table costs no more than a tight one (80 x 1 token over 250 to
+// 9000 keys, 32 / 8 heads, tables of 9000 / 131072: 47.9 / 48.0 us; parts of 1536 adjoining keys 50.3 / 105; 128 x 1 over 200 to 600,
+// 131072: 21 us for 130).
+//
+// From a workgroup a CU on (units: sequences x KV heads x row tiles): runs of 2048 keys, since a sequence cut further pays more starts, and
+// parts for three rounds of the three workgroups that a CU holds, at least three, to even out the lengths. us by parts, runs of 2048:
+// 32 x 1 over 1000 to 32000 (256 units): 3 / 6 / 8 / 10: 123 / 83.7 / 82.9 / 77.4; 80 x 1 (640): 1 / 2 / 3 / 4 / 8: 52.7 / 52.5 / 47.9 / 49.6 /
+// 49.6; 200 x 1 (1600): 1 / 2 / 3 / 4: 120 / 110 / 108 / 110; 80 x 1 in 3 by runs of 1024 / 2048 / 4096: 51.0 / 47.9 / 54.4. Under two
+// fragments, whose outputs are larger, runs of 16384 and two rounds of two: 8 x 64 over 500 to 20000 (512): 1 / 2 / 4 / 8: 132 / 114 / 113 / 127;
+// 4 x 256 over 200 to 20000 (1024): 160 / 173 / - / 176.
+//
+// Below that, as many parts as cost least if the table were filled: the workgroups of the fullest CU, each its keys and 300 more for
+// its start, and 900 for a join (a workgroup of eight waves takes about 5 ns a key), over one part and the numbers from as many as
+// all CUs take at once. us: 28 / 4 heads, 2 x 1 over 131072: 16 / 32 (256 workgroups) / 64: 43.0 / 29.0 / 29.4; 32 / 8 heads, 1 x 1 over 20000:
+// 16 / 32 / 64: 14.8 / 12.7 / 13.3; 24 x 1 over 2000 to 6000: 1 / 2 / 4: 30.8 / 31.9 / 27.3; 32 / 32 heads, 4 x 1 over 80 to 720: 1 / 2: 8.9 /
+// 11.5. Runs of 256 keys, a tile of half of the waves: 1 x 1 over 20000 in runs of 128 / 256 / 512 / 1024: 12.8 / 12.7 / 13.9 / 13.5.
+void pages4_attention_parts(int Hkv, int g, int B, int max_new, int capacity, int* parts, int* run) {
   const int qf = query_fragments4(g, max_new);
   const long rows = (long)g * max_new, units = ((rows + 16 * qf - 1) / (16 * qf)) * Hkv * B;
-  const long most = qf == 1 ? 1536 : 16384;
-  long parts = 1;
+  long n = 1, r = 2;
   if (units >= 256) {
-    parts = (capacity + most - 1) / most;
+    r = qf == 1 ? 5 : 8;
+    n = qf == 1 ? 2304 / units : 1024 / units;
+    n = qf == 1 && n < 3 ? 3 : n;
+    const long all = (capacity + (64L << r) - 1) >> (r + 6);
+    n = n > all ? all : n;
   } else {
     long best = capacity + 300;
     for (long k = 256 / units, i = 0; i < 8; ++k, ++i) {
       const long cost = (units * k + 255) / 256 * (capacity / k + 300) + 900;
-      if (k > 1 && cost < best) best = cost, parts = k;
+      if (k > 1 && cost < best) best = cost, n = k;
     }
   }
-  parts = parts < 1 ? 1 : parts > 128 ? 128 : parts;
-  return (int)(((capacity + parts - 1) / parts + 63) / 64 * 64);
+  *parts = (int)(n < 1 ? 1 : n > 128 ? 128 : n);
+  *run = (int)r;
 }
 
 template <int DH>

@@ -463,3 +463,57 @@ def test_more_workgroups_than_cus(dcl, dh, heads, hkv, page, n, lo, hi, new, cau
         return torch.arange(m) // page != 1 if b == at else torch.ones(m, dtype=torch.bool)
     check4(pool, out, lse, q, cu, counts, heads, causal, 0.1, seen=seen)
     assert bool((out[int(cu[-1]):] == 7).all())
+
+
+@pytest.mark.parametrize("dh,heads,hkv,page,lens,counts,causal,width", [
+    (128, 8, 2, 64, [1600, 100, 0, 3000, 40, 1537, 1535], [1] * 7, True, None),
+    (64, 16, 1, 16, [2000, 1471, 1473, 5, 64], [1, 0, 1, 1, 1], True, 512),
+    (128, 4, 2, 32, [0, 0, 1700, 0, 1530, 12, 0], [0, 1, 8, 2, 8, 0, 1], True, None),
+    (128, 2, 2, 256, [9000], [2], False, 64),
+    (64, 6, 3, 128, [6000, 20, 4000], [3, 3, 1], False, None),
+    (128, 16, 2, 1024, [1024, 4096, 2048], [2, 1, 2], True, 16),
+])
+def test_parts_take_runs_in_turn(dcl, dh, heads, hkv, page, lens, counts, causal, width):
+    """Sequences that end inside a run, with one, before the second part's first, and far below what the table could name; a
+    missing page, and NaN behind every end."""
+    pool = Pool4(dcl, lens, page, hkv, dh, seed=51, fill=0x7F, width=width)
+    at = max(range(len(lens)), key=lambda b: lens[b])
+    gone = pool.table[at, 1].clone()
+    pool.table[at, 1] = -1
+    out, lse, q, cu, args = attend(dcl, pool, counts, heads, causal, 0.1, pad=3)
+    again = attend(dcl, pool, counts, heads, causal, 0.1, pad=3)
+    pool.table[at, 1] = gone
+    assert args[-1] > 256 and torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+    def seen(b, m):
+        return torch.arange(m) // page != 1 if b == at else torch.ones(m, dtype=torch.bool)
+    check4(pool, out, lse, q, cu, counts, heads, causal, 0.1, seen=seen)
+    assert bool((out[int(cu[-1]):] == 7).all())
+
+
+@pytest.mark.parametrize("n", [63, 64, 65, 193, 256, 257])
+def test_parts_of_many_sequences(dcl, n):
+    lens = [2500 if i % 61 == 5 else 1540 if i % 61 == 7 else (29 * i) % 90 for i in range(n)]
+    pool = Pool4(dcl, lens, 16, 2, 64, seed=52, fill=0x7F, width=1024)
+    out, lse, q, cu, args = attend(dcl, pool, [1] * n, 2, True, 0.2)
+    assert args[-1] > 256
+    check4(pool, out, lse, q, cu, [1] * n, 2, True, 0.2)
+
+
+def test_lengths_that_are_none_stay_in_bounds(dcl):
+    """Borders and lengths out of any order: rows that no sequence has stay, those of the sound one are right."""
+    lens = [2000, 1800, 40]
+    pool = Pool4(dcl, lens, 64, 2, 128, seed=53, fill=0x7F)
+    dev, table = pool.device(), pool.table.cuda()
+    q = torch.randn(3, 4, 128, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    nb = dcl.dcl_pages_attention_workspace_bytes(dev, 4, 3, 3, 1, table.shape[1])
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+
+    def run(length, cu):
+        out = torch.full((3, 4, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+        dcl.dcl_pages_attention(dev, table, torch.tensor(length, dtype=torch.int32).cuda(),
+                                torch.tensor(cu, dtype=torch.int32).cuda(), 3, 3, 1, q, 4, 0.1, True, out, None, ws, nb)
+        return out.float().cpu()
+    good = run(lens, [0, 1, 2, 3])
+    assert torch.equal(run([2000, -5, 2 ** 31 - 1], [0, 1, 1, -7]), torch.cat([good[:1], torch.full((2, 4, 128), 7.0)]))
+    assert torch.equal(run([2 ** 31 - 1, 1800, 40], [9, 1, 2, 2 ** 31 - 1])[1:], good[1:])
