@@ -116,6 +116,27 @@ def test_many_pages_come_back_at_once(dcl):
         dev.check(ref)
 
 
+@pytest.mark.parametrize("B,page,width,hi,cut", [
+    (64, 16, 600, 300, 40),                 # a few pages of what the tables could name
+    (300, 16, 100, 110, 200),               # some 1000 of them
+    (700, 16, 40, 150, 200),                # more than the first launch takes by itself
+    (4096, 16, 8, 40, 17),                  # sequences that its tables in shared memory hold
+    (4097, 16, 8, 40, 17),
+])
+def test_pages_come_back_from_wide_tables(dcl, B, page, width, hi, cut):
+    r = random.Random(B)
+    ref = state(r, B, page, width, 0, hi, 3)
+    dev = OnDevice(dcl, ref, 1)
+    for b in range(0, B, 7):                # entries that name no page, which come back from nowhere
+        ref.table[b][0] = r.choice([-1, ref.n_pages, 2 ** 31 - 1])
+    dev.table = ints(ref.table)
+    for turn in range(3):
+        keep = [max(-1, n - r.randint(0, cut)) if r.random() < 0.5 else n for n in ref.len]
+        ref.shrink(keep)
+        dev.shrink(ints(keep))
+        dev.check(ref)
+
+
 def test_what_was_taken_goes_back_where_it_came_from(dcl):
     r = random.Random(3)
     ref = state(r, 50, 16, 20, 1, 200, 300)
