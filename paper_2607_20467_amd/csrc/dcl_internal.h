@@ -200,6 +200,16 @@ void launch_pages_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, h
 void launch_pages4_write(const Pages& p, const bf16_t* k, long ks, const bf16_t* v, long vs, hipStream_t s);
 void launch_pages4_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, hipStream_t s);
 
+// Division by a number that the host knows, exact for all of 32 bits (Granlund and Montgomery's multiplication): five instructions
+// where the compiler's own takes some twenty, all before a workgroup's first load.
+struct Divisor {
+  uint32_t mul, shift1, shift2;
+  __device__ __forceinline__ int operator()(uint32_t n) const {
+    const uint32_t t = __umulhi(mul, n);
+    return (int)((t + ((n - t) >> shift1)) >> shift2);
+  }
+};
+
 struct PagesAttn {
   Pages p;
   const bf16_t* q;               // [T, H, dh], row stride q_stride
@@ -212,6 +222,7 @@ struct PagesAttn {
   int run;                       // 4 bits: part i has the runs i, i + nsplit, .. of 2^run tiles of 64 keys
   uint32_t q_sign;               // the scale's sign, for both halves of a word of queries
   float scale_log2;              // its magnitude times log2(e), a normal number
+  Divisor by_tiles, by_heads, by_seqs, by_parts, by_group;  // 4 bits: row_tiles, p.Hkv, p.B, nsplit, g
 };
 // Keys of one part: from sizes that the host knows (capacity: positions that a row of the table can name).
 int pages_attention_span(int Hkv, int g, int B, int max_new, int capacity, int e4m3);

@@ -435,9 +435,9 @@ __global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_at
   __shared__ float2 xml[NW][64];
   const Pages& p = a.p;
   // units: row tiles of one (part, sequence, KV head) follow each other on one XCD and share its L2
-  const int u = blockIdx.x, item = (u / (8 * a.row_tiles)) * 8 + (u & 7), tile = (u >> 3) % a.row_tiles;
+  const int u = blockIdx.x, eight = u >> 3, group = a.by_tiles(eight), item = 8 * group + (u & 7), tile = eight - group * a.row_tiles;
   if (item >= a.nsplit * p.B * p.Hkv) return;
-  const int h = item % p.Hkv, b = (item / p.Hkv) % p.B, part = item / (p.Hkv * p.B);
+  const int hb = a.by_heads(item), h = item - hb * p.Hkv, part = a.by_seqs(hb), b = hb - part * p.B;
   const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* row = p.table + (size_t)b * p.max_pages;
   // The part's i-th tile: every nsplit-th run of 2^run tiles is its own.
@@ -455,7 +455,7 @@ __global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_at
   const int n = min(r.n, p.max_new), rows = n * a.g, row0 = tile * 16 * QF, plen = 1 << p.shift;
   const int kend = min(len, p.max_pages << p.shift);  // keys that the table can name
   // the part's tiles: whole runs, and what the last run has of one
-  const int tiles = (kend + KT - 1) / KT, runs = tiles >> a.run, each = runs / a.nsplit, over = runs - each * a.nsplit;
+  const int tiles = (kend + KT - 1) / KT, runs = tiles >> a.run, each = a.by_parts(runs), over = runs - each * a.nsplit;
   const int t1 = ((each + (part < over)) << a.run) + (part == over ? tiles & ((1 << a.run) - 1) : 0);
   if (row0 >= rows || (part > 0 && t1 == 0)) return;  // part 0 always answers
   const bool kept = a.nsplit > 1 && tiles > 1 << a.run;  // more than this part: for the join
@@ -523,7 +523,7 @@ __global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_at
   int lim[QF], lim_min = kend;
 #pragma unroll
   for (int f = 0; f < QF; ++f) {
-    const int rr = min(row0 + 16 * f + lq, rows - 1), i = rr / a.g, head = h * a.g + rr % a.g;
+    const int rr = min(row0 + 16 * f + lq, rows - 1), i = a.by_group(rr), head = h * a.g + rr - i * a.g;
     const bf16_t* q = a.q + (size_t)(r.first + i) * a.q_stride + (size_t)head * DH;
     if constexpr (SCALED) {
       raw[f] = load_query(q, lg);
@@ -537,7 +537,7 @@ __global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_at
     }
     lim[f] = a.causal ? min(kend, max(0, len - r.n + i + 1)) : kend;
   }
-  if (a.causal) lim_min = min(kend, max(0, len - r.n + row0 / a.g + 1));
+  if (a.causal) lim_min = min(kend, max(0, len - r.n + a.by_group(row0) + 1));
   int i = wid, t = tile_of(i), t_next = t;  // the part's tile, and which of the sequence it is
   if (i < t1) {
     find_pages(i);
@@ -696,7 +696,8 @@ __global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_at
       e[w] = __builtin_amdgcn_exp2f(ml.x - ref);  // a wave without keys: (-inf, 0), and zeros for an output
       lt += ml.y * e[w];
     }
-    const size_t at = (size_t)(r.first + rr / a.g) * a.H + h * a.g + rr % a.g;
+    const int i = a.by_group(rr);
+    const size_t at = (size_t)(r.first + i) * a.H + h * a.g + rr - i * a.g;
     const float inv = lt == 0.f ? 0.f : 1.0f / lt;  // a row without keys is zeros
 #pragma unroll
     for (int dt = wid; dt < DT; dt += NW) {
@@ -718,12 +719,12 @@ __global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_at
 // The parts of a (row, head) joined: DH / 4 lanes take its dimensions, G such groups every G-th part, eight of them asked for at
 // once, with their references; then the groups in order. One pass, so that two loads follow each other, the lengths and the parts.
 template <int DH, int G>
-__global__ void __launch_bounds__(256) pages4_join_kernel(PagesAttn a, int head_blocks) {
+__global__ void __launch_bounds__(256) pages4_join_kernel(PagesAttn a, int head_blocks, Divisor by_blocks, Divisor by_new) {
   constexpr int L = DH / 4, PER = 256 / L, AT = 8;
   __shared__ float4 xo[PER][L];
   __shared__ float2 xml[PER];
   const Pages& p = a.p;
-  const int hb = blockIdx.x % head_blocks, bi = blockIdx.x / head_blocks, i = bi % p.max_new, b = bi / p.max_new;
+  const int bi = by_blocks(blockIdx.x), hb = blockIdx.x - bi * head_blocks, b = by_new(bi), i = bi - b * p.max_new;
   const SeqRows r = seq_rows(p.cu, b, p.T);
   const int len = seq_len(p.len, b);
   const int grp = threadIdx.x / L, c = threadIdx.x % L, head = G > 1 ? hb : hb * PER + grp;
@@ -830,10 +831,20 @@ void pages4_attention_parts(int Hkv, int g, int B, int max_new, int capacity, in
   *run = (int)r;
 }
 
+static Divisor divisor(uint32_t d) {  // d >= 1
+  const int l = d < 2 ? 0 : 32 - __builtin_clz(d - 1);
+  return {(uint32_t)((((1ull << l) - d) << 32) / d + 1), l < 1 ? 0u : 1u, l < 1 ? 0u : (uint32_t)l - 1};
+}
+
 template <int DH>
 static void run_pages4_attention(PagesAttn& a, hipStream_t s) {
   const int qf = query_fragments4(a.g, a.p.max_new);
   a.row_tiles = (int)(((long)a.g * a.p.max_new + 16 * qf - 1) / (16 * qf));
+  a.by_tiles = divisor(a.row_tiles);
+  a.by_heads = divisor(a.p.Hkv);
+  a.by_seqs = divisor(a.p.B);
+  a.by_parts = divisor(a.nsplit);
+  a.by_group = divisor(a.g);
   const long items = (long)a.nsplit * a.p.B * a.p.Hkv;
   const dim3 grid((unsigned)((items + 7) / 8 * 8 * a.row_tiles));
   const bool wide_groups = items * a.row_tiles <= 256;  // one a CU: eight waves take its keys (1 x 1 token over 20000: 13.1 / 12.7 us with four / eight)
@@ -846,8 +857,8 @@ static void run_pages4_attention(PagesAttn& a, hipStream_t s) {
     const bool wide = a.nsplit > 16;
     const int blocks = wide ? a.H : (a.H + PER - 1) / PER;
     const dim3 all((unsigned)blocks * a.p.max_new * a.p.B);
-    if (wide) hipLaunchKernelGGL((pages4_join_kernel<DH, PER>), all, dim3(256), 0, s, a, blocks);
-    else hipLaunchKernelGGL((pages4_join_kernel<DH, 1>), all, dim3(256), 0, s, a, blocks);
+    if (wide) hipLaunchKernelGGL((pages4_join_kernel<DH, PER>), all, dim3(256), 0, s, a, blocks, divisor(blocks), divisor(a.p.max_new));
+    else hipLaunchKernelGGL((pages4_join_kernel<DH, 1>), all, dim3(256), 0, s, a, blocks, divisor(blocks), divisor(a.p.max_new));
   }
 }
 
