@@ -18,18 +18,16 @@ namespace dcl {
 struct SeqRows {
   int first, n;
 };
-DCL_HD SeqRows seq_rows(const int32_t* cu, int b, int T) {
-  int lo = cu[b], hi = cu[b + 1];
+DCL_HD SeqRows rows_between(int lo, int hi, int T) {
   lo = lo < 0 ? 0 : lo > T ? T : lo;
   hi = hi < lo ? lo : hi > T ? T : hi;
   return {lo, hi - lo};
 }
+DCL_HD SeqRows seq_rows(const int32_t* cu, int b, int T) { return rows_between(cu[b], cu[b + 1], T); }
 
 // Length of a sequence as the kernels use it: [0, 2^30], so that positions and their sums stay in 32 bits.
-DCL_HD int seq_len(const int32_t* len, int b) {
-  const int n = len[b];
-  return n < 0 ? 0 : n > (1 << 30) ? (1 << 30) : n;
-}
+DCL_HD int length_of(int n) { return n < 0 ? 0 : n > (1 << 30) ? (1 << 30) : n; }
+DCL_HD int seq_len(const int32_t* len, int b) { return length_of(len[b]); }
 
 // Page that holds positions [16 c, 16 c + 16) of a sequence whose table row is `row` (max_pages entries, pages of
 // 2^shift positions), or -1: past the table, or an entry outside [0, n_pages).
