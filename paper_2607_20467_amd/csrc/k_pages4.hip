@@ -84,8 +84,8 @@ __device__ __forceinline__ uint4 stream_load(const void* p) {
 // One workgroup takes 64 positions (aligned to 64 in the sequence) of one KV head, eight dimensions a lane. Keys go out as they
 // come, through LDS so that they are stored in 16-byte pieces; a value's dimensions i and i + 16 of a group, which share a byte, are
 // two lanes apart, and values and scales turn position-innermost in LDS, in chunks of 16 positions that never straddle a page.
-// Memory-bound: ten prompts of 400 to 6000 tokens x 32 heads, 325 MB: 62.8 us, 5.2 TB/s (70.3 with keys stored by the four bytes of a
-// lane); one token of each of 48 sequences x 8 heads: 5.6 us, a chain of loads.
+// Memory-bound: ten prompts of 400 to 6000 tokens x 32 heads, 325 MB: 60 us, 5.4 TB/s (70 with keys stored by the four bytes of a
+// lane, 63 with page numbers looked up behind the rows); one token of each of 48 sequences x 8 heads: 5.4 us, a chain of loads.
 constexpr int kGroup4 = 64;
 
 template <int DH>
@@ -189,8 +189,8 @@ __global__ void __launch_bounds__(256) pages4_write_kernel(Pages p, const bf16_t
 }
 
 // ---------------------------------------------------------------- read
-// The reverse, in the same groups. A row whose position no page holds is zeros. The same ten prompts: 70.3 us, 4.6 TB/s, four fifths of
-// it stores of 256 bytes a row and head; nine sequences of 300 to 5000 positions x 8 heads, 99 MB: 17.7 us, 5.6 TB/s.
+// The reverse, in the same groups. A row whose position no page holds is zeros. The same ten prompts: 69 us, 4.7 TB/s, four fifths of
+// it stores of 256 bytes a row and head; nine sequences of 300 to 5000 positions x 8 heads, 99 MB: 17.4 us, 5.7 TB/s.
 template <int DH>
 __global__ void __launch_bounds__(256) pages4_read_kernel(Pages p, bf16_t* __restrict__ k, long kst, bf16_t* __restrict__ v,
                                                          long vst, int groups, Divisor by_heads, Divisor by_groups) {
@@ -289,10 +289,10 @@ void launch_pages4_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, 
 // dimensions.
 //
 // With one token it is bound by HBM behind its starts: 2 sequences of 100000 to 131072 keys, 28 / 4 heads, 133 MB: 29 us with the join
-// (4.5), the kernel alone 5 TB/s; 80 of 250 to 9000, 32 / 8 heads, 204 MB: 48 us, 4.2 TB/s. A tile of 64 keys under one fragment takes 400
+// (4.5), the kernel alone 5.3 TB/s; 80 of 250 to 9000, 32 / 8 heads, 204 MB: 47 us, 4.3 TB/s. A tile of 64 keys under one fragment takes 400
 // vector instructions (192 convert its values, 110 are the softmax's) and 40 matrix ones, 1.0 us of a SIMD where HBM brings one in
 // 1.7. Under blocks the two add up: 512 tokens of 4 sequences over 4096 keys, 32 / 8 heads: vector pipes busy 3/4 of the time,
-// matrix pipes 2/5 of it, 196 us, 0.65 PFLOP/s; 64 tokens of 8 over 1280, 32 heads: 24 us. Sharing the converted values between waves
+// matrix pipes 2/5 of it, 190 us, 0.66 PFLOP/s; 64 tokens of 8 over 1280, 32 heads: 22.5 us. Sharing the converted values between waves
 // through LDS saved a quarter of the vector instructions and lost it again to barriers and LDS reads (8 x 64 tokens 28 to 32 us,
 // 4 x 512 205 to 264, where this form took 27 and 202); four fragments a wave spill (44 us).
 __device__ __forceinline__ f32x4_t mfma16q(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
