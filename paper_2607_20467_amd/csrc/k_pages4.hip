@@ -21,14 +21,16 @@ __device__ __forceinline__ int e2m1_exponent(uint32_t amax_bits) {  // bfloat16 
 }
 __device__ __forceinline__ float scale4(uint32_t e) { return __uint_as_float(e << 23); }  // 255: no finite number
 
-// Largest magnitude of eight bfloat16, as bits: 0x7F80 and more for infinities and NaN.
-__device__ __forceinline__ uint32_t magnitude8(const uint4& x) {
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  uint32_t m = 0;
+// Largest magnitude of N pairs of bfloat16, as bits: 0x7F80 and more for infinities and NaN.
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+template <int N>
+__device__ __forceinline__ uint32_t magnitude(const uint32_t (&w)[N]) {
+  u16x2_t m = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) m = max(m, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
-  return m;
+  for (int i = 0; i < N; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_t, w[i] & 0x7FFF7FFFu));
+  return max((uint32_t)m[0], (uint32_t)m[1]);
 }
+__device__ __forceinline__ uint32_t magnitude8(const uint4& x) { return magnitude({x.x, x.y, x.z, x.w}); }
 // The largest numbers' magnitudes cut to the last one below 3.5 * 2^126.
 constexpr uint32_t kTop4 = 0x7F5Fu;
 __device__ __forceinline__ void cut8(uint4& x) {
@@ -345,11 +347,16 @@ __device__ __forceinline__ void four_parts(uint32_t a, uint32_t b, float s1, flo
   part[0][at] = (int)p1;
   part[1][at] = __builtin_bit_cast(int, two);
 }
-__device__ __forceinline__ QueryParts query_parts(const RawQuery& q, int lq, int lg, uint32_t sign) {
+__device__ __forceinline__ QueryParts query_parts(RawQuery& q, int lq, int lg, uint32_t sign) {
+  if (sign) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q.x[i].x ^= sign, q.x[i].y ^= sign, q.x[i].z ^= sign, q.x[i].w ^= sign;
+  }
   int e[2];  // exponents of the groups that the lane's two halves belong to
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    uint32_t m = max(magnitude8(q.x[2 * half]), magnitude8(q.x[2 * half + 1]));
+    const uint4 &x = q.x[2 * half], &y = q.x[2 * half + 1];
+    uint32_t m = magnitude({x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w});
     m = max(m, (uint32_t)__shfl_xor((int)m, 16, 64));
     const int b = (int)(m >> 7) - 8 + ((m & 127) > 96 ? 1 : 0);  // m = 1.f * 2^(E - 127), 448 = 1.75 * 2^8
     e[half] = m >= 0x7F80u ? 255 : max(b, 5);                    // the second part's is 4 less
@@ -363,8 +370,8 @@ __device__ __forceinline__ QueryParts query_parts(const RawQuery& q, int lq, int
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint4 x = q.x[2 * half + i];
-      four_parts(x.x ^ sign, x.y ^ sign, s1, s2, r.part, 4 * half + 2 * i);
-      four_parts(x.z ^ sign, x.w ^ sign, s1, s2, r.part, 4 * half + 2 * i + 1);
+      four_parts(x.x, x.y, s1, s2, r.part, 4 * half + 2 * i);
+      four_parts(x.z, x.w, s1, s2, r.part, 4 * half + 2 * i + 1);
     }
   }
   return r;
