@@ -10,7 +10,7 @@ namespace dcl {
 // The angle: pos * turns[i] in float64 is exact to 2^-52 of itself, at most 2^31 / (2 pi) turns, so that its fraction is exact to
 // 2^-23 of a turn at the farthest position and to 2^-24 below 2^28; as float32 in [-0.5, 0.5] it keeps 2^-26.
 //
-// Memory-bound for many rows: 8192 of 32 + 8 heads of 128, 168 MB: 36 us, 4.7 TB/s (with pairs in different lanes, which an exchange
+// Memory-bound for many rows: 8192 of 32 + 8 heads of 128, 168 MB: 31 us, 5.4 TB/s (with pairs in different lanes, which an exchange
 // brings together, 43 to 74: its twelve LDS-crossbar instructions a head group and twice the angles). Four rows: 3.5 us, a chain of
 // position, angle, head.
 //
@@ -28,6 +28,13 @@ __device__ __forceinline__ float sum_head(float v) {
   v = plus_lane<0x4E>(v);                          // quads 2 3 0 1
   v = plus_lane<0x141>(v);                         // lane 7 - i of eight
   return L == 16 ? plus_lane<0x140>(v) : v;        // lane 15 - i of sixteen
+}
+
+// Read once: past the caches, so that they keep what is written (8192 rows 36.5 us with plain loads, 31.1 so, 32.1 with the stores past
+// them too).
+__device__ __forceinline__ uint2 load_once(const bf16_t* p) {
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint2, __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(p)));
 }
 
 template <int DH>
@@ -75,7 +82,7 @@ __global__ void __launch_bounds__(256) heads_kernel(HeadsArgs a, int groups_q, i
       const int h = g * HW + sub;
       if (h >= heads) continue;  // a head's lanes together
       const bf16_t* src = in + (size_t)h * DH;
-      const uint2 ux = *reinterpret_cast<const uint2*>(src + dx), uz = *reinterpret_cast<const uint2*>(src + dz);
+      const uint2 ux = load_once(src + dx), uz = load_once(src + dz);
       float x[4] = {__uint_as_float(ux.x << 16), __uint_as_float(ux.x & 0xFFFF0000u), __uint_as_float(ux.y << 16),
                     __uint_as_float(ux.y & 0xFFFF0000u)};
       float z[4] = {__uint_as_float(uz.x << 16), __uint_as_float(uz.x & 0xFFFF0000u), __uint_as_float(uz.y << 16),
@@ -117,7 +124,7 @@ __global__ void __launch_bounds__(256) heads_kernel(HeadsArgs a, int groups_q, i
 void launch_heads_norm_rope(const HeadsArgs& a, hipStream_t s) {  // T above 0
   const int HW = 512 / a.dh, gq = (a.H + HW - 1) / HW, groups = gq + (a.Hkv + HW - 1) / HW;
   // A wave per group of heads while that leaves CUs idle, otherwise about 16384 of them, that share a row evenly (8192 rows of ten
-  // groups, waves at most 4096 / 8192 / 16384 / 32768: 37.9 / 37.9 / 36.4 / 38.3 us).
+  // groups, waves at most 4096 / 8192 / 16384 / 32768: 32.2 / 32.3 / 31.1 / 32.0 us).
   const long waves = (long)a.T * groups;
   int chunks = (int)(waves <= 16384 ? groups : 16384 / a.T);
   chunks = chunks < 1 ? 1 : chunks;
