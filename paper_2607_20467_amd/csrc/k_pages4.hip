@@ -88,6 +88,8 @@ __device__ __forceinline__ uint4 stream_load(const void* p) {
 // two lanes apart, and values and scales turn position-innermost in LDS, in chunks of 16 positions that never straddle a page.
 // Memory-bound: ten prompts of 400 to 6000 tokens x 32 heads, 325 MB: 60 us, 5.4 TB/s (70 with keys stored by the four bytes of a
 // lane, 63 with page numbers looked up behind the rows); one token of each of 48 sequences x 8 heads: 5.4 us, a chain of loads.
+// Rows are read past the caches (62 us with plain loads), pages stored through them, for what reads them next: the ten prompts written
+// and read back 128.8 -> 108.7 us.
 constexpr int kGroup4 = 64;
 
 template <int DH>
@@ -152,8 +154,8 @@ __global__ void __launch_bounds__(256) pages4_write_kernel(Pages p, const bf16_t
   if (tid < kGroup4 * (HB / 16)) {
     const int x = g0 + tid / (HB / 16), page = page_found(entry_k, p.max_pages, p.n_pages, p.shift, chunk_k);
     if (x >= start && x < start + n && page >= 0)
-      stream_store(p.k + (((size_t)page * p.Hkv + h) * plen + (x & (plen - 1))) * HB + 16 * (tid % (HB / 16)),
-                   *reinterpret_cast<const uint4*>(sk + 16 * tid));
+      *reinterpret_cast<uint4*>(p.k + (((size_t)page * p.Hkv + h) * plen + (x & (plen - 1))) * HB + 16 * (tid % (HB / 16))) =
+          *reinterpret_cast<const uint4*>(sk + 16 * tid);
   }
   // rows of positions: HB of values, 2 G of scales
   for (int u = tid; u < (HB + 2 * G) * 4; u += 256) {
@@ -183,7 +185,7 @@ __global__ void __launch_bounds__(256) pages4_write_kernel(Pages p, const bf16_t
       for (int j = 0; j < 4; ++j)
         w[j] = src[4 * j * step] | src[(4 * j + 1) * step] << 8 | src[(4 * j + 2) * step] << 16 |
                (uint32_t)src[(4 * j + 3) * step] << 24;
-      stream_store(dst, make_uint4(w[0], w[1], w[2], w[3]));
+      *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
       for (int j = lo; j < hi; ++j) dst[j] = src[j * step];
     }
@@ -192,7 +194,7 @@ __global__ void __launch_bounds__(256) pages4_write_kernel(Pages p, const bf16_t
 
 // ---------------------------------------------------------------- read
 // The reverse, in the same groups. A row whose position no page holds is zeros. The same ten prompts: 69 us, 4.7 TB/s, four fifths of
-// it stores of 256 bytes a row and head; nine sequences of 300 to 5000 positions x 8 heads, 99 MB: 17.4 us, 5.7 TB/s.
+// it stores of 256 bytes a row and head (48 us behind the call that wrote them: the pages are in the last cache); nine sequences of 300 to 5000 positions x 8 heads, 99 MB: 17.4 us, 5.7 TB/s.
 template <int DH>
 __global__ void __launch_bounds__(256) pages4_read_kernel(Pages p, bf16_t* __restrict__ k, long kst, bf16_t* __restrict__ v,
                                                          long vst, int groups, Divisor by_heads, Divisor by_groups) {
