@@ -439,13 +439,17 @@ __device__ __forceinline__ void widen_values8(const uint32_t (&w)[2], const uint
   hi = make_uint4(h[0], h[1], h[2], h[3]);
 }
 
-// Scale bytes of four keys: those that are not there (`keep` masks the ones that are) become 1, so that any code is a number. Where
-// a group of NaN is left, it becomes 1 too and the return value is not 0: the rows that see it are given NaN apart.
+// Scale bytes of four keys: those that are not there (`keep` masks the ones that are) become 1, so that any code is a number. The return
+// value marks bytes of 253 and more, under which a code can stand for an infinity (4 and 6 under 253, 2 to 6 under 254) or NaN.
 __device__ __forceinline__ uint32_t sane_scales(uint32_t& s, uint32_t keep) {
   s = (s & keep) | (0x7F7F7F7Fu & ~keep);
-  const uint32_t odd = ((s & 0x7F7F7F7Fu) + 0x01010101u) & s & 0x80808080u;  // a byte of 255
-  s ^= odd;                                                                   // 255 -> 127
-  return odd;
+  return ((s & 0x7F7F7F7Fu) + 0x03030303u) & s & 0x80808080u;
+}
+// Those codes made finite; the rows that see them are given NaN apart. s, w: scales and codes of four keys, odd: the marks.
+__device__ __forceinline__ void finite_codes(uint32_t& s, uint32_t& w, uint32_t odd) {
+  const uint32_t from_2 = odd & (s << 6), from_4 = odd & ~(s << 6);  // 254 and 255; 253
+  w &= ~((w & 0x44444444u & (from_2 >> 7) * 255u) | (w & (w << 1) & 0x44444444u & (from_4 >> 7) * 255u));
+  s ^= odd & (s << 6) & (s << 7);                                     // 255 -> 127
 }
 __device__ __forceinline__ uint32_t first_bytes(int n) {  // a mask of the first n bytes of a word
   return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
@@ -652,20 +656,35 @@ __global__ void __launch_bounds__(64 * NW, QF == 1 && NW == 4 ? 3 : 2) pages4_at
           vsr[g][j] = e;
         }
       if (__builtin_amdgcn_ballot_w64(odd != 0)) {  // rare
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            uint32_t e = vsr[g][j], w = vr[g][j];
+            finite_codes(e, w, sane_scales(e, ~0u));
+            vsr[g][j] = e;
+            vr[g][j] = w;
+          }
 #pragma unroll 1
         for (int y = 0; y < KT; ++y) {
           const int key = KT * t + y, pid = page_of(row, p.max_pages, p.n_pages, p.shift, key >> 4);
           if (pid < 0 || key >= kend) continue;
-          const uint8_t* at = p.vs + ((size_t)pid * p.Hkv + h) * G * plen + (key & (plen - 1));
+          const size_t ph = (size_t)pid * p.Hkv + h;
+          const int off = key & (plen - 1);
 #pragma unroll
           for (int g = 0; g < G; ++g) {
-            if (at[g * plen] != 255) continue;
+            const uint32_t e = p.vs[((ph * G + g) << p.shift) + off];
+            if (e < 253) continue;
+            const uint32_t least = e == 253 ? 0x66u : e == 254 ? 0x44u : 0u;  // bits of the codes that are no numbers
 #pragma unroll
-            for (int f = 0; f < QF; ++f)
-              if (key < lim[f]) {
-                o[f][2 * g] += __uint_as_float(0x7FC00000u);
-                o[f][2 * g + 1] += __uint_as_float(0x7FC00000u);
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t miss = ~p.v[((ph * HB + 16 * g + 4 * lg + x) << p.shift) + off] & least;
+#pragma unroll
+              for (int f = 0; f < QF; ++f) {
+                if (key < lim[f] && (miss & 15) == 0) o[f][2 * g][x] = __uint_as_float(0x7FC00000u);
+                if (key < lim[f] && (miss & 0xF0) == 0) o[f][2 * g + 1][x] = __uint_as_float(0x7FC00000u);
               }
+            }
           }
         }
       }

@@ -230,6 +230,30 @@ def test_nan_groups_reach_only_rows_that_see_them(dcl, dh, heads):
     assert torch.isnan(out[12, 1]).all() and torch.isfinite(out[12, 0]).all() and torch.isfinite(out[13, 0]).all()
 
 
+@pytest.mark.parametrize("dh,heads", [(64, 2), (128, 8)])
+def test_infinite_values_reach_only_rows_that_see_them(dcl, dh, heads):
+    """Scale bytes a caller may put into its pages, under which some codes stand for 2^128 and more: nothing to the rows that do
+    not see them, NaN to those that do, in the dimensions of these codes; what is finite under them counts as it is."""
+    pool = Pool4(dcl, [150, 40], 32, 2, dh, seed=31)
+    counts, last = [9, 6], dh // 32 - 1
+    for b, x, h, g, byte in ((0, 145, 0, 0, 254), (0, 148, 1, last, 253), (1, 37, 0, last, 253), (1, 38, 1, 0, 255)):
+        pool.vs[pool.table[b, x // 32].long(), h, g, x % 32] = byte
+    out, lse, q, cu, _ = attend(dcl, pool, counts, heads, True, 0.125)
+    group, odd = heads // 2, 0
+    for b, n in enumerate(counts):
+        k, v = pool.rows(b)
+        v = torch.where(v.abs() >= 2.0 ** 128, math.nan, v)
+        sees = torch.arange(pool.lens[b])[None, :] <= (pool.lens[b] - n + torch.arange(n))[:, None]
+        for h in range(heads):
+            rows = slice(int(cu[b]), int(cu[b]) + n)
+            want, _, tol, _ = attention_rows4(q[rows, h].double(), k[:, h // group], v[:, h // group], 0.125, sees)
+            got, ok = out[rows, h], ~torch.isnan(want)
+            assert torch.equal(torch.isnan(got), ~ok), (b, h)
+            assert bool(((got - want).abs()[ok] <= tol[ok]).all()), (b, h)
+            odd += int((~ok).sum())
+    assert odd > 100 and torch.isfinite(out[:4]).all()
+
+
 def test_large_scores_and_rescaling(dcl):
     """Scores whose maximum keeps growing along the sequence, and a scale of either sign."""
     for scale in (1.0, -0.7, 0.0):
