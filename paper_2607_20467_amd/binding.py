@@ -408,16 +408,30 @@ def dcl_debug_gemm_plan(Nw: int, T: int, K: int, lm_head: int = False, max_split
 # ---------------------------------------------------------------- serving operators: packed batches, pages
 
 # Latency counts in these calls, so that a sound argument passes in a few attribute reads; what is wrong with an
-# unsound one is worked out only then.
+# unsound one is worked out only then. Those of a paged step pass in one native call (csrc/operands.cpp), which answers None to
+# whatever it does not take for sound; without that module the checks here do its work.
 _torch = None
+_native = None
+
+
+def _load_native():
+    try:
+        from . import _operands
+    except ModuleNotFoundError:
+        return None
+    lib = load_library()
+    _operands.bind(*(ctypes.cast(getattr(lib, "dcl_" + n), ctypes.c_void_p).value for n in (
+        "pages_extend", "pages_shrink", "heads_norm_rope", "pages_write", "pages_read", "pages_attention")))
+    return _operands
 
 
 def _device():
     """The current device's index (the call's stream belongs to it); -2, which no tensor is on, before
     torch uses any."""
-    global _torch
+    global _torch, _native
     if _torch is None:
         import torch
+        _native = _load_native()
         for kinds in (_I32, _F32, _B16, _I64):
             kinds.types = frozenset(getattr(torch, k) for k in kinds if hasattr(torch, k))
         _torch = torch
@@ -563,12 +577,16 @@ class KVPages:
             head_dim, dtype
         self.struct = DclPages(self.k.data_ptr(), self.v.data_ptr(), _ptr(self.k_scale), _ptr(self.v_scale), n_pages,
                                page_len, n_kv_heads, head_dim, dtype)
-        self.ref = ctypes.byref(self.struct)
+        self.ref, self.address = ctypes.byref(self.struct), ctypes.addressof(self.struct)
 
 
 def dcl_pages_write(pages: KVPages, table, length, cu, B: int, T: int, max_new: int, k, v, stream=None) -> None:
     """Rows k, v [T, n_kv_heads, head_dim] into the pages (``table`` [B, max_pages], ``length`` [B], ``cu`` [B + 1])."""
     w, dev = "dcl_pages_write", _device()
+    if _native is not None and type(pages) is KVPages and pages.device == dev:
+        st = _native.pages_write(dev, _queue(stream, dev), pages.address, B, T, max_new, table, length, cu, k, v)
+        if st is not None:
+            return _check(st, w)
     a = _batch(pages, table, length, cu, B, T, max_new, w, dev)
     kp, ks = _packed(k, "k", w, T, pages.n_kv_heads, pages.head_dim, dev)
     vp, vs = _packed(v, "v", w, T, pages.n_kv_heads, pages.head_dim, dev)
@@ -578,6 +596,10 @@ def dcl_pages_write(pages: KVPages, table, length, cu, B: int, T: int, max_new: 
 def dcl_pages_read(pages: KVPages, table, length, cu, B: int, T: int, max_new: int, k, v, stream=None) -> None:
     """The last rows of each sequence out of the pages into k, v [T, n_kv_heads, head_dim]."""
     w, dev = "dcl_pages_read", _device()
+    if _native is not None and type(pages) is KVPages and pages.device == dev:
+        st = _native.pages_read(dev, _queue(stream, dev), pages.address, B, T, max_new, table, length, cu, k, v)
+        if st is not None:
+            return _check(st, w)
     a = _batch(pages, table, length, cu, B, T, max_new, w, dev)
     kp, ks = _packed(k, "k", w, T, pages.n_kv_heads, pages.head_dim, dev)
     vp, vs = _packed(v, "v", w, T, pages.n_kv_heads, pages.head_dim, dev)
@@ -606,6 +628,11 @@ def dcl_pages_extend(pages: KVPages, table, length, count, B: int, T: int, free_
     """Room for count [B] new tokens (None: one each) behind length [B] in ``table`` [B, max_pages], pages from the list
     free_pages [n_pages] of which n_free [1] are free; cu [B + 1], pos [T] (or None) and slot [T] (int64, or None) are outputs."""
     w, dev = "dcl_pages_extend", _device()
+    if _native is not None and type(pages) is KVPages and dev >= 0:
+        st = _native.pages_extend(dev, _queue(stream, dev), pages.address, B, T, table, length, count, free_pages, n_free, cu,
+                                  pos, slot, ws, ws_bytes)
+        if st is not None:
+            return _check(st, w)
     lead, free = _turn(pages, table, length, count, "count", B, free_pages, n_free, w, dev)
     n = max(T, 0)
     _check(load_library().dcl_pages_extend(*lead, T, *free, _here(cu, "cu", w, _I32, max(B, 0) + 1, dev),
@@ -617,6 +644,11 @@ def dcl_pages_shrink(pages: KVPages, table, length, keep, B: int, free_pages, n_
                      stream=None) -> None:
     """Sequences cut to keep [B] positions (where 0 <= keep < length), their pages back on the list."""
     w, dev = "dcl_pages_shrink", _device()
+    if _native is not None and type(pages) is KVPages and dev >= 0:
+        st = _native.pages_shrink(dev, _queue(stream, dev), pages.address, B, table, length, keep, free_pages, n_free, ws,
+                                  ws_bytes)
+        if st is not None:
+            return _check(st, w)
     lead, free = _turn(pages, table, length, keep, "keep", B, free_pages, n_free, w, dev)
     _check(load_library().dcl_pages_shrink(*lead, *free, _space(ws, w, ws_bytes, dev), ws_bytes, _queue(stream, dev)), w)
 
@@ -627,6 +659,11 @@ def dcl_heads_norm_rope(q, k, pos, T: int, n_heads: int, n_kv_heads: int, head_d
     head by head with gains g_q, g_k [head_dim] (float32, or None) and rotated by pos [T]; outputs like them (rows may be
     apart), or the inputs themselves."""
     w, dev = "dcl_heads_norm_rope", _device()
+    if _native is not None and dev >= 0:
+        st = _native.heads_norm_rope(dev, _queue(stream, dev), T, n_heads, n_kv_heads, head_dim, rot_dim, eps, rope_base, q, q_out,
+                                     k, k_out, pos, g_q, g_k)
+        if st is not None:
+            return _check(st, w)
     qp = qs = qo = qos = kp = ks = ko = kos = 0
     if n_heads > 0:
         qp, qs = _packed(q, "q", w, T, n_heads, head_dim, dev)
@@ -650,6 +687,11 @@ def dcl_pages_attention(pages: KVPages, table, length, cu, B: int, T: int, max_n
                         causal: bool, out, lse, ws, ws_bytes: int, stream=None) -> None:
     """q [T, n_heads, head_dim] over the pages; out like q (contiguous), lse [T, n_heads] float32 or None."""
     w, dev = "dcl_pages_attention", _device()
+    if _native is not None and type(pages) is KVPages and pages.device == dev:
+        st = _native.pages_attention(dev, _queue(stream, dev), pages.address, B, T, max_new, table, length, cu, n_heads, causal,
+                                     scale, q, out, lse, ws, ws_bytes)
+        if st is not None:
+            return _check(st, w)
     a = _batch(pages, table, length, cu, B, T, max_new, w, dev)
     qp, qs = _packed(q, "q", w, T, n_heads, pages.head_dim, dev)
     n = max(T, 0) * n_heads

@@ -12,6 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdcl.so")
 SOURCES = ["abi.hip", "abi_serving.hip", "k_small.hip", "k_gemm.hip", "k_attn.hip", "k_pages.hip",
            "k_pages4.hip", "k_turn.hip", "k_heads.hip", "k_prompt.hip", "k_sample.hip"]
+OPERANDS = os.path.join(HERE, "_operands.so")       # calls from Python in one step (csrc/operands.cpp)
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # (source, extra flags) of each object; the GEMM family's instantiations are spread over three of them
 OBJECTS = [("k_gemm.hip", ["-DDCL_GEMM_PART=1"]), ("k_gemm.hip", ["-DDCL_GEMM_PART=2"]),
@@ -28,11 +29,29 @@ FLAGS = [
 
 
 def sources():
-    return [os.path.join(CSRC, s) for s in SOURCES]
+    return [os.path.join(CSRC, s) for s in SOURCES] + [os.path.join(CSRC, "operands.cpp")]
+
+
+def build_operands(verbose: bool = False) -> str:
+    """Compile the Python extension, host code against torch's headers. Returns its path."""
+    import sysconfig
+
+    import torch
+    at, tmp = os.path.dirname(torch.__file__), OPERANDS + ".tmp%d" % os.getpid()
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, "-D__HIP_PLATFORM_AMD__",
+           "-isystem", os.path.join(at, "include"), "-isystem", sysconfig.get_paths()["include"],
+           "-isystem", os.path.join(os.path.dirname(os.path.dirname(HIPCC)), "include"), "-I", os.path.join(ROOT, "include"),
+           os.path.join(CSRC, "operands.cpp"), "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", tmp]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.check_call(cmd)
+    os.replace(tmp, OPERANDS)
+    return OPERANDS
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every HIP source into libdcl.so (always recompiles). Returns the library path."""
+    """Compile every HIP source into libdcl.so, and the Python extension beside it (always recompiles). Returns the library path."""
     tmp = LIB + ".tmp%d" % os.getpid()
     objdir = tempfile.mkdtemp(prefix="dcl_build_")
     try:
@@ -45,8 +64,10 @@ def build(verbose: bool = False) -> str:
                 print(" ".join(cmd), flush=True)
             subprocess.check_call(cmd)
             return obj
-        with ThreadPoolExecutor(max_workers=min(len(OBJECTS), os.cpu_count() or 1)) as pool:
+        with ThreadPoolExecutor(max_workers=min(len(OBJECTS) + 1, os.cpu_count() or 1)) as pool:
+            extension = pool.submit(build_operands, verbose)
             objs = list(pool.map(compile_one, range(len(OBJECTS))))
+            extension.result()
         subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", *objs, "-o", tmp])
     finally:
         shutil.rmtree(objdir, ignore_errors=True)
@@ -55,9 +76,9 @@ def build(verbose: bool = False) -> str:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(OPERANDS):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(OPERANDS))
     deps = sources() + [os.path.join(CSRC, "dcl_internal.h"), os.path.join(CSRC, "gemm_tuned.inc"), os.path.join(CSRC, "pages_index.h"),
                         os.path.join(ROOT, "include", "dcl.h")]
     return any(os.path.getmtime(p) > t for p in deps)
