@@ -399,6 +399,8 @@ __device__ __forceinline__ bool move_reference(const f32x4_t (&sc)[4], float sca
 // divides takes them unrounded.
 __device__ __forceinline__ void probabilities(f32x4_t (&sc)[4], float scale, float m, float& l, bf16x8_t (&pf)[2], bf16x8_t (&rest)[2]) {
   const float mr = -reference_of(m);
+  uint32_t first = 0xBF80u;
+  asm("" : "+v"(first));  // kept in a register: as an inline -1.0 the product would take it as 0xBF800000
 #pragma unroll
   for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
@@ -410,8 +412,12 @@ __device__ __forceinline__ void probabilities(f32x4_t (&sc)[4], float scale, flo
   for (int s2 = 0; s2 < 2; ++s2) {
     const f32x4_t &x = sc[2 * s2], &y = sc[2 * s2 + 1];
     const uint4 w = make_uint4(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(y[0], y[1]), f2bf2(y[2], y[3]));
-    auto left = [](uint32_t two, float p0, float p1) {
-      return f2bf2(p0 - __uint_as_float(two << 16), p1 - __uint_as_float(two & 0xFFFF0000u));
+    // p minus its part by products with (-1, 0) and (0, -1): one instruction where taking the part out and subtracting are two (8 x 64
+    // tokens 22.4 -> 22.0 us); exact, found so for four million numbers below 2^9
+    auto left = [&](uint32_t two, float p0, float p1) {
+      const bf16x2_t t = __builtin_bit_cast(bf16x2_t, two);
+      return f2bf2(__builtin_amdgcn_fdot2_f32_bf16(t, __builtin_bit_cast(bf16x2_t, first), p0, false),
+                   __builtin_amdgcn_fdot2_f32_bf16(t, __builtin_bit_cast(bf16x2_t, 0xBF800000u), p1, false));
     };
     pf[s2] = __builtin_bit_cast(bf16x8_t, w);
     rest[s2] = __builtin_bit_cast(bf16x8_t, make_uint4(left(w.x, x[0], x[1]), left(w.y, x[2], x[3]),
