@@ -78,23 +78,21 @@ __device__ __forceinline__ int find_last(const int32_t* at, int lo, int hi, int 
 constexpr int kBackGroups = 64;
 size_t pages_turn_ws_ints(int B) { return 2 + 2 * (size_t)B + kBackGroups; }
 
-// The same for the values x, not falling, of a wave's lanes, by all lanes together: 64 borders a look, the first lane's and the last
-// one's place (three looks for 2^16 sequences, where a lane alone waits for sixteen loads one after the other), then each
-// lane between the two.
-__device__ __forceinline__ int wave_find(const int32_t* at, int hi, int x) {
-  int lo = 0;
-  const int lane = threadIdx.x & 63;
-  while (hi - lo > 1) {
-    const int step = (hi - lo + 63) >> 6, i = lo + step * lane;
-    const int n = __popcll(__builtin_amdgcn_ballot_w64(i < hi && at[min(i, hi - 1)] <= x));
-    lo += step * (n - 1);
-    hi = min(lo + step, hi);
-  }
-  return lo;
-}
+// The same for the values x, not falling, of a wave's lanes, by all lanes together: 64 borders a look, for the first lane's place and
+// the last one's at once (three looks for 2^16 sequences, where a lane alone waits for sixteen loads one after the other), then
+// each lane between the two.
 __device__ __forceinline__ int find_rising(const int32_t* at, int n, int x) {
-  const int lo = wave_find(at, n, __builtin_amdgcn_readfirstlane(x)), hi = wave_find(at, n, __builtin_amdgcn_readlane(x, 63));
-  return find_last(at, lo, hi + 1, x);
+  const int lane = threadIdx.x & 63, x0 = __builtin_amdgcn_readfirstlane(x), x1 = __builtin_amdgcn_readlane(x, 63);
+  int lo0 = 0, hi0 = n, lo1 = 0, hi1 = n;
+  while (max(hi0 - lo0, hi1 - lo1) > 1) {  // a range of one stays as it is
+    const int step0 = (hi0 - lo0 + 63) >> 6, i0 = lo0 + step0 * lane, step1 = (hi1 - lo1 + 63) >> 6, i1 = lo1 + step1 * lane;
+    const int v0 = at[min(i0, hi0 - 1)], v1 = at[min(i1, hi1 - 1)];
+    lo0 += step0 * (__popcll(__builtin_amdgcn_ballot_w64(i0 < hi0 && v0 <= x0)) - 1);
+    lo1 += step1 * (__popcll(__builtin_amdgcn_ballot_w64(i1 < hi1 && v1 <= x1)) - 1);
+    hi0 = min(lo0 + step0, hi0);
+    hi1 = min(lo1 + step1, hi1);
+  }
+  return find_last(at, lo0, lo1 + 1, x);
 }
 
 // ---------------------------------------------------------------- extend
@@ -280,11 +278,21 @@ __device__ void back_write(const PagesTurn& a, const int32_t* start, const int32
   }
 }
 
-template <int W, bool WHOLE>
+__device__ __forceinline__ void back_span(long total, int* from, int* to) {
+  const long per = (total + kBackGroups - 1) / kBackGroups;
+  *from = (int)min(per * blockIdx.x, total);
+  *to = (int)min(per * (blockIdx.x + 1), total);
+}
+
+// WHOLE: one workgroup does it all. SPREAD: the sequences are one window, whose sums each of the workgroups makes for itself, so that it
+// can count its share of the entries in the same launch; lengths stay until the next one, since others may still read them.
+// ALONE: one workgroup for any number of sequences, before two launches.
+enum { WHOLE, SPREAD, ALONE };
+template <int W, int MODE>
 __global__ void __launch_bounds__(W) shrink_kernel(PagesTurn a) {
-  constexpr int IT = WHOLE ? 1 : kItems;
+  constexpr int IT = MODE == WHOLE ? 1 : kItems;
   __shared__ uint32_t sh[4][W / 64];
-  __shared__ int32_t s_start[W * IT], s_first[W * IT];
+  __shared__ int32_t s_start[MODE == ALONE ? 1 : W * IT], s_first[MODE == ALONE ? 1 : W * IT];
   const int tid = threadIdx.x;
   const int list = max(0, min(*a.n_free, a.n_pages));
   const int capacity = a.max_pages << a.shift;  // at most 2^28
@@ -307,7 +315,7 @@ __global__ void __launch_bounds__(W) shrink_kernel(PagesTurn a) {
       len[i] = len_next[i];
       keep[i] = keep_next[i];
     }
-    if (!WHOLE) ahead(b0 + W * IT);
+    if (MODE == ALONE) ahead(b0 + W * IT);
     asm volatile("" ::"v"(list));  // every wave has read it before the barriers behind which it is written
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
@@ -316,7 +324,7 @@ __global__ void __launch_bounds__(W) shrink_kernel(PagesTurn a) {
       if (keep[i] >= 0 && keep[i] < len[i] && len[i] <= capacity) {
         first[i] = pages_for(keep[i], a.shift);
         n[i] = pages_for(len[i], a.shift) - first[i];
-        a.len[b0 + i] = keep[i];
+        if (MODE != SPREAD) a.len[b0 + i] = keep[i];
       }
       sum += n[i];
     }
@@ -325,11 +333,11 @@ __global__ void __launch_bounds__(W) shrink_kernel(PagesTurn a) {
     for (int i = 0; i < IT; ++i) {
       const int b = b0 + i;
       if (b < a.B) {
-        if (w == 0) {
+        if (MODE != ALONE) {
           s_start[b] = (int)at;
           s_first[b] = first[i];
         }
-        if (!WHOLE) {
+        if (MODE == ALONE || (MODE == SPREAD && blockIdx.x == 0)) {
           a.ws[2 + b] = (int)at;
           a.ws[2 + a.B + b] = first[i];
         }
@@ -338,18 +346,24 @@ __global__ void __launch_bounds__(W) shrink_kernel(PagesTurn a) {
     }
     lds_barrier();  // before sh is written again, and s_start read
   }
-  // How many come back the host does not know, only what the table could name: a few under a wide one are done with here, and
-  // nothing is left to the workgroups of the next two launches (extend and shrink of 1000 sequences by up to 32 tokens, tables of
-  // 2048 pages of 16: 28.6 us from a graph without this, 23.3 with it; of 64 by one token 11.4 and 11.7).
-  const bool here = WHOLE || (a.B <= W * IT && total <= 2 * W);
+  // How many come back the host does not know, only what the table could name: a few under a wide one are done with here by one
+  // workgroup, and nothing but the lengths is left to the next launch (extend and shrink of 1000 sequences by up to 32 tokens, tables
+  // of 2048 pages of 16: 17.1 us from a graph).
+  const bool here = MODE == WHOLE || (MODE == SPREAD && total <= 2 * W);
   int after = list;
-  if (here) {
+  if (here && blockIdx.x == 0) {
     const uint32_t all = back_count<W, true>(a, s_start, s_first, 0, (int)total, sh[1]);
     back_write<W, true>(a, s_start, s_first, 0, (int)total, 0, all, list, sh[2]);
     after = (int)min((long)list + all, (long)a.n_pages);
   }
-  if (tid == 0) {
-    if (WHOLE) {
+  if (MODE == SPREAD) {
+    int from, to;
+    back_span(here ? 0 : total, &from, &to);
+    const uint32_t n = back_count<W, true>(a, s_start, s_first, from, to, sh[0]);
+    if (tid == 0) a.ws[2 + 2 * a.B + blockIdx.x] = (int)n;
+  }
+  if (tid == 0 && blockIdx.x == 0) {
+    if (MODE == WHOLE) {
       *a.n_free = after;
     } else {
       a.ws[0] = after;
@@ -358,26 +372,25 @@ __global__ void __launch_bounds__(W) shrink_kernel(PagesTurn a) {
   }
 }
 
-__device__ __forceinline__ void back_span(const PagesTurn& a, int* from, int* to) {
-  const long total = a.ws[1], per = (total + kBackGroups - 1) / kBackGroups;
-  *from = (int)min(per * blockIdx.x, total);
-  *to = (int)min(per * (blockIdx.x + 1), total);
-}
-
 __global__ void __launch_bounds__(kWindow) back_count_kernel(PagesTurn a) {
   __shared__ uint32_t sh[kWindow / 64];
   int from, to;
-  back_span(a, &from, &to);
+  back_span(a.ws[1], &from, &to);
   const uint32_t n = back_count<kWindow, false>(a, a.ws + 2, a.ws + 2 + a.B, from, to, sh);
   if (threadIdx.x == 0) a.ws[2 + 2 * a.B + blockIdx.x] = (int)n;
 }
 
+template <bool LENGTHS>  // the lengths are cut here
 __global__ void __launch_bounds__(kWindow) back_write_kernel(PagesTurn a) {
   __shared__ uint32_t sh[3][kWindow / 64];
   __shared__ uint32_t s_before;
   int from, to;
-  back_span(a, &from, &to);
-  const int tid = threadIdx.x, list = a.ws[0];
+  back_span(a.ws[1], &from, &to);
+  const int tid = threadIdx.x, list = a.ws[0], b = blockIdx.x * kWindow + tid;
+  if (LENGTHS && b < a.B) {
+    const int len = a.len[b], keep = a.ask[b];
+    if (keep >= 0 && keep < len && len <= a.max_pages << a.shift) a.len[b] = keep;
+  }
   const uint32_t n = tid < kBackGroups ? (uint32_t)a.ws[2 + 2 * a.B + tid] : 0;
   uint32_t all = 0;
   const uint32_t upto = running_sum<kWindow>(n, all, sh[0]);
@@ -389,16 +402,21 @@ __global__ void __launch_bounds__(kWindow) back_write_kernel(PagesTurn a) {
 
 void launch_pages_shrink(const PagesTurn& a, hipStream_t s) {
   if (a.B <= kSmall && (long)a.B * a.max_pages <= 32 * kSmall) {
-    hipLaunchKernelGGL((shrink_kernel<kSmall, true>), dim3(1), dim3(kSmall), 0, s, a);
+    hipLaunchKernelGGL((shrink_kernel<kSmall, WHOLE>), dim3(1), dim3(kSmall), 0, s, a);
     return;
   }
   if (a.B <= kWindow && (long)a.B * a.max_pages <= 16 * kWindow) {
-    hipLaunchKernelGGL((shrink_kernel<kWindow, true>), dim3(1), dim3(kWindow), 0, s, a);
+    hipLaunchKernelGGL((shrink_kernel<kWindow, WHOLE>), dim3(1), dim3(kWindow), 0, s, a);
     return;
   }
-  hipLaunchKernelGGL((shrink_kernel<kWindow, false>), dim3(1), dim3(kWindow), 0, s, a);
+  if (a.B <= kWindow * kItems) {
+    hipLaunchKernelGGL((shrink_kernel<kWindow, SPREAD>), dim3(kBackGroups), dim3(kWindow), 0, s, a);
+    hipLaunchKernelGGL(back_write_kernel<true>, dim3(kBackGroups), dim3(kWindow), 0, s, a);
+    return;
+  }
+  hipLaunchKernelGGL((shrink_kernel<kWindow, ALONE>), dim3(1), dim3(kWindow), 0, s, a);
   hipLaunchKernelGGL(back_count_kernel, dim3(kBackGroups), dim3(kWindow), 0, s, a);
-  hipLaunchKernelGGL(back_write_kernel, dim3(kBackGroups), dim3(kWindow), 0, s, a);
+  hipLaunchKernelGGL(back_write_kernel<false>, dim3(kBackGroups), dim3(kWindow), 0, s, a);
 }
 
 }  // namespace dcl
