@@ -293,10 +293,10 @@ void launch_pages4_read(const Pages& p, bf16_t* k, long ks, bf16_t* v, long vs, 
 // dimensions.
 //
 // With one token it is bound by HBM behind its starts: 2 sequences of 100000 to 131072 keys, 28 / 4 heads, 133 MB: 29 us with the join
-// (4.5), the kernel alone 5.3 TB/s; 80 of 250 to 9000, 32 / 8 heads, 204 MB: 47 us, 4.3 TB/s. A tile of 64 keys under one fragment takes 400
-// vector instructions (192 convert its values, 110 are the softmax's) and 40 matrix ones, 1.0 us of a SIMD where HBM brings one in
+// (4.5), the kernel alone 5.3 TB/s; 80 of 250 to 9000, 32 / 8 heads, 204 MB: 46 us, 4.4 TB/s. A tile of 64 keys under one fragment takes 300
+// vector instructions (160 convert its values, 90 are the softmax's) and 40 matrix ones, 0.8 us of a SIMD where HBM brings one in
 // 1.7. Under blocks the two add up: 512 tokens of 4 sequences over 4096 keys, 32 / 8 heads: vector pipes busy 3/4 of the time,
-// matrix pipes 2/5 of it, 190 us, 0.66 PFLOP/s; 64 tokens of 8 over 1280, 32 heads: 22.5 us. Sharing the converted values between waves
+// matrix pipes 2/5 of it, 181 us, 0.69 PFLOP/s; 64 tokens of 8 over 1280, 32 heads: 21.8 us. Sharing the converted values between waves
 // through LDS saved a quarter of the vector instructions and lost it again to barriers and LDS reads (8 x 64 tokens 28 to 32 us,
 // 4 x 512 205 to 264, where this form took 27 and 202); four fragments a wave spill (44 us).
 __device__ __forceinline__ f32x4_t mfma16q(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {

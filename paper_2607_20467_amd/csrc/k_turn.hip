@@ -12,8 +12,8 @@ namespace dcl {
 // used.
 //
 // These are launches and chains of loads, not bytes: 64 sequences with a token each 2.9 us to extend and 1.6 to shrink; 3000 with 257000
-// rows 6.2 (the sums, one workgroup) and 5.8 (the rows), and back 4.5, 4.9 and 4.5; 65536 sequences 97 and 71 for the sums, 6 and 4 us a
-// window of 4096, whose strided loads and stores one CU makes alone.
+// rows 6.2 (the sums, one workgroup) and 5.3 (the rows), and back 5.5 (sums and counts) and 4.4 (pages and lengths); 65536 sequences 98
+// and 71 for the sums, 6 and 4 us a window of 4096, whose strided loads and stores one CU makes alone.
 constexpr int kSmall = 256, kWindow = 1024;  // threads of the workgroup: few sequences and rows, or any
 constexpr int kItems = 4;                    // sequences of a thread where there are many
 constexpr uint32_t kMost = 0x7FFFFFFFu;
