@@ -415,14 +415,23 @@ _native = None
 
 
 def _load_native():
+    """The extension that was built for this torch, None (and a warning) where there is none or it does not load."""
+    import warnings
+    from importlib import util
+    from .build import operands_path
+    path = operands_path()
     try:
-        from . import _operands
-    except ModuleNotFoundError:
+        spec = util.spec_from_file_location(__package__ + "._operands", path)
+        module = util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError as e:
+        warnings.warn(f"calls of the paged step take 3 to 4 us longer without their extension {path}: {e}", RuntimeWarning,
+                      stacklevel=4)
         return None
     lib = load_library()
-    _operands.bind(*(ctypes.cast(getattr(lib, "dcl_" + n), ctypes.c_void_p).value for n in (
+    module.bind(*(ctypes.cast(getattr(lib, "dcl_" + n), ctypes.c_void_p).value for n in (
         "pages_extend", "pages_shrink", "heads_norm_rope", "pages_write", "pages_read", "pages_attention")))
-    return _operands
+    return module
 
 
 def _device():

@@ -12,7 +12,6 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdcl.so")
 SOURCES = ["abi.hip", "abi_serving.hip", "k_small.hip", "k_gemm.hip", "k_attn.hip", "k_pages.hip",
            "k_pages4.hip", "k_turn.hip", "k_heads.hip", "k_prompt.hip", "k_sample.hip"]
-OPERANDS = os.path.join(HERE, "_operands.so")       # calls from Python in one step (csrc/operands.cpp)
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # (source, extra flags) of each object; the GEMM family's instantiations are spread over three of them
 OBJECTS = [("k_gemm.hip", ["-DDCL_GEMM_PART=1"]), ("k_gemm.hip", ["-DDCL_GEMM_PART=2"]),
@@ -32,12 +31,25 @@ def sources():
     return [os.path.join(CSRC, s) for s in SOURCES] + [os.path.join(CSRC, "operands.cpp")]
 
 
+def operands_path() -> str:
+    """The Python extension (csrc/operands.cpp: calls from Python in one step). It reads torch's objects as the headers lay them out,
+    so that one for another torch or interpreter has another name and is never loaded."""
+    import sysconfig
+
+    import torch
+    return os.path.join(HERE, "_operands." + str(torch.__version__) + sysconfig.get_config_var("EXT_SUFFIX"))
+
+
 def build_operands(verbose: bool = False) -> str:
     """Compile the Python extension, host code against torch's headers. Returns its path."""
     import sysconfig
 
     import torch
-    at, tmp = os.path.dirname(torch.__file__), OPERANDS + ".tmp%d" % os.getpid()
+    for name in os.listdir(HERE):                     # those of earlier builds, for a library that is about to be replaced
+        if name.startswith("_operands.") and name.endswith(".so"):
+            os.remove(os.path.join(HERE, name))
+    at, path = os.path.dirname(torch.__file__), operands_path()
+    tmp = path + ".tmp%d" % os.getpid()
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, "-D__HIP_PLATFORM_AMD__",
            "-isystem", os.path.join(at, "include"), "-isystem", sysconfig.get_paths()["include"],
@@ -46,8 +58,8 @@ def build_operands(verbose: bool = False) -> str:
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)
-    os.replace(tmp, OPERANDS)
-    return OPERANDS
+    os.replace(tmp, path)
+    return path
 
 
 def build(verbose: bool = False) -> str:
@@ -76,9 +88,9 @@ def build(verbose: bool = False) -> str:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(OPERANDS):
+    if not os.path.exists(LIB) or not os.path.exists(operands_path()):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(OPERANDS))
+    t = min(os.path.getmtime(LIB), os.path.getmtime(operands_path()))
     deps = sources() + [os.path.join(CSRC, "dcl_internal.h"), os.path.join(CSRC, "gemm_tuned.inc"), os.path.join(CSRC, "pages_index.h"),
                         os.path.join(ROOT, "include", "dcl.h")]
     return any(os.path.getmtime(p) > t for p in deps)
