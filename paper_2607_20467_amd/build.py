@@ -4,6 +4,7 @@ import shutil
 import subprocess
 import sys
 import tempfile
+import warnings
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -40,14 +41,19 @@ def operands_path() -> str:
     return os.path.join(HERE, "_operands." + str(torch.__version__) + sysconfig.get_config_var("EXT_SUFFIX"))
 
 
+def drop_operands() -> None:
+    """Extensions of any torch: each enters the library as the header was when it was built."""
+    for name in os.listdir(HERE):
+        if name.startswith("_operands.") and name.endswith(".so"):
+            os.remove(os.path.join(HERE, name))
+
+
 def build_operands(verbose: bool = False) -> str:
     """Compile the Python extension, host code against torch's headers. Returns its path."""
     import sysconfig
 
     import torch
-    for name in os.listdir(HERE):                     # those of earlier builds, for a library that is about to be replaced
-        if name.startswith("_operands.") and name.endswith(".so"):
-            os.remove(os.path.join(HERE, name))
+    drop_operands()
     at, path = os.path.dirname(torch.__file__), operands_path()
     tmp = path + ".tmp%d" % os.getpid()
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
@@ -63,7 +69,8 @@ def build_operands(verbose: bool = False) -> str:
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every HIP source into libdcl.so, and the Python extension beside it (always recompiles). Returns the library path."""
+    """Compile every HIP source into libdcl.so, and the Python extension beside it (always recompiles). Returns the library path. What the
+    extension lacks (a host compiler, torch's headers) costs the library nothing."""
     tmp = LIB + ".tmp%d" % os.getpid()
     objdir = tempfile.mkdtemp(prefix="dcl_build_")
     try:
@@ -79,11 +86,17 @@ def build(verbose: bool = False) -> str:
         with ThreadPoolExecutor(max_workers=min(len(OBJECTS) + 1, os.cpu_count() or 1)) as pool:
             extension = pool.submit(build_operands, verbose)
             objs = list(pool.map(compile_one, range(len(OBJECTS))))
-            extension.result()
         subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", *objs, "-o", tmp])
+    except BaseException:
+        drop_operands()                                 # the library stays as it was
+        raise
     finally:
         shutil.rmtree(objdir, ignore_errors=True)
     os.replace(tmp, LIB)
+    try:
+        extension.result()
+    except (OSError, subprocess.CalledProcessError, ImportError) as e:
+        warnings.warn(f"the extension for calls from Python is not built: {e}", RuntimeWarning, stacklevel=2)
     return LIB
 
 

@@ -103,3 +103,49 @@ def test_the_extension_that_fits_is_used(copy):
     from paper_2607_20467_amd import build
     shutil.copy(build.operands_path(), copy)
     assert run_calls(copy.parent) == ["native", "0"]
+
+
+STAND_IN = """#!%s
+import sys
+open(sys.argv[sys.argv.index("-o") + 1], "wb").write(b"built")
+"""
+
+
+@pytest.mark.parametrize("how", ["compiler is missing", "compiler fails"])
+def test_the_library_is_built_where_the_extension_is_not(tmp_path, monkeypatch, how):
+    """With a stand-in for hipcc: the library is there, a warning says what is not, and no extension of an older build stays to enter the
+    new library."""
+    from paper_2607_20467_amd import build
+    hipcc, cxx, at = (tmp_path / n for n in ("hipcc", "cxx", "package"))
+    at.mkdir()
+    hipcc.write_text(STAND_IN % sys.executable)
+    cxx.write_text("#!/bin/sh\nexit 1\n")
+    for f in (hipcc, cxx):
+        f.chmod(0o755)
+    if how == "compiler is missing":
+        cxx = tmp_path / "none"
+    monkeypatch.setenv("CXX", str(cxx))
+    for name, value in (("HIPCC", str(hipcc)), ("HERE", str(at)), ("LIB", str(at / "libdcl.so"))):
+        monkeypatch.setattr(build, name, value)
+    with open(build.operands_path(), "wb") as f:
+        f.write(b"older")
+    with pytest.warns(RuntimeWarning, match="extension"):
+        assert build.build() == str(at / "libdcl.so")
+    assert (at / "libdcl.so").read_bytes() == b"built"
+    assert os.listdir(at) == ["libdcl.so"]
+
+
+def test_a_library_that_does_not_build_is_no_library(tmp_path, monkeypatch):
+    from paper_2607_20467_amd import build
+    """Nor does an extension for it stay."""
+    hipcc, cxx = tmp_path / "hipcc", tmp_path / "cxx"
+    hipcc.write_text("#!/bin/sh\nexit 1\n")
+    cxx.write_text(STAND_IN % sys.executable)
+    for f in (hipcc, cxx):
+        f.chmod(0o755)
+    monkeypatch.setenv("CXX", str(cxx))
+    for name, value in (("HIPCC", str(hipcc)), ("HERE", str(tmp_path)), ("LIB", str(tmp_path / "libdcl.so"))):
+        monkeypatch.setattr(build, name, value)
+    with pytest.raises(subprocess.CalledProcessError):
+        build.build()
+    assert sorted(os.listdir(tmp_path)) == ["cxx", "hipcc"]
