@@ -7,8 +7,9 @@ namespace dcl {
 // pairs, 4 c .. and r / 2 + 4 c .. (behind the rotated ones, eight that follow each other): nothing is exchanged but the sum
 // of squares, and a wave, which stays with its row, works each angle out once for all of its heads.
 //
-// The angle: pos * turns[i] in float64 is exact to 2^-52 of itself, at most 2^31 / (2 pi) turns, so that its fraction is exact to
-// 2^-23 of a turn at the farthest position and to 2^-24 below 2^28; as float32 in [-0.5, 0.5] it keeps 2^-26.
+// The angle: pos * turns[i] in float64, below 2^31 / (2 pi) < 2^29 turns. Two roundings, of the turns a position (half a step 2^-56 and
+// less, 2^31 times) and of the product (half a step of 2^-24), leave 2^-24 of a turn at the farthest position; as float32 in [-0.5, 0.5]
+// the fraction keeps 2^-26.
 //
 // Memory-bound for many rows: 8192 of 32 + 8 heads of 128, 168 MB: 31 us, 5.4 TB/s (with pairs in different lanes, which an exchange
 // brings together, 43 to 74: its twelve LDS-crossbar instructions a head group and twice the angles). Four rows: 3.5 us, a chain of

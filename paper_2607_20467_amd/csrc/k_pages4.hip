@@ -315,8 +315,9 @@ __device__ __forceinline__ float reference_of(float m) { return m == -INFINITY ?
 // A query against keys that stay in their 4 bits: gfx950's scaled product takes 128 dimensions of e2m1 times e4m3, every 32 of either
 // side under a power-of-two scale of their own, which is how the keys lie in their pages. The query enters as two e4m3 parts,
 // the nearest and the nearest to what it leaves under a 16th of its scale. Their eight significant bits are a bfloat16's, down
-// to 2^-14 of the group's largest; what is smaller keeps a step of 2^-22 of it. (e4m3 reaches from 2^-9 to 448; the scale is the
-// least power of two with the group's largest at most 448 times it.)
+// to 2^-14 of the group's largest; below, the step is 2^-13 of the scale, which the largest is more than 224 times: an error below
+// 2^-21.8 of it. (e4m3 reaches from 2^-9 to 448; the scale is the least power of two with the group's largest at most 448 times it, and
+// not below 2^-122, from where on the step is 2^-135 at most and every bfloat16, a multiple of 2^-133, is kept whole.)
 //
 // The product's own order (found by one-hot operands): lane group g holds dimensions 32 g .. of the e2m1 operand, 16 g .. and 64 +
 // 16 g .. of the e4m3 one; a scale operand's lane group g is that of dimensions 32 g .. on both sides.
