@@ -372,8 +372,9 @@ size_t dcl_pages_attention_workspace_bytes(const dcl_pages* pages, int32_t n_hea
  * keep 16 bits in the product with v; sums are float32. Over E2M1 pages with head_dim 128 an element of q is kept to 2^-21 of the
  * largest of its 32 dimensions, and an infinity in them counts as NaN. An E2M1 value that stands for 2^128 or more (never
  * written by dcl_pages_write) makes the rows that see it NaN or infinite in its dimension. The host does not know the
- * lengths: of the other types the parts are cut from max_pages, so that a table much wider than the sequences need costs time and workspace; E2M1 pages
- * are dealt to the parts in turn, whatever the table could name. Calls that overlap in time need their own workspaces. */
+ * lengths: how many parts there may be, and with them the workspace, follows from max_pages, so that a table much wider than the
+ * sequences need costs workspace and time (more workgroups, and the join of parts where a tight table has one). E2M1 pages are dealt
+ * to the parts in turn, so that each has its share at any length; of the other types the parts are cut from max_pages. Calls that overlap in time need their own workspaces. */
 dcl_status dcl_pages_attention(const dcl_pages* pages, const int32_t* table, int32_t max_pages, const int32_t* len,
                                const int32_t* cu, int32_t B, int32_t T, int32_t max_new, const void* q,
                                int64_t q_stride, int32_t n_heads, float scale, int32_t causal, void* out, float* lse,

@@ -89,7 +89,7 @@ __device__ __forceinline__ uint4 stream_load(const void* p) {
 // Memory-bound: ten prompts of 400 to 6000 tokens x 32 heads, 325 MB: 60 us, 5.4 TB/s (70 with keys stored by the four bytes of a
 // lane, 63 with page numbers looked up behind the rows); one token of each of 48 sequences x 8 heads: 5.4 us, a chain of loads.
 // Rows are read past the caches (62 us with plain loads), pages stored through them, for what reads them next: the ten prompts written
-// and read back 128.8 -> 108.7 us.
+// and read back 128.8 -> 108.7 us. Heads of 64: the same prompts, 162 MB, 34 us, 4.7 TB/s.
 constexpr int kGroup4 = 64;
 
 template <int DH>
@@ -194,7 +194,8 @@ __global__ void __launch_bounds__(256) pages4_write_kernel(Pages p, const bf16_t
 
 // ---------------------------------------------------------------- read
 // The reverse, in the same groups. A row whose position no page holds is zeros. The same ten prompts: 69 us, 4.7 TB/s, four fifths of
-// it stores of 256 bytes a row and head (48 us behind the call that wrote them: the pages are in the last cache); nine sequences of 300 to 5000 positions x 8 heads, 99 MB: 17.4 us, 5.7 TB/s.
+// it stores of 256 bytes a row and head (48 us behind the call that wrote them: the pages are in the last cache); nine sequences of 300 to 5000 positions x 8 heads, 99 MB: 17.4 us, 5.7 TB/s
+// (heads of 64, 50 MB: 10.5 us, 4.7 TB/s).
 template <int DH>
 __global__ void __launch_bounds__(256) pages4_read_kernel(Pages p, bf16_t* __restrict__ k, long kst, bf16_t* __restrict__ v,
                                                          long vst, int groups, Divisor by_heads, Divisor by_groups) {
@@ -859,9 +860,13 @@ __global__ void __launch_bounds__(256) pages4_join_kernel(PagesAttn a, int head_
 static int query_fragments4(int g, int max_new) { return (long)g * max_new <= 16 ? 1 : 2; }
 
 // How many parts, and how long the runs of keys that they take in turn. The host knows no lengths, only what the table could name;
-// runs in turn give every part its share at any length, so that a wide table costs no more than a tight one (80 x 1 token over 250 to
-// 9000 keys, 32 / 8 heads, tables of 9000 / 131072: 47.9 / 48.0 us; parts of 1536 adjoining keys 50.3 / 105; 128 x 1 over 200 to 600,
-// 131072: 21 us for 130).
+// runs in turn give every part its share at any length, so that a wide table costs no more than a tight one that has as many parts (80 x 1
+// token over 250 to 9000 keys, 32 / 8 heads, tables of 9000 / 131072: 46.5 / 46.2 us; parts of 1536 adjoining keys 50.3 / 105, when runs in turn
+// took 47.9). Where the tight one has fewer, the wide one adds workgroups, the join and its workspace: 128 x 1 over 200 to 600: 18.6 / 20.3 us
+// (adjoining keys: 130); 64 tokens of 8 sequences over 1280, 32 heads: 23.2 / 24.6.
+//
+// The tables below were measured when the rules were made, each line with one draw of lengths: their figures compare within a line. (Now:
+// 32 x 1 with 320000 keys in all 76 us, 80 x 1 with 186000 46, 200 x 1 with 473000 102, 64 tokens of 8 over 500 to 20000 with 58000 122.)
 //
 // From a workgroup a CU on (units: sequences x KV heads x row tiles): runs of 2048 keys, since a sequence cut further pays more starts, and
 // parts for three rounds of the three workgroups that a CU holds, at least three, to even out the lengths. us by parts, runs of 2048:

@@ -52,6 +52,16 @@ def test_attention_workspace_of_four_bits(dcl):
     assert r == 3 and "workspace" in msg
 
 
+@pytest.mark.parametrize("B,T,max_new,heads,hkv,tight,wide", [(8, 512, 64, 32, 32, 20, 2048), (128, 128, 1, 32, 8, 10, 2048)])
+def test_a_wide_table_asks_for_the_workspace_of_parts(dcl, B, T, max_new, heads, hkv, tight, wide):
+    """As the header has it: the lengths are the device's, so that parts and workspace follow from what the table could name."""
+    def need(width):
+        n = dcl.load_library().dcl_pages_attention_workspace_bytes(
+            ctypes.byref(pool4(dcl, head_dim=128, n_kv_heads=hkv, page_len=64)), heads, B, T, max_new, width)
+        return n // (T * heads * (128 * 4 + 8))           # outputs, and a reference and a sum, of each part
+    assert need(tight) == 0 and need(wide) >= 2
+
+
 EXTEND = dict(table=256, max_pages=2, len=256, count=256, B=1, T=4, free=256, n_free=256, cu=256, pos=256, slot=256, ws=256,
               ws_bytes=1 << 20, stream=None)
 SHRINK = dict(table=256, max_pages=2, len=256, keep=256, B=1, free=256, n_free=256, ws=256, ws_bytes=1 << 20, stream=None)
